@@ -278,6 +278,153 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
                     const void* saved, void* dxp, void* dw_gate, void* dw_up, void* dw_down,
                     void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------ 8-bit serving
+ * The forward-only pass with int8 weights and activations, and the attention
+ * beside it over an int8 cache.  Bytes are the bound of serving, so weights
+ * and cache are held in 8 bits; every sum is exact (int32) or fp32.
+ *
+ * Integer rows ("int8 rows"): a row x of K values is held as
+ *   q_k = rint(127 x_k / a), a = max |x_k|, and the scale s = a / 127,
+ * so x ~ s q.  A row of zeros has s = 0; a row with an infinity or NaN has
+ * s = NaN and q = 0, so everything computed from it is NaN.
+ */
+
+/* flags (moe_i8_dims.flags, moe_kv_attn.flags) */
+#define MOE_F_OUT_FP32 8u /* moe_i8_dims: the output is fp32, else bf16 */
+#define MOE_F_CAUSAL 16u  /* moe_kv_attn: a token sees the keys up to its own position, else all */
+
+#define MOE_I8_MAX_K 131072 /* sums of K products of int8 stay below 2^31 */
+
+/* Rows of x ([rows, K] bf16, row pitch ldx elements) as int8 rows: q [rows, K],
+ * scale [rows].  rows >= 1; K a multiple of 16, at most MOE_I8_MAX_K; ldx >= K,
+ * a multiple of 8. */
+int moe_i8_quant_rows(int32_t rows, int32_t K, const void* x, int64_t ldx, int8_t* q, float* scale, void* stream);
+
+/* Weights laid out for the int8 products, once: w [E, K, N] bf16 -> q [E, N, K],
+ * one int8 row and scale[e][n] per output channel.  E, N >= 1; K as above. */
+int moe_i8_quant_weight(int32_t E, int32_t K, int32_t N, const void* w, int8_t* q, float* scale, void* stream);
+
+/* Product of int8 rows: out[m][n] = a_scale[m] b_scale[n] sum_k a[m][k] b[n][k].
+ * M, N >= 1, K a multiple of 16. */
+typedef struct moe_i8_dims {
+  int32_t M, N, K;
+  uint32_t flags; /* MOE_F_OUT_FP32 */
+} moe_i8_dims;
+
+/*   a [M, K], a_scale [M]; b [N, K], b_scale [N]
+ *   out  [M, N] bf16 or fp32, row pitch ldo >= N elements */
+int moe_i8_matmul(const moe_i8_dims* d, const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale,
+                  void* out, int64_t ldo, void* stream);
+
+/* The same from bf16 rows x ([M, K], row pitch ldx), quantised on the way.
+ *   ws  moe_i8_linear_workspace_bytes(d) bytes of scratch */
+size_t moe_i8_linear_workspace_bytes(const moe_i8_dims* d);
+int moe_i8_linear(const moe_i8_dims* d, const void* x, int64_t ldx, const int8_t* b, const float* b_scale, void* out,
+                  int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
+/* Expert weights in int8 (moe_i8_quant_weight of [E, H, F] and [E, F, H]). */
+typedef struct moe_i8_experts {
+  const int8_t* w_gate;  /* [E, F, H] */
+  const int8_t* w_up;    /* [E, F, H] */
+  const int8_t* w_down;  /* [E, H, F] */
+  const float* s_gate;   /* [E, F] */
+  const float* s_up;     /* [E, F] */
+  const float* s_down;   /* [E, H] */
+} moe_i8_experts;
+
+/* moe_experts_fwd in 8 bits, forward only: O = A W_down, A = silu(G) U held as
+ * int8 rows, G and U int8 products of the int8 rows of xp.  d->flags must be 0.
+ *   ws  moe_experts_i8_workspace_bytes(d) bytes of scratch */
+size_t moe_experts_i8_workspace_bytes(const moe_experts_dims* d);
+int moe_experts_i8(const moe_experts_dims* d, const void* xp, const int32_t* counts, const moe_i8_experts* w, void* o,
+                   void* ws, size_t ws_bytes, void* stream);
+
+/* moe_infer with the experts in 8 bits; the router stays bf16 (its selection is
+ * moe_infer's), the combine fp32.  Arguments as moe_infer.
+ *   ws  moe_infer_i8_workspace_bytes(d) bytes of scratch */
+size_t moe_infer_i8_workspace_bytes(const moe_dims* d);
+int moe_infer_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i8_experts* w, const uint8_t* token_mask,
+                 void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* A paged cache of keys and values in 8 bits.  Block i holds block_tokens
+ * tokens of one request; per block and head one scale each for keys and
+ * values: key = k_scale k.  Values are stored token-last, the layout in which
+ * the attention's product reads them. */
+typedef struct moe_kv_cache {
+  int32_t n_blocks;     /* >= 1 */
+  int32_t block_tokens; /* 16, 32, 64 or 128 */
+  int32_t kv_heads;     /* >= 1 */
+  int32_t head_dim;     /* 64 or 128 */
+  int8_t* k;            /* [n_blocks, kv_heads, block_tokens, head_dim] */
+  int8_t* v;            /* [n_blocks, kv_heads, head_dim, block_tokens] */
+  float* k_scale;       /* [n_blocks, kv_heads] */
+  float* v_scale;       /* [n_blocks, kv_heads] */
+} moe_kv_cache;
+
+/* A batch of B requests whose new tokens are packed request after request
+ * into T rows: request b has rows row_start[b] .. row_start[b + 1] (clamped to
+ * [0, T]), the last of its kv_len[b] tokens.  Its token p lies in block
+ * block_table[b][p / block_tokens]; entries outside [0, n_blocks) and tokens
+ * past W blocks have no place: they are not written, and no query sees them.
+ * All three arrays are on the device. */
+typedef struct moe_kv_batch {
+  int32_t B, T, W;
+  const int32_t* row_start;   /* [B + 1] */
+  const int32_t* kv_len;      /* [B] */
+  const int32_t* block_table; /* [B, W] */
+} moe_kv_batch;
+
+/* Tables of one step, built on the device from request lengths: request b has
+ * old_len[b] tokens in the cache and gets new_len[b] more (negative counts as
+ * 0).  Blocks its table lacks are taken in request order from the top of the
+ * stack free_ids[0 .. n_free).
+ *   block_table [B, W]  the blocks taken are written (-1 once the stack is
+ *                       empty), all other entries are left alone
+ *   row_start [B + 1], kv_len [B]   as in moe_kv_batch (row_start not clamped)
+ *   positions, slots, seq [T]       per packed token its position in its
+ *                       request, block * block_tokens + offset (-1: no place)
+ *                       and its request; -1 past the last token
+ *   state [2]           {blocks left on the stack, blocks that were missing} */
+typedef struct moe_kv_plan_dims {
+  int32_t B, T, W;      /* B, W >= 1, T >= 0 */
+  int32_t n_blocks, block_tokens;
+  int32_t free_cap;     /* entries of free_ids */
+} moe_kv_plan_dims;
+int moe_kv_plan(const moe_kv_plan_dims* d, const int32_t* old_len, const int32_t* new_len, int32_t* block_table,
+                const int32_t* free_ids, const int32_t* n_free, int32_t* row_start, int32_t* kv_len,
+                int32_t* positions, int32_t* slots, int32_t* seq, int32_t* state, void* stream);
+
+/* Write the batch's new keys and values (k, v: T rows of [kv_heads, head_dim]
+ * bf16, row pitch ld elements, a multiple of 8) into their blocks.  A block's
+ * scale is that of the largest value written to it since its first token: it
+ * only grows, and the tokens it already holds are rounded again when it does.
+ * A non-finite key or value makes the scale of its block and head NaN. */
+int moe_kv_append(const moe_kv_cache* c, const moe_kv_batch* b, const void* k, const void* v, int64_t ld,
+                  void* stream);
+
+/* Read the first kv_start[b + 1] - kv_start[b] tokens of each request back as
+ * bf16 rows kv_start[b] .. (kv_start [B + 1] on the device, clamped to
+ * [0, total]): k_out, v_out [total, kv_heads, head_dim].  Tokens without a
+ * place read as 0. */
+int moe_kv_read(const moe_kv_cache* c, int32_t B, int32_t W, const int32_t* block_table, const int32_t* kv_start,
+                int32_t total, void* k_out, void* v_out, void* stream);
+
+/* Attention of the batch's new tokens over their requests' cache: per head
+ *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale <q, k_j>),
+ * over the keys the token sees (none: out = 0).  Query head i reads kv head
+ * i / (heads / kv_heads).
+ *   q, out  T rows of [heads, head_dim] bf16, row pitches ldq and ldo elements (multiples of 8) */
+typedef struct moe_kv_attn {
+  int32_t heads;  /* a multiple of kv_heads */
+  int32_t max_q;  /* no request has more new tokens (rows past it are not written) */
+  int32_t max_kv; /* no request has more tokens (keys past it are not seen); at most W * block_tokens counts */
+  float scale;    /* finite */
+  uint32_t flags; /* MOE_F_CAUSAL */
+} moe_kv_attn;
+size_t moe_kv_attention_workspace_bytes(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* a);
+int moe_kv_attention(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* a, const void* q, int64_t ldq,
+                     void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
 /* Per-kernel timing.  With tracing on, every kernel the library launches is
  * bracketed by two HIP events recorded on its launch stream (no host
  * synchronisation at launch time).  moe_trace_read waits for the recorded

@@ -1,0 +1,175 @@
+// Rows of values as int8 with one scale: a row's largest magnitude a maps to
+// 127, q = rint(127 x / a), s = a / 127.
+//
+// The quotient is n / a with n = 127 x, which is exact for a bf16 x (8 + 7
+// bits).  It is formed as t = n (1 / a) and one residual step
+// t + (n - a t) (1 / a), whose result is the rounded quotient: an exact half
+// (x = a / 2: 63.5) stays one, so q is the same as from a division at 3
+// instead of about 10 instructions a value.
+#include "serve.hpp"
+#include "trace.hpp"
+
+namespace moe {
+
+namespace {
+
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+// One row's rounding: x -> q for the largest magnitude `top` (as fp32 bits).
+// `pre` brings both into a range where 127 x and 1 / top are normal numbers.
+struct Rounder {
+  float pre, top, inv, scale;
+  bool live;
+  __device__ __forceinline__ explicit Rounder(uint32_t top_bits) {
+    const float t = __uint_as_float(top_bits);
+    live = top_bits < kInfBits && top_bits != 0u;
+    pre = t < 1e-30f ? 0x1p100f : t > 1e30f ? 0x1p-100f : 1.0f;
+    top = t * pre;
+    inv = live ? 1.0f / top : 0.0f;
+    scale = top_bits >= kInfBits ? __uint_as_float(0x7fc00000u) : t / 127.0f;
+  }
+  __device__ __forceinline__ int operator()(float x) const {
+    const float n = x * pre * 127.0f;
+    const float t = n * inv;
+    const float r = __builtin_rintf(fmaf(fmaf(-top, t, n), inv, t));
+    return live ? static_cast<int>(r) : 0;
+  }
+};
+
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v = max(v, static_cast<uint32_t>(shfl_xor(static_cast<int>(v), m)));
+  return v;
+}
+
+__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
+  return (a & 255) | ((b & 255) << 8) | ((c & 255) << 16) | (static_cast<uint32_t>(d) << 24);
+}
+
+// Largest magnitude of 8 bf16 as fp32 bits (NaN > infinity > finite).
+__device__ __forceinline__ uint32_t top8(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7fff0000u, (w[i] << 16) & 0x7fff0000u));
+  return m;
+}
+
+__device__ __forceinline__ uint2 quant8(const uint4& v, const Rounder& r) {
+  return make_uint2(pack4(r(lo_bf(v.x)), r(hi_bf(v.x)), r(lo_bf(v.y)), r(hi_bf(v.y))),
+                    pack4(r(lo_bf(v.z)), r(hi_bf(v.z)), r(lo_bf(v.w)), r(hi_bf(v.w))));
+}
+
+// One wave per row.  Up to kHeld passes of 512 columns stay in registers; what
+// lies beyond is read again for the rounding.
+constexpr int kHeld = 8;
+
+__global__ __launch_bounds__(256) void k_i8_quant_rows(const bf16_t* __restrict__ x, int64_t ldx, int rows, int K,
+                                                       const int32_t* __restrict__ n_valid, int8_t* __restrict__ q,
+                                                       float* __restrict__ scale) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= rows || (n_valid != nullptr && row >= *n_valid)) return;
+  const bf16_t* src = x + row * ldx;
+  uint4 held[kHeld];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int c = i * 512 + lane * 8;
+    held[i] = c < K ? *reinterpret_cast<const uint4*>(src + c) : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) m = max(m, top8(held[i]));
+  for (int c = kHeld * 512 + lane * 8; c < K; c += 512) m = max(m, top8(*reinterpret_cast<const uint4*>(src + c)));
+  const Rounder r(wave_umax(m));
+  int8_t* dst = q + row * K;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int c = i * 512 + lane * 8;
+    if (c < K) *reinterpret_cast<uint2*>(dst + c) = quant8(held[i], r);
+  }
+  for (int c = kHeld * 512 + lane * 8; c < K; c += 512)
+    *reinterpret_cast<uint2*>(dst + c) = quant8(*reinterpret_cast<const uint4*>(src + c), r);
+  if (lane == 0) scale[row] = r.scale;
+}
+
+// One wave per routed row: the row's largest magnitude is that of its
+// partials.  A value is a * (partial's largest / 32767), within 2^-16 of that
+// largest: 0.002 of a step of q at most.
+__global__ __launch_bounds__(256) void k_i8_requant(const int16_t* __restrict__ a, const float* __restrict__ a_top,
+                                                    int rows, int F, const int32_t* __restrict__ n_valid,
+                                                    int8_t* __restrict__ q, float* __restrict__ scale) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= rows || row >= *n_valid) return;
+  const int parts = F / kI8Cols;
+  const float* top = a_top + row * parts;
+  uint32_t m = 0;
+  for (int i = lane; i < parts; i += 64) m = max(m, __float_as_uint(top[i]));
+  const Rounder r(wave_umax(m));
+  for (int c = lane * 8; c < F; c += 512) {
+    const uint4 v = *reinterpret_cast<const uint4*>(a + row * F + c);
+    const float step = top[c / kI8Cols] * (1.0f / 32767.0f);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    int b[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      b[2 * i] = r(static_cast<float>(static_cast<int16_t>(w[i] & 0xffff)) * step);
+      b[2 * i + 1] = r(static_cast<float>(static_cast<int16_t>(w[i] >> 16)) * step);
+    }
+    *reinterpret_cast<uint2*>(q + row * F + c) = make_uint2(pack4(b[0], b[1], b[2], b[3]), pack4(b[4], b[5], b[6], b[7]));
+  }
+  if (lane == 0) scale[row] = r.scale;
+}
+
+// 64 output channels per workgroup: their largest magnitudes over K first,
+// then 64 x 64 blocks rounded and transposed through LDS.
+__global__ __launch_bounds__(256) void k_i8_quant_weight(const bf16_t* __restrict__ w, int K, int N,
+                                                         int8_t* __restrict__ q, float* __restrict__ scale) {
+  __shared__ uint32_t tops[4][64];
+  __shared__ int8_t tile[64][64 + 16];
+  const int n0 = blockIdx.x * 64, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int n = n0 + lane;
+  const bf16_t* src = w + static_cast<int64_t>(blockIdx.y) * K * N;
+  uint32_t m = 0;
+  if (n < N)
+    for (int k = wv; k < K; k += 4) m = max(m, static_cast<uint32_t>(src[static_cast<int64_t>(k) * N + n] & 0x7fff) << 16);
+  tops[wv][lane] = m;
+  __syncthreads();
+  const Rounder r(max(max(tops[0][lane], tops[1][lane]), max(tops[2][lane], tops[3][lane])));
+  const int64_t out = static_cast<int64_t>(blockIdx.y) * N + n0;
+  if (wv == 0 && n < N) scale[out + lane] = r.scale;
+  for (int k0 = 0; k0 < K; k0 += 64) {
+    for (int k = wv; k < 64; k += 4)
+      tile[lane][k] = k0 + k < K && n < N ? static_cast<int8_t>(r(bf2f(src[static_cast<int64_t>(k0 + k) * N + n]))) : 0;
+    __syncthreads();
+    const int row = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16;
+    if (n0 + row < N && k0 + c < K)
+      *reinterpret_cast<uint4*>(q + (out + row) * K + k0 + c) = *reinterpret_cast<const uint4*>(&tile[row][c]);
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+hipError_t launch_i8_quant_rows(const bf16_t* x, int64_t ldx, int rows, int K, const int32_t* n_valid, int8_t* q,
+                                float* scale, hipStream_t s) {
+  TraceScope trace_scope(K_I8_QUANT, s);
+  hipLaunchKernelGGL(k_i8_quant_rows, dim3(cdiv(rows, 4)), dim3(256), 0, s, x, ldx, rows, K, n_valid, q, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_i8_requant(const int16_t* a, const float* a_top, int rows, int F, const int32_t* n_valid, int8_t* q,
+                             float* scale, hipStream_t s) {
+  TraceScope trace_scope(K_I8_QUANT, s);
+  hipLaunchKernelGGL(k_i8_requant, dim3(cdiv(rows, 4)), dim3(256), 0, s, a, a_top, rows, F, n_valid, q, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_i8_quant_weight(const bf16_t* w, int E, int K, int N, int8_t* q, float* scale, hipStream_t s) {
+  TraceScope trace_scope(K_I8_WEIGHT, s);
+  hipLaunchKernelGGL(k_i8_quant_weight, dim3(cdiv(N, 64), E), dim3(256), 0, s, w, K, N, q, scale);
+  return hipGetLastError();
+}
+
+}  // namespace moe

@@ -7,17 +7,18 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <initializer_list>
-#include <utility>
 
+#include "api.hpp"
 #include "launch.hpp"
 #include "moe.h"
 
 using namespace moe;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
+
+namespace moe {
 
 int fail(int code, const char* fmt, ...) {
   va_list ap;
@@ -31,24 +32,6 @@ int ok() {
   g_err[0] = '\0';
   return MOE_OK;
 }
-
-constexpr size_t kAlign = 256;
-size_t up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
-
-// Sequential carve-up of a buffer into 256-byte aligned regions.
-struct Carve {
-  char* base;
-  size_t off = 0;
-  explicit Carve(void* b) : base(static_cast<char*>(b)) {}
-  template <typename T>
-  T* take(size_t count) {
-    T* p = base ? reinterpret_cast<T*>(base + off) : nullptr;
-    off += up(count * sizeof(T));
-    return p;
-  }
-};
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int check_dims(const moe_dims* d) {
   if (d == nullptr) return fail(MOE_ERR_ARG, "dims is NULL");
@@ -71,8 +54,6 @@ int check_dims(const moe_dims* d) {
   return MOE_OK;
 }
 
-bool router_losses(const moe_dims* d) { return d->aux_loss_coef != 0.0f || d->z_loss_coef != 0.0f; }
-
 int check_experts_dims(const moe_experts_dims* d) {
   if (d == nullptr) return fail(MOE_ERR_ARG, "dims is NULL");
   if (d->rows < 1 || d->H < 1 || d->E < 1 || d->F < 1)
@@ -86,6 +67,10 @@ int check_experts_dims(const moe_experts_dims* d) {
   return MOE_OK;
 }
 
+namespace {
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+}  // namespace
+
 int check_ptrs(std::initializer_list<std::pair<const char*, const void*>> ps) {
   for (const auto& p : ps) {
     if (p.second == nullptr) return fail(MOE_ERR_ARG, "%s is NULL", p.first);
@@ -93,6 +78,17 @@ int check_ptrs(std::initializer_list<std::pair<const char*, const void*>> ps) {
   }
   return MOE_OK;
 }
+
+int hip_status(hipError_t e, const char* where) {
+  if (e != hipSuccess) return fail(MOE_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
+  return ok();
+}
+
+}  // namespace moe
+
+namespace {
+
+bool router_losses(const moe_dims* d) { return d->aux_loss_coef != 0.0f || d->z_loss_coef != 0.0f; }
 
 // ---- layout of the block's `saved` buffer
 struct Saved {
@@ -257,11 +253,6 @@ ExpWs exp_ws_layout(const moe_experts_dims* d, void* base) {
   w.plan = c.take<int32_t>(static_cast<size_t>(wgrad_plan_ints(d->E)));
   w.bytes = c.off;
   return w;
-}
-
-int hip_status(hipError_t e, const char* where) {
-  if (e != hipSuccess) return fail(MOE_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
-  return ok();
 }
 
 // MOE_F_RECOMPUTE: the forward kept no G and U.  Recompute them with the

@@ -32,6 +32,16 @@ enum KernelId {
   K_LORA_WGRAD,
   K_GATE_BWD,
   K_WGRAD_PLAN,
+  K_I8_QUANT,
+  K_I8_WEIGHT,
+  K_I8_MATMUL,
+  K_I8_GATEUP,
+  K_I8_DOWN,
+  K_KV_PLAN,
+  K_KV_APPEND,
+  K_KV_READ,
+  K_KV_ATTENTION,
+  K_KV_COMBINE,
   K_NUM_KERNELS
 };
 

@@ -1,0 +1,618 @@
+"""GPU tests of the 8-bit serving operators against plain 64-bit forms.
+
+Tolerances, from the formats: an int8 product is exact, its fp32 result takes
+three roundings (2^-24 each), a bf16 result (8 significant bits) one
+more of 2^-8.  Rows of bf16
+values are rounded to int8 exactly as in 64 bits.  The SwiGLU activation is
+held to 2^-16 of its largest value before its rounding: 0.002 of a step, so at
+most one value in 250 lands one step off, sqrt(1/250) = 0.063 steps rms against
+the 10 and more steps rms of a row, 0.6% of the output's norm.  Attention rounds
+each probability to bf16: 2^-8 of sum p |v|, and its output: 2^-8 of itself.
+"""
+import numpy as np
+import pytest
+
+from tests import serve_ref as R
+
+pytestmark = pytest.mark.gpu
+
+BF = 2.0 ** -8
+SLACK = 1.02  # fp32 sums and exponentials beside the roundings named above
+
+
+def gen(seed):
+    return np.random.default_rng(seed)
+
+
+def bf16(x):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda().to(torch.bfloat16)
+
+
+def dev(x, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def i32(x):
+    return dev(np.asarray(x, dtype=np.int32))
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+# ------------------------------------------------------------------ int8 rows and products
+@pytest.mark.parametrize("rows,K", [(1, 16), (3, 128), (5, 1040), (130, 2048), (2, 4096), (3, 4112), (2, 16384)])
+def test_quant_rows_is_the_64_bit_rounding(rows, K):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("quant_rows", rows, K)
+    x = gen(rows + K).standard_normal((rows, K)) * np.exp(gen(1).uniform(-60, 60, (rows, 1)))
+    t = bf16(x)
+    t[0, : K // 2] = t[0].abs().max() / 2  # exact halves: 63.5 steps
+    q = torch.empty((rows, K), dtype=torch.int8, device="cuda")
+    s = torch.empty(rows, device="cuda")
+    moe.moe_i8_quant_rows(t, q, s)
+    rq, rs = R.quant_rows(host(t))
+    assert np.array_equal(host(q), rq)
+    assert np.array_equal(s.cpu().numpy(), rs[:, 0].astype(np.float32))
+
+
+def test_quant_rows_zeros_extremes_and_strides():
+    import torch
+    import paper_2608_00916_amd as moe
+    say("quant_rows extremes")
+    big = torch.zeros((6, 640), dtype=torch.bfloat16, device="cuda")
+    x = big[:, 128:384]  # rows 640 apart
+    x[1, 3], x[1, 4] = 3.3e38, -1.0
+    x[2, 7] = 1e-40  # a denormal bf16
+    x[3, 0] = float("inf")
+    x[4, 255] = float("nan")
+    x[5] = 1.0
+    q = torch.empty((6, 256), dtype=torch.int8, device="cuda")
+    s = torch.empty(6, device="cuda")
+    moe.moe_i8_quant_rows(x, q, s)
+    q, s = host(q), host(s)
+    assert s[0] == 0 and not q[0].any()
+    assert q[1, 3] == 127 and q[1, 4] == 0 and np.isfinite(s[1])
+    assert q[2, 7] == 127 and s[2] >= 0
+    assert np.isnan(s[3]) and np.isnan(s[4]) and not q[3].any() and not q[4].any()
+    assert (q[5] == 127).all()
+
+
+@pytest.mark.parametrize("shape", [(1, 128, 64), (2, 144, 100), (3, 64, 33)])
+def test_quant_weight_layout(shape):
+    import paper_2608_00916_amd as moe
+    say("quant_weight", shape)
+    E, K, N = shape
+    w = bf16(gen(7).standard_normal(shape))
+    w[0, :, 1] = 0
+    q, s = moe.moe_i8_quant_weight(w)
+    rq, rs = R.quant_rows(host(w).transpose(0, 2, 1))
+    assert np.array_equal(host(q), rq)
+    assert np.array_equal(s.cpu().numpy(), rs[..., 0].astype(np.float32))
+
+
+def int8_rows(g, rows, K):
+    return g.integers(-127, 128, (rows, K)).astype(np.int8), g.uniform(0.5, 1.5, rows).astype(np.float32) / 100
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 5120, 2048), (2, 33, 48), (7, 1001, 640), (16, 257, 4096), (17, 64, 80),
+                                   (33, 130, 1040), (64, 128, 128), (65, 127, 144), (129, 255, 272), (300, 513, 400),
+                                   (1000, 384, 2064)])
+@pytest.mark.parametrize("fp32", [False, True])
+def test_matmul(M, N, K, fp32):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 matmul", M, N, K, fp32)
+    g = gen(M * 7 + N * 3 + K)
+    (a, sa), (b, sb) = int8_rows(g, M, K), int8_rows(g, N, K)
+    wide = torch.full((M, N + 24), 7.0, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+    moe.moe_i8_matmul(dev(a), dev(sa), dev(b), dev(sb), wide[:, :N])  # rows N + 24 apart
+    ref = (a.astype(np.float64) @ b.astype(np.float64).T) * sa.astype(np.float64)[:, None] * sb.astype(np.float64)
+    err = np.abs(host(wide[:, :N]) - ref)
+    assert (err <= np.abs(ref) * (4 * 2.0 ** -24 + (0 if fp32 else BF))).all()
+    assert (wide[:, N:] == 7).all()
+
+
+def test_matmul_full_range():
+    """K products of 127 * 127 at the largest K: the sum needs 31 bits."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 matmul full range")
+    K = moe._lib.MOE_I8_MAX_K
+    for M in (1, 80):
+        a = torch.full((M, K), 127, dtype=torch.int8, device="cuda")
+        b = torch.full((3, K), 127, dtype=torch.int8, device="cuda")
+        b[1], b[2] = -127, 0
+        out = torch.empty((M, 3), device="cuda")
+        one = torch.ones(max(M, 3), device="cuda")
+        moe.moe_i8_matmul(a, one[:M], b, one[:3], out)
+        assert np.allclose(host(out), np.array([[127.0 * 127 * K, -127.0 * 127 * K, 0]] * M), rtol=2.0 ** -23)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 640, 512), (5, 40, 48), (20, 1001, 640), (64, 96, 4608), (200, 130, 1040)])
+def test_linear_equals_its_two_steps(M, N, K):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 linear", M, N, K)
+    g = gen(M + N + K)
+    x = bf16(g.standard_normal((M, K + 16)))[:, 8:K + 8]
+    b, sb = (dev(t) for t in int8_rows(g, N, K))
+    q, s = torch.empty((M, K), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    moe.moe_i8_quant_rows(x, q, s)
+    want = torch.empty((M, N), device="cuda")
+    moe.moe_i8_matmul(q, s, b, sb, want)
+    lin = moe.I8Linear(M + 3, b, sb, out_fp32=True)
+    assert torch.equal(lin.forward(x), want)
+    assert torch.equal(lin.forward(x), want)
+    rows = lin.forward(x[:1])
+    assert rows.shape == (1, N) and torch.equal(rows, want[:1])
+
+
+def test_linear_marks_a_non_finite_row():
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 linear non-finite")
+    for M in (3, 100):
+        x = bf16(gen(3).standard_normal((M, 256)))
+        x[1, 9] = float("inf")
+        x[2] = 0
+        b, sb = (dev(t) for t in int8_rows(gen(4), 40, 256))
+        y = host(moe.I8Linear(M, b, sb).forward(x))
+        assert np.isnan(y[1]).all() and not y[2].any() and np.isfinite(np.delete(y, 1, 0)).all()
+
+
+# ------------------------------------------------------------------ experts
+def expert_weights(g, E, H, F):
+    import paper_2608_00916_amd as moe
+    t, w = [], []
+    for shape in ((E, F, H), (E, F, H), (E, H, F)):
+        q, s = int8_rows(g, shape[0] * shape[1], shape[2])
+        q, s = q.reshape(shape), s.reshape(shape[:2]) * np.float32(0.05)
+        t += [dev(q), dev(s)]
+        w.append(q.astype(np.float64) * s.astype(np.float64)[..., None])
+    return moe.i8_weights(*t), w
+
+
+@pytest.mark.parametrize("rows,counts,H,F", [
+    (1, [1], 128, 128),
+    (40, [0, 1, 0, 39], 256, 128),
+    (300, [128, 129, 0, 43], 128, 384),
+    (700, [257, 0, 131, 300], 384, 640),
+    (520, [1] * 8 + [512], 512, 256),
+])
+def test_experts(rows, counts, H, F):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("experts i8", rows, counts, H, F)
+    g = gen(rows + H)
+    E = len(counts)
+    w8, w = expert_weights(g, E, H, F)
+    x = bf16(g.standard_normal((rows, H)))
+    op = moe.MoEExpertsI8(rows, H, E, F)
+    op.ws.fill_(0xFF)
+    op.o.fill_(5.0)
+    o = op.forward(x, i32(counts), w8)
+    first = o.clone()
+    assert torch.equal(op.forward(x, i32(counts), w8), first)
+    xs, r0 = host(x), 0
+    for e, n in enumerate(counts):
+        if n:
+            ref = R.expert(xs[r0:r0 + n], w[0][e], w[1][e], w[2][e])
+            got = host(first[r0:r0 + n])
+            assert np.linalg.norm(got - ref) <= (BF + 0.006) * np.linalg.norm(ref)
+        r0 += n
+    assert (first[r0:] == 5).all()  # rows past the counts are not written
+
+
+def test_experts_rows_past_the_capacity_and_the_counts():
+    import torch
+    import paper_2608_00916_amd as moe
+    say("experts i8 capacity")
+    g = gen(5)
+    w8, _ = expert_weights(g, 3, 128, 128)
+    x = bf16(g.standard_normal((200, 128)))
+    want = moe.MoEExpertsI8(200, 128, 3, 128).forward(x, i32([100, 50, 50]), w8)
+    op = moe.MoEExpertsI8(200, 128, 3, 128)
+    assert torch.equal(op.forward(x, i32([100, 50, 500]), w8), want)  # dropped past 200
+    x[150:] = float("nan")
+    op.o.fill_(5.0)
+    got = op.forward(x, i32([100, 50, 0]), w8)
+    assert torch.equal(got[:150], want[:150]) and (got[150:] == 5).all()
+
+
+def test_experts_non_finite_row_stays_alone():
+    import torch
+    import paper_2608_00916_amd as moe
+    say("experts i8 non-finite")
+    w8, _ = expert_weights(gen(6), 2, 256, 128)
+    x = bf16(gen(7).standard_normal((90, 256)))
+    want = moe.MoEExpertsI8(90, 256, 2, 128).forward(x, i32([45, 45]), w8).clone()
+    x[50, 3] = float("inf")
+    got = moe.MoEExpertsI8(90, 256, 2, 128).forward(x, i32([45, 45]), w8)
+    assert torch.isnan(got[50]).all()
+    keep = [i for i in range(90) if i != 50]
+    assert torch.equal(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("T,H,E,F,k,masked", [(1, 128, 8, 128, 2, False), (70, 256, 16, 128, 4, True),
+                                              (600, 512, 32, 384, 8, False)])
+def test_infer_is_routing_experts_and_combine(T, H, E, F, k, masked):
+    """moe_infer_i8 selects as moe_fwd does, and each routed row is moe_experts_i8's."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("infer i8", T, H, E, F, k, masked)
+    g = gen(T)
+    w8, _ = expert_weights(g, E, H, F)
+    x, w_r = bf16(g.standard_normal((T, H))), bf16(0.05 * g.standard_normal((H, E)))
+    mask = dev((g.random(T) > 0.3).astype(np.uint8)) if masked else None
+    blk = moe.MoEBlock(T, H, E, F, k, mask=masked)
+    z = torch.zeros((E, H, F), dtype=torch.bfloat16, device="cuda")
+    blk.forward(x, w_r, z, z, z.view(E, F, H), mask)
+    v = blk.views
+    n = int(v["offsets"][-1])
+    o = torch.zeros((1, H), dtype=torch.bfloat16, device="cuda")
+    if n:
+        o = moe.MoEExpertsI8(n, H, E, F).forward(x[v["row_token"][:n].long()].contiguous(), v["counts"].clone(), w8)
+    got = host(moe.MoEInferI8(T, H, E, F, k, mask=masked).forward(x, w_r, w8, mask))
+    row, gate = v["row_of"].cpu().numpy(), host(v["gates"])
+    ref = (gate[..., None] * host(o)[np.maximum(row, 0)] * (row >= 0)[..., None]).sum(1)
+    assert (np.abs(got - ref) <= BF * SLACK * np.abs(ref) + 1e-6 * np.abs(ref).max()).all()
+
+
+# ------------------------------------------------------------------ tables
+@pytest.mark.parametrize("B,T_pad,bt,W,free,seed", [
+    (1, 0, 16, 4, 40, 0), (1, 5, 64, 1, 0, 1), (7, 3, 16, 12, 1000, 2), (33, 0, 32, 6, 20, 3), (300, 100, 128, 3, 1000, 4),
+    (4100, 17, 16, 5, 100000, 5), (9000, 0, 64, 2, 3000, 6),
+])
+def test_plan(B, T_pad, bt, W, free, seed):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("plan", B, bt, W, free)
+    g = gen(seed)
+    n_blocks = 30000
+    old = g.integers(-2, W * bt + 1, B)
+    new = g.integers(-3, 2 * bt, B) * (g.random(B) > 0.3)
+    table = g.integers(-3, n_blocks + 3, (B, W)).astype(np.int32)  # also places that are none
+    ids = g.integers(-2, n_blocks + 2, free + 3).astype(np.int32)
+    T = int(np.maximum(new, 0).sum()) + T_pad
+    plan = moe.KVPlan(B, T, W, n_blocks, bt)
+    t = dev(table)
+    for _ in range(2):  # a second build on its own output changes nothing
+        plan.build(i32(old), i32(new), t, dev(ids), i32([free]))
+        ref_table = table.tolist()
+        ref = R.plan(old.tolist(), new.tolist(), ref_table, ids.tolist(), free, T, n_blocks, bt)
+        got = [x.tolist() for x in (plan.row_start, plan.kv_len, plan.positions, plan.slots, plan.seq, plan.state)]
+        for name, a, b in zip(("row_start", "kv_len", "positions", "slots", "seq", "state"), got, ref):
+            assert a == list(b), name
+        assert t.tolist() == ref_table
+
+
+def test_plan_fewer_rows_than_tokens_and_a_bad_count():
+    import paper_2608_00916_amd as moe
+    say("plan short T")
+    t = i32(np.full((2, 4), -1))
+    plan = moe.KVPlan(2, 5, 4, 10, 16)
+    plan.build(i32([0, 3]), i32([4, 20]), t, i32([7, 8]), i32([999]))  # more than the stack holds: all of it
+    assert plan.row_start.tolist() == [0, 4, 24]
+    assert plan.slots.tolist() == [8 * 16, 8 * 16 + 1, 8 * 16 + 2, 8 * 16 + 3, -1]
+    assert plan.state.tolist() == [0, 0] and t.tolist() == [[8, -1, -1, -1], [-1, 7, -1, -1]]
+
+
+# ------------------------------------------------------------------ the cache
+class Pages:
+    """A cache on the GPU and the same blocks in numpy."""
+
+    def __init__(self, g, lens, bt, heads, D, spare=3, W=None):
+        import paper_2608_00916_amd as moe
+        need = [-(-n // bt) for n in lens]
+        n = sum(need) + spare
+        ids = g.permutation(n)
+        self.bt, self.heads, self.D, self.W = bt, heads, D, W or max(1, max(need))
+        self.table = np.full((len(lens), self.W), -1, np.int32)
+        at = 0
+        for b, m in enumerate(need):
+            self.table[b, :m] = ids[at:at + m]
+            at += m
+        self.k, self.v = (g.integers(-127, 128, (n, heads, bt, D)).astype(np.int8) for _ in range(2))
+        self.ks, self.vs = (g.uniform(0.5, 1.5, (n, heads)).astype(np.float32) / 64 for _ in range(2))
+        self.cache = moe.KVCache.of(dev(self.k), dev(self.v.transpose(0, 1, 3, 2)), dev(self.ks), dev(self.vs))
+
+    def rows(self, b, n):
+        """Keys and values of request b's first n tokens, NaN without a place."""
+        k = np.full((n, self.heads, self.D), np.nan)
+        v = k.copy()
+        for t in range(n):
+            i = t // self.bt
+            blk = self.table[b, i] if i < self.W else -1
+            if 0 <= blk < len(self.k):
+                k[t] = self.k[blk, :, t % self.bt].astype(np.float64) * self.ks[blk].astype(np.float64)[:, None]
+                v[t] = self.v[blk, :, t % self.bt].astype(np.float64) * self.vs[blk].astype(np.float64)[:, None]
+        return k, v
+
+    def append(self, b, p, k, v):
+        """Tokens p .. p + n of request b, block by block."""
+        while len(k):
+            off = p % self.bt
+            m = min(self.bt - off, len(k))
+            blk = self.table[b, p // self.bt] if 0 <= p // self.bt < self.W else -1
+            if 0 <= blk < len(self.k):
+                for h in range(self.heads):
+                    for q, s, x in ((self.k, self.ks, k), (self.v, self.vs, v)):
+                        q[blk, h], s[blk, h] = R.append_block(q[blk, h], s[blk, h], x[:m, h], off)
+            k, v, p = k[m:], v[m:], p + m
+
+
+@pytest.mark.parametrize("bt", [16, 32, 64, 128])
+@pytest.mark.parametrize("D,heads", [(64, 3), (128, 1)])
+def test_append_and_read(bt, D, heads):
+    """Three steps into the same requests: single tokens, ragged runs over block
+    ends, an idle request, growing magnitudes; the values read back are those of
+    the same fp32 steps, and within a rounding of a step for each step taken."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("append", bt, D, heads)
+    g = gen(bt + D)
+    lens = [2 * bt + 5, bt, 1, 3 * bt, 7]
+    pg = Pages(g, [n + 160 for n in lens], bt, heads, D)
+    old = [0, 0, 0, 0, 0]
+    seen = [np.zeros((0, 2, heads, D))] * 5
+    for step, new in enumerate((lens, [1, 1, 0, 1, 1], [bt + 3, 2, 40, 0, 150 - bt])):
+        T = sum(new)
+        k, v = ((4.0 ** step) * g.standard_normal((T, heads, D)) for _ in range(2))
+        kv = bf16(np.concatenate([k, v], 1))  # keys and values side by side: rows 2 heads D apart
+        k, v = host(kv[:, :heads]), host(kv[:, heads:])
+        start = np.concatenate([[0], np.cumsum(new)])
+        after = [o + n for o, n in zip(old, new)]
+        pg.cache.append(kv[:, :heads], kv[:, heads:], i32(start), i32(after), dev(pg.table))
+        for b in range(5):
+            s = slice(start[b], start[b + 1])
+            pg.append(b, old[b], k[s], v[s])
+            seen[b] = np.concatenate([seen[b], np.stack([k[s], v[s]], 1)])
+        old = after
+        kv_start = np.concatenate([[0], np.cumsum(after)])
+        ko, vo = (torch.full((sum(after), heads, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        pg.cache.read(dev(pg.table), i32(kv_start), ko, vo)
+        for b in range(5):
+            s = slice(kv_start[b], kv_start[b + 1])
+            rk, rv = pg.rows(b, after[b])
+            for got, ref, which in ((host(ko[s]), rk, 0), (host(vo[s]), rv, 1)):
+                assert (np.abs(got - ref) <= BF * SLACK * np.abs(ref)).all()
+                scale = (pg.ks, pg.vs)[which]
+                for t in range(after[b]):
+                    sc = scale[pg.table[b, t // bt]].astype(np.float64)[:, None]
+                    assert (np.abs(ref[t] - seen[b][t, which]) <= 0.5 * (step + 1) * sc * 1.001).all()
+    assert np.array_equal(host(pg.cache.k_scale), pg.ks) and np.array_equal(host(pg.cache.v_scale), pg.vs)
+
+
+def test_append_without_a_place_and_non_finite():
+    import torch
+    say("append without a place")
+    g = gen(11)
+    pg = Pages(g, [64, 64, 64], 32, 2, 64)
+    pg.table[0, 1] = -1
+    pg.table[1, 1] = 10 ** 6
+    before = pg.cache.k.clone(), pg.cache.v.clone(), pg.cache.k_scale.clone()
+    k, v = bf16(g.standard_normal((9, 2, 64))), bf16(g.standard_normal((9, 2, 64)))
+    k[7, 0, 5] = float("nan")
+    v[8, 1, 5] = float("-inf")
+    # request 0 ends past its place, 1 outside the cache, 2 past its table's width but for its first 3
+    pg.cache.append(k, v, i32([0, 2, 4, 9]), i32([40, 40, 66]), dev(pg.table))
+    ok = [i for i in range(len(pg.k)) if i != pg.table[2, 1]]
+    assert torch.equal(pg.cache.k[ok], before[0][ok]) and torch.equal(pg.cache.v[ok], before[1][ok])
+    assert torch.equal(pg.cache.k_scale[ok], before[2][ok])
+    # the NaN key and the infinite value lie past the table: no scale is NaN; now inside it
+    assert not torch.isnan(pg.cache.k_scale).any()
+    pg.cache.append(k, v, i32([0, 0, 0, 9]), i32([0, 0, 64]), dev(pg.table))
+    blk = int(pg.table[2, 1])
+    assert torch.isnan(pg.cache.k_scale[blk]).tolist() == [True, False]
+    assert torch.isnan(pg.cache.v_scale[blk]).tolist() == [False, True]
+    # a block's first token starts it anew
+    pg.cache.append(k[:1], v[:1], i32([0, 0, 0, 1]), i32([0, 0, 33]), dev(pg.table))
+    assert not torch.isnan(pg.cache.k_scale).any() and not torch.isnan(pg.cache.v_scale).any()
+
+
+# ------------------------------------------------------------------ attention
+def attend(pg, q_lens, kv_lens, heads, causal=True, max_q=None, max_kv=None, scale=None, seed=0, q=None, stream=None):
+    import torch
+    import paper_2608_00916_amd as moe
+    T = sum(q_lens)
+    start = np.concatenate([[0], np.cumsum(q_lens)])
+    if q is None:
+        q = bf16(2.0 * gen(seed).standard_normal((T, heads + 1, pg.D)))[:, :heads]  # rows heads + 1 apart
+    max_q, max_kv = max_q or max(max(q_lens), 1), max_kv or max(max(kv_lens), 1)
+    op = moe.KVAttention(pg.cache, T, heads, len(q_lens), max_q, max_kv, causal, scale)
+    op.ws.fill_(0xFF)
+    op.out.fill_(3.0)
+    args = (q, pg.cache, dev(pg.table), i32(start), i32(kv_lens))
+    out = op.forward(*args)
+    torch.cuda.synchronize()
+    got = host(out)
+    assert torch.equal(op.forward(*args), torch.from_numpy(got).cuda().to(out.dtype))  # the same bits again
+    scale = pg.D ** -0.5 if scale is None else scale
+    qh = host(q)
+    for b, (n, L) in enumerate(zip(q_lens, kv_lens)):
+        m = min(n, max_q)
+        if n == 0:
+            continue
+        rows = slice(start[b], start[b] + m)
+        kv = max(0, min(L, max_kv, pg.W * pg.bt))
+        k, v = pg.rows(b, kv)
+        ref, mag = R.attention(qh[rows], k, v, L - n, kv, causal, scale)
+        err = np.abs(got[rows] - ref)
+        assert (err <= BF * SLACK * (mag + np.abs(ref)) + 1e-6).all(), (b, n, L, float(err.max()))
+        assert (got[start[b] + m:start[b + 1]] == 3).all()
+    return out
+
+
+@pytest.mark.parametrize("bt", [16, 32, 64, 128])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (8, 1), (6, 2), (14, 2)])
+def test_decode(bt, D, heads, kv_heads):
+    """One token each: short and long requests, block and tile ends, an idle one."""
+    say("decode", bt, D, heads, kv_heads)
+    lens = [1, bt - 1, bt, bt + 1, 63, 64, 65, 257, 700]
+    pg = Pages(gen(bt), lens, bt, kv_heads, D)
+    attend(pg, [1, 1, 1, 1, 0, 1, 1, 1, 1], lens, heads)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,D,bt", [(8, 1, 128, 64), (4, 2, 64, 16), (5, 1, 128, 32), (3, 3, 64, 128),
+                                                 (16, 1, 128, 16), (40, 2, 64, 64)])
+def test_chunks_of_a_prompt(causal, heads, kv_heads, D, bt):
+    """Ragged runs of new tokens: whole prompts, tails, single tokens among them."""
+    say("prompt chunks", causal, heads, kv_heads, D, bt)
+    kv = [100, 37, 333, 1, 0, 200, 129]
+    pg = Pages(gen(D + bt), kv, bt, kv_heads, D)
+    attend(pg, [100, 1, 70, 1, 0, 33, 128], kv, heads, causal)
+
+
+def test_many_requests_of_few_tokens():
+    say("many requests")
+    g = gen(21)
+    kv = g.integers(3, 90, 130).tolist()
+    pg = Pages(g, kv, 16, 2, 64)
+    attend(pg, [min(int(n), 3) for n in kv], kv, 4)
+
+
+def test_long_keys_are_split_and_joined():
+    say("long keys")
+    pg = Pages(gen(22), [5000, 9, 2600], 64, 1, 128)
+    attend(pg, [1, 1, 1], [5000, 9, 2600], 8)
+    attend(pg, [40, 2, 19], [5000, 9, 2600], 8)
+    attend(pg, [40, 2, 19], [5000, 9, 2600], 8, causal=False, scale=0.3)
+    attend(pg, [150, 2, 190], [5000, 9, 2600], 8)
+
+
+def test_rows_without_a_key():
+    """More new tokens than the cache holds: the first see nothing, and are 0."""
+    say("rows without a key")
+    pg = Pages(gen(23), [5, 70, 64], 16, 2, 64)
+    out = attend(pg, [8, 75, 0], [5, 70, 0], 4)
+    assert not out[:3].any() and not out[8:13].any()
+    attend(pg, [8, 75, 3], [0, 70, 0], 4, causal=False)
+
+
+def test_blocks_without_a_place_are_not_seen():
+    say("blocks without a place")
+    pg = Pages(gen(24), [300, 300, 300], 32, 2, 64)
+    pg.table[0, 0] = -1
+    pg.table[1, 3] = 99999
+    pg.table[2, :] = -1
+    for n in (1, 40):
+        out = attend(pg, [n, n, n], [300, 300, 300], 6)
+        assert not out[2 * n:].any()
+
+
+def test_limits_of_the_call():
+    """max_kv and the table's width hide keys; rows past max_q are not written."""
+    say("limits")
+    pg = Pages(gen(25), [300, 200], 32, 1, 64)
+    attend(pg, [1, 1], [300, 200], 4, max_kv=130, causal=False)
+    attend(pg, [20, 30], [300, 200], 4, max_q=25, max_kv=290)
+    attend(pg, [1, 1], [10 ** 6, 200], 4, causal=False, max_kv=10 ** 6)
+
+
+def test_a_bad_block_stays_where_it_is():
+    """A NaN scale in a block that a query does not see leaves it alone; one that
+    it sees makes it NaN.  Large scores do not overflow."""
+    import torch
+    say("NaN scale, large scores")
+    pg = Pages(gen(26), [200, 200], 16, 1, 128)
+    for n in (1, 50):
+        q = bf16(gen(27).standard_normal((2 * n, 8, 128)))
+        want = attend(pg, [n, n], [120, 200], 8, q=q).clone()
+        for s in (pg.cache.k_scale, pg.cache.v_scale):
+            keep = s.clone()
+            s[int(pg.table[0, 9])] = float("nan")  # past the 120 tokens of request 0
+            s[int(pg.table[1, 0])] = float("nan")  # seen by request 1
+            import paper_2608_00916_amd as moe
+            op = moe.KVAttention(pg.cache, 2 * n, 8, 2, n, 200)
+            got = op.forward(q, pg.cache, dev(pg.table), i32([0, n, 2 * n]), i32([120, 200]))
+            assert torch.equal(got[:n], want[:n]) and torch.isnan(got[n:]).all()
+            s.copy_(keep)
+    attend(pg, [1, 40], [120, 200], 8, scale=50.0)
+
+
+def test_places_past_2_31_bytes():
+    """Blocks whose keys start more than 2^31 bytes into the cache."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("large cache")
+    n, bt, heads, D = 70000, 64, 4, 128
+    cache = moe.KVCache(n, bt, heads, D)
+    small = moe.KVCache(8, bt, heads, D)
+    g = gen(28)
+    k, v = (bf16(g.standard_normal((200, heads, D))) for _ in range(2))
+    ids = [69999, 66000, 65537, 69998]
+    far, near = i32([ids]), i32([[0, 1, 2, 3]])
+    assert min(ids) * heads * bt * D > 2 ** 31
+    start, kv = i32([0, 200]), i32([200])
+    q1, q2 = bf16(g.standard_normal((1, 32, D))), bf16(g.standard_normal((200, 32, D)))
+    got = []
+    for c, table in ((cache, far), (small, near)):
+        c.append(k, v, start, kv, table)
+        ko, vo = (torch.empty((200, heads, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        c.read(table, start, ko, vo)
+        a = moe.KVAttention(c, 1, 32, 1, 1, 200).forward(q1, c, table, i32([0, 1]), kv)
+        b = moe.KVAttention(c, 200, 32, 1, 200, 200).forward(q2, c, table, start, kv)
+        got.append((ko, vo, a, b))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+def test_one_step_on_another_stream_and_in_a_graph():
+    """Plan, append and attention of two steps, captured once and replayed: the
+    tables, the cache and the output are those of the eager calls each time."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("graph")
+    g = gen(29)
+    B, heads, kvh, D, bt, W, n = 3, 8, 2, 64, 16, 8, 40
+
+    def fresh():
+        return (moe.KVCache(n, bt, kvh, D), i32(np.full((B, W), -1)), moe.KVPlan(B, 12, W, n, bt),
+                moe.KVAttention(moe.KVCache(n, bt, kvh, D).d, 12, heads, B, 6, W * bt))
+
+    free, n_free = i32(g.permutation(n)), i32([n])
+    old, new = i32([0, 0, 0]), i32([6, 1, 5])
+    k, v = (bf16(g.standard_normal((12, kvh, D))) for _ in range(2))
+    q = bf16(g.standard_normal((12, heads, D)))
+    lin_w, lin_s = (dev(t) for t in int8_rows(g, 64, heads * D))
+
+    def step(state, lin):
+        cache, table, plan, att = state
+        plan.build(old, new, table, free, n_free)
+        cache.append(k, v, plan.row_start, plan.kv_len, table)
+        o = att.forward(q, cache, table, plan.row_start, plan.kv_len)
+        return lin.forward(o.view(12, heads * D))
+
+    eager, lin = fresh(), moe.I8Linear(12, lin_w, lin_s)
+    want = [step(eager, lin).clone()]
+    captured, lin2 = fresh(), moe.I8Linear(12, lin_w, lin_s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(captured, lin2)
+    side.synchronize()
+    assert torch.equal(lin2.out, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured, lin2)
+    for i in range(4):
+        k.copy_(bf16((i + 1) * g.standard_normal((12, kvh, D))))
+        q.copy_(bf16(g.standard_normal((12, heads, D))))
+        want = step(eager, lin).clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(lin2.out, want)
+        assert torch.equal(captured[0].k, eager[0].k) and torch.equal(captured[0].k_scale, eager[0].k_scale)
+        assert torch.equal(captured[1], eager[1])
