@@ -2,19 +2,23 @@
 //
 // A request's new tokens and the heads that share a kv head form one matrix of
 // rows r = (token, head), so that few tokens still fill a matrix-core tile.
-// The int8 keys and values become bf16 in registers, which is exact; a
-// block's scale multiplies its scores (keys) and its probabilities (values),
-// so the products themselves see small integers.
+// The int8 keys and values become fp16, which is exact; a block's scale
+// multiplies its scores (keys) and its probabilities (values), so the products
+// themselves see integers.  Queries become fp16 divided by a power of two per
+// row (their 8 significant bits fit in 11).
 //
 // Scores are formed transposed, S^T = K Q^T, and the output as O^T = V^T P^T:
 // what one lane holds of S^T after the first product (4 tokens of one row per
 // fragment) is what it must supply of P^T to the second, so probabilities
 // never leave their lane.  For that, fragment j of a 64-token tile takes its 16
 // tokens in the order 16 (m / 4) + 4 j + m % 4: lane group g (l / 16) then owns
-// tokens 16 g .. 16 g + 15 of the tile, one 16-byte load of each value row.
+// tokens 16 g .. 16 g + 15 of the tile, 16 consecutive values of each value row.
 //
-// Softmax statistics are fp32; probabilities are rounded to bf16 for the
-// second product (at most 2^-8 each, independent of each other), their sum is not.
+// Softmax statistics are fp32.  Probabilities are rounded to fp16 for the
+// second product (11 bits, an eighth of the output's own rounding), times the
+// value scale: with s a key's score and c its value scale, the running maximum
+// is that of s + log2 c, so the weights 2^15 c exp2(s - max) lie in [0, 2^15]
+// and keep all their bits down to 2^-29 of the largest.
 #include "serve.hpp"
 #include "trace.hpp"
 
@@ -24,6 +28,12 @@ namespace {
 
 constexpr int kTile = 64;  // tokens per step
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kBoost = 32768.0f;     // largest weight
+constexpr float kMinScale = 0x1p-100f;  // of values: a block of zeros has scale 0
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct AttnArgs {
   moe_kv_cache c;
@@ -34,19 +44,38 @@ struct AttnArgs {
   int64_t ldo;
   int heads, group;   // query heads, and per kv head
   int max_q, max_kv;
-  int row_tiles;      // 16-row tiles per request and kv head
-  int chunk, chunks;  // tokens per workgroup, chunks per row tile
-  float scale2;       // scale log2(e)
+  int chunk, chunks;  // keys per workgroup, workgroups per row tile
+  float scale2;       // |scale| log2(e)
+  bool negative;      // scale < 0: the queries change sign
   bool causal;
-  float* part_o;      // [items][16][D]
-  float* part_ml;     // [items][16][2]
+  float* part_o;      // [items][rows][D]
+  float* part_ml;     // [items][rows][2]
 };
 
-// 8 int8 -> 8 bf16 (exact).
-__device__ __forceinline__ uint4 bf16_of(uint32_t lo, uint32_t hi) {
-  auto f = [](uint32_t w, int i) { return static_cast<float>(static_cast<int8_t>(w >> (8 * i))); };
-  return make_uint4(pack_bf16x2(f(lo, 0), f(lo, 1)), pack_bf16x2(f(lo, 2), f(lo, 3)), pack_bf16x2(f(hi, 0), f(hi, 1)),
-                    pack_bf16x2(f(hi, 2), f(hi, 3)));
+__device__ __forceinline__ f32x4 mfma_f16(const uint4& p, const uint4& q, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p), __builtin_bit_cast(f16x8, q), acc, 0, 0,
+                                                0);
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+}
+
+// 8 int8 -> 8 fp16 (exact): byte + 128 becomes the low bits of 1024 + (byte + 128).
+__device__ __forceinline__ uint4 f16_of(uint32_t lo, uint32_t hi) {
+  const f16x2 bias = {static_cast<_Float16>(-1152.0f), static_cast<_Float16>(-1152.0f)};
+  auto two = [&](uint32_t w, uint32_t sel) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, sel)) + bias);
+  };
+  lo ^= 0x80808080u;
+  hi ^= 0x80808080u;
+  return make_uint4(two(lo, 0x04010400u), two(lo, 0x04030402u), two(hi, 0x04010400u), two(hi, 0x04030402u));
+}
+
+// 8 bf16 times f -> 8 fp16.
+__device__ __forceinline__ uint4 f16_of_bf16(const uint4& v, float f) {
+  return make_uint4(pack_f16(lo_bf(v.x) * f, hi_bf(v.x) * f), pack_f16(lo_bf(v.y) * f, hi_bf(v.y) * f),
+                    pack_f16(lo_bf(v.z) * f, hi_bf(v.z) * f), pack_f16(lo_bf(v.w) * f, hi_bf(v.w) * f));
 }
 
 // Rows of one request and the keys they see.
@@ -55,11 +84,12 @@ struct Request {
   int kv, pos0;        // tokens in the cache, position of the first new token
 };
 
+__device__ __forceinline__ int row_start(const AttnArgs& p, int i) { return min(max(p.b.row_start[i], 0), p.b.T); }
+
 __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
-  auto start = [&](int i) { return min(max(p.b.row_start[i], 0), p.b.T); };
   Request r;
-  r.first = start(b);
-  const int all = max(start(b + 1) - r.first, 0), len = p.b.kv_len[b];
+  r.first = row_start(p, b);
+  const int all = max(row_start(p, b + 1) - r.first, 0), len = p.b.kv_len[b];
   r.n = min(all, p.max_q);
   r.rows = r.n * p.group;
   r.kv = max(0, min(min(len, p.max_kv), p.b.W * p.c.block_tokens));
@@ -72,36 +102,138 @@ __device__ __forceinline__ int key_limit(const AttnArgs& p, const Request& r, in
   return p.causal ? min(r.kv, r.pos0 + i + 1) : r.kv;
 }
 
-// One workgroup: 16 rows against one chunk of keys; its four waves take the
-// chunk's 64-token steps in turn and merge at the end.
+// Few rows (at most kFew: single tokens, or a few of one kv head): one
+// workgroup per request, kv head and chunk of keys; its four waves take the
+// chunk's 64-token steps in turn, each key read once into registers, and merge
+// at the end.
+constexpr int kFew = 16;
+// More: kMany rows per workgroup, 32 per wave; keys and values pass through LDS
+// as fp16.
+constexpr int kMany = 128;
+
+// Unit u of the row tiles of many rows: its request and tile.  A request whose
+// rows start at packed row s owns units s g / kMany + b and following.
+struct Unit {
+  int b, tile;
+};
+__device__ __forceinline__ Unit row_unit(const AttnArgs& p, int u) {
+  auto at = [&](int m) { return static_cast<int>(static_cast<int64_t>(row_start(p, m)) * p.group / kMany) + m; };
+  int lo = 0, hi = p.b.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (at(mid) <= u) lo = mid;
+    else hi = mid;
+  }
+  return {lo, u - at(lo)};
+}
+
+// Query fragments of one row, slices of 8 dims from dim(i), and the factor
+// that turns a product with them into the score's base-2 exponent.
+template <int N, class Dim>
+__device__ __forceinline__ float load_query(const AttnArgs& p, const bf16_t* row, Dim dim, uint4 (&f)[N]) {
+  uint4 v[N];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = *reinterpret_cast<const uint4*>(row + dim(i));
+    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, max(w[j] & 0x7f800000u, (w[j] << 16) & 0x7f800000u));
+  }
+  m = max(m, static_cast<uint32_t>(shfl_xor(static_cast<int>(m), 16)));
+  m = max(m, static_cast<uint32_t>(shfl_xor(static_cast<int>(m), 32)));
+  // 2^e of the largest magnitude, kept where 2^e and 2^-e are normal (a row
+  // with an infinity stays infinite)
+  const uint32_t e = min(max(m >> 23, 1u), 253u);
+  const float down = __uint_as_float((254u - e) << 23);
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = f16_of_bf16(v[i], p.negative ? -down : down);
+  return __uint_as_float(e << 23) * p.scale2;
+}
+
+// One row's softmax state, and its update by the 16 scores s[j][i] c that a
+// lane holds of it: on return s holds the weights, and `shrink` what earlier
+// sums must be multiplied by.  `first` is the token of s[0][0].
+struct Softmax {
+  float m = -INFINITY, l = 0.0f;
+  template <bool kMask>
+  __device__ __forceinline__ float update(f32x4 (&s)[4], float c, float vs, int first, int limit) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (kMask && first + 4 * j + i >= limit) s[j][i] = -INFINITY;
+        top = fmaxf(top, s[j][i]);
+      }
+    if (kMask) {  // a block that the row does not see may hold anything
+      if (first >= limit) c = vs = 1.0f;
+    }
+    vs = fmaxf(vs, kMinScale) + (vs != vs ? vs : 0.0f);
+    // c >= 0; a masked score stays -infinity where c is 0
+    top = top == -INFINITY ? -INFINITY : fmaf(top, c, __builtin_amdgcn_logf(vs));
+    top = fmaxf(top, shfl_xor(top, 16));
+    top = fmaxf(top, shfl_xor(top, 32));
+    const float m1 = fmaxf(m, top);
+    const float base = m1 == -INFINITY ? 0.0f : m1;  // no key seen yet: every term is 0
+    const float shrink = __builtin_amdgcn_exp2f(m - base);
+    m = m1;
+    const float w = vs * kBoost;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float e = __builtin_amdgcn_exp2f(fmaf(s[j][i], c, -base));
+        if (kMask && first + 4 * j + i >= limit) e = 0.0f;
+        sum += e;
+        s[j][i] = e * w;
+      }
+    l = fmaf(l, shrink, sum);
+    return shrink;
+  }
+};
+
+// Weights of 16 tokens as the second product's operand.
+__device__ __forceinline__ void pack_weights(const f32x4 (&s)[4], uint4 (&pf)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    pf[i] = make_uint4(pack_f16(s[2 * i][0], s[2 * i][1]), pack_f16(s[2 * i][2], s[2 * i][3]),
+                       pack_f16(s[2 * i + 1][0], s[2 * i + 1][1]), pack_f16(s[2 * i + 1][2], s[2 * i + 1][3]));
+}
+
+// Row r of the request and kv head in the output.
+__device__ __forceinline__ bf16_t* out_row(const AttnArgs& p, const Request& rq, int h, int r, int D) {
+  return p.out + static_cast<int64_t>(rq.first + r / p.group) * p.ldo + (h * p.group + r % p.group) * D;
+}
+
+// Factor that turns a row's sums into its output (0 for a row without a key).
+__device__ __forceinline__ float normaliser(float l) { return l == 0.0f ? 0.0f : 1.0f / (l * kBoost); }
+
 template <int D>
 __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
   constexpr int kP = D / 64, kDt = D / 16;
   __shared__ float lds_o[4][16][D];
   __shared__ float lds_m[4][16], lds_l[4][16];
-  const int chunk = blockIdx.x % p.chunks, rt = blockIdx.x / p.chunks % p.row_tiles;
-  const int b = blockIdx.x / p.chunks / p.row_tiles, h = blockIdx.y;
+  const int chunk = blockIdx.x % p.chunks, b = blockIdx.x / p.chunks, h = blockIdx.y;
   const Request rq = request(p, b);
-  const int r0 = rt * 16;
-  if (r0 >= rq.rows) return;
+  if (rq.rows == 0 || rq.rows > kFew) return;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, g = lane >> 4;
   const int t0 = chunk * p.chunk;
-  const int t1 = min(t0 + p.chunk, key_limit(p, rq, min(r0 + 15, rq.rows - 1) / p.group));
+  const int t1 = min(t0 + p.chunk, key_limit(p, rq, rq.n - 1));
   if (t0 >= t1 && chunk > 0) return;
   const int bt = p.c.block_tokens, shift = __builtin_ctz(bt);
 
-  // this lane's row
-  const int row = min(r0 + (lane & 15), rq.rows - 1);
-  const int tok = row / p.group, head = h * p.group + row % p.group;
+  // this lane's row; dims 64 i + 16 g + 8 s of slice (i, s): the order in which
+  // one 16-byte load of a key supplies two slices
+  const int row = min(lane & 15, rq.rows - 1);
+  const int tok = row / p.group;
   const int limit = key_limit(p, rq, tok);
-  uint4 qf[kP][2];
-  const bf16_t* qrow = p.q + (rq.first + tok) * p.ldq + head * D;
-#pragma unroll
-  for (int i = 0; i < kP; ++i)
-#pragma unroll
-    for (int s = 0; s < 2; ++s) qf[i][s] = *reinterpret_cast<const uint4*>(qrow + 64 * i + 16 * g + 8 * s);
+  uint4 qf[2 * kP];
+  const float c = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
+                             [&](int i) { return 64 * (i >> 1) + 16 * g + 8 * (i & 1); }, qf);
 
-  float m = -INFINITY, l = 0.0f;
+  Softmax sm;
   f32x4 o[kDt];
 #pragma unroll
   for (int d = 0; d < kDt; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -125,168 +257,384 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
       for (int i = 0; i < kP; ++i) kf[j][i] = *reinterpret_cast<const uint4*>(kp + 4 * j * D + 64 * i);
 #pragma unroll
     for (int d = 0; d < kDt; ++d) vf[d] = *reinterpret_cast<const uint4*>(vp + d * 16 * bt);
-    const float ks = p.c.k_scale[pv] * p.scale2, vs = p.c.v_scale[pv];
+    const float ks = p.c.k_scale[pv], vs = p.c.v_scale[pv];
 
-    float sc[4][4];
-    float top = -INFINITY;
+    f32x4 s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kP; ++i) {
-        acc = mfma16x16x32(bf16_of(kf[j][i].x, kf[j][i].y), qf[i][0], acc);
-        acc = mfma16x16x32(bf16_of(kf[j][i].z, kf[j][i].w), qf[i][1], acc);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[j][i] = seen && t + 16 * g + 4 * j + i < limit ? acc[i] * ks : -INFINITY;
-        top = fmaxf(top, sc[j][i]);
+        s[j] = mfma_f16(f16_of(kf[j][i].x, kf[j][i].y), qf[2 * i], s[j]);
+        s[j] = mfma_f16(f16_of(kf[j][i].z, kf[j][i].w), qf[2 * i + 1], s[j]);
       }
     }
-    top = fmaxf(top, shfl_xor(top, 16));
-    top = fmaxf(top, shfl_xor(top, 32));
-    const float m1 = fmaxf(m, top);
-    const float base = m1 == -INFINITY ? 0.0f : m1;  // no key seen yet: every term is 0
-    const float shrink = exp2f(m - base);
-    m = m1;
-    l *= shrink;
-#pragma unroll
-    for (int d = 0; d < kDt; ++d) o[d] *= shrink;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e = exp2f(sc[j][i] - base);
-        l += e;
-        sc[j][i] = e == 0.0f ? 0.0f : e * vs;  // a masked place stays 0 whatever its scale
-      }
+    const float shrink = sm.update<true>(s, ks * c, vs, t + 16 * g, seen ? limit : 0);
     uint4 pf[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-      pf[s] = make_uint4(pack_bf16x2(sc[2 * s][0], sc[2 * s][1]), pack_bf16x2(sc[2 * s][2], sc[2 * s][3]),
-                         pack_bf16x2(sc[2 * s + 1][0], sc[2 * s + 1][1]), pack_bf16x2(sc[2 * s + 1][2], sc[2 * s + 1][3]));
+    pack_weights(s, pf);
 #pragma unroll
     for (int d = 0; d < kDt; ++d) {
-      o[d] = mfma16x16x32(bf16_of(vf[d].x, vf[d].y), pf[0], o[d]);
-      o[d] = mfma16x16x32(bf16_of(vf[d].z, vf[d].w), pf[1], o[d]);
+      o[d] *= shrink;
+      o[d] = mfma_f16(f16_of(vf[d].x, vf[d].y), pf[0], o[d]);
+      o[d] = mfma_f16(f16_of(vf[d].z, vf[d].w), pf[1], o[d]);
     }
   }
-  l += shfl_xor(l, 16);
-  l += shfl_xor(l, 32);
+  sm.l += shfl_xor(sm.l, 16);
+  sm.l += shfl_xor(sm.l, 32);
 
   // merge the waves: o[d][i] is dimension 16 d + 4 g + i of row lane % 16
   if (lane < 16) {
-    lds_m[wv][lane] = m;
-    lds_l[wv][lane] = l;
+    lds_m[wv][lane] = sm.m;
+    lds_l[wv][lane] = sm.l;
   }
 #pragma unroll
   for (int d = 0; d < kDt; ++d) *reinterpret_cast<f32x4*>(&lds_o[wv][lane & 15][16 * d + 4 * g]) = o[d];
   __syncthreads();
   constexpr int kPer = D / 16;  // dimensions per thread
   const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kPer;
-  if (r0 + r >= rq.rows) return;
+  if (r >= rq.rows) return;
   float mm = -INFINITY, ll = 0.0f, acc[kPer] = {};
 #pragma unroll
   for (int w = 0; w < 4; ++w) mm = fmaxf(mm, lds_m[w][r]);
   const float base = mm == -INFINITY ? 0.0f : mm;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const float f = exp2f(lds_m[w][r] - base);
+    const float f = __builtin_amdgcn_exp2f(lds_m[w][r] - base);
     ll += f * lds_l[w][r];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] += f * lds_o[w][r][d0 + i];
   }
   if (p.chunks == 1) {
-    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-    bf16_t* dst = p.out + (rq.first + (r0 + r) / p.group) * p.ldo + (h * p.group + (r0 + r) % p.group) * D + d0;
+    const float inv = normaliser(ll);
+    bf16_t* dst = out_row(p, rq, h, r, D) + d0;
 #pragma unroll
     for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
     return;
   }
-  const int64_t item = (static_cast<int64_t>(b) * p.c.kv_heads + h) * p.row_tiles * p.chunks + rt * p.chunks + chunk;
+  const int64_t at = ((static_cast<int64_t>(b) * p.c.kv_heads + h) * p.chunks + chunk) * kFew + r;
   if ((threadIdx.x & 15) == 0) {
-    p.part_ml[(item * 16 + r) * 2] = mm;
-    p.part_ml[(item * 16 + r) * 2 + 1] = ll;
+    p.part_ml[at * 2] = mm;
+    p.part_ml[at * 2 + 1] = ll;
   }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) p.part_o[(item * 16 + r) * D + d0 + i] = acc[i];
+  for (int i = 0; i < kPer; ++i) p.part_o[at * D + d0 + i] = acc[i];
 }
 
-// One workgroup per 16 rows: the chunks joined in order.
 template <int D>
+__global__ __launch_bounds__(256, 2) void k_kv_attention_rows(AttnArgs p) {
+  constexpr int kS = D / 32, kDt = D / 16;
+  // keys [64][D], chunks of 8 dims XOR-swizzled; values [D][64], likewise
+  __shared__ __attribute__((aligned(16))) uint4 lds_k[2][kTile * D / 8];
+  __shared__ __attribute__((aligned(16))) uint4 lds_v[2][kTile * D / 8];
+  const int chunk = blockIdx.x % p.chunks, h = blockIdx.y;
+  const Unit unit = row_unit(p, blockIdx.x / p.chunks);
+  const Request rq = request(p, unit.b);
+  const int tiles = cdiv(rq.rows, kMany);
+  if (rq.rows <= kFew || unit.tile < 0 || unit.tile >= tiles) return;
+  const int r0 = (tiles - 1 - unit.tile) * kMany;  // the longest rows first
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4;
+  const int t0 = chunk * p.chunk;
+  const int t1 = min(t0 + p.chunk, key_limit(p, rq, min(r0 + kMany - 1, rq.rows - 1) / p.group));
+  if (t0 >= t1 && chunk > 0) return;
+  const int bt = p.c.block_tokens, shift = __builtin_ctz(bt);
+
+  // this lane's rows, one per 16-row block of the wave
+  int limit[2];
+  float c[2];
+  uint4 qf[2][kS];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int row = min(r0 + wv * 32 + n * 16 + (lane & 15), rq.rows - 1), tok = row / p.group;
+    limit[n] = key_limit(p, rq, tok);
+    c[n] = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
+                      [&](int i) { return 32 * i + 8 * g; }, qf[n]);
+  }
+  // keys below this are seen by every row of the wave
+  const int all_see = key_limit(p, rq, min(r0 + wv * 32, rq.rows - 1) / p.group);
+
+  const int32_t* table = p.b.block_table + static_cast<int64_t>(unit.b) * p.b.W;
+  const int last = p.b.W - 1;
+  // Staging: thread tid copies keys of tokens tk, tk + tk_step (16 dims from
+  // 16 ck) and values of dims dv, dv + 64 (16 tokens from 16 cv).
+  constexpr int kK = D / 64;  // passes
+  constexpr int kTokStep = 256 / (D / 16);
+  const int tk = tid / (D / 16), ck = tid % (D / 16), dv = tid >> 2, cv = tid & 3;
+  auto place = [&](int t) {  // block of token t, -1: none
+    const int i = t >> shift;
+    const int id = table[min(i, last)];
+    return i <= last && id >= 0 && id < p.c.n_blocks ? id : -1;
+  };
+  struct Ids {
+    int k[kK], v, own;
+  };
+  auto load_ids = [&](int t) {
+    Ids x;
+#pragma unroll
+    for (int i = 0; i < kK; ++i) x.k[i] = place(t + tk + i * kTokStep);
+    x.v = place(t + 16 * cv);
+    x.own = place(t + 16 * g);
+    return x;
+  };
+  uint4 kreg[kK] = {}, vreg[kK] = {};
+  float ks = 0.0f, vs = 0.0f;
+  bool seen = false;
+  auto load_tile = [&](int t, const Ids& x) {
+#pragma unroll
+    for (int i = 0; i < kK; ++i) {
+      const int64_t at = static_cast<int64_t>(max(x.k[i], 0)) * p.c.kv_heads + h;
+      kreg[i] = *reinterpret_cast<const uint4*>(p.c.k + at * bt * D + ((t + tk + i * kTokStep) & (bt - 1)) * D + 16 * ck);
+    }
+    const int64_t at = static_cast<int64_t>(max(x.v, 0)) * p.c.kv_heads + h;
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+      vreg[i] = *reinterpret_cast<const uint4*>(p.c.v + at * bt * D + (dv + 64 * i) * bt + ((t + 16 * cv) & (bt - 1)));
+    const int64_t own = static_cast<int64_t>(max(x.own, 0)) * p.c.kv_heads + h;
+    ks = p.c.k_scale[own];
+    vs = p.c.v_scale[own];
+    seen = x.own >= 0;
+  };
+  // Rows of one key fragment (tokens 16 (m / 4) + 4 j + m % 4) and of one value
+  // fragment (16 consecutive dims) lie in distinct banks.
+  auto k_at = [&](int tok, int chunk8) { return tok * (D / 8) + (chunk8 ^ ((((tok >> 4) << 2) | (tok & 3)) & (D / 8 - 1))); };
+  auto v_at = [&](int dim, int chunk8) { return dim * 8 + (chunk8 ^ ((dim >> 1) & 7)); };
+  auto store_tile = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kK; ++i) {
+      lds_k[buf][k_at(tk + i * kTokStep, 2 * ck)] = f16_of(kreg[i].x, kreg[i].y);
+      lds_k[buf][k_at(tk + i * kTokStep, 2 * ck + 1)] = f16_of(kreg[i].z, kreg[i].w);
+      lds_v[buf][v_at(dv + 64 * i, 2 * cv)] = f16_of(vreg[i].x, vreg[i].y);
+      lds_v[buf][v_at(dv + 64 * i, 2 * cv + 1)] = f16_of(vreg[i].z, vreg[i].w);
+    }
+  };
+
+  Softmax sm[2];
+  f32x4 o[2][kDt];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int d = 0; d < kDt; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  Ids ids = load_ids(t0);
+  if (t0 < t1) load_tile(t0, ids);
+  ids = load_ids(t0 + kTile);
+  store_tile(0);
+  float ks_now = ks, vs_now = vs;
+  bool seen_now = seen;
+  int buf = 0;
+  for (int t = t0; t < t1; t += kTile, buf ^= 1) {
+    __syncthreads();
+    const bool more = t + kTile < t1;
+    if (more) {
+      load_tile(t + kTile, ids);
+      ids = load_ids(t + 2 * kTile);
+    }
+    f32x4 s[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int m = lane & 15;
+#pragma unroll
+    for (int i = 0; i < kS; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint4 kf = lds_k[buf][k_at(16 * (m >> 2) + 4 * j + (m & 3), 4 * i + g)];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) s[n][j] = mfma_f16(kf, qf[n][i], s[n][j]);
+      }
+    uint4 pf[2][2];
+    float shrink[2];
+    const bool mask = t + kTile > all_see || __any(!seen_now);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      shrink[n] = mask ? sm[n].update<true>(s[n], ks_now * c[n], vs_now, t + 16 * g, seen_now ? limit[n] : 0)
+                       : sm[n].update<false>(s[n], ks_now * c[n], vs_now, 0, 0);
+      pack_weights(s[n], pf[n]);
+    }
+    if (__any(shrink[0] != 1.0f || shrink[1] != 1.0f)) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int d = 0; d < kDt; ++d) o[n][d] *= shrink[n];
+    }
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 vf = lds_v[buf][v_at(16 * d + m, 2 * g + i)];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) o[n][d] = mfma_f16(vf, pf[n][i], o[n][d]);
+      }
+    if (more) {
+      store_tile(buf ^ 1);
+      ks_now = ks;
+      vs_now = vs;
+      seen_now = seen;
+    }
+  }
+
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    float l = sm[n].l;
+    l += shfl_xor(l, 16);
+    l += shfl_xor(l, 32);
+    const int r = r0 + wv * 32 + n * 16 + (lane & 15);
+    if (r >= rq.rows) continue;
+    if (p.chunks == 1) {
+      const float inv = normaliser(l);
+      bf16_t* dst = out_row(p, rq, h, r, D) + 4 * g;
+#pragma unroll
+      for (int d = 0; d < kDt; ++d)
+        *reinterpret_cast<uint2*>(dst + 16 * d) = make_uint2(pack_bf16x2(o[n][d][0] * inv, o[n][d][1] * inv),
+                                                             pack_bf16x2(o[n][d][2] * inv, o[n][d][3] * inv));
+      continue;
+    }
+    const int64_t at =
+        ((static_cast<int64_t>(blockIdx.x / p.chunks) * p.c.kv_heads + h) * p.chunks + chunk) * kMany + (r - r0);
+    if (g == 0) {
+      p.part_ml[at * 2] = sm[n].m;
+      p.part_ml[at * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < kDt; ++d) *reinterpret_cast<f32x4*>(p.part_o + at * D + 16 * d + 4 * g) = o[n][d];
+  }
+}
+
+// The chunks of a row joined in order: 16 threads per row, 16 rows per
+// workgroup; kRows rows per row tile of the kernel that wrote them.
+template <int D, int kRows>
 __global__ __launch_bounds__(256) void k_kv_combine(AttnArgs p) {
   constexpr int kPer = D / 16;
-  const int rt = blockIdx.x % p.row_tiles, b = blockIdx.x / p.row_tiles, h = blockIdx.y;
-  const Request rq = request(p, b);
-  const int r0 = rt * 16, r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kPer;
-  if (r0 + r >= rq.rows) return;
-  const int limit = key_limit(p, rq, min(r0 + 15, rq.rows - 1) / p.group);
+  const int h = blockIdx.y;
+  const Unit unit = kRows == kFew ? Unit{static_cast<int>(blockIdx.x), 0} : row_unit(p, blockIdx.x);
+  const Request rq = request(p, unit.b);
+  const int tiles = cdiv(rq.rows, kRows);
+  if ((kRows == kFew) != (rq.rows <= kFew) || unit.tile < 0 || unit.tile >= tiles) return;
+  const int r0 = (tiles - 1 - unit.tile) * kRows;
+  const int i = blockIdx.z * 16 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * kPer;
+  const int r = r0 + i;
+  if (r >= rq.rows) return;
+  const int limit = key_limit(p, rq, min(r0 + kRows - 1, rq.rows - 1) / p.group);
   const int n = max(1, min(p.chunks, cdiv(limit, p.chunk)));
-  const int64_t item = ((static_cast<int64_t>(b) * p.c.kv_heads + h) * p.row_tiles + rt) * p.chunks;
+  const int64_t at = (static_cast<int64_t>(blockIdx.x) * p.c.kv_heads + h) * p.chunks * kRows + i;
+  const float* ml = p.part_ml + at * 2;
   float mm = -INFINITY;
-  for (int c = 0; c < n; ++c) mm = fmaxf(mm, p.part_ml[((item + c) * 16 + r) * 2]);
+  for (int c = 0; c < n; ++c) mm = fmaxf(mm, ml[c * kRows * 2]);
   const float base = mm == -INFINITY ? 0.0f : mm;
   float ll = 0.0f, acc[kPer] = {};
+  const float* po = p.part_o + at * D + d0;
+#pragma unroll 4
   for (int c = 0; c < n; ++c) {
-    const int64_t at = (item + c) * 16 + r;
-    const float f = exp2f(p.part_ml[at * 2] - base);
-    ll += f * p.part_ml[at * 2 + 1];
+    const float f = __builtin_amdgcn_exp2f(ml[c * kRows * 2] - base);
+    ll += f * ml[c * kRows * 2 + 1];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += f * p.part_o[at * D + d0 + i];
+    for (int x = 0; x < kPer; x += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(po + static_cast<int64_t>(c) * kRows * D + x);
+      acc[x] += f * v.x;
+      acc[x + 1] += f * v.y;
+      acc[x + 2] += f * v.z;
+      acc[x + 3] += f * v.w;
+    }
   }
-  const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-  bf16_t* dst = p.out + (rq.first + (r0 + r) / p.group) * p.ldo + (h * p.group + (r0 + r) % p.group) * D + d0;
+  const float inv = normaliser(ll);
+  bf16_t* dst = out_row(p, rq, h, r, D) + d0;
 #pragma unroll
-  for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
+  for (int x = 0; x < kPer; x += 2) *reinterpret_cast<uint32_t*>(dst + x) = pack_bf16x2(acc[x] * inv, acc[x + 1] * inv);
 }
 
+// How the keys are split over workgroups: about `want` workgroups in all,
+// at least `least` keys each.  More than one chunk only while the row tiles
+// are fewer than `want`, so there are at most 2 `want` partial results.
 struct Split {
-  int row_tiles, chunk, chunks;
+  int64_t tiles;  // row tiles, times kv heads
+  int chunk, chunks;
+  int64_t items() const { return chunks > 1 ? tiles * chunks : 0; }
 };
 
-// Keys per workgroup: about kItems workgroups in all (12 per CU: enough for
-// lengths to even out), at least 256 keys each.  Where a row tile has more
-// than one chunk there are fewer than kItems row tiles, so at most 2 kItems
-// partial results.
-constexpr int kItems = 3072;
-
-Split split(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
+Split split(int64_t tiles, int64_t max_kv, int want, int least) {
   Split s;
+  s.tiles = tiles;
+  const int64_t per = max_kv * tiles / want;
+  s.chunk = static_cast<int>(cdiv64(per < least ? least : per, least) * least);
+  s.chunks = static_cast<int>(cdiv64(max_kv, s.chunk));
+  return s;
+}
+
+constexpr int kFewItems = 3072, kFewLeast = 256;
+constexpr int kManyItems = 1024, kManyLeast = 512;
+
+struct Plan {
+  bool many;  // some request may have more than kFew rows
+  int units;  // row tiles of those
+  Split few, rows;
+};
+
+Plan plan(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
   const int64_t places = static_cast<int64_t>(b.W) * c.block_tokens;
   const int64_t max_kv = a.max_kv < places ? a.max_kv : places;
-  s.row_tiles = cdiv((a.max_q < b.T ? a.max_q : b.T) * (a.heads / c.kv_heads), 16);
-  const int64_t tiles = static_cast<int64_t>(s.row_tiles) * b.B * c.kv_heads;
-  const int64_t per = max_kv * tiles / kItems;
-  s.chunk = static_cast<int>(cdiv64(per < 256 ? 256 : per, 256) * 256);
-  s.chunks = static_cast<int>(cdiv64(max_kv < 1 ? 1 : max_kv, s.chunk));
-  return s;
+  const int64_t group = a.heads / c.kv_heads;
+  Plan p;
+  p.many = (a.max_q < b.T ? a.max_q : b.T) * group > kFew;
+  p.units = static_cast<int>(b.T * group / kMany) + b.B;
+  p.few = split(static_cast<int64_t>(b.B) * c.kv_heads, max_kv, kFewItems, kFewLeast);
+  p.rows = split(static_cast<int64_t>(p.units) * c.kv_heads, max_kv, kManyItems, kManyLeast);
+  return p;
+}
+
+template <int D>
+void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
+  const int heads = p.c.kv_heads;
+  if (pl.many) {
+    p.chunk = pl.rows.chunk;
+    p.chunks = pl.rows.chunks;
+    p.part_o = ws;
+    p.part_ml = ws + pl.rows.items() * kMany * D;
+    ws = p.part_ml + pl.rows.items() * kMany * 2;
+    {
+      TraceScope trace_scope(K_KV_ATTENTION, s);
+      hipLaunchKernelGGL(k_kv_attention_rows<D>, dim3(pl.units * p.chunks, heads), dim3(256), 0, s, p);
+    }
+    if (p.chunks > 1) {
+      TraceScope trace_scope(K_KV_COMBINE, s);
+      hipLaunchKernelGGL((k_kv_combine<D, kMany>), dim3(pl.units, heads, kMany / 16), dim3(256), 0, s, p);
+    }
+  }
+  p.chunk = pl.few.chunk;
+  p.chunks = pl.few.chunks;
+  p.part_o = ws;
+  p.part_ml = ws + pl.few.items() * kFew * D;
+  {
+    TraceScope trace_scope(K_KV_ATTENTION, s);
+    hipLaunchKernelGGL(k_kv_attention<D>, dim3(p.b.B * p.chunks, heads), dim3(256), 0, s, p);
+  }
+  if (p.chunks > 1) {
+    TraceScope trace_scope(K_KV_COMBINE, s);
+    hipLaunchKernelGGL((k_kv_combine<D, kFew>), dim3(p.b.B, heads, 1), dim3(256), 0, s, p);
+  }
 }
 
 }  // namespace
 
-size_t kv_attention_ws(const moe_kv_cache& c) {
-  return static_cast<size_t>(2 * kItems) * 16 * (c.head_dim + 2) * sizeof(float);
+// An upper bound that does not shrink with T, W or max_kv, so that one
+// workspace serves every smaller batch.
+size_t kv_attention_ws(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
+  const Plan p = plan(c, b, a);
+  auto items = [&](const Split& s, int64_t want, int64_t least) {
+    const int64_t all = s.tiles * cdiv64(a.max_kv, least);
+    return all < 2 * want ? all : 2 * want;
+  };
+  int64_t rows = items(p.few, kFewItems, kFewLeast) * kFew;
+  if (p.many) rows += items(p.rows, kManyItems, kManyLeast) * kMany;
+  return static_cast<size_t>(rows) * (c.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_kv_attention(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a, const bf16_t* q,
                                int64_t ldq, bf16_t* out, int64_t ldo, void* ws, hipStream_t s) {
-  const Split sp = split(c, b, a);
-  const int64_t items = static_cast<int64_t>(sp.row_tiles) * sp.chunks * b.B * c.kv_heads;
-  AttnArgs p{c, b, q, ldq, out, ldo, a.heads, a.heads / c.kv_heads, a.max_q, a.max_kv, sp.row_tiles, sp.chunk, sp.chunks,
-             a.scale * kLog2e, (a.flags & MOE_F_CAUSAL) != 0, static_cast<float*>(ws), nullptr};
-  p.part_ml = p.part_o + items * 16 * c.head_dim;
-  {
-    TraceScope trace_scope(K_KV_ATTENTION, s);
-    const dim3 grid(sp.row_tiles * sp.chunks * b.B, c.kv_heads);
-    if (c.head_dim == 64) hipLaunchKernelGGL(k_kv_attention<64>, grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(k_kv_attention<128>, grid, dim3(256), 0, s, p);
-  }
-  if (sp.chunks > 1) {
-    TraceScope trace_scope(K_KV_COMBINE, s);
-    const dim3 grid(sp.row_tiles * b.B, c.kv_heads);
-    if (c.head_dim == 64) hipLaunchKernelGGL(k_kv_combine<64>, grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(k_kv_combine<128>, grid, dim3(256), 0, s, p);
-  }
+  const AttnArgs p{c,       b,       q,       ldq, out, ldo, a.heads, a.heads / c.kv_heads,
+                   a.max_q, a.max_kv, 0, 0,   (a.scale < 0 ? -a.scale : a.scale) * kLog2e,
+                   a.scale < 0, (a.flags & MOE_F_CAUSAL) != 0, nullptr, nullptr};
+  if (c.head_dim == 64) launch<64>(p, plan(c, b, a), static_cast<float*>(ws), s);
+  else launch<128>(p, plan(c, b, a), static_cast<float*>(ws), s);
   return hipGetLastError();
 }
 

@@ -55,7 +55,7 @@ hipError_t launch_kv_read(const moe_kv_cache& c, int B, int W, const int32_t* bl
                           int total, bf16_t* k_out, bf16_t* v_out, hipStream_t s);
 
 // ---- attention over it (kv_attention.hip)
-size_t kv_attention_ws(const moe_kv_cache& c);
+size_t kv_attention_ws(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a);
 hipError_t launch_kv_attention(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a, const bf16_t* q,
                                int64_t ldq, bf16_t* out, int64_t ldo, void* ws, hipStream_t s);
 

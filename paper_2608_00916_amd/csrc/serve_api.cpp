@@ -192,10 +192,10 @@ int check_attn(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* 
   if (a->max_q < 1 || a->max_kv < 1) return fail(MOE_ERR_ARG, "max_q=%d and max_kv=%d must be positive", a->max_q, a->max_kv);
   if (!std::isfinite(a->scale)) return fail(MOE_ERR_ARG, "scale is not finite");
   if (a->flags & ~MOE_F_CAUSAL) return fail(MOE_ERR_ARG, "unknown flags 0x%x", a->flags);
-  // workgroups are numbered in 32 bits: 16-row tiles, and up to 128 chunks where they are few
-  const int64_t rows = static_cast<int64_t>(std::min(a->max_q, std::max(b->T, 1))) * (a->heads / c->kv_heads);
-  if (rows > (1ll << 30) || cdiv64(rows, 16) * b->B > (1ll << 30))
-    return fail(MOE_ERR_ARG, "max_q=%d x heads=%d x B=%d too large", a->max_q, a->heads, b->B);
+  // workgroups and a request's rows are numbered in 32 bits
+  const int64_t group = a->heads / c->kv_heads;
+  if (std::min(a->max_q, b->T) * group > (1ll << 30) || b->T * group / 16 + b->B > (1ll << 30))
+    return fail(MOE_ERR_ARG, "T=%d x heads=%d too large", b->T, a->heads);
   return MOE_OK;
 }
 
@@ -356,7 +356,7 @@ int moe_kv_read(const moe_kv_cache* c, int32_t B, int32_t W, const int32_t* bloc
 
 size_t moe_kv_attention_workspace_bytes(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* a) {
   if (check_cache(c) != MOE_OK || check_batch_dims(c, b) != MOE_OK || check_attn(c, b, a) != MOE_OK) return 0;
-  return kv_attention_ws(*c);
+  return kv_attention_ws(*c, *b, *a);
 }
 
 int moe_kv_attention(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* a, const void* q, int64_t ldq,
@@ -369,7 +369,7 @@ int moe_kv_attention(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_
   if (int rc = check_pitch("ldq", ldq, row, 8)) return rc;
   if (int rc = check_pitch("ldo", ldo, row, 8)) return rc;
   if (int rc = check_ptrs({{"q", q}, {"out", out}, {"ws", ws}})) return rc;
-  const size_t need = kv_attention_ws(*c);
+  const size_t need = kv_attention_ws(*c, *b, *a);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   return hip_status(launch_kv_attention(*c, *b, *a, static_cast<const bf16_t*>(q), ldq, static_cast<bf16_t*>(out), ldo,
                                         ws, static_cast<hipStream_t>(stream)),
