@@ -1,0 +1,250 @@
+// Core of the int8 products on the gfx950 matrix cores: tiles of
+// C[m][n] = sum_k A[m][k] B[n][k], exact in int32, streamed by persistent
+// workgroups.
+//
+// Both operands are K-contiguous, so a step is 128 bytes of each of a tile's
+// BM + BN rows.  They go straight from global memory into LDS (16 bytes per
+// lane, no registers); v_mfma_i32_16x16x64_i8 takes 16 consecutive k per lane,
+// one ds_read_b128.  A row's eight 16-byte chunks are XOR-swizzled so that the
+// 16 rows of one fragment read lie in distinct banks; the copy into LDS is
+// linear in the lanes, so the swizzle is applied to the global address.
+//
+// The B fragment is fed first, so a lane holds four consecutive fragment rows
+// of B.  Fragment n of a wave takes rows 4 FN (i / 4) + 4 n + i % 4 (i < 16):
+// lane l then holds C[m = l % 16][4 FN (l / 16) + 4 n + i], 4 FN consecutive
+// columns over its FN = 4 fragments, stored 16 bytes at a time.
+//
+// Two LDS stages: the copies of step k + 1 run under the products of step k,
+// and those of the next tile's first step under this tile's last one.  Loads
+// and stores share one in-order counter, so a tile's first step waits for all
+// but the stores of the tile before (whose number is known where the wave's
+// part of it is whole), and they have that step to drain.  What bounds it is the bytes a step must bring from L2
+// for its products, hence the 256 x 256 tile over 8 waves (128 x 64 each):
+// 8192^3 at 2370 TOPS; 128 x 256 reaches 1720, or 2000 with three stages, 128 x
+// 128 over 4 waves 1660.  More, shorter stages (64 bytes of k) are 5% slower.
+//
+// The copies are buffer loads whose resource ends with the operand's last row
+// in the tile: rows past it read zeros, and so do chunks past K, so no load
+// leaves its operand.
+#pragma once
+
+#include "common.hpp"
+
+namespace moe {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kI8Step = 128;  // k per step
+
+__device__ __forceinline__ i32x4 mfma_i8(const uint4& p, const uint4& q, i32x4 acc) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, p), __builtin_bit_cast(i32x4, q), acc, 0, 0,
+                                               0);
+}
+
+// 16 bytes per lane from a buffer resource to LDS at base + 16 lane; offsets at
+// or past the resource's size read zeros (the check covers the per-lane offset
+// only, so all of the offset is in it).
+__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, int8_t* lds_base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds_base), 16,
+                                           static_cast<int>(off), 0, 0, 0);
+}
+
+constexpr uint32_t kI8Oob = 0x80000000u;  // an offset past every resource
+
+// Rows of one operand's tile: contiguous (row r at base + r K, `rows` of them),
+// or, for a gathered A, row r at base + index[r] K.
+struct I8Source {
+  const int8_t* base;
+  int rows;
+  const int32_t* index = nullptr;
+};
+
+// All but the last N of this wave's vector loads (copies into LDS are counted
+// as such) and stores are done.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N < 64, "the counter has 6 bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// All waves are here; LDS reads before it have returned (their products were
+// issued).  Unlike __syncthreads it leaves vector memory in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// BM x BN tile over WM x WN waves.
+template <int BM_, int BN_, int WM_, int WN_>
+struct I8Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int kWaves = WM * WN;
+  static constexpr int kThreads = 64 * kWaves;
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  static constexpr int kRun = 4 * FN;  // consecutive columns a lane holds
+  static constexpr int kStage = (BM + BN) * kI8Step;
+  static constexpr int kCopies = (BM + BN) / 8 / kWaves;  // of 8 rows, per wave and step
+  static constexpr int kCopiesA = BM / 8 / kWaves;
+  static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "rows must split evenly over the waves");
+  static_assert(FN == 4, "a lane holds 16 columns, and the B swizzle separates rows 16 apart");
+};
+
+// Chunk position of chunk c of row r of either operand.  LDS has 64 banks (256
+// bytes, two rows): the XOR separates the row pairs of one fragment.
+__device__ __forceinline__ int a_swizzle(int r, int c) { return c ^ ((r >> 1) & 7); }
+__device__ __forceinline__ int b_swizzle(int r, int c) {  // fragment rows: 4 together, 16 apart
+  return c ^ (((r >> 1) & 1) | (((r >> 4) & 3) << 1));
+}
+
+// Streams tiles blockIdx.x, + gridDim.x, ... of `tiles`.  Job:
+//   Tile tile(int t)              a tile (uniform), with .rows valid rows of A
+//   I8Source a(const Tile&)       the tile's rows of A
+//   I8Source b(const Tile&, int)  of B, part 0 .. kParts - 1: B row q is row
+//   int b_part(q), b_row(q)       b_row(q) of part b_part(q)
+//   void prefetch(const Tile&)    called before the tile's last step
+//   bool kSkip                    waves without a valid row skip the products
+//   void finish(const Tile&, acc) its results; waves without a valid row skip it
+//   bool whole(const Tile&)       every lane of this wave stores all its results:
+//                                 then finish issues kStores stores
+// kGather: rows of A through an index, at 64-bit offsets.
+template <class C, bool kTail, bool kGather, class Job>
+__device__ __forceinline__ void i8_stream(int K, int tiles, Job& job, int8_t* st0, int8_t* st1) {
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wv / C::WN, wn = wv % C::WN;
+  const int steps = cdiv(K, kI8Step);
+  // copy i of this wave covers stage rows 8 (i kWaves + wv) ..: lane / 8, chunk lane % 8
+  auto row0 = [&](int i) { return (i * C::kWaves + wv) * 8; };
+  auto a_chunk = [&](int i) { return a_swizzle(row0(i) + (lane >> 3), lane & 7) * 16; };
+  auto b_chunk = [&](int i) { return b_swizzle(row0(i) - C::BM + (lane >> 3), lane & 7) * 16; };
+  I8Source sa{nullptr, 0}, sb[Job::kParts];
+  const int8_t* gather[kGather ? C::kCopiesA : 1];
+  auto sources = [&](const typename Job::Tile& t) {
+    sa = job.a(t);
+#pragma unroll
+    for (int q = 0; q < Job::kParts; ++q) sb[q] = job.b(t, q);
+    if constexpr (kGather) {
+#pragma unroll
+      for (int i = 0; i < C::kCopiesA; ++i)
+        gather[i] = sa.base + static_cast<int64_t>(sa.index[min(row0(i) + (lane >> 3), sa.rows - 1)]) * K + a_chunk(i);
+    }
+  };
+  auto rsrc = [&](const I8Source& x) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(x.base), 0, x.rows * K, 0x00020000);
+  };
+  auto load = [&](int kt, int8_t* st) {
+    const bool part = kTail && (kt + 1) * kI8Step > K;
+    const __amdgpu_buffer_rsrc_t ra = rsrc(sa);
+    __amdgpu_buffer_rsrc_t rb[Job::kParts];
+#pragma unroll
+    for (int q = 0; q < Job::kParts; ++q) rb[q] = rsrc(sb[q]);
+#pragma unroll
+    for (int i = 0; i < C::kCopies; ++i) {
+      int8_t* dst = st + row0(i) * kI8Step;
+      if (i < C::kCopiesA) {
+        if constexpr (kGather) {
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(gather[i] + kt * kI8Step),
+                                           (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+        } else {
+          uint32_t off = static_cast<uint32_t>((lane >> 3) * K + a_chunk(i) + (row0(i) * K + kt * kI8Step));
+          if (part && kt * kI8Step + a_chunk(i) >= K) off = kI8Oob;
+          copy_to_lds(ra, off, dst);
+        }
+      } else {
+        const int q = row0(i) - C::BM;  // 8 rows of B, of one part
+        const int pt = Job::b_part(q);
+        uint32_t off = static_cast<uint32_t>((lane >> 3) * K + b_chunk(i) + (Job::b_row(q) * K + kt * kI8Step));
+        if (part && kt * kI8Step + b_chunk(i) >= K) off = kI8Oob;
+        copy_to_lds(Job::kParts > 1 && pt ? rb[Job::kParts - 1] : rb[0], off, dst);
+      }
+    }
+  };
+  const int g = lane >> 4, i16 = lane & 15;
+  i32x4 acc[C::FM][C::FN];
+  auto compute = [&](const int8_t* st) {
+    const int8_t* at = st + (wm * C::FM * 16 + i16) * kI8Step;
+    const int brow = C::kRun * (i16 >> 2) + (i16 & 3);
+    const int8_t* bt = st + (C::BM + wn * C::FN * 16 + brow) * kI8Step;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 b[C::FN];
+      const int ca = a_swizzle(i16, s * 4 + g) * 16;
+#pragma unroll
+      for (int n = 0; n < C::FN; ++n)
+        b[n] = *reinterpret_cast<const uint4*>(bt + n * 4 * kI8Step + b_swizzle(brow, s * 4 + g) * 16);
+#pragma unroll
+      for (int m = 0; m < C::FM; ++m) {
+        const uint4 a = *reinterpret_cast<const uint4*>(at + m * 16 * kI8Step + ca);
+#pragma unroll
+        for (int n = 0; n < C::FN; ++n) acc[m][n] = mfma_i8(b[n], a, acc[m][n]);
+      }
+      // the fragments of two rows ahead are read under the products of one
+      if (s == 0) __builtin_amdgcn_sched_group_barrier(0x100, C::FN + 2, 0);
+#pragma unroll
+      for (int m = 0; m < C::FM; ++m) {
+        __builtin_amdgcn_sched_group_barrier(0x008, C::FN, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+    }
+  };
+
+  int t = blockIdx.x;
+  if (t >= tiles) return;
+  typename Job::Tile cur = job.tile(t);
+  sources(cur);
+  load(0, st0);
+  wait_vm<0>();
+  while (true) {
+    typename Job::Tile next = cur;
+    const int tn = t + gridDim.x;
+    auto load_next = [&] {
+      if (tn >= tiles) return;
+      next = job.tile(tn);
+      sources(next);
+      load(0, st0);
+    };
+    const bool live = !Job::kSkip || wm * C::FM * 16 < cur.rows;
+#pragma unroll
+    for (int m = 0; m < C::FM; ++m)
+#pragma unroll
+      for (int n = 0; n < C::FN; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
+    lds_barrier();
+    for (int kt = 0;; kt += 2) {
+      if (kt + 1 < steps) load(kt + 1, st1);
+      else job.prefetch(cur);
+      if (live) compute(st0);
+      if (kt + 1 >= steps) break;
+      wait_vm<0>();
+      lds_barrier();
+      if (kt + 2 < steps) {
+        load(kt + 2, st0);
+      } else {
+        job.prefetch(cur);
+        load_next();
+      }
+      if (live) compute(st1);
+      if (kt + 2 >= steps) break;
+      wait_vm<0>();
+      lds_barrier();
+    }
+    if (steps & 1) {
+      lds_barrier();  // every wave is done with st0
+      load_next();
+    }
+    if (live) job.finish(cur, acc);
+    if (tn >= tiles) break;
+    if (live && job.whole(cur)) wait_vm<Job::kStores>();
+    else wait_vm<0>();
+    t = tn;
+    cur = next;
+  }
+}
+
+// Tile i of n in the order of the XCDs: workgroups go to the 8 XCDs in turn,
+// and each XCD takes a contiguous run of tiles.
+__device__ __forceinline__ int xcd_order(int i, int n) {
+  const int x = i & 7, per = n >> 3, rest = n & 7;
+  return x * per + min(x, rest) + (i >> 3);
+}
+
+}  // namespace moe

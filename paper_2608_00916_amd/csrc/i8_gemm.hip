@@ -1,19 +1,7 @@
-// Products of int8 rows on the gfx950 matrix cores: C[m][n] = sum_k A[m][k]
-// B[n][k], exact in int32, scaled by one factor per row of A and of B.
-//
-// Both operands are K-contiguous, so a tile step is KB bytes of each of its
-// BM + BN rows.  They go straight from global memory into LDS (16 bytes per
-// lane); v_mfma_i32_16x16x64_i8 takes 16 consecutive k per lane, one
-// ds_read_b128.  A row's 16-byte chunks are XOR-swizzled so that the 16 rows
-// of one fragment read lie in distinct banks; the copy into LDS is linear in
-// the lanes, so the swizzle is applied to the global address instead.
-//
-// Rows past the last one read that row again (their results are not stored),
-// and chunks past K are cleared in the A fragments of the last step, so no
-// load leaves its operand.
-//
-// The B fragment is fed first: lane l then holds C[m = l % 16][n = 4 (l / 16)
-// + i], four consecutive columns of one row.
+// Products of int8 rows: dense, few rows (each weight read once, straight into
+// registers), and grouped over the experts.
+#include "i8_core.hpp"
+#include "i8_round.hpp"
 #include "serve.hpp"
 #include "trace.hpp"
 
@@ -21,322 +9,507 @@ namespace moe {
 
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
+// ---------------------------------------------------------------- dense
+struct DenseArgs {
+  const int8_t* a;
+  const float* sa;
+  const int8_t* b;
+  const float* sb;
+  int M, N, K;
+  void* out;
+  int64_t ldo;
+};
 
-__device__ __forceinline__ i32x4 mfma_i8(const uint4& p, const uint4& q, i32x4 acc) {
-  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, p), __builtin_bit_cast(i32x4, q), acc, 0, 0,
-                                               0);
+// Tiles in bands of kBand row tiles, down the rows first: the tiles that run
+// at once on an XCD share their rows of A and of B in its L2.
+// kWide: N and the output's pitch allow 16-byte stores.
+template <class C, bool F32, bool kWide>
+struct DenseJob {
+  static constexpr int kBand = C::BM == 256 ? 4 : 8;
+  struct Tile {
+    int m0, n0, rows;
+  };
+  DenseArgs p;
+  float sa[C::FM];
+  float4 sb[C::FN];
+
+  __device__ __forceinline__ Tile tile(int i) const {
+    const int mt = cdiv(p.M, C::BM), nt = cdiv(p.N, C::BN);
+    const int t = xcd_order(i, mt * nt);
+    const int band = t / (kBand * nt), in = t % (kBand * nt);
+    const int h = min(kBand, mt - band * kBand);
+    const int m0 = (band * kBand + in % h) * C::BM;
+    return {m0, in / h * C::BN, min(C::BM, p.M - m0)};
+  }
+  static constexpr int kParts = 1;
+  static constexpr bool kSkip = false;
+  __device__ __forceinline__ I8Source a(const Tile& t) const {
+    return {p.a + static_cast<int64_t>(t.m0) * p.K, t.rows};
+  }
+  __device__ __forceinline__ I8Source b(const Tile& t, int) const {
+    return {p.b + static_cast<int64_t>(t.n0) * p.K, min(C::BN, p.N - t.n0)};
+  }
+  static __device__ __forceinline__ int b_part(int) { return 0; }
+  static __device__ __forceinline__ int b_row(int q) { return q; }
+  __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
+  __device__ __forceinline__ int col0() const {
+    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * C::kRun;
+  }
+  __device__ __forceinline__ void prefetch(const Tile& t) {
+#pragma unroll
+    for (int m = 0; m < C::FM; ++m) sa[m] = p.sa[min(t.m0 + row0() + m * 16, p.M - 1)];
+    const int c = t.n0 + col0();
+#pragma unroll
+    for (int n = 0; n < C::FN; ++n) {
+      if (kWide) sb[n] = *reinterpret_cast<const float4*>(p.sb + min(c + n * 4, p.N - 4));
+      else sb[n] = make_float4(p.sb[min(c + n * 4, p.N - 1)], p.sb[min(c + n * 4 + 1, p.N - 1)],
+                               p.sb[min(c + n * 4 + 2, p.N - 1)], p.sb[min(c + n * 4 + 3, p.N - 1)]);
+    }
+  }
+  static constexpr int kStores = C::FM * (F32 ? 4 : 2);
+  __device__ __forceinline__ bool whole(const Tile& t) const {
+    return kWide && t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16 && t.n0 + C::BN <= p.N;
+  }
+  __device__ __forceinline__ void finish(const Tile& t, const i32x4 (&acc)[C::FM][C::FN]) const {
+    const int c = t.n0 + col0(), r0 = t.m0 + row0();
+    constexpr int kSize = F32 ? 4 : 2;
+    char* dst = static_cast<char*>(p.out) + (r0 * p.ldo + c) * kSize;
+#pragma unroll
+    for (int m = 0; m < C::FM; ++m, dst += p.ldo * (16 * kSize)) {
+      if (r0 + m * 16 >= p.M) continue;
+      float v[C::kRun];
+#pragma unroll
+      for (int n = 0; n < C::FN; ++n) {
+        v[4 * n] = static_cast<float>(acc[m][n][0]) * sa[m] * sb[n].x;
+        v[4 * n + 1] = static_cast<float>(acc[m][n][1]) * sa[m] * sb[n].y;
+        v[4 * n + 2] = static_cast<float>(acc[m][n][2]) * sa[m] * sb[n].z;
+        v[4 * n + 3] = static_cast<float>(acc[m][n][3]) * sa[m] * sb[n].w;
+      }
+      if (!kWide) {
+#pragma unroll
+        for (int i = 0; i < C::kRun; ++i) {
+          if (c + i >= p.N) continue;
+          if (F32) reinterpret_cast<float*>(dst)[i] = v[i];
+          else reinterpret_cast<bf16_t*>(dst)[i] = f2bf(v[i]);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < C::kRun; i += 16 / kSize) {
+        if (c + i >= p.N) continue;
+        uint4 w;
+        if (F32) w = __builtin_bit_cast(uint4, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+        else w = make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                            pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
+        *reinterpret_cast<uint4*>(dst + i * kSize) = w;
+      }
+    }
+  }
+};
+
+template <class C, bool kTail, bool F32, bool kWide>
+__global__ __launch_bounds__(C::kThreads) void k_i8_matmul(DenseArgs p) {
+  __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
+  __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
+  DenseJob<C, F32, kWide> job{p};
+  i8_stream<C, kTail, false>(p.K, cdiv(p.M, C::BM) * cdiv(p.N, C::BN), job, st0, st1);
 }
 
-// 16 bytes per lane from global memory to LDS at base + 16 lane.
-__device__ __forceinline__ void copy_to_lds(const int8_t* src, int8_t* lds_base) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
-                                   (__attribute__((address_space(3))) void*)(lds_base), 16, 0, 0);
+// ---------------------------------------------------------------- few rows
+// 16 columns per workgroup, its 8 waves taking the 64-byte slices of k in turn,
+// so that a CU has every byte of its weight rows in flight at once; the waves'
+// sums meet in LDS.  With kFused the rows of A are bf16, and every workgroup
+// rounds them to int8 in LDS itself: one launch, no trip through memory.
+constexpr int kFewWaves = 8;
+constexpr int kFusedRows = 16, kFusedBytes = 49152;
+
+// MT: 16-row blocks of A.
+template <int MT, bool kFused, bool F32>
+__global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(DenseArgs p, const bf16_t* __restrict__ x, int64_t ldx) {
+  extern __shared__ __attribute__((aligned(16))) int8_t a8[];  // kFused: [M][K + 16]
+  __shared__ i32x4 sums[kFewWaves][MT][64];
+  __shared__ float scales[kFusedRows];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, g = lane >> 4, i16 = lane & 15;
+  const int n0 = blockIdx.x * 16;
+  const int8_t* brow = p.b + static_cast<int64_t>(min(n0 + i16, p.N - 1)) * p.K;
+  constexpr int kAhead = 4;  // slices in flight per wave
+  const int slices = cdiv(p.K, 64);
+  uint4 b[kAhead];
+  auto load_b = [&](int s) { return *reinterpret_cast<const uint4*>(brow + min(s * 64 + g * 16, p.K - 16)); };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) b[i] = load_b(min(wv + i * kFewWaves, slices - 1));
+  if constexpr (kFused) {
+    for (int r = wv; r < p.M; r += kFewWaves) {
+      const bf16_t* src = x + r * ldx;
+      uint32_t m = 0;
+      for (int c = lane * 8; c < p.K; c += 512) m = max(m, top8(*reinterpret_cast<const uint4*>(src + c)));
+      const Rounder f(wave_umax(m));
+      for (int c = lane * 8; c < p.K; c += 512)
+        *reinterpret_cast<uint2*>(a8 + r * (p.K + 16) + c) = quant8(*reinterpret_cast<const uint4*>(src + c), f);
+      if (lane == 0) scales[r] = f.scale;
+    }
+    __syncthreads();
+  }
+  i32x4 acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = i32x4{0, 0, 0, 0};
+  for (int s0 = wv; s0 < slices; s0 += kAhead * kFewWaves) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int s = s0 + i * kFewWaves;
+      const int k = s * 64 + g * 16;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int row = m * 16 + i16;
+        uint4 a = make_uint4(0, 0, 0, 0);
+        if (row < p.M && k < p.K)
+          a = kFused ? *reinterpret_cast<const uint4*>(a8 + row * (p.K + 16) + k)
+                     : *reinterpret_cast<const uint4*>(p.a + static_cast<int64_t>(row) * p.K + k);
+        acc[m] = mfma_i8(b[i], a, acc[m]);
+      }
+      b[i] = load_b(min(s + kAhead * kFewWaves, slices - 1));
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) sums[wv][m][lane] = acc[m];
+  __syncthreads();
+  for (int i = threadIdx.x; i < MT * 256; i += 64 * kFewWaves) {
+    const int m = i >> 8, r = i >> 4 & 15, c = i & 15, row = m * 16 + r, col = n0 + c;
+    if (row >= p.M || col >= p.N) continue;
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) sum += sums[w][m][(c >> 2) * 16 + r][c & 3];
+    const float v = static_cast<float>(sum) * (kFused ? scales[row] : p.sa[row]) * p.sb[col];
+    if (F32) static_cast<float*>(p.out)[row * p.ldo + col] = v;
+    else static_cast<bf16_t*>(p.out)[row * p.ldo + col] = f2bf(v);
+  }
 }
 
-// Every wave's copies into LDS have landed (a wave's own count as vector loads).
-__device__ __forceinline__ void copies_landed() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// ---------------------------------------------------------------- grouped
+// Row tiles of the experts, BM rows each: the running count of tiles per expert, in LDS.
+template <class C>
+struct RowTiles {
+  const int32_t* offsets;
+  const int* first;  // [E + 1]
+  int E;
+  __device__ __forceinline__ void find(int i, int* e, int* row, int* rows) const {
+    int lo = 0, hi = E;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    *e = __builtin_amdgcn_readfirstlane(lo);
+    const int off = uniform_load(offsets + *e), end = uniform_load(offsets + *e + 1);
+    *row = off + (i - __builtin_amdgcn_readfirstlane(first[*e])) * C::BM;
+    *rows = min(C::BM, end - *row);
+  }
+};
+
+// first[0 .. E]: every thread calls it.
+template <class C>
+__device__ __forceinline__ void count_row_tiles(const int32_t* offsets, int E, int* first) {
+  const int e = threadIdx.x;
+  if (e < 64) {  // one wave, up to 4 experts a lane (E <= 256)
+    int n[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = e * 4 + i;
+      n[i] = x < E ? cdiv(offsets[x + 1] - offsets[x], C::BM) : 0;
+      sum += n[i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int u = __shfl_up(incl, off, 64);
+      incl += e >= off ? u : 0;
+    }
+    int run = incl - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (e * 4 + i <= E) first[e * 4 + i] = run;
+      run += n[i];
+    }
+    if (e == 63 && E == 256) first[256] = run;
+  }
   __syncthreads();
 }
 
-// BM x BN tile over WM x WN waves in K steps of KB bytes.
-template <int BM_, int BN_, int WM_, int WN_, int KB_>
-struct I8Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_;
-  static constexpr int kWaves = WM * WN;
-  static constexpr int kThreads = 64 * kWaves;
-  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  static constexpr int kStage = (BM + BN) * KB;
-  static constexpr int kChunks = KB / 16;               // 16-byte chunks of a row
-  static constexpr int kRowsPer = 64 / kChunks;         // rows one wave-wide copy covers
-  static constexpr int kCopies = (BM + BN) / kRowsPer / kWaves;  // copies per wave and step
-  static_assert(kCopies * kRowsPer * kWaves == BM + BN, "a step's rows must split evenly over the waves");
-  static_assert(BM % (kRowsPer * kWaves) == 0, "a copy must not straddle A and B");
+struct GroupedArgs {
+  const int32_t* offsets;
+  int E;
+  const int8_t* x;      // rows of A
+  const float* sx;      // their scales
+  const int32_t* rows;  // gate/up: row of x of each routed row, or null
+  moe_i8_experts w;
+  int H, F;
+  int16_t* act;  // gate/up out
+  float* top;
+  bf16_t* o;  // down out
 };
 
-// Chunk position of chunk c of row r.  LDS has 64 banks (256 bytes): rows of
-// 128 bytes repeat every 2, rows of 64 bytes every 4.
-template <int KB>
-__device__ __forceinline__ int swizzle(int r, int c) {
-  return KB == 128 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
-}
-
-// One tile: a_row(r) and b_row(r) give the first byte of tile row r of either
-// operand (any r below BM, BN; rows without data repeat another).
-template <class C, class ARow, class BRow>
-__device__ __forceinline__ void i8_tile(int K, ARow a_row, BRow b_row, int8_t* st0, int8_t* st1,
-                                        i32x4 (&acc)[C::FM][C::FN]) {
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wv / C::WN, wn = wv % C::WN;
-  const int8_t* src[C::kCopies];
-  int chunk[C::kCopies];
-#pragma unroll
-  for (int i = 0; i < C::kCopies; ++i) {
-    const int r = (i * C::kWaves + wv) * C::kRowsPer + lane / C::kChunks;
-    chunk[i] = swizzle<C::KB>(r, lane % C::kChunks);
-    src[i] = (r < C::BM ? a_row(r) : b_row(r - C::BM));
-  }
-  const int steps = cdiv(K, C::KB);
-  auto load = [&](int kt, int8_t* st) {
-    const bool last = (kt + 1) * C::KB > K;
-#pragma unroll
-    for (int i = 0; i < C::kCopies; ++i) {
-      int off = kt * C::KB + chunk[i] * 16;
-      if (last && off >= K) off = 0;
-      copy_to_lds(src[i] + off, st + (i * C::kWaves + wv) * 1024);
-    }
+// Gate and up columns side by side: a lane's first kRun / 2 columns are of
+// gate, the others the same columns of up.  A tile is BN / 2 columns of both;
+// a wave's 32 columns of one row are one partial of the activation.
+template <class C, bool kGather>
+struct GateUpJob {
+  static constexpr int kHalf = C::kRun / 2, kPart = kI8Cols, kCols = C::BN / 2;
+  struct Tile {
+    int e, row, rows, col;
   };
-#pragma unroll
-  for (int m = 0; m < C::FM; ++m)
-#pragma unroll
-    for (int n = 0; n < C::FN; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
-  const int g = lane >> 4, row = lane & 15;
-  auto compute = [&](int kt, const int8_t* st) {
-    const int8_t* at = st + (wm * C::FM * 16 + row) * C::KB;
-    const int8_t* bt = st + (C::BM + wn * C::FN * 16 + row) * C::KB;
-#pragma unroll
-    for (int s = 0; s < C::KB / 64; ++s) {
-      uint4 a[C::FM], b[C::FN];
-      const int c = swizzle<C::KB>(row, s * 4 + g) * 16;
-#pragma unroll
-      for (int n = 0; n < C::FN; ++n) b[n] = *reinterpret_cast<const uint4*>(bt + n * 16 * C::KB + c);
-#pragma unroll
-      for (int m = 0; m < C::FM; ++m) a[m] = *reinterpret_cast<const uint4*>(at + m * 16 * C::KB + c);
-      if ((kt + 1) * C::KB > K && kt * C::KB + s * 64 + g * 16 >= K)
-#pragma unroll
-        for (int m = 0; m < C::FM; ++m) a[m] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int m = 0; m < C::FM; ++m)
-#pragma unroll
-        for (int n = 0; n < C::FN; ++n) acc[m][n] = mfma_i8(b[n], a[m], acc[m][n]);
-    }
-  };
-  load(0, st0);
-  for (int kt = 0; kt < steps; kt += 2) {
-    copies_landed();
-    if (kt + 1 < steps) load(kt + 1, st1);
-    compute(kt, st0);
-    if (kt + 1 >= steps) break;
-    copies_landed();
-    if (kt + 2 < steps) load(kt + 2, st0);
-    compute(kt + 1, st1);
+  GroupedArgs p;
+  RowTiles<C> rt;
+  float s[C::FM];
+  float4 sg[C::FN / 2], su[C::FN / 2];
+
+  // the column tiles of a row tile in turn: they share its rows of x
+  __device__ __forceinline__ Tile tile(int i) const {
+    const int nt = p.F / kCols;
+    const int t = xcd_order(i, rt.first[rt.E] * nt);
+    Tile x;
+    rt.find(t / nt, &x.e, &x.row, &x.rows);
+    x.col = t % nt * kCols;
+    return x;
   }
-}
-
-// Tile coordinates of a 1-D grid: the grid's workgroups go to the 8 XCDs in
-// turn; each XCD takes a contiguous run of tiles.
-__device__ __forceinline__ int xcd_order(int i, int n) {
-  const int x = i & 7, per = n >> 3, rest = n & 7;
-  return x * per + min(x, rest) + (i >> 3);
-}
-
-using Dense = I8Tile<128, 128, 2, 2, 128>;
-
-template <bool F32>
-__global__ __launch_bounds__(Dense::kThreads) void k_i8_matmul(const int8_t* __restrict__ a,
-                                                               const float* __restrict__ sa,
-                                                               const int8_t* __restrict__ b,
-                                                               const float* __restrict__ sb, int M, int N, int K,
-                                                               void* __restrict__ out, int64_t ldo) {
-  using C = Dense;
-  __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
-  __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
-  const int nt = cdiv(N, C::BN);
-  const int t = xcd_order(blockIdx.x, gridDim.x);
-  const int m0 = t / nt * C::BM, n0 = t % nt * C::BN;
-  i32x4 acc[C::FM][C::FN];
-  i8_tile<C>(
-      K, [&](int r) { return a + static_cast<int64_t>(min(m0 + r, M - 1)) * K; },
-      [&](int r) { return b + static_cast<int64_t>(min(n0 + r, N - 1)) * K; }, st0, st1, acc);
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int mb = m0 + wv / C::WN * C::FM * 16 + (lane & 15), nb = n0 + wv % C::WN * C::FN * 16 + (lane >> 4) * 4;
+  static constexpr int kParts = 2;  // gate, up
+  static constexpr bool kSkip = C::WM > 1;
+  __device__ __forceinline__ int64_t source(int row) const { return kGather ? p.rows[row] : row; }
+  __device__ __forceinline__ I8Source a(const Tile& t) const {
+    if (kGather) return {p.x, t.rows, p.rows + t.row};
+    return {p.x + static_cast<int64_t>(t.row) * p.H, t.rows};
+  }
+  __device__ __forceinline__ I8Source b(const Tile& t, int part) const {
+    return {(part ? p.w.w_up : p.w.w_gate) + (static_cast<int64_t>(t.e) * p.F + t.col) * p.H, kCols};
+  }
+  static __device__ __forceinline__ int b_part(int q) { return q / kHalf & 1; }
+  static __device__ __forceinline__ int b_row(int q) {
+    const int r = q % (16 * C::FN);
+    return q / (16 * C::FN) * kPart + kHalf * (r / C::kRun) + r % kHalf;
+  }
+  __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
+  __device__ __forceinline__ int col0() const {
+    return (threadIdx.x >> 6) % C::WN * kPart + ((threadIdx.x & 63) >> 4) * kHalf;
+  }
+  __device__ __forceinline__ void prefetch(const Tile& t) {
 #pragma unroll
-  for (int m = 0; m < C::FM; ++m) {
-    const int row = mb + m * 16;
-    if (row >= M) continue;
-    const float s = sa[row];
+    for (int m = 0; m < C::FM; ++m) s[m] = p.sx[source(t.row + min(row0() + m * 16, t.rows - 1))];
+    const int64_t c = static_cast<int64_t>(t.e) * p.F + t.col + col0();
 #pragma unroll
-    for (int n = 0; n < C::FN; ++n) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = nb + n * 16 + i;
-        if (col >= N) continue;
-        const float v = static_cast<float>(acc[m][n][i]) * s * sb[col];
-        if (F32) static_cast<float*>(out)[row * ldo + col] = v;
-        else static_cast<bf16_t*>(out)[row * ldo + col] = f2bf(v);
-      }
+    for (int n = 0; n < C::FN / 2; ++n) {
+      sg[n] = *reinterpret_cast<const float4*>(p.w.s_gate + c + n * 4);
+      su[n] = *reinterpret_cast<const float4*>(p.w.s_up + c + n * 4);
     }
   }
-}
-
-// The tile of the row-tile table that workgroup column `t` takes, or rows = 0.
-struct RowTile {
-  int first, e, rows;
-};
-__device__ __forceinline__ RowTile row_tile(const int2* desc, int t) {
-  const int32_t* d = reinterpret_cast<const int32_t*>(desc + t);
-  const int first = uniform_load(d), y = uniform_load(d + 1);
-  return {first, y & 255, y >> 8};
-}
-
-// Gate and up columns side by side: each wave takes matching halves.
-using GateUp = I8Tile<128, 256, 2, 4, 128>;
-
-__global__ __launch_bounds__(GateUp::kThreads) void k_i8_gateup(I8Rows rt, const int8_t* __restrict__ x,
-                                                                const float* __restrict__ sx,
-                                                                const int32_t* __restrict__ rows, moe_i8_experts w,
-                                                                int H, int F, int16_t* __restrict__ a,
-                                                                float* __restrict__ a_top) {
-  using C = GateUp;
-  __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
-  __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
-  __shared__ uint32_t tops[C::BM];
-  constexpr int kHalf = C::FN / 2;  // fragments of gate, then of up, per wave
-  const int parts = F / kI8Cols;
-  const int tiles = uniform_load(rt.tile_start + rt.E) * parts;
-  for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
-    const int t = xcd_order(i, tiles);
-    const int p = t % parts;
-    const RowTile tile = row_tile(rt.tile_desc, t / parts);
-    const int64_t col0 = static_cast<int64_t>(tile.e) * F + p * kI8Cols;
-    i32x4 acc[C::FM][C::FN];
-    __syncthreads();  // the stages and `tops` are free
-    if (threadIdx.x < C::BM) tops[threadIdx.x] = 0;
-    i8_tile<C>(
-        H,
-        [&](int r) {
-          const int64_t row = tile.first + min(r, tile.rows - 1);
-          return x + (rows != nullptr ? rows[row] : row) * static_cast<int64_t>(H);
-        },
-        [&](int r) {  // wave wn's 64 columns: 32 of gate, the same 32 of up
-          const int8_t* m = (r & 32) ? w.w_up : w.w_gate;
-          return m + (col0 + (r >> 6) * 32 + (r & 31)) * H;
-        },
-        st0, st1, acc);
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int mb = wv / C::WN * C::FM * 16 + (lane & 15), nb = wv % C::WN * 32 + (lane >> 4) * 4;
-    float4 sg[kHalf], su[kHalf];
-#pragma unroll
-    for (int n = 0; n < kHalf; ++n) {
-      sg[n] = *reinterpret_cast<const float4*>(w.s_gate + col0 + nb + n * 16);
-      su[n] = *reinterpret_cast<const float4*>(w.s_up + col0 + nb + n * 16);
-    }
-    float act[C::FM][kHalf][4];
+  static constexpr int kStores = 2 * C::FM;
+  __device__ __forceinline__ bool whole(const Tile& t) const {
+    return t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16;
+  }
+  // With G = s g, U = s u (s the row's scale): silu(G) U = s^2 g u / (1 + e^-G).
+  // The factor s^2 is common to the row, so it is left to its largest value.
+  __device__ __forceinline__ void finish(const Tile& t, const i32x4 (&acc)[C::FM][C::FN]) const {
+    static_assert(kHalf == 8, "one 16-byte store a row");
+    const int parts = p.F / kPart;
 #pragma unroll
     for (int m = 0; m < C::FM; ++m) {
-      const int r = mb + m * 16;
-      const int64_t row = tile.first + min(r, tile.rows - 1);
-      const float s = sx[rows != nullptr ? rows[row] : row];
-      uint32_t top = 0;
+      const int r = row0() + m * 16;
+      const float e = s[m] * -1.4426950408889634f;
+      float v[kHalf], top = 0.0f;
+      uint32_t bad = 0;
 #pragma unroll
-      for (int n = 0; n < kHalf; ++n) {
+      for (int n = 0; n < C::FN / 2; ++n) {
         const float g4[4] = {sg[n].x, sg[n].y, sg[n].z, sg[n].w}, u4[4] = {su[n].x, su[n].y, su[n].z, su[n].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float gate = static_cast<float>(acc[m][n][i]) * s * g4[i];
-          const float up = static_cast<float>(acc[m][n + kHalf][i]) * s * u4[i];
-          act[m][n][i] = silu_f(gate) * up;
-          top = max(top, __float_as_uint(act[m][n][i]) & 0x7fffffffu);
+          const float gate = static_cast<float>(acc[m][n][i]) * g4[i];
+          const float up = static_cast<float>(acc[m][n + C::FN / 2][i]) * u4[i];
+          const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(gate * e));
+          v[4 * n + i] = gate * up * sig;
+          bad = max(bad, __float_as_uint(v[4 * n + i]) & 0x7fffffffu);
         }
       }
-      // the row's other columns: lanes 16 apart, then the waves beside this one
-      top = max(top, static_cast<uint32_t>(shfl_xor(static_cast<int>(top), 16)));
-      top = max(top, static_cast<uint32_t>(shfl_xor(static_cast<int>(top), 32)));
-      if (lane < 16) atomicMax(&tops[r], top);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int m = 0; m < C::FM; ++m) {
-      const int r = mb + m * 16;
-      if (r >= tile.rows) continue;
-      const int64_t row = tile.first + r;
-      const uint32_t tb = tops[r];
-      const float top = __uint_as_float(tb);
-      const float inv = tb == 0 || tb >= 0x7f800000u ? 0.0f : 32767.0f / top;
-#pragma unroll
-      for (int n = 0; n < kHalf; ++n) {
-        int v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = tb >= 0x7f800000u ? 0 : static_cast<int>(__builtin_rintf(act[m][n][i] * inv));
-        *reinterpret_cast<uint2*>(a + row * F + p * kI8Cols + nb + n * 16) =
-            make_uint2((v[0] & 0xffff) | (static_cast<uint32_t>(v[1]) << 16),
-                       (v[2] & 0xffff) | (static_cast<uint32_t>(v[3]) << 16));
-      }
-      if (wv % C::WN == 0 && lane < 16) a_top[row * parts + p] = top;
+      bad = max(bad, static_cast<uint32_t>(shfl_xor(static_cast<int>(bad), 16)));
+      bad = max(bad, static_cast<uint32_t>(shfl_xor(static_cast<int>(bad), 32)));
+      top = __uint_as_float(bad);
+      if (r >= t.rows) continue;
+      // zeros stay zeros; an infinity or NaN is left to the row's largest value
+      const float inv = bad != 0 && bad < 0x7f800000u ? 1.0f / top : 0.0f;
+      auto two = [&](int i) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_i16(v[i] * inv, v[i + 1] * inv));
+      };
+      const int64_t row = t.row + r;
+      *reinterpret_cast<uint4*>(p.act + row * p.F + t.col + col0()) = make_uint4(two(0), two(2), two(4), two(6));
+      if ((threadIdx.x & 63) < 16) p.top[row * parts + (t.col + col0()) / kPart] = top * s[m] * s[m];
     }
   }
-}
+};
 
-using Down = I8Tile<128, 128, 2, 2, 128>;
+template <class C, bool>
+struct DownJob {
+  struct Tile {
+    int e, row, rows, col;
+  };
+  GroupedArgs p;
+  RowTiles<C> rt;
+  float s[C::FM];
+  float4 sw[C::FN];
 
-__global__ __launch_bounds__(Down::kThreads) void k_i8_down(I8Rows rt, const int8_t* __restrict__ a,
-                                                            const float* __restrict__ sa, moe_i8_experts w, int H,
-                                                            int F, bf16_t* __restrict__ o) {
-  using C = Down;
+  __device__ __forceinline__ Tile tile(int i) const {
+    const int nt = cdiv(p.H, C::BN);
+    const int t = xcd_order(i, rt.first[rt.E] * nt);
+    Tile x;
+    rt.find(t / nt, &x.e, &x.row, &x.rows);
+    x.col = t % nt * C::BN;
+    return x;
+  }
+  static constexpr int kParts = 1;
+  static constexpr bool kSkip = C::WM > 1;
+  __device__ __forceinline__ I8Source a(const Tile& t) const {
+    return {p.x + static_cast<int64_t>(t.row) * p.F, t.rows};
+  }
+  __device__ __forceinline__ I8Source b(const Tile& t, int) const {
+    return {p.w.w_down + (static_cast<int64_t>(t.e) * p.H + t.col) * p.F, min(C::BN, p.H - t.col)};
+  }
+  static __device__ __forceinline__ int b_part(int) { return 0; }
+  static __device__ __forceinline__ int b_row(int q) { return q; }
+  __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
+  __device__ __forceinline__ int col0() const {
+    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * C::kRun;
+  }
+  __device__ __forceinline__ void prefetch(const Tile& t) {
+#pragma unroll
+    for (int m = 0; m < C::FM; ++m) s[m] = p.sx[t.row + min(row0() + m * 16, t.rows - 1)];
+#pragma unroll
+    for (int n = 0; n < C::FN; ++n)
+      sw[n] = *reinterpret_cast<const float4*>(p.w.s_down + static_cast<int64_t>(t.e) * p.H +
+                                               min(t.col + col0() + n * 4, p.H - 4));
+  }
+  static constexpr int kStores = 2 * C::FM;
+  __device__ __forceinline__ bool whole(const Tile& t) const {
+    return t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16 && t.col + C::BN <= p.H;
+  }
+  __device__ __forceinline__ void finish(const Tile& t, const i32x4 (&acc)[C::FM][C::FN]) const {
+    const int c = t.col + col0();
+    if (c >= p.H) return;  // H is a multiple of 128: a lane's columns are all there or none is
+#pragma unroll
+    for (int m = 0; m < C::FM; ++m) {
+      const int r = row0() + m * 16;
+      if (r >= t.rows) continue;
+      bf16_t* dst = p.o + static_cast<int64_t>(t.row + r) * p.H + c;
+#pragma unroll
+      for (int n = 0; n < C::FN; n += 2) {
+        const auto f = [&](int nn, int i, float w) { return static_cast<float>(acc[m][nn][i]) * s[m] * w; };
+        *reinterpret_cast<uint4*>(dst + 4 * n) =
+            make_uint4(pack_bf16x2(f(n, 0, sw[n].x), f(n, 1, sw[n].y)), pack_bf16x2(f(n, 2, sw[n].z), f(n, 3, sw[n].w)),
+                       pack_bf16x2(f(n + 1, 0, sw[n + 1].x), f(n + 1, 1, sw[n + 1].y)),
+                       pack_bf16x2(f(n + 1, 2, sw[n + 1].z), f(n + 1, 3, sw[n + 1].w)));
+      }
+    }
+  }
+};
+
+template <class C, template <class, bool> class Job, bool kGather>
+__global__ __launch_bounds__(C::kThreads) void k_i8_grouped(GroupedArgs p, int K, int col_tiles) {
   __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
   __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
-  const int nt = H / C::BN;
-  const int tiles = uniform_load(rt.tile_start + rt.E) * nt;
-  for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
-    const int t = xcd_order(i, tiles);
-    const RowTile tile = row_tile(rt.tile_desc, t / nt);
-    const int n0 = t % nt * C::BN;
-    const int64_t col0 = static_cast<int64_t>(tile.e) * H + n0;
-    i32x4 acc[C::FM][C::FN];
-    __syncthreads();  // the stages are free
-    i8_tile<C>(
-        F, [&](int r) { return a + static_cast<int64_t>(tile.first + min(r, tile.rows - 1)) * F; },
-        [&](int r) { return w.w_down + (col0 + r) * F; }, st0, st1, acc);
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int mb = wv / C::WN * C::FM * 16 + (lane & 15), nb = wv % C::WN * C::FN * 16 + (lane >> 4) * 4;
-#pragma unroll
-    for (int m = 0; m < C::FM; ++m) {
-      const int r = mb + m * 16;
-      if (r >= tile.rows) continue;
-      const int64_t row = tile.first + r;
-      const float s = sa[row];
-#pragma unroll
-      for (int n = 0; n < C::FN; ++n) {
-        const float4 sc = *reinterpret_cast<const float4*>(w.s_down + col0 + nb + n * 16);
-        *reinterpret_cast<uint2*>(o + row * H + n0 + nb + n * 16) =
-            make_uint2(pack_bf16x2(static_cast<float>(acc[m][n][0]) * s * sc.x, static_cast<float>(acc[m][n][1]) * s * sc.y),
-                       pack_bf16x2(static_cast<float>(acc[m][n][2]) * s * sc.z, static_cast<float>(acc[m][n][3]) * s * sc.w));
-      }
-    }
-  }
+  __shared__ int first[MOE_MAX_EXPERTS + 1];
+  count_row_tiles<C>(p.offsets, p.E, first);
+  Job<C, kGather> job{p, {p.offsets, first, p.E}};
+  i8_stream<C, false, kGather>(K, __builtin_amdgcn_readfirstlane(first[p.E]) * col_tiles, job, st0, st1);
 }
 
-constexpr int kMaxGrid = 4096;
+constexpr int kCus = 256;
 
-int max_tiles(const I8Rows& r) { return cdiv(r.rows_cap, 128) + r.E; }
+using Tall = I8Tile<256, 256, 2, 4>;   // 128 KB of LDS: one workgroup per CU
+using Small = I8Tile<128, 128, 2, 2>;  // 64 KB: two
+using Low = I8Tile<32, 256, 1, 4>;     // 72 KB: two
+
+template <class C, bool kTail, bool F32>
+void launch_dense(const DenseArgs& p, int per_cu, hipStream_t s) {
+  const int64_t tiles = static_cast<int64_t>(cdiv(p.M, C::BM)) * cdiv(p.N, C::BN);
+  const dim3 grid(static_cast<int>(tiles < kCus * per_cu ? tiles : kCus * per_cu)), block(C::kThreads);
+  if (p.N % 8 == 0 && p.ldo % 8 == 0) hipLaunchKernelGGL((k_i8_matmul<C, kTail, F32, true>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((k_i8_matmul<C, kTail, F32, false>), grid, block, 0, s, p);
+}
+
+template <class C>
+void launch_dense(const DenseArgs& p, bool f32, int per_cu, hipStream_t s) {
+  const bool tail = p.K % kI8Step != 0;
+  if (tail && f32) launch_dense<C, true, true>(p, per_cu, s);
+  else if (tail) launch_dense<C, true, false>(p, per_cu, s);
+  else if (f32) launch_dense<C, false, true>(p, per_cu, s);
+  else launch_dense<C, false, false>(p, per_cu, s);
+}
+
+constexpr int kFewRows = 64;
+
+template <int MT, bool kFused>
+void launch_few(const DenseArgs& p, const bf16_t* x, int64_t ldx, bool f32, hipStream_t s) {
+  const dim3 grid(cdiv(p.N, 16)), block(64 * kFewWaves);
+  const int lds = kFused ? p.M * (p.K + 16) : 0;
+  if (f32) hipLaunchKernelGGL((k_i8_few<MT, kFused, true>), grid, block, lds, s, p, x, ldx);
+  else hipLaunchKernelGGL((k_i8_few<MT, kFused, false>), grid, block, lds, s, p, x, ldx);
+}
+
+template <class C, template <class, bool> class Job, bool kGather>
+void launch_grouped(const GroupedArgs& p, int rows_cap, int K, int col_tiles, int per_cu, hipStream_t s) {
+  const int64_t tiles = (cdiv64(rows_cap, C::BM) + p.E) * col_tiles;
+  const dim3 grid(static_cast<int>(tiles < kCus * per_cu ? tiles : kCus * per_cu));
+  hipLaunchKernelGGL((k_i8_grouped<C, Job, kGather>), grid, dim3(C::kThreads), 0, s, p, K, col_tiles);
+}
+
+template <class C>
+void launch_gateup(const GroupedArgs& p, int rows_cap, int per_cu, hipStream_t s) {
+  const int col_tiles = p.F / (C::BN / 2);
+  if (p.rows != nullptr) launch_grouped<C, GateUpJob, true>(p, rows_cap, p.H, col_tiles, per_cu, s);
+  else launch_grouped<C, GateUpJob, false>(p, rows_cap, p.H, col_tiles, per_cu, s);
+}
+
+template <class C>
+void launch_down(const GroupedArgs& p, int rows_cap, int per_cu, hipStream_t s) {
+  launch_grouped<C, DownJob, false>(p, rows_cap, p.F, cdiv(p.H, C::BN), per_cu, s);
+}
+
+// Few rows per expert: reading the weights bounds the products, and low tiles
+// keep two workgroups' copies in flight.
+bool few_rows(int rows_cap, int E) { return rows_cap <= 24ll * E; }
 
 }  // namespace
 
 hipError_t launch_i8_matmul(const int8_t* a, const float* sa, const int8_t* b, const float* sb, int M, int N, int K,
                             void* out, int64_t ldo, bool f32, hipStream_t s) {
   TraceScope trace_scope(K_I8_MATMUL, s);
-  const dim3 grid(cdiv(M, Dense::BM) * cdiv(N, Dense::BN));
-  if (f32) hipLaunchKernelGGL(k_i8_matmul<true>, grid, dim3(Dense::kThreads), 0, s, a, sa, b, sb, M, N, K, out, ldo);
-  else hipLaunchKernelGGL(k_i8_matmul<false>, grid, dim3(Dense::kThreads), 0, s, a, sa, b, sb, M, N, K, out, ldo);
+  const DenseArgs p{a, sa, b, sb, M, N, K, out, ldo};
+  if (M <= 16) launch_few<1, false>(p, nullptr, 0, f32, s);
+  else if (M <= 32) launch_few<2, false>(p, nullptr, 0, f32, s);
+  else if (M <= kFewRows) launch_few<4, false>(p, nullptr, 0, f32, s);
+  else if (static_cast<int64_t>(cdiv(M, 256)) * cdiv(N, 256) >= kCus) launch_dense<Tall>(p, f32, 1, s);
+  else launch_dense<Small>(p, f32, 2, s);
   return hipGetLastError();
+}
+
+bool launch_i8_linear_fused(const bf16_t* x, int64_t ldx, const int8_t* b, const float* sb, int M, int N, int K,
+                            void* out, int64_t ldo, bool f32, hipStream_t s) {
+  if (M > kFusedRows || static_cast<int64_t>(M) * (K + 16) > kFusedBytes) return false;
+  TraceScope trace_scope(K_I8_MATMUL, s);
+  launch_few<1, true>(DenseArgs{nullptr, nullptr, b, sb, M, N, K, out, ldo}, x, ldx, f32, s);
+  return true;
 }
 
 hipError_t launch_i8_gateup(const I8Rows& r, const int8_t* x, const float* sx, const int32_t* rows,
                             const moe_i8_experts& w, int H, int F, int16_t* a, float* a_top, hipStream_t s) {
   TraceScope trace_scope(K_I8_GATEUP, s);
-  const int64_t tiles = static_cast<int64_t>(max_tiles(r)) * (F / kI8Cols);
-  const int grid = static_cast<int>(tiles < kMaxGrid ? tiles : kMaxGrid);
-  hipLaunchKernelGGL(k_i8_gateup, dim3(grid), dim3(GateUp::kThreads), 0, s, r, x, sx, rows, w, H, F, a, a_top);
+  const GroupedArgs p{r.offsets, r.E, x, sx, rows, w, H, F, a, a_top, nullptr};
+  if (few_rows(r.rows_cap, r.E)) launch_gateup<Low>(p, r.rows_cap, 2, s);
+  else launch_gateup<Tall>(p, r.rows_cap, 1, s);
   return hipGetLastError();
 }
 
 hipError_t launch_i8_down(const I8Rows& r, const int8_t* a, const float* sa, const moe_i8_experts& w, int H, int F,
                           bf16_t* o, hipStream_t s) {
   TraceScope trace_scope(K_I8_DOWN, s);
-  const int64_t tiles = static_cast<int64_t>(max_tiles(r)) * (H / Down::BN);
-  const int grid = static_cast<int>(tiles < kMaxGrid ? tiles : kMaxGrid);
-  hipLaunchKernelGGL(k_i8_down, dim3(grid), dim3(Down::kThreads), 0, s, r, a, sa, w, H, F, o);
+  const GroupedArgs p{r.offsets, r.E, a, sa, nullptr, w, H, F, nullptr, nullptr, o};
+  if (few_rows(r.rows_cap, r.E)) launch_down<Low>(p, r.rows_cap, 2, s);
+  else launch_down<Tall>(p, r.rows_cap, 1, s);
   return hipGetLastError();
 }
 

@@ -5,14 +5,13 @@
 // starting at row s gets the units floor(s / u) + c b, ... of a grid, which
 // never overlap the next request's because n rows need at most
 // floor(n / u) + c of them; a unit finds its request by binary search.
+#include "i8_round.hpp"
 #include "serve.hpp"
 #include "trace.hpp"
 
 namespace moe {
 
 namespace {
-
-constexpr uint32_t kInfBits = 0x7f800000u;
 
 // ---------------------------------------------------------------- plan
 constexpr int kPlanPer = 16;                 // requests per thread and round
@@ -144,14 +143,6 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
 }
 
 // ---------------------------------------------------------------- write
-__device__ __forceinline__ uint32_t top8(const uint4& v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7fff0000u, (w[i] << 16) & 0x7fff0000u));
-  return m;
-}
-
 __device__ __forceinline__ int round8(float x) { return static_cast<int>(fminf(fmaxf(__builtin_rintf(x), -127.0f), 127.0f)); }
 
 // One workgroup per block that the batch writes to, kv head, and keys

@@ -11,9 +11,6 @@
 namespace moe {
 
 // ---- int8 rows (i8_quant.hip)
-// Columns of one partial of the SwiGLU activation (see launch_i8_gateup).
-constexpr int kI8Cols = 128;
-
 // q, scale of `rows` bf16 rows; with n_valid (device) rows from *n_valid on
 // are left alone.
 hipError_t launch_i8_quant_rows(const bf16_t* x, int64_t ldx, int rows, int K, const int32_t* n_valid, int8_t* q,
@@ -30,14 +27,20 @@ hipError_t launch_i8_quant_weight(const bf16_t* w, int E, int K, int N, int8_t* 
 hipError_t launch_i8_matmul(const int8_t* a, const float* sa, const int8_t* b, const float* sb, int M, int N, int K,
                             void* out, int64_t ldo, bool f32, hipStream_t s);
 
-// Rows grouped by expert: the row-tile table of launch.hpp (128-row tiles).
+// The same from a few bf16 rows, rounded to int8 on the way; false (and
+// nothing launched) where there are more than that takes.
+bool launch_i8_linear_fused(const bf16_t* x, int64_t ldx, const int8_t* b, const float* sb, int M, int N, int K,
+                            void* out, int64_t ldo, bool f32, hipStream_t s);
+
+// Rows grouped by expert: expert e's are offsets[e] .. offsets[e + 1].
 struct I8Rows {
   int rows_cap, E;
-  const int32_t* tile_start;
-  const int2* tile_desc;
+  const int32_t* offsets;
 };
+// Columns of one partial of the SwiGLU activation.
+constexpr int kI8Cols = 32;
 // A = silu(G) U of each routed row (x row rows[r], or r where rows is null),
-// as int16 of the largest value among each kI8Cols columns.
+// as int16 of the largest value among each kI8Cols columns (a_top).
 hipError_t launch_i8_gateup(const I8Rows& r, const int8_t* x, const float* sx, const int32_t* rows,
                             const moe_i8_experts& w, int H, int F, int16_t* a, float* a_top, hipStream_t s);
 // O = A W_down.

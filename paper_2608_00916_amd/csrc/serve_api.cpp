@@ -148,10 +148,10 @@ int check_infer_i8(const moe_dims* d) {
 
 // The expert products on routed rows; x8 row rows[r], or r where rows is null.
 int expert_products(const I8Rows& rt, const int8_t* x8, const float* sx, const int32_t* rows, const moe_i8_experts* w,
-                    int H, int F, const int32_t* n_rows, const RowsWs& ws, bf16_t* o, hipStream_t s) {
+                    int H, int F, const RowsWs& ws, bf16_t* o, hipStream_t s) {
   hipError_t e = launch_i8_gateup(rt, x8, sx, rows, *w, H, F, ws.a, ws.a_top, s);
   if (e != hipSuccess) return hip_status(e, "gate/up");
-  e = launch_i8_requant(ws.a, ws.a_top, rt.rows_cap, F, n_rows, ws.a8, ws.sa, s);
+  e = launch_i8_requant(ws.a, ws.a_top, rt.rows_cap, F, rt.offsets + rt.E, ws.a8, ws.sa, s);
   if (e != hipSuccess) return hip_status(e, "activation rows");
   e = launch_i8_down(rt, ws.a8, ws.sa, *w, H, F, o, s);
   return hip_status(e, "down");
@@ -246,7 +246,10 @@ int moe_i8_linear(const moe_i8_dims* d, const void* x, int64_t ldx, const int8_t
   const LinearWs w = linear_layout(d, ws);
   if (ws_bytes < w.bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, w.bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_i8_quant_rows(static_cast<const bf16_t*>(x), ldx, d->M, d->K, nullptr, w.q, w.scale, s);
+  const bf16_t* xb = static_cast<const bf16_t*>(x);
+  if (launch_i8_linear_fused(xb, ldx, b, b_scale, d->M, d->N, d->K, out, ldo, d->flags & MOE_F_OUT_FP32, s))
+    return hip_status(hipGetLastError(), "int8 product");
+  hipError_t e = launch_i8_quant_rows(xb, ldx, d->M, d->K, nullptr, w.q, w.scale, s);
   if (e != hipSuccess) return hip_status(e, "quant rows");
   e = launch_i8_matmul(w.q, w.scale, b, b_scale, d->M, d->N, d->K, out, ldo, d->flags & MOE_F_OUT_FP32, s);
   return hip_status(e, "int8 product");
@@ -269,8 +272,8 @@ int moe_experts_i8(const moe_experts_dims* d, const void* xp, const int32_t* cou
   if (e != hipSuccess) return hip_status(e, "offsets");
   e = launch_i8_quant_rows(static_cast<const bf16_t*>(xp), d->H, d->rows, d->H, l.offsets + d->E, l.x8, l.sx, s);
   if (e != hipSuccess) return hip_status(e, "quant rows");
-  return expert_products({d->rows, d->E, l.tile_start, l.tile_desc}, l.x8, l.sx, nullptr, w, d->H, d->F,
-                         l.offsets + d->E, l.rows, static_cast<bf16_t*>(o), s);
+  return expert_products({d->rows, d->E, l.offsets}, l.x8, l.sx, nullptr, w, d->H, d->F, l.rows,
+                         static_cast<bf16_t*>(o), s);
 }
 
 size_t moe_infer_i8_workspace_bytes(const moe_dims* d) {
@@ -299,9 +302,7 @@ int moe_infer_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i8
   // a token is rounded once, and its k rows read that
   e = launch_i8_quant_rows(xb, H, T, H, nullptr, l.x8, l.sx, s);
   if (e != hipSuccess) return hip_status(e, "quant rows");
-  if (int rc = expert_products({T * k, E, l.tile_start, l.tile_desc}, l.x8, l.sx, l.row_token, w, H, F, l.offsets + E,
-                               l.rows, l.o, s))
-    return rc;
+  if (int rc = expert_products({T * k, E, l.offsets}, l.x8, l.sx, l.row_token, w, H, F, l.rows, l.o, s)) return rc;
   return hip_status(launch_combine(l.o, l.gates, l.row_of, T, H, k, static_cast<bf16_t*>(y), s), "combine");
 }
 

@@ -26,8 +26,8 @@ _ref = ctypes.byref
 
 
 def _p(t, dtype=None):
-    if t is None:
-        return None
+    if t is None or type(t) is int:  # a pointer checked before
+        return t
     if not t.is_cuda:
         raise ValueError("tensor must be on the GPU")
     if not t.is_contiguous():
@@ -124,7 +124,8 @@ def moe_i8_linear(d, x, b, b_scale, out, ws, stream=None):
     if (out.dtype == torch.float32) != bool(d.flags & MOE_F_OUT_FP32):
         raise ValueError(f"out is {out.dtype}, which the dims do not say")
     po, ldo = _out_rows(out, d.M, d.N)
-    check(lib().moe_i8_linear(_ref(d), px, ldx, _p(b), _p(b_scale), po, ldo, _p(ws), ws.numel(), _s(stream)))
+    check(lib().moe_i8_linear(_ref(d), px, ldx, _p(b, torch.int8), _p(b_scale, torch.float32), po, ldo, _p(ws),
+                              ws.numel(), _s(stream)))
 
 
 class I8Linear:
@@ -134,7 +135,6 @@ class I8Linear:
     def __init__(self, M, weight, scale, out_fp32=False):
         N, K = weight.shape
         _shape("scale", scale, (N,))
-        _p(weight, torch.int8), _p(scale, torch.float32)
         self.weight, self.scale = weight, scale
         self.d = i8_dims(M, N, K, out_fp32)
         nb = moe_i8_linear_workspace_bytes(self.d)
@@ -142,19 +142,19 @@ class I8Linear:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, weight.device)
         self.out = torch.empty((M, N), dtype=torch.float32 if out_fp32 else torch.bfloat16, device=weight.device)
-        self._m = {M: (self.d, self.out)}
+        # pointers of what it owns, checked once
+        self._b = _p(weight, torch.int8), _p(scale, torch.float32), _p(self.out), N, _p(self.ws), nb
 
     def forward(self, x, stream=None):
-        """The product of x [m, K], m <= M; a view of the output's first m rows."""
-        m = x.shape[0]
-        d, out = self._m.get(m, (None, None))
-        if d is None:
-            if not 1 <= m <= self.d.M:
-                raise ValueError(f"{m} rows, made for 1 to {self.d.M}")
-            d = MoeI8Dims(m, self.d.N, self.d.K, self.d.flags)
-            out = self.out[:m]
-        moe_i8_linear(d, x, self.weight, self.scale, out, self.ws, stream)
-        return out
+        """The product of x [m, K], m <= M (rows may be strided); a view of the output's first m rows."""
+        d, m = self.d, x.shape[0]
+        if m != d.M:
+            if not 1 <= m <= d.M:
+                raise ValueError(f"{m} rows, made for 1 to {d.M}")
+            d = MoeI8Dims(m, d.N, d.K, d.flags)
+        _shape("x", x, (m, d.K))
+        check(lib().moe_i8_linear(_ref(d), *_rows(x), *self._b, _s(stream)))
+        return self.out if m == self.d.M else self.out[:m]
 
 
 # ------------------------------------------------------------------ experts in 8 bits
@@ -206,13 +206,15 @@ class MoEExpertsI8:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, device)
         self.o = torch.empty((rows, H), dtype=torch.bfloat16, device=device)
+        self._b = _p(self.o), _p(self.ws), nb  # pointers of what it owns
 
     def forward(self, xp, counts, w: MoeI8Experts, stream=None):
         d = self.d
         _check_weights(w, d.E, d.H, d.F)
         _shape("xp", xp, (d.rows, d.H))
         _shape("counts", counts, (d.E,))
-        moe_experts_i8(d, xp, counts, w, self.o, self.ws, stream)
+        check(lib().moe_experts_i8(_ref(d), _p(xp, torch.bfloat16), _p(counts, torch.int32), _ref(w), *self._b,
+                                   _s(stream)))
         return self.o
 
 
@@ -294,6 +296,7 @@ class KVPlan:
 
         self.row_start, self.kv_len, self.state = ints(B + 1), ints(B), ints(2)
         self.positions, self.slots, self.seq = ints(T), ints(T), ints(T)
+        self._b = [_p(t) for t in (self.row_start, self.kv_len, self.positions, self.slots, self.seq, self.state)]
 
     def build(self, old_len, new_len, block_table, free_ids, n_free, stream=None):
         """Tables of this step; takes the blocks that the requests lack into block_table."""
@@ -303,8 +306,7 @@ class KVPlan:
         _shape("block_table", block_table, (d.B, d.W))
         _shape("n_free", n_free, (1,))
         d.free_cap = free_ids.numel()
-        moe_kv_plan(d, old_len, new_len, block_table, free_ids, n_free, self.row_start, self.kv_len, self.positions,
-                    self.slots, self.seq, self.state, stream)
+        moe_kv_plan(d, old_len, new_len, block_table, free_ids, n_free, *self._b, stream)
 
 
 class KVCache:
@@ -356,9 +358,14 @@ class KVAttention:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, device)
         self.out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=device)
+        self._b = _p(self.out), heads * D, _p(self.ws), nb  # of what it owns
 
     def forward(self, q, cache: KVCache, block_table, row_start, kv_len, stream=None):
         """Attention of the packed queries q [t, heads, head_dim], t <= T (rows may be strided)."""
-        out = self.out if q.shape[0] == self.T else self.out[:q.shape[0]]
-        moe_kv_attention(cache.d, kv_batch(q.shape[0], row_start, kv_len, block_table), self.a, q, out, self.ws, stream)
-        return out
+        t = q.shape[0]
+        if t > self.T or block_table.shape[0] != self.B:
+            raise ValueError(f"{t} tokens of {block_table.shape[0]} requests, made for {self.T} of {self.B}")
+        _shape("q", q, (t, self.a.heads, cache.d.head_dim))
+        check(lib().moe_kv_attention(_ref(cache.d), _ref(kv_batch(t, row_start, kv_len, block_table)), _ref(self.a),
+                                     *_rows(q), *self._b, _s(stream)))
+        return self.out if t == self.T else self.out[:t]

@@ -121,6 +121,22 @@ def test_matmul(M, N, K, fp32):
     assert (wide[:, N:] == 7).all()
 
 
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 256), (4093, 4091, 144), (5000, 3600, 128), (4096, 4104, 400)])
+@pytest.mark.parametrize("fp32", [False, True])
+def test_matmul_large(M, N, K, fp32):
+    """Many tiles: several a workgroup, ragged at both edges, odd and even step counts."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 matmul large", M, N, K, fp32)
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    a, b = (torch.randint(-127, 128, (n, K), dtype=torch.int8, device="cuda", generator=g) for n in (M, N))
+    sa, sb = (torch.rand(n, device="cuda", generator=g) + 0.5 for n in (M, N))
+    out = torch.full((M, N), 7.0, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+    moe.moe_i8_matmul(a, sa, b, sb, out)
+    ref = (a.double() @ b.double().T) * sa.double()[:, None] * sb.double()
+    assert ((out.double() - ref).abs() <= ref.abs() * (4 * 2.0 ** -24 + (0 if fp32 else BF))).all()
+
+
 def test_matmul_full_range():
     """K products of 127 * 127 at the largest K: the sum needs 31 bits."""
     import torch
@@ -187,6 +203,7 @@ def expert_weights(g, E, H, F):
     (300, [128, 129, 0, 43], 128, 384),
     (700, [257, 0, 131, 300], 384, 640),
     (520, [1] * 8 + [512], 512, 256),
+    (80, [0, 75, 0, 5, 0, 0, 0, 0], 256, 256),
 ])
 def test_experts(rows, counts, H, F):
     import torch
