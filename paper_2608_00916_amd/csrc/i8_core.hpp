@@ -97,8 +97,29 @@ __device__ __forceinline__ int b_swizzle(int r, int c) {  // fragment rows: 4 to
   return c ^ (((r >> 1) & 1) | (((r >> 4) & 3) << 1));
 }
 
-// Streams tiles blockIdx.x, + gridDim.x, ... of `tiles`.  Job:
-//   Tile tile(int t)              a tile (uniform), with .rows valid rows of A
+// Work items of a persistent grid over n tiles.  Where the last, incomplete
+// round would fill at most half of the workgroups, its tiles are cut into two
+// halves of BM / 2 rows, on which half of the waves work.  Odd workgroups take
+// their half tile first: their epilogues, whose stores would otherwise all meet
+// at the memory, then fall between those of the even ones.
+struct Items {
+  int tiles, full;  // tiles, and those left whole (a multiple of the grid unless all are)
+  __device__ __forceinline__ Items(bool cut, int n) : tiles(n) {
+    const int rem = n % static_cast<int>(gridDim.x);
+    full = cut && 2 * rem <= static_cast<int>(gridDim.x) ? n - rem : n;
+  }
+  __device__ __forceinline__ int count() const { return 2 * tiles - full; }
+  // tile of item i, and its half (-1: whole)
+  __device__ __forceinline__ void at(int i, int* tile, int* half) const {
+    const int w = blockIdx.x, grid = gridDim.x;
+    if ((w & 1) && w < count() - full) i = i == w ? full + w : i - grid;
+    *half = i < full ? -1 : (i - full) & 1;
+    *tile = i < full ? i : full + (i - full) / 2;
+  }
+};
+
+// Streams work items blockIdx.x, + gridDim.x, ... of `items`.  Job:
+//   Tile tile(int i)              an item's tile (uniform), with .rows valid rows of A (<= 0: nothing to do)
 //   I8Source a(const Tile&)       the tile's rows of A
 //   I8Source b(const Tile&, int)  of B, part 0 .. kParts - 1: B row q is row
 //   int b_part(q), b_row(q)       b_row(q) of part b_part(q)
@@ -109,7 +130,7 @@ __device__ __forceinline__ int b_swizzle(int r, int c) {  // fragment rows: 4 to
 //                                 then finish issues kStores stores
 // kGather: rows of A through an index, at 64-bit offsets.
 template <class C, bool kTail, bool kGather, class Job>
-__device__ __forceinline__ void i8_stream(int K, int tiles, Job& job, int8_t* st0, int8_t* st1) {
+__device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st0, int8_t* st1) {
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wv / C::WN, wn = wv % C::WN;
   const int steps = cdiv(K, kI8Step);
@@ -188,18 +209,26 @@ __device__ __forceinline__ void i8_stream(int K, int tiles, Job& job, int8_t* st
     }
   };
 
-  int t = blockIdx.x;
-  if (t >= tiles) return;
-  typename Job::Tile cur = job.tile(t);
+  // the first item with rows from i on
+  auto find = [&](int i, typename Job::Tile& x) {
+    for (; i < items; i += gridDim.x) {
+      x = job.tile(i);
+      if (x.rows > 0) break;
+    }
+    return i;
+  };
+  typename Job::Tile cur;
+  int t = find(blockIdx.x, cur);
+  if (t >= items) return;
   sources(cur);
   load(0, st0);
   wait_vm<0>();
   while (true) {
     typename Job::Tile next = cur;
-    const int tn = t + gridDim.x;
+    int tn = items;
     auto load_next = [&] {
-      if (tn >= tiles) return;
-      next = job.tile(tn);
+      tn = find(t + gridDim.x, next);
+      if (tn >= items) return;
       sources(next);
       load(0, st0);
     };
@@ -232,7 +261,7 @@ __device__ __forceinline__ void i8_stream(int K, int tiles, Job& job, int8_t* st
       load_next();
     }
     if (live) job.finish(cur, acc);
-    if (tn >= tiles) break;
+    if (tn >= items) break;
     if (live && job.whole(cur)) wait_vm<Job::kStores>();
     else wait_vm<0>();
     t = tn;

@@ -30,19 +30,23 @@ struct DenseJob {
     int m0, n0, rows;
   };
   DenseArgs p;
+  Items items;
+  float* swap;  // !kWide: 16 rows of this wave's 64 columns, float4s XOR-swizzled by row
   float sa[C::FM];
   float4 sb[C::FN];
 
   __device__ __forceinline__ Tile tile(int i) const {
     const int mt = cdiv(p.M, C::BM), nt = cdiv(p.N, C::BN);
-    const int t = xcd_order(i, mt * nt);
+    int t, half;
+    items.at(i, &t, &half);
+    t = xcd_order(t, mt * nt);
     const int band = t / (kBand * nt), in = t % (kBand * nt);
     const int h = min(kBand, mt - band * kBand);
-    const int m0 = (band * kBand + in % h) * C::BM;
-    return {m0, in / h * C::BN, min(C::BM, p.M - m0)};
+    const int m0 = (band * kBand + in % h) * C::BM + (half > 0 ? C::BM / 2 : 0);
+    return {m0, in / h * C::BN, min(half < 0 ? C::BM : C::BM / 2, p.M - m0)};
   }
   static constexpr int kParts = 1;
-  static constexpr bool kSkip = false;
+  static constexpr bool kSkip = C::WM > 1;
   __device__ __forceinline__ I8Source a(const Tile& t) const {
     return {p.a + static_cast<int64_t>(t.m0) * p.K, t.rows};
   }
@@ -76,7 +80,6 @@ struct DenseJob {
     char* dst = static_cast<char*>(p.out) + (r0 * p.ldo + c) * kSize;
 #pragma unroll
     for (int m = 0; m < C::FM; ++m, dst += p.ldo * (16 * kSize)) {
-      if (r0 + m * 16 >= p.M) continue;
       float v[C::kRun];
 #pragma unroll
       for (int n = 0; n < C::FN; ++n) {
@@ -85,15 +88,25 @@ struct DenseJob {
         v[4 * n + 2] = static_cast<float>(acc[m][n][2]) * sa[m] * sb[n].z;
         v[4 * n + 3] = static_cast<float>(acc[m][n][3]) * sa[m] * sb[n].w;
       }
-      if (!kWide) {
+      if constexpr (!kWide) {
+        // rows of odd pitch: 64 consecutive columns of a row per store
+        const int lane = threadIdx.x & 63, rows = p.M - (r0 + m * 16 - (lane & 15));
+        const int col = c - (lane >> 4) * C::kRun + lane;
 #pragma unroll
-        for (int i = 0; i < C::kRun; ++i) {
-          if (c + i >= p.N) continue;
-          if (F32) reinterpret_cast<float*>(dst)[i] = v[i];
-          else reinterpret_cast<bf16_t*>(dst)[i] = f2bf(v[i]);
+        for (int n = 0; n < C::FN; ++n)
+          *reinterpret_cast<float4*>(swap + (lane & 15) * 64 + 4 * ((4 * (lane >> 4) + n) ^ (lane & 15))) =
+              make_float4(v[4 * n], v[4 * n + 1], v[4 * n + 2], v[4 * n + 3]);
+        char* line = static_cast<char*>(p.out) + ((r0 + m * 16 - (lane & 15)) * p.ldo + col) * kSize;
+        for (int r = 0; r < min(rows, 16); ++r, line += p.ldo * kSize) {
+          const float x = swap[r * 64 + (4 * ((lane >> 2) ^ r) | (lane & 3))];
+          if (col >= p.N) continue;
+          if (F32) *reinterpret_cast<float*>(line) = x;
+          else *reinterpret_cast<bf16_t*>(line) = f2bf(x);
         }
+        __builtin_amdgcn_sched_barrier(0);  // one row of fragments at a time: registers
         continue;
       }
+      if (r0 + m * 16 >= p.M) continue;
 #pragma unroll
       for (int i = 0; i < C::kRun; i += 16 / kSize) {
         if (c + i >= p.N) continue;
@@ -111,8 +124,11 @@ template <class C, bool kTail, bool F32, bool kWide>
 __global__ __launch_bounds__(C::kThreads) void k_i8_matmul(DenseArgs p) {
   __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
   __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
-  DenseJob<C, F32, kWide> job{p};
-  i8_stream<C, kTail, false>(p.K, cdiv(p.M, C::BM) * cdiv(p.N, C::BN), job, st0, st1);
+  using Job = DenseJob<C, F32, kWide>;
+  __shared__ __attribute__((aligned(16))) float swap[kWide ? 4 : C::kWaves * 16 * 64];
+  const Items items(C::WM > 1, cdiv(p.M, C::BM) * cdiv(p.N, C::BN));
+  Job job{p, items, swap + (kWide ? 0 : (threadIdx.x >> 6) * 16 * 64)};
+  i8_stream<C, kTail, false>(p.K, items.count(), job, st0, st1);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -192,7 +208,7 @@ struct RowTiles {
   const int32_t* offsets;
   const int* first;  // [E + 1]
   int E;
-  __device__ __forceinline__ void find(int i, int* e, int* row, int* rows) const {
+  __device__ __forceinline__ void find(int i, int half, int* e, int* row, int* rows) const {
     int lo = 0, hi = E;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -201,8 +217,8 @@ struct RowTiles {
     }
     *e = __builtin_amdgcn_readfirstlane(lo);
     const int off = uniform_load(offsets + *e), end = uniform_load(offsets + *e + 1);
-    *row = off + (i - __builtin_amdgcn_readfirstlane(first[*e])) * C::BM;
-    *rows = min(C::BM, end - *row);
+    *row = off + (i - __builtin_amdgcn_readfirstlane(first[*e])) * C::BM + (half > 0 ? C::BM / 2 : 0);
+    *rows = min(half < 0 ? C::BM : C::BM / 2, end - *row);
   }
 };
 
@@ -259,15 +275,18 @@ struct GateUpJob {
   };
   GroupedArgs p;
   RowTiles<C> rt;
+  Items items;
   float s[C::FM];
   float4 sg[C::FN / 2], su[C::FN / 2];
 
   // the column tiles of a row tile in turn: they share its rows of x
   __device__ __forceinline__ Tile tile(int i) const {
     const int nt = p.F / kCols;
-    const int t = xcd_order(i, rt.first[rt.E] * nt);
+    int t, half;
+    items.at(i, &t, &half);
+    t = xcd_order(t, items.tiles);
     Tile x;
-    rt.find(t / nt, &x.e, &x.row, &x.rows);
+    rt.find(t / nt, half, &x.e, &x.row, &x.rows);
     x.col = t % nt * kCols;
     return x;
   }
@@ -350,14 +369,17 @@ struct DownJob {
   };
   GroupedArgs p;
   RowTiles<C> rt;
+  Items items;
   float s[C::FM];
   float4 sw[C::FN];
 
   __device__ __forceinline__ Tile tile(int i) const {
     const int nt = cdiv(p.H, C::BN);
-    const int t = xcd_order(i, rt.first[rt.E] * nt);
+    int t, half;
+    items.at(i, &t, &half);
+    t = xcd_order(t, items.tiles);
     Tile x;
-    rt.find(t / nt, &x.e, &x.row, &x.rows);
+    rt.find(t / nt, half, &x.e, &x.row, &x.rows);
     x.col = t % nt * C::BN;
     return x;
   }
@@ -413,8 +435,9 @@ __global__ __launch_bounds__(C::kThreads) void k_i8_grouped(GroupedArgs p, int K
   __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
   __shared__ int first[MOE_MAX_EXPERTS + 1];
   count_row_tiles<C>(p.offsets, p.E, first);
-  Job<C, kGather> job{p, {p.offsets, first, p.E}};
-  i8_stream<C, false, kGather>(K, __builtin_amdgcn_readfirstlane(first[p.E]) * col_tiles, job, st0, st1);
+  const Items items(C::WM > 1, __builtin_amdgcn_readfirstlane(first[p.E]) * col_tiles);
+  Job<C, kGather> job{p, {p.offsets, first, p.E}, items};
+  i8_stream<C, false, kGather>(K, items.count(), job, st0, st1);
 }
 
 constexpr int kCus = 256;
@@ -423,10 +446,12 @@ using Tall = I8Tile<256, 256, 2, 4>;   // 128 KB of LDS: one workgroup per CU
 using Small = I8Tile<128, 128, 2, 2>;  // 64 KB: two
 using Low = I8Tile<32, 256, 1, 4>;     // 72 KB: two
 
+int grid_of(int64_t items, int per_cu) { return static_cast<int>(items < kCus * per_cu ? items : kCus * per_cu); }
+
 template <class C, bool kTail, bool F32>
 void launch_dense(const DenseArgs& p, int per_cu, hipStream_t s) {
   const int64_t tiles = static_cast<int64_t>(cdiv(p.M, C::BM)) * cdiv(p.N, C::BN);
-  const dim3 grid(static_cast<int>(tiles < kCus * per_cu ? tiles : kCus * per_cu)), block(C::kThreads);
+  const dim3 grid(grid_of(2 * tiles, per_cu)), block(C::kThreads);
   if (p.N % 8 == 0 && p.ldo % 8 == 0) hipLaunchKernelGGL((k_i8_matmul<C, kTail, F32, true>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((k_i8_matmul<C, kTail, F32, false>), grid, block, 0, s, p);
 }
@@ -440,7 +465,7 @@ void launch_dense(const DenseArgs& p, bool f32, int per_cu, hipStream_t s) {
   else launch_dense<C, false, false>(p, per_cu, s);
 }
 
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 128;
 
 template <int MT, bool kFused>
 void launch_few(const DenseArgs& p, const bf16_t* x, int64_t ldx, bool f32, hipStream_t s) {
@@ -453,7 +478,7 @@ void launch_few(const DenseArgs& p, const bf16_t* x, int64_t ldx, bool f32, hipS
 template <class C, template <class, bool> class Job, bool kGather>
 void launch_grouped(const GroupedArgs& p, int rows_cap, int K, int col_tiles, int per_cu, hipStream_t s) {
   const int64_t tiles = (cdiv64(rows_cap, C::BM) + p.E) * col_tiles;
-  const dim3 grid(static_cast<int>(tiles < kCus * per_cu ? tiles : kCus * per_cu));
+  const dim3 grid(grid_of(2 * tiles, per_cu));
   hipLaunchKernelGGL((k_i8_grouped<C, Job, kGather>), grid, dim3(C::kThreads), 0, s, p, K, col_tiles);
 }
 
@@ -481,7 +506,8 @@ hipError_t launch_i8_matmul(const int8_t* a, const float* sa, const int8_t* b, c
   const DenseArgs p{a, sa, b, sb, M, N, K, out, ldo};
   if (M <= 16) launch_few<1, false>(p, nullptr, 0, f32, s);
   else if (M <= 32) launch_few<2, false>(p, nullptr, 0, f32, s);
-  else if (M <= kFewRows) launch_few<4, false>(p, nullptr, 0, f32, s);
+  else if (M <= 64) launch_few<4, false>(p, nullptr, 0, f32, s);
+  else if (M <= kFewRows) launch_few<8, false>(p, nullptr, 0, f32, s);
   else if (static_cast<int64_t>(cdiv(M, 256)) * cdiv(N, 256) >= kCus) launch_dense<Tall>(p, f32, 1, s);
   else launch_dense<Small>(p, f32, 2, s);
   return hipGetLastError();
