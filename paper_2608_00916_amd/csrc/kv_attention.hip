@@ -17,8 +17,10 @@
 // Softmax statistics are fp32.  Probabilities are rounded to fp16 for the
 // second product (11 bits, an eighth of the output's own rounding), times the
 // value scale: with s a key's score and c its value scale, the running maximum
-// is that of s + log2 c, so the weights 2^15 c exp2(s - max) lie in [0, 2^15]
-// and keep all their bits down to 2^-29 of the largest.
+// is that of s + log2 c, so the weights w = 2^7 c exp2(s - max) are bounded by
+// the format whatever c is, and keep all their bits down to 2^-21 of the
+// largest.  The sum of the probabilities (times 2^7) is that of w / c, one
+// factor per 16 tokens.
 #include "serve.hpp"
 #include "trace.hpp"
 
@@ -28,7 +30,8 @@ namespace {
 
 constexpr int kTile = 64;  // tokens per step
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kBoost = 32768.0f;     // largest weight
+constexpr float kBoostLog2 = 7.0f;     // weights of the maximum are 2^7 ...
+constexpr float kSlack = 8.0f;         // ... and at most 2^15: fp16 ends at 2^16
 constexpr float kMinScale = 0x1p-100f;  // of values: a block of zeros has scale 0
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -110,6 +113,10 @@ constexpr int kFew = 16;
 // More: kMany rows per workgroup, 32 per wave; keys and values pass through LDS
 // as fp16.
 constexpr int kMany = 128;
+#ifndef KB_TEST
+#define KB_TEST 2
+#endif
+constexpr int kBlocks = KB_TEST;
 
 // Unit u of the row tiles of many rows: its request and tile.  A request whose
 // rows start at packed row s owns units s g / kMany + b and following.
@@ -151,13 +158,15 @@ __device__ __forceinline__ float load_query(const AttnArgs& p, const bf16_t* row
   return __uint_as_float(e << 23) * p.scale2;
 }
 
-// One row's softmax state, and its update by the 16 scores s[j][i] c that a
-// lane holds of it: on return s holds the weights, and `shrink` what earlier
-// sums must be multiplied by.  `first` is the token of s[0][0].
+// One row's softmax state.  `weigh` turns the 16 scores s[j][i] c that a lane
+// holds of the row into weights; `first` is the token of s[0][0].  The sums are
+// relative to `m`, which follows the running maximum only when that has grown
+// by kSlack: scaling what has been summed up costs as much as the weights do.
+// `shrink` is then the factor for it, 1 otherwise.
 struct Softmax {
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f, shrink = 1.0f;
   template <bool kMask>
-  __device__ __forceinline__ float update(f32x4 (&s)[4], float c, float vs, int first, int limit) {
+  __device__ __forceinline__ void weigh(f32x4 (&s)[4], float c, float vs, int first, int limit) {
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -170,27 +179,30 @@ struct Softmax {
       if (first >= limit) c = vs = 1.0f;
     }
     vs = fmaxf(vs, kMinScale) + (vs != vs ? vs : 0.0f);
+    const float lv = __builtin_amdgcn_logf(vs);
     // c >= 0; a masked score stays -infinity where c is 0
-    top = top == -INFINITY ? -INFINITY : fmaf(top, c, __builtin_amdgcn_logf(vs));
+    top = top == -INFINITY ? -INFINITY : fmaf(top, c, lv);
     top = fmaxf(top, shfl_xor(top, 16));
     top = fmaxf(top, shfl_xor(top, 32));
-    const float m1 = fmaxf(m, top);
-    const float base = m1 == -INFINITY ? 0.0f : m1;  // no key seen yet: every term is 0
-    const float shrink = __builtin_amdgcn_exp2f(m - base);
-    m = m1;
-    const float w = vs * kBoost;
+    shrink = 1.0f;
+    if (__any(top > m + kSlack)) {
+      const float m1 = top > m + kSlack ? top : m;
+      shrink = m1 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m1);
+      l *= shrink;
+      m = m1;
+    }
+    const float shift = m == -INFINITY ? 0.0f : lv + kBoostLog2 - m;  // no key seen yet: every weight is 0
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float e = __builtin_amdgcn_exp2f(fmaf(s[j][i], c, -base));
-        if (kMask && first + 4 * j + i >= limit) e = 0.0f;
-        sum += e;
-        s[j][i] = e * w;
+        float w = __builtin_amdgcn_exp2f(fmaf(s[j][i], c, shift));
+        if (kMask && first + 4 * j + i >= limit) w = 0.0f;
+        sum += w;
+        s[j][i] = w;
       }
-    l = fmaf(l, shrink, sum);
-    return shrink;
+    l = fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
   }
 };
 
@@ -208,7 +220,7 @@ __device__ __forceinline__ bf16_t* out_row(const AttnArgs& p, const Request& rq,
 }
 
 // Factor that turns a row's sums into its output (0 for a row without a key).
-__device__ __forceinline__ float normaliser(float l) { return l == 0.0f ? 0.0f : 1.0f / (l * kBoost); }
+__device__ __forceinline__ float normaliser(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
 template <int D>
 __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
@@ -269,12 +281,15 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
         s[j] = mfma_f16(f16_of(kf[j][i].z, kf[j][i].w), qf[2 * i + 1], s[j]);
       }
     }
-    const float shrink = sm.update<true>(s, ks * c, vs, t + 16 * g, seen ? limit : 0);
+    sm.weigh<true>(s, ks * c, vs, t + 16 * g, seen ? limit : 0);
+    if (__any(sm.shrink != 1.0f)) {
+#pragma unroll
+      for (int d = 0; d < kDt; ++d) o[d] *= sm.shrink;
+    }
     uint4 pf[2];
     pack_weights(s, pf);
 #pragma unroll
     for (int d = 0; d < kDt; ++d) {
-      o[d] *= shrink;
       o[d] = mfma_f16(f16_of(vf[d].x, vf[d].y), pf[0], o[d]);
       o[d] = mfma_f16(f16_of(vf[d].z, vf[d].w), pf[1], o[d]);
     }
@@ -320,8 +335,10 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
   for (int i = 0; i < kPer; ++i) p.part_o[at * D + d0 + i] = acc[i];
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_kv_attention_rows(AttnArgs p) {
+// NB 16-row blocks per wave.
+template <int D, int NB>
+__global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_attention_rows(AttnArgs p) {
+  constexpr int kThreads = 64 * kMany / 16 / NB;
   constexpr int kS = D / 32, kDt = D / 16;
   // keys [64][D], chunks of 8 dims XOR-swizzled; values [D][64], likewise
   __shared__ __attribute__((aligned(16))) uint4 lds_k[2][kTile * D / 8];
@@ -332,85 +349,99 @@ __global__ __launch_bounds__(256, 2) void k_kv_attention_rows(AttnArgs p) {
   const int tiles = cdiv(rq.rows, kMany);
   if (rq.rows <= kFew || unit.tile < 0 || unit.tile >= tiles) return;
   const int r0 = (tiles - 1 - unit.tile) * kMany;  // the longest rows first
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4, m = lane & 15;
   const int t0 = chunk * p.chunk;
   const int t1 = min(t0 + p.chunk, key_limit(p, rq, min(r0 + kMany - 1, rq.rows - 1) / p.group));
   if (t0 >= t1 && chunk > 0) return;
   const int bt = p.c.block_tokens, shift = __builtin_ctz(bt);
 
   // this lane's rows, one per 16-row block of the wave
-  int limit[2];
-  float c[2];
-  uint4 qf[2][kS];
+  const int wr0 = r0 + wv * 16 * NB;
+  int limit[NB];
+  float c[NB];
+  uint4 qf[NB][kS];
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const int row = min(r0 + wv * 32 + n * 16 + (lane & 15), rq.rows - 1), tok = row / p.group;
+  for (int n = 0; n < NB; ++n) {
+    const int row = min(wr0 + n * 16 + m, rq.rows - 1), tok = row / p.group;
     limit[n] = key_limit(p, rq, tok);
     c[n] = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
                       [&](int i) { return 32 * i + 8 * g; }, qf[n]);
   }
   // keys below this are seen by every row of the wave
-  const int all_see = key_limit(p, rq, min(r0 + wv * 32, rq.rows - 1) / p.group);
+  const int all_see = key_limit(p, rq, min(wr0, rq.rows - 1) / p.group);
 
+  // Staging: a wave copies pieces of 64 x 16 bytes, of keys (kTok tokens of one
+  // 16-token group: one block, found through the scalar cache) or of values (16
+  // dims; lane group g copies tokens 16 g .., the ones it needs the scales of).
   const int32_t* table = p.b.block_table + static_cast<int64_t>(unit.b) * p.b.W;
   const int last = p.b.W - 1;
-  // Staging: thread tid copies keys of tokens tk, tk + tk_step (16 dims from
-  // 16 ck) and values of dims dv, dv + 64 (16 tokens from 16 cv).
-  constexpr int kK = D / 64;  // passes
-  constexpr int kTokStep = 256 / (D / 16);
-  const int tk = tid / (D / 16), ck = tid % (D / 16), dv = tid >> 2, cv = tid & 3;
-  auto place = [&](int t) {  // block of token t, -1: none
-    const int i = t >> shift;
-    const int id = table[min(i, last)];
-    return i <= last && id >= 0 && id < p.c.n_blocks ? id : -1;
-  };
+  constexpr int kTok = 1024 / D, kWaves = kThreads / 64;
+  constexpr int kPieces = D / 16 / kWaves;  // of keys, and of values, per wave
+  static_assert(kPieces >= 1 && kPieces * kWaves * 16 == D, "pieces must split evenly over the waves");
+  const int wave = __builtin_amdgcn_readfirstlane(wv);
+  auto k_tok = [&](int i) { return (wave + i * kWaves) * kTok; };  // first token of a piece
+  const int64_t stride = static_cast<int64_t>(p.c.kv_heads) * bt * D;  // of blocks
+  const int8_t* const k_head = p.c.k + static_cast<int64_t>(h) * bt * D;
+  const int8_t* const v_head = p.c.v + static_cast<int64_t>(h) * bt * D;
+  int v_off[kPieces], k_off[kPieces];  // within a block, but for the tile's place in it
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    k_off[i] = ((k_tok(i) + lane / (D / 16)) & (bt - 1)) * D + lane % (D / 16) * 16;
+    v_off[i] = (16 * (wv + i * kWaves) + m) * bt + (16 * g & (bt - 1));
+  }
+  // Block numbers of a tile; tokens past the table are past every limit.
   struct Ids {
-    int k[kK], v, own;
+    int key[kPieces], own;
   };
   auto load_ids = [&](int t) {
     Ids x;
 #pragma unroll
-    for (int i = 0; i < kK; ++i) x.k[i] = place(t + tk + i * kTokStep);
-    x.v = place(t + 16 * cv);
-    x.own = place(t + 16 * g);
+    for (int i = 0; i < kPieces; ++i) x.key[i] = uniform_load(table + min((t + k_tok(i)) >> shift, last));
+    x.own = table[min((t + 16 * g) >> shift, last)];
     return x;
   };
-  uint4 kreg[kK] = {}, vreg[kK] = {};
+  auto valid = [&](int id) { return static_cast<uint32_t>(id) < static_cast<uint32_t>(p.c.n_blocks); };
+  uint4 kreg[kPieces] = {}, vreg[kPieces] = {};
   float ks = 0.0f, vs = 0.0f;
   bool seen = false;
   auto load_tile = [&](int t, const Ids& x) {
+    const int at = t & (bt - 1);
 #pragma unroll
-    for (int i = 0; i < kK; ++i) {
-      const int64_t at = static_cast<int64_t>(max(x.k[i], 0)) * p.c.kv_heads + h;
-      kreg[i] = *reinterpret_cast<const uint4*>(p.c.k + at * bt * D + ((t + tk + i * kTokStep) & (bt - 1)) * D + 16 * ck);
-    }
-    const int64_t at = static_cast<int64_t>(max(x.v, 0)) * p.c.kv_heads + h;
+    for (int i = 0; i < kPieces; ++i)
+      kreg[i] = *reinterpret_cast<const uint4*>(k_head + (valid(x.key[i]) ? x.key[i] : 0) * stride + at * D + k_off[i]);
+    seen = valid(x.own);
+    const int own = seen ? x.own : 0;
+    const int8_t* vp = v_head + own * stride + at;
 #pragma unroll
-    for (int i = 0; i < kK; ++i)
-      vreg[i] = *reinterpret_cast<const uint4*>(p.c.v + at * bt * D + (dv + 64 * i) * bt + ((t + 16 * cv) & (bt - 1)));
-    const int64_t own = static_cast<int64_t>(max(x.own, 0)) * p.c.kv_heads + h;
-    ks = p.c.k_scale[own];
-    vs = p.c.v_scale[own];
-    seen = x.own >= 0;
+    for (int i = 0; i < kPieces; ++i) vreg[i] = *reinterpret_cast<const uint4*>(vp + v_off[i]);
+    ks = p.c.k_scale[static_cast<int64_t>(own) * p.c.kv_heads + h];
+    vs = p.c.v_scale[static_cast<int64_t>(own) * p.c.kv_heads + h];
   };
-  // Rows of one key fragment (tokens 16 (m / 4) + 4 j + m % 4) and of one value
-  // fragment (16 consecutive dims) lie in distinct banks.
-  auto k_at = [&](int tok, int chunk8) { return tok * (D / 8) + (chunk8 ^ ((((tok >> 4) << 2) | (tok & 3)) & (D / 8 - 1))); };
-  auto v_at = [&](int dim, int chunk8) { return dim * 8 + (chunk8 ^ ((dim >> 1) & 7)); };
+  // LDS positions (of 16 bytes).  Reads take 16 lanes at a time, 4 consecutive
+  // ones from each of 4 places of two lane groups; the swizzles keep them, and
+  // the writes, in distinct banks.
+  auto k_at = [&](int tok, int c8) { return tok * (D / 8) + (c8 ^ ((((tok >> 4) << 2) | (tok & 3)) & (D / 8 - 1))); };
+  auto v_at = [&](int dim, int c8) { return dim * 8 + (((c8 >> 1) | (c8 & 1) << 2) ^ ((dim >> 1) & 7)); };
   auto store_tile = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < kK; ++i) {
-      lds_k[buf][k_at(tk + i * kTokStep, 2 * ck)] = f16_of(kreg[i].x, kreg[i].y);
-      lds_k[buf][k_at(tk + i * kTokStep, 2 * ck + 1)] = f16_of(kreg[i].z, kreg[i].w);
-      lds_v[buf][v_at(dv + 64 * i, 2 * cv)] = f16_of(vreg[i].x, vreg[i].y);
-      lds_v[buf][v_at(dv + 64 * i, 2 * cv + 1)] = f16_of(vreg[i].z, vreg[i].w);
+    for (int i = 0; i < kPieces; ++i) {
+      const int tok = k_tok(i) + lane / (D / 16), c8 = lane % (D / 16) * 2, dim = 16 * (wv + i * kWaves) + m;
+      lds_k[buf][k_at(tok, c8)] = f16_of(kreg[i].x, kreg[i].y);
+      lds_k[buf][k_at(tok, c8 + 1)] = f16_of(kreg[i].z, kreg[i].w);
+      lds_v[buf][v_at(dim, 2 * g)] = f16_of(vreg[i].x, vreg[i].y);
+      lds_v[buf][v_at(dim, 2 * g + 1)] = f16_of(vreg[i].z, vreg[i].w);
     }
   };
-
-  Softmax sm[2];
-  f32x4 o[2][kDt];
+  int k_read[kS], v_read[2];  // this lane's positions in fragment 0
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
+  for (int i = 0; i < kS; ++i) k_read[i] = (16 * (m >> 2) + (m & 3)) * (D / 8) + ((4 * i + g) ^ (m & (D / 8 - 1)));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v_read[i] = v_at(m, 2 * g + i);
+
+  Softmax sm[NB];
+  f32x4 o[NB][kDt];
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
 #pragma unroll
     for (int d = 0; d < kDt; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
@@ -428,42 +459,42 @@ __global__ __launch_bounds__(256, 2) void k_kv_attention_rows(AttnArgs p) {
       load_tile(t + kTile, ids);
       ids = load_ids(t + 2 * kTile);
     }
-    f32x4 s[2][4];
+    f32x4 s[NB][4];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int m = lane & 15;
 #pragma unroll
     for (int i = 0; i < kS; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint4 kf = lds_k[buf][k_at(16 * (m >> 2) + 4 * j + (m & 3), 4 * i + g)];
+        const uint4 kf = lds_k[buf][k_read[i] + 4 * j * (D / 8)];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) s[n][j] = mfma_f16(kf, qf[n][i], s[n][j]);
+        for (int n = 0; n < NB; ++n) s[n][j] = mfma_f16(kf, qf[n][i], s[n][j]);
       }
-    uint4 pf[2][2];
-    float shrink[2];
+    uint4 pf[NB][2];
+    bool changed = false;
     const bool mask = t + kTile > all_see || __any(!seen_now);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      shrink[n] = mask ? sm[n].update<true>(s[n], ks_now * c[n], vs_now, t + 16 * g, seen_now ? limit[n] : 0)
-                       : sm[n].update<false>(s[n], ks_now * c[n], vs_now, 0, 0);
+    for (int n = 0; n < NB; ++n) {
+      if (mask) sm[n].template weigh<true>(s[n], ks_now * c[n], vs_now, t + 16 * g, seen_now ? limit[n] : 0);
+      else sm[n].template weigh<false>(s[n], ks_now * c[n], vs_now, 0, 0);
       pack_weights(s[n], pf[n]);
+      changed |= sm[n].shrink != 1.0f;
     }
-    if (__any(shrink[0] != 1.0f || shrink[1] != 1.0f)) {
+    if (__any(changed)) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int d = 0; d < kDt; ++d) o[n][d] *= shrink[n];
+        for (int d = 0; d < kDt; ++d) o[n][d] *= sm[n].shrink;
     }
 #pragma unroll
     for (int d = 0; d < kDt; ++d)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint4 vf = lds_v[buf][v_at(16 * d + m, 2 * g + i)];
+        const uint4 vf = lds_v[buf][v_read[i] + 16 * 8 * d];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) o[n][d] = mfma_f16(vf, pf[n][i], o[n][d]);
+        for (int n = 0; n < NB; ++n) o[n][d] = mfma_f16(vf, pf[n][i], o[n][d]);
       }
     if (more) {
       store_tile(buf ^ 1);
@@ -474,11 +505,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_attention_rows(AttnArgs p) {
   }
 
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
+  for (int n = 0; n < NB; ++n) {
     float l = sm[n].l;
     l += shfl_xor(l, 16);
     l += shfl_xor(l, 32);
-    const int r = r0 + wv * 32 + n * 16 + (lane & 15);
+    const int r = wr0 + n * 16 + m;
     if (r >= rq.rows) continue;
     if (p.chunks == 1) {
       const float inv = normaliser(l);
@@ -592,7 +623,8 @@ void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
     ws = p.part_ml + pl.rows.items() * kMany * 2;
     {
       TraceScope trace_scope(K_KV_ATTENTION, s);
-      hipLaunchKernelGGL(k_kv_attention_rows<D>, dim3(pl.units * p.chunks, heads), dim3(256), 0, s, p);
+      hipLaunchKernelGGL((k_kv_attention_rows<D, kBlocks>), dim3(pl.units * p.chunks, heads),
+                         dim3(64 * kMany / 16 / kBlocks), 0, s, p);
     }
     if (p.chunks > 1) {
       TraceScope trace_scope(K_KV_COMBINE, s);
