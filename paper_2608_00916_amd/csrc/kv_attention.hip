@@ -118,12 +118,36 @@ constexpr int kMany = 128;
 #endif
 constexpr int kBlocks = KB_TEST;
 
-// Unit u of the row tiles of many rows: its request and tile.  A request whose
-// rows start at packed row s owns units s g / kMany + b and following.
+// Unit u of the row tiles of many rows: its request and tile (-1: none).  Work
+// per tile goes with the request's keys, so the requests with the most keys
+// come first (a last round of long ones took 28% of 16 ragged requests).  Up to
+// 64 requests are ranked here, a lane each; beyond that there are workgroups
+// enough, and a request whose rows start at packed row s simply owns units
+// s g / kMany + b and following.
+constexpr int kRanked = 64;
+
 struct Unit {
   int b, tile;
 };
 __device__ __forceinline__ Unit row_unit(const AttnArgs& p, int u) {
+  if (p.b.B <= kRanked) {
+    const int lane = threadIdx.x & 63;
+    int units = 0, keys = 0;
+    if (lane < p.b.B) {
+      const Request r = request(p, lane);
+      units = r.rows > kFew ? cdiv(r.rows, kMany) : 0;
+      keys = r.kv;
+    }
+    int before = 0;
+    for (int i = 0; i < p.b.B; ++i) {
+      const int k = __builtin_amdgcn_readlane(keys, i), n = __builtin_amdgcn_readlane(units, i);
+      before += k > keys || (k == keys && i < lane) ? n : 0;
+    }
+    const unsigned long long mine = __ballot(u >= before && u < before + units);
+    if (mine == 0) return {0, -1};
+    const int b = __builtin_ctzll(mine);
+    return {b, u - __builtin_amdgcn_readlane(before, b)};
+  }
   auto at = [&](int m) { return static_cast<int>(static_cast<int64_t>(row_start(p, m)) * p.group / kMany) + m; };
   int lo = 0, hi = p.b.B;
   while (hi - lo > 1) {
@@ -343,8 +367,9 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
   // keys [64][D], chunks of 8 dims XOR-swizzled; values [D][64], likewise
   __shared__ __attribute__((aligned(16))) uint4 lds_k[2][kTile * D / 8];
   __shared__ __attribute__((aligned(16))) uint4 lds_v[2][kTile * D / 8];
-  const int chunk = blockIdx.x % p.chunks, h = blockIdx.y;
-  const Unit unit = row_unit(p, blockIdx.x / p.chunks);
+  const int heads = p.c.kv_heads, h = blockIdx.x % heads, chunk = blockIdx.x / heads % p.chunks;
+  const int u = blockIdx.x / heads / p.chunks;
+  const Unit unit = row_unit(p, u);
   const Request rq = request(p, unit.b);
   const int tiles = cdiv(rq.rows, kMany);
   if (rq.rows <= kFew || unit.tile < 0 || unit.tile >= tiles) return;
@@ -521,7 +546,7 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
       continue;
     }
     const int64_t at =
-        ((static_cast<int64_t>(blockIdx.x / p.chunks) * p.c.kv_heads + h) * p.chunks + chunk) * kMany + (r - r0);
+        ((static_cast<int64_t>(u) * heads + h) * p.chunks + chunk) * kMany + (r - r0);
     if (g == 0) {
       p.part_ml[at * 2] = sm[n].m;
       p.part_ml[at * 2 + 1] = l;
@@ -623,7 +648,7 @@ void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
     ws = p.part_ml + pl.rows.items() * kMany * 2;
     {
       TraceScope trace_scope(K_KV_ATTENTION, s);
-      hipLaunchKernelGGL((k_kv_attention_rows<D, kBlocks>), dim3(pl.units * p.chunks, heads),
+      hipLaunchKernelGGL((k_kv_attention_rows<D, kBlocks>), dim3(pl.units * p.chunks * heads),
                          dim3(64 * kMany / 16 / kBlocks), 0, s, p);
     }
     if (p.chunks > 1) {

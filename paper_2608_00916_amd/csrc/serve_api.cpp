@@ -175,8 +175,8 @@ int check_batch_dims(const moe_kv_cache* c, const moe_kv_batch* b) {
   if (b == nullptr) return fail(MOE_ERR_ARG, "batch is NULL");
   if (b->B < 1 || b->W < 1 || b->T < 0)
     return fail(MOE_ERR_ARG, "B, W must be positive, T not negative (B=%d W=%d T=%d)", b->B, b->W, b->T);
-  if (static_cast<int64_t>(b->W) * c->block_tokens > 0x7fffffffll || b->B > (1 << 24))
-    return fail(MOE_ERR_ARG, "B=%d or W=%d too large", b->B, b->W);
+  if (static_cast<int64_t>(b->W) * c->block_tokens > (1ll << 30) || b->B > (1 << 24))
+    return fail(MOE_ERR_ARG, "B=%d exceeds 2^24 or W=%d 2^30 tokens", b->B, b->W);
   return MOE_OK;
 }
 
@@ -194,7 +194,7 @@ int check_attn(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* 
   if (a->flags & ~MOE_F_CAUSAL) return fail(MOE_ERR_ARG, "unknown flags 0x%x", a->flags);
   // workgroups and a request's rows are numbered in 32 bits
   const int64_t group = a->heads / c->kv_heads;
-  if (std::min(a->max_q, b->T) * group > (1ll << 30) || b->T * group / 16 + b->B > (1ll << 30))
+  if (std::min(a->max_q, b->T) * group > (1ll << 30) || (b->T * group / 16 + b->B) * c->kv_heads > (1ll << 30))
     return fail(MOE_ERR_ARG, "T=%d x heads=%d too large", b->T, a->heads);
   return MOE_OK;
 }
