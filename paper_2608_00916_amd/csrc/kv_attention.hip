@@ -182,15 +182,37 @@ __device__ __forceinline__ float load_query(const AttnArgs& p, const bf16_t* row
   return __uint_as_float(e << 23) * p.scale2;
 }
 
-// One row's softmax state.  `weigh` turns the 16 scores s[j][i] c that a lane
-// holds of the row into weights; `first` is the token of s[0][0].  The sums are
-// relative to `m`, which follows the running maximum only when that has grown
-// by kSlack: scaling what has been summed up costs as much as the weights do.
-// `shrink` is then the factor for it, 1 otherwise.
+// The scales of the 16 tokens that a lane holds of a tile.
+struct Scales {
+  float key, value_log2, value_inv;
+  __device__ __forceinline__ void set(float ks, float vs) {
+    vs = vs != vs ? vs : fmaxf(vs, kMinScale);
+    key = ks;
+    value_log2 = __builtin_amdgcn_logf(vs);
+    value_inv = __builtin_amdgcn_rcpf(vs);
+  }
+};
+
+// One row's softmax state.  `weigh` turns the 16 scores s[j][i] (times the key
+// scale and c) that a lane holds of the row into weights; `first` is the token
+// of s[0][0].  The sums are relative to `m`, which follows the running maximum
+// only when that has grown by kSlack: a lane finds that by itself, and only
+// then do the lanes of a row meet.  `shrink` is then the factor for earlier
+// sums, 1 otherwise.
 struct Softmax {
   float m = -INFINITY, l = 0.0f, shrink = 1.0f;
   template <bool kMask>
-  __device__ __forceinline__ void weigh(f32x4 (&s)[4], float c, float vs, int first, int limit) {
+  __device__ __forceinline__ void weigh(f32x4 (&s)[4], float c, Scales sc, int first, int limit) {
+    c *= sc.key;
+    if (kMask) {
+      // a block that the row does not see may hold anything; masked scores
+      // stay -infinity, so c must not be 0
+      if (first >= limit) {
+        c = 1.0f;
+        sc.set(1.0f, 1.0f);
+      }
+      c = c == 0.0f ? kMinScale : c;
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -199,34 +221,28 @@ struct Softmax {
         if (kMask && first + 4 * j + i >= limit) s[j][i] = -INFINITY;
         top = fmaxf(top, s[j][i]);
       }
-    if (kMask) {  // a block that the row does not see may hold anything
-      if (first >= limit) c = vs = 1.0f;
-    }
-    vs = fmaxf(vs, kMinScale) + (vs != vs ? vs : 0.0f);
-    const float lv = __builtin_amdgcn_logf(vs);
-    // c >= 0; a masked score stays -infinity where c is 0
-    top = top == -INFINITY ? -INFINITY : fmaf(top, c, lv);
-    top = fmaxf(top, shfl_xor(top, 16));
-    top = fmaxf(top, shfl_xor(top, 32));
+    top = fmaf(top, c, sc.value_log2);
     shrink = 1.0f;
     if (__any(top > m + kSlack)) {
-      const float m1 = top > m + kSlack ? top : m;
-      shrink = m1 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m1);
-      l *= shrink;
-      m = m1;
+      top = fmaxf(top, shfl_xor(top, 16));
+      top = fmaxf(top, shfl_xor(top, 32));
+      if (top > m + kSlack) {
+        shrink = __builtin_amdgcn_exp2f(m - top);
+        l *= shrink;
+        m = top;
+      }
     }
-    const float shift = m == -INFINITY ? 0.0f : lv + kBoostLog2 - m;  // no key seen yet: every weight is 0
-    float sum = 0.0f;
+    // no key seen yet: every weight is 0
+    const float shift = kMask && m == -INFINITY ? 0.0f : sc.value_log2 + kBoostLog2 - m;
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float w = __builtin_amdgcn_exp2f(fmaf(s[j][i], c, shift));
-        if (kMask && first + 4 * j + i >= limit) w = 0.0f;
-        sum += w;
-        s[j][i] = w;
+        s[j][i] = __builtin_amdgcn_exp2f(fmaf(s[j][i], c, shift));
+        sum[i & 1] += s[j][i];
       }
-    l = fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
+    l = fmaf(sum[0] + sum[1], sc.value_inv, l);
   }
 };
 
@@ -305,7 +321,9 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
         s[j] = mfma_f16(f16_of(kf[j][i].z, kf[j][i].w), qf[2 * i + 1], s[j]);
       }
     }
-    sm.weigh<true>(s, ks * c, vs, t + 16 * g, seen ? limit : 0);
+    Scales sc;
+    sc.set(ks, vs);
+    sm.weigh<true>(s, c, sc, t + 16 * g, seen ? limit : 0);
     if (__any(sm.shrink != 1.0f)) {
 #pragma unroll
       for (int d = 0; d < kDt; ++d) o[d] *= sm.shrink;
@@ -474,7 +492,8 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
   if (t0 < t1) load_tile(t0, ids);
   ids = load_ids(t0 + kTile);
   store_tile(0);
-  float ks_now = ks, vs_now = vs;
+  Scales sc;
+  sc.set(ks, vs);
   bool seen_now = seen;
   int buf = 0;
   for (int t = t0; t < t1; t += kTile, buf ^= 1) {
@@ -502,8 +521,8 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
     const bool mask = t + kTile > all_see || __any(!seen_now);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      if (mask) sm[n].template weigh<true>(s[n], ks_now * c[n], vs_now, t + 16 * g, seen_now ? limit[n] : 0);
-      else sm[n].template weigh<false>(s[n], ks_now * c[n], vs_now, 0, 0);
+      if (mask) sm[n].template weigh<true>(s[n], c[n], sc, t + 16 * g, seen_now ? limit[n] : 0);
+      else sm[n].template weigh<false>(s[n], c[n], sc, 0, 0);
       pack_weights(s[n], pf[n]);
       changed |= sm[n].shrink != 1.0f;
     }
@@ -523,8 +542,7 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
       }
     if (more) {
       store_tile(buf ^ 1);
-      ks_now = ks;
-      vs_now = vs;
+      sc.set(ks, vs);
       seen_now = seen;
     }
   }
