@@ -47,6 +47,7 @@ struct AttnArgs {
   int64_t ldo;
   int heads, group;   // query heads, and per kv head
   int max_q, max_kv;
+  int few;            // rows that count as few
   int chunk, chunks;  // keys per workgroup, workgroups per row tile
   float scale2;       // |scale| log2(e)
   bool negative;      // scale < 0: the queries change sign
@@ -105,18 +106,14 @@ __device__ __forceinline__ int key_limit(const AttnArgs& p, const Request& r, in
   return p.causal ? min(r.kv, r.pos0 + i + 1) : r.kv;
 }
 
-// Few rows (at most kFew: single tokens, or a few of one kv head): one
-// workgroup per request, kv head and chunk of keys; its four waves take the
-// chunk's 64-token steps in turn, each key read once into registers, and merge
-// at the end.
-constexpr int kFew = 16;
+// Few rows (single tokens, or a few of one kv head; at most 16, or 32 where
+// some request has more than 16): one workgroup per request, kv head and chunk
+// of keys; its four waves take the chunk's 64-token steps in turn, each key read
+// once into registers, and merge at the end.
 // More: kMany rows per workgroup, 32 per wave; keys and values pass through LDS
 // as fp16.
 constexpr int kMany = 128;
-#ifndef KB_TEST
-#define KB_TEST 2
-#endif
-constexpr int kBlocks = KB_TEST;
+constexpr int kBlocks = 2;
 
 // Unit u of the row tiles of many rows: its request and tile (-1: none).  Work
 // per tile goes with the request's keys, so the requests with the most keys
@@ -135,7 +132,7 @@ __device__ __forceinline__ Unit row_unit(const AttnArgs& p, int u) {
     int units = 0, keys = 0;
     if (lane < p.b.B) {
       const Request r = request(p, lane);
-      units = r.rows > kFew ? cdiv(r.rows, kMany) : 0;
+      units = r.rows > p.few ? cdiv(r.rows, kMany) : 0;
       keys = r.kv;
     }
     int before = 0;
@@ -262,42 +259,48 @@ __device__ __forceinline__ bf16_t* out_row(const AttnArgs& p, const Request& rq,
 // Factor that turns a row's sums into its output (0 for a row without a key).
 __device__ __forceinline__ float normaliser(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-template <int D>
+// NB blocks of 16 rows.
+template <int D, int NB>
 __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
   constexpr int kP = D / 64, kDt = D / 16;
   __shared__ float lds_o[4][16][D];
-  __shared__ float lds_m[4][16], lds_l[4][16];
+  __shared__ float lds_m[NB][4][16], lds_l[NB][4][16];
   const int chunk = blockIdx.x % p.chunks, b = blockIdx.x / p.chunks, h = blockIdx.y;
   const Request rq = request(p, b);
-  if (rq.rows == 0 || rq.rows > kFew) return;
+  if (rq.rows == 0 || rq.rows > p.few) return;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, g = lane >> 4;
   const int t0 = chunk * p.chunk;
   const int t1 = min(t0 + p.chunk, key_limit(p, rq, rq.n - 1));
   if (t0 >= t1 && chunk > 0) return;
   const int bt = p.c.block_tokens, shift = __builtin_ctz(bt);
 
-  // this lane's row; dims 64 i + 16 g + 8 s of slice (i, s): the order in which
+  // this lane's rows; dims 64 i + 16 g + 8 s of slice (i, s): the order in which
   // one 16-byte load of a key supplies two slices
-  const int row = min(lane & 15, rq.rows - 1);
-  const int tok = row / p.group;
-  const int limit = key_limit(p, rq, tok);
-  uint4 qf[2 * kP];
-  const float c = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
-                             [&](int i) { return 64 * (i >> 1) + 16 * g + 8 * (i & 1); }, qf);
-
-  Softmax sm;
-  f32x4 o[kDt];
+  int limit[NB];
+  float c[NB];
+  uint4 qf[NB][2 * kP];
 #pragma unroll
-  for (int d = 0; d < kDt; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < NB; ++n) {
+    const int row = min(n * 16 + (lane & 15), rq.rows - 1), tok = row / p.group;
+    limit[n] = key_limit(p, rq, tok);
+    c[n] = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
+                      [&](int i) { return 64 * (i >> 1) + 16 * g + 8 * (i & 1); }, qf[n]);
+  }
+
+  Softmax sm[NB];
+  f32x4 o[NB][kDt];
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int d = 0; d < kDt; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int32_t* table = p.b.block_table + static_cast<int64_t>(b) * p.b.W;
   const int last = p.b.W - 1;
   const int gk = (lane & 15) >> 2;  // the 16-token group this lane loads keys of
   for (int t = t0 + wv * kTile; t < t1; t += 4 * kTile) {
-    // blocks of the key group and of the value group; past the table: none
-    const int ik = (t + 16 * gk) >> shift, iv = (t + 16 * g) >> shift;
-    const int bk = table[min(ik, last)], bv = table[min(iv, last)];
-    const bool seen = iv <= last && bv >= 0 && bv < p.c.n_blocks;
+    // blocks of the key group and of the value group; tokens past the table are past every limit
+    const int bk = table[min((t + 16 * gk) >> shift, last)], bv = table[min((t + 16 * g) >> shift, last)];
+    const bool seen = bv >= 0 && bv < p.c.n_blocks;
     const int64_t pk = static_cast<int64_t>(bk >= 0 && bk < p.c.n_blocks ? bk : 0) * p.c.kv_heads + h;
     const int64_t pv = static_cast<int64_t>(seen ? bv : 0) * p.c.kv_heads + h;
     const int8_t* kp = p.c.k + pk * bt * D + ((t + 16 * gk + (lane & 3)) & (bt - 1)) * D + 16 * g;
@@ -311,70 +314,94 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
     for (int d = 0; d < kDt; ++d) vf[d] = *reinterpret_cast<const uint4*>(vp + d * 16 * bt);
     const float ks = p.c.k_scale[pv], vs = p.c.v_scale[pv];
 
-    f32x4 s[4];
+    f32x4 s[NB][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int n = 0; n < NB; ++n) s[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kP; ++i) {
-        s[j] = mfma_f16(f16_of(kf[j][i].x, kf[j][i].y), qf[2 * i], s[j]);
-        s[j] = mfma_f16(f16_of(kf[j][i].z, kf[j][i].w), qf[2 * i + 1], s[j]);
+        const uint4 lo = f16_of(kf[j][i].x, kf[j][i].y), hi = f16_of(kf[j][i].z, kf[j][i].w);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          s[n][j] = mfma_f16(lo, qf[n][2 * i], s[n][j]);
+          s[n][j] = mfma_f16(hi, qf[n][2 * i + 1], s[n][j]);
+        }
       }
     }
     Scales sc;
     sc.set(ks, vs);
-    sm.weigh<true>(s, c, sc, t + 16 * g, seen ? limit : 0);
-    if (__any(sm.shrink != 1.0f)) {
+    uint4 pf[NB][2];
 #pragma unroll
-      for (int d = 0; d < kDt; ++d) o[d] *= sm.shrink;
+    for (int n = 0; n < NB; ++n) {
+      sm[n].template weigh<true>(s[n], c[n], sc, t + 16 * g, seen ? limit[n] : 0);
+      if (__any(sm[n].shrink != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < kDt; ++d) o[n][d] *= sm[n].shrink;
+      }
+      pack_weights(s[n], pf[n]);
     }
-    uint4 pf[2];
-    pack_weights(s, pf);
 #pragma unroll
     for (int d = 0; d < kDt; ++d) {
-      o[d] = mfma_f16(f16_of(vf[d].x, vf[d].y), pf[0], o[d]);
-      o[d] = mfma_f16(f16_of(vf[d].z, vf[d].w), pf[1], o[d]);
+      const uint4 lo = f16_of(vf[d].x, vf[d].y), hi = f16_of(vf[d].z, vf[d].w);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        o[n][d] = mfma_f16(lo, pf[n][0], o[n][d]);
+        o[n][d] = mfma_f16(hi, pf[n][1], o[n][d]);
+      }
     }
   }
-  sm.l += shfl_xor(sm.l, 16);
-  sm.l += shfl_xor(sm.l, 32);
 
-  // merge the waves: o[d][i] is dimension 16 d + 4 g + i of row lane % 16
-  if (lane < 16) {
-    lds_m[wv][lane] = sm.m;
-    lds_l[wv][lane] = sm.l;
-  }
+  // merge the waves: o[n][d][i] is dimension 16 d + 4 g + i of row 16 n + lane % 16
 #pragma unroll
-  for (int d = 0; d < kDt; ++d) *reinterpret_cast<f32x4*>(&lds_o[wv][lane & 15][16 * d + 4 * g]) = o[d];
-  __syncthreads();
+  for (int n = 0; n < NB; ++n) {
+    float l = sm[n].l;
+    l += shfl_xor(l, 16);
+    l += shfl_xor(l, 32);
+    if (lane < 16) {
+      lds_m[n][wv][lane] = sm[n].m;
+      lds_l[n][wv][lane] = l;
+    }
+  }
   constexpr int kPer = D / 16;  // dimensions per thread
   const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kPer;
-  if (r >= rq.rows) return;
-  float mm = -INFINITY, ll = 0.0f, acc[kPer] = {};
 #pragma unroll
-  for (int w = 0; w < 4; ++w) mm = fmaxf(mm, lds_m[w][r]);
-  const float base = mm == -INFINITY ? 0.0f : mm;
+  for (int n = 0; n < NB; ++n) {
+    if (n > 0) {
+      if (n * 16 >= rq.rows) return;
+      __syncthreads();  // the block before is merged
+    }
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = __builtin_amdgcn_exp2f(lds_m[w][r] - base);
-    ll += f * lds_l[w][r];
+    for (int d = 0; d < kDt; ++d) *reinterpret_cast<f32x4*>(&lds_o[wv][lane & 15][16 * d + 4 * g]) = o[n][d];
+    __syncthreads();
+    const int row = n * 16 + r;
+    if (row >= rq.rows) continue;
+    float mm = -INFINITY, ll = 0.0f, acc[kPer] = {};
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += f * lds_o[w][r][d0 + i];
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, lds_m[n][w][r]);
+    const float base = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(lds_m[n][w][r] - base);
+      ll += f * lds_l[n][w][r];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[i] += f * lds_o[w][r][d0 + i];
+    }
+    if (p.chunks == 1) {
+      const float inv = normaliser(ll);
+      bf16_t* dst = out_row(p, rq, h, row, D) + d0;
+#pragma unroll
+      for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
+      continue;
+    }
+    const int64_t at = ((static_cast<int64_t>(b) * p.c.kv_heads + h) * p.chunks + chunk) * (16 * NB) + row;
+    if ((threadIdx.x & 15) == 0) {
+      p.part_ml[at * 2] = mm;
+      p.part_ml[at * 2 + 1] = ll;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) p.part_o[at * D + d0 + i] = acc[i];
   }
-  if (p.chunks == 1) {
-    const float inv = normaliser(ll);
-    bf16_t* dst = out_row(p, rq, h, r, D) + d0;
-#pragma unroll
-    for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
-    return;
-  }
-  const int64_t at = ((static_cast<int64_t>(b) * p.c.kv_heads + h) * p.chunks + chunk) * kFew + r;
-  if ((threadIdx.x & 15) == 0) {
-    p.part_ml[at * 2] = mm;
-    p.part_ml[at * 2 + 1] = ll;
-  }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) p.part_o[at * D + d0 + i] = acc[i];
 }
 
 // NB 16-row blocks per wave.
@@ -390,7 +417,7 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
   const Unit unit = row_unit(p, u);
   const Request rq = request(p, unit.b);
   const int tiles = cdiv(rq.rows, kMany);
-  if (rq.rows <= kFew || unit.tile < 0 || unit.tile >= tiles) return;
+  if (rq.rows <= p.few || unit.tile < 0 || unit.tile >= tiles) return;
   const int r0 = (tiles - 1 - unit.tile) * kMany;  // the longest rows first
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4, m = lane & 15;
   const int t0 = chunk * p.chunk;
@@ -410,6 +437,7 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
     c[n] = load_query(p, p.q + static_cast<int64_t>(rq.first + tok) * p.ldq + (h * p.group + row % p.group) * D,
                       [&](int i) { return 32 * i + 8 * g; }, qf[n]);
   }
+  const bool idle = wr0 >= rq.rows;  // this wave only stages
   // keys below this are seen by every row of the wave
   const int all_see = key_limit(p, rq, min(wr0, rq.rows - 1) / p.group);
 
@@ -495,56 +523,61 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
   Scales sc;
   sc.set(ks, vs);
   bool seen_now = seen;
-  int buf = 0;
-  for (int t = t0; t < t1; t += kTile, buf ^= 1) {
+  auto step = [&](int t, int buf) {
     __syncthreads();
     const bool more = t + kTile < t1;
     if (more) {
       load_tile(t + kTile, ids);
       ids = load_ids(t + 2 * kTile);
     }
-    f32x4 s[NB][4];
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < kS; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 kf = lds_k[buf][k_read[i] + 4 * j * (D / 8)];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) s[n][j] = mfma_f16(kf, qf[n][i], s[n][j]);
-      }
-    uint4 pf[NB][2];
-    bool changed = false;
-    const bool mask = t + kTile > all_see || __any(!seen_now);
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      if (mask) sm[n].template weigh<true>(s[n], c[n], sc, t + 16 * g, seen_now ? limit[n] : 0);
-      else sm[n].template weigh<false>(s[n], c[n], sc, 0, 0);
-      pack_weights(s[n], pf[n]);
-      changed |= sm[n].shrink != 1.0f;
-    }
-    if (__any(changed)) {
+    if (!idle) {
+      f32x4 s[NB][4];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int d = 0; d < kDt; ++d) o[n][d] *= sm[n].shrink;
-    }
+        for (int j = 0; j < 4; ++j) s[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int d = 0; d < kDt; ++d)
+      for (int i = 0; i < kS; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint4 vf = lds_v[buf][v_read[i] + 16 * 8 * d];
+        for (int j = 0; j < 4; ++j) {
+          const uint4 kf = lds_k[buf][k_read[i] + 4 * j * (D / 8)];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) o[n][d] = mfma_f16(vf, pf[n][i], o[n][d]);
+          for (int n = 0; n < NB; ++n) s[n][j] = mfma_f16(kf, qf[n][i], s[n][j]);
+        }
+      uint4 pf[NB][2];
+      bool changed = false;
+      const bool mask = t + kTile > all_see || __any(!seen_now);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        if (mask) sm[n].template weigh<true>(s[n], c[n], sc, t + 16 * g, seen_now ? limit[n] : 0);
+        else sm[n].template weigh<false>(s[n], c[n], sc, 0, 0);
+        pack_weights(s[n], pf[n]);
+        changed |= sm[n].shrink != 1.0f;
       }
+      if (__any(changed)) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int d = 0; d < kDt; ++d) o[n][d] *= sm[n].shrink;
+      }
+#pragma unroll
+      for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint4 vf = lds_v[buf][v_read[i] + 16 * 8 * d];
+#pragma unroll
+          for (int n = 0; n < NB; ++n) o[n][d] = mfma_f16(vf, pf[n][i], o[n][d]);
+        }
+    }
     if (more) {
       store_tile(buf ^ 1);
       sc.set(ks, vs);
       seen_now = seen;
     }
+  };
+  for (int t = t0; t < t1; t += 2 * kTile) {  // two steps: LDS positions are constants
+    step(t, 0);
+    if (t + kTile < t1) step(t + kTile, 1);
   }
 
 #pragma unroll
@@ -574,41 +607,77 @@ __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_at
   }
 }
 
-// The chunks of a row joined in order: 16 threads per row, 16 rows per
-// workgroup; kRows rows per row tile of the kernel that wrote them.
+// The chunks of a row of few joined.  Their number may be large and the rows
+// few: one workgroup per row, of whose 16 groups of 16 threads each takes every
+// 16th chunk, in order; the groups' sums meet in LDS.  kRows rows per chunk.
 template <int D, int kRows>
 __global__ __launch_bounds__(256) void k_kv_combine(AttnArgs p) {
   constexpr int kPer = D / 16;
+  __shared__ float lds_o[16][D], lds_l[16];
+  const int b = blockIdx.x, h = blockIdx.y, r = blockIdx.z;
+  const Request rq = request(p, b);
+  if (rq.rows > p.few || r >= rq.rows) return;
+  const int n = max(1, min(p.chunks, cdiv(key_limit(p, rq, rq.n - 1), p.chunk)));
+  const int64_t at = (static_cast<int64_t>(b) * p.c.kv_heads + h) * p.chunks * kRows + r;
+  const float* ml = p.part_ml + at * 2;
+  const int grp = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kPer;
+  const float* po = p.part_o + at * D + d0;
+  float mm = -INFINITY;
+  for (int c = threadIdx.x & 15; c < n; c += 16) mm = fmaxf(mm, ml[c * kRows * 2]);
+#pragma unroll
+  for (int x = 8; x >= 1; x >>= 1) mm = fmaxf(mm, shfl_xor(mm, x));
+  const float base = mm == -INFINITY ? 0.0f : mm;
+  float ll = 0.0f, acc[kPer] = {};
+#pragma unroll 2
+  for (int c = grp; c < n; c += 16) {
+    const float f = __builtin_amdgcn_exp2f(ml[c * kRows * 2] - base);
+    ll += f * ml[c * kRows * 2 + 1];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) acc[x] += f * po[static_cast<int64_t>(c) * kRows * D + x];
+  }
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) lds_o[grp][d0 + x] = acc[x];
+  if (d0 == 0) lds_l[grp] = ll;
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  float l = 0.0f, a0 = 0.0f, a1 = 0.0f;
+  for (int x = 0; x < min(n, 16); ++x) {
+    l += lds_l[x];
+    a0 += lds_o[x][2 * threadIdx.x];
+    a1 += lds_o[x][2 * threadIdx.x + 1];
+  }
+  const float inv = normaliser(l);
+  *reinterpret_cast<uint32_t*>(out_row(p, rq, h, r, D) + 2 * threadIdx.x) = pack_bf16x2(a0 * inv, a1 * inv);
+}
+
+// The chunks of a row of many joined, in order: 16 threads per row, 16 rows per workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void k_kv_combine_rows(AttnArgs p) {
+  constexpr int kPer = D / 16;
   const int h = blockIdx.y;
-  const Unit unit = kRows == kFew ? Unit{static_cast<int>(blockIdx.x), 0} : row_unit(p, blockIdx.x);
+  const Unit unit = row_unit(p, blockIdx.x);
   const Request rq = request(p, unit.b);
-  const int tiles = cdiv(rq.rows, kRows);
-  if ((kRows == kFew) != (rq.rows <= kFew) || unit.tile < 0 || unit.tile >= tiles) return;
-  const int r0 = (tiles - 1 - unit.tile) * kRows;
+  const int tiles = cdiv(rq.rows, kMany);
+  if (rq.rows <= p.few || unit.tile < 0 || unit.tile >= tiles) return;
+  const int r0 = (tiles - 1 - unit.tile) * kMany;
   const int i = blockIdx.z * 16 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * kPer;
   const int r = r0 + i;
   if (r >= rq.rows) return;
-  const int limit = key_limit(p, rq, min(r0 + kRows - 1, rq.rows - 1) / p.group);
+  const int limit = key_limit(p, rq, min(r0 + kMany - 1, rq.rows - 1) / p.group);
   const int n = max(1, min(p.chunks, cdiv(limit, p.chunk)));
-  const int64_t at = (static_cast<int64_t>(blockIdx.x) * p.c.kv_heads + h) * p.chunks * kRows + i;
+  const int64_t at = (static_cast<int64_t>(blockIdx.x) * p.c.kv_heads + h) * p.chunks * kMany + i;
   const float* ml = p.part_ml + at * 2;
   float mm = -INFINITY;
-  for (int c = 0; c < n; ++c) mm = fmaxf(mm, ml[c * kRows * 2]);
+  for (int c = 0; c < n; ++c) mm = fmaxf(mm, ml[c * kMany * 2]);
   const float base = mm == -INFINITY ? 0.0f : mm;
   float ll = 0.0f, acc[kPer] = {};
   const float* po = p.part_o + at * D + d0;
 #pragma unroll 4
   for (int c = 0; c < n; ++c) {
-    const float f = __builtin_amdgcn_exp2f(ml[c * kRows * 2] - base);
-    ll += f * ml[c * kRows * 2 + 1];
+    const float f = __builtin_amdgcn_exp2f(ml[c * kMany * 2] - base);
+    ll += f * ml[c * kMany * 2 + 1];
 #pragma unroll
-    for (int x = 0; x < kPer; x += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(po + static_cast<int64_t>(c) * kRows * D + x);
-      acc[x] += f * v.x;
-      acc[x + 1] += f * v.y;
-      acc[x + 2] += f * v.z;
-      acc[x + 3] += f * v.w;
-    }
+    for (int x = 0; x < kPer; ++x) acc[x] += f * po[static_cast<int64_t>(c) * kMany * D + x];
   }
   const float inv = normaliser(ll);
   bf16_t* dst = out_row(p, rq, h, r, D) + d0;
@@ -634,58 +703,70 @@ Split split(int64_t tiles, int64_t max_kv, int want, int least) {
   return s;
 }
 
-constexpr int kFewItems = 3072, kFewLeast = 256;
-constexpr int kManyItems = 1024, kManyLeast = 512;
+constexpr int kFewItems = 3072, kFewLeast = 512;
+constexpr int kManyItems = 512, kManyLeast = 512;
 
 struct Plan {
-  bool many;  // some request may have more than kFew rows
+  bool many;  // some request may have more than `few_rows` rows
   int units;  // row tiles of those
+  int few_rows;
   Split few, rows;
 };
 
 Plan plan(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
   const int64_t places = static_cast<int64_t>(b.W) * c.block_tokens;
   const int64_t max_kv = a.max_kv < places ? a.max_kv : places;
-  const int64_t group = a.heads / c.kv_heads;
+  const int64_t group = a.heads / c.kv_heads, most = (a.max_q < b.T ? a.max_q : b.T) * group;
   Plan p;
-  p.many = (a.max_q < b.T ? a.max_q : b.T) * group > kFew;
+  p.few_rows = most <= 16 ? 16 : 32;
+  p.many = most > p.few_rows;
   p.units = static_cast<int>(b.T * group / kMany) + b.B;
   p.few = split(static_cast<int64_t>(b.B) * c.kv_heads, max_kv, kFewItems, kFewLeast);
   p.rows = split(static_cast<int64_t>(p.units) * c.kv_heads, max_kv, kManyItems, kManyLeast);
   return p;
 }
 
-template <int D>
-void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
-  const int heads = p.c.kv_heads;
-  if (pl.many) {
-    p.chunk = pl.rows.chunk;
-    p.chunks = pl.rows.chunks;
-    p.part_o = ws;
-    p.part_ml = ws + pl.rows.items() * kMany * D;
-    ws = p.part_ml + pl.rows.items() * kMany * 2;
-    {
-      TraceScope trace_scope(K_KV_ATTENTION, s);
-      hipLaunchKernelGGL((k_kv_attention_rows<D, kBlocks>), dim3(pl.units * p.chunks * heads),
-                         dim3(64 * kMany / 16 / kBlocks), 0, s, p);
-    }
-    if (p.chunks > 1) {
-      TraceScope trace_scope(K_KV_COMBINE, s);
-      hipLaunchKernelGGL((k_kv_combine<D, kMany>), dim3(pl.units, heads, kMany / 16), dim3(256), 0, s, p);
-    }
-  }
-  p.chunk = pl.few.chunk;
-  p.chunks = pl.few.chunks;
+template <int D, int NB>
+void launch_few(AttnArgs p, const Split& sp, float* ws, hipStream_t s) {
+  constexpr int kRows = 16 * NB;
+  p.chunk = sp.chunk;
+  p.chunks = sp.chunks;
   p.part_o = ws;
-  p.part_ml = ws + pl.few.items() * kFew * D;
+  p.part_ml = ws + sp.items() * kRows * D;
   {
     TraceScope trace_scope(K_KV_ATTENTION, s);
-    hipLaunchKernelGGL(k_kv_attention<D>, dim3(p.b.B * p.chunks, heads), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((k_kv_attention<D, NB>), dim3(p.b.B * p.chunks, p.c.kv_heads), dim3(256), 0, s, p);
   }
   if (p.chunks > 1) {
     TraceScope trace_scope(K_KV_COMBINE, s);
-    hipLaunchKernelGGL((k_kv_combine<D, kFew>), dim3(p.b.B, heads, 1), dim3(256), 0, s, p);
+    const int rows = p.max_q * p.group < kRows ? p.max_q * p.group : kRows;
+    hipLaunchKernelGGL((k_kv_combine<D, kRows>), dim3(p.b.B, p.c.kv_heads, rows), dim3(256), 0, s, p);
   }
+}
+
+template <int D>
+void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
+  const int heads = p.c.kv_heads;
+  p.few = pl.few_rows;
+  if (pl.many) {
+    AttnArgs q = p;
+    q.chunk = pl.rows.chunk;
+    q.chunks = pl.rows.chunks;
+    q.part_o = ws;
+    q.part_ml = ws + pl.rows.items() * kMany * D;
+    ws = q.part_ml + pl.rows.items() * kMany * 2;
+    {
+      TraceScope trace_scope(K_KV_ATTENTION, s);
+      hipLaunchKernelGGL((k_kv_attention_rows<D, kBlocks>), dim3(pl.units * q.chunks * heads),
+                         dim3(64 * kMany / 16 / kBlocks), 0, s, q);
+    }
+    if (q.chunks > 1) {
+      TraceScope trace_scope(K_KV_COMBINE, s);
+      hipLaunchKernelGGL(k_kv_combine_rows<D>, dim3(pl.units, heads, kMany / 16), dim3(256), 0, s, q);
+    }
+  }
+  if (pl.few_rows == 16) launch_few<D, 1>(p, pl.few, ws, s);
+  else launch_few<D, 2>(p, pl.few, ws, s);
 }
 
 }  // namespace
@@ -698,7 +779,7 @@ size_t kv_attention_ws(const moe_kv_cache& c, const moe_kv_batch& b, const moe_k
     const int64_t all = s.tiles * cdiv64(a.max_kv, least);
     return all < 2 * want ? all : 2 * want;
   };
-  int64_t rows = items(p.few, kFewItems, kFewLeast) * kFew;
+  int64_t rows = items(p.few, kFewItems, kFewLeast) * 32;
   if (p.many) rows += items(p.rows, kManyItems, kManyLeast) * kMany;
   return static_cast<size_t>(rows) * (c.head_dim + 2) * sizeof(float);
 }
@@ -706,7 +787,7 @@ size_t kv_attention_ws(const moe_kv_cache& c, const moe_kv_batch& b, const moe_k
 hipError_t launch_kv_attention(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a, const bf16_t* q,
                                int64_t ldq, bf16_t* out, int64_t ldo, void* ws, hipStream_t s) {
   const AttnArgs p{c,       b,       q,       ldq, out, ldo, a.heads, a.heads / c.kv_heads,
-                   a.max_q, a.max_kv, 0, 0,   (a.scale < 0 ? -a.scale : a.scale) * kLog2e,
+                   a.max_q, a.max_kv, 0, 0, 0, (a.scale < 0 ? -a.scale : a.scale) * kLog2e,
                    a.scale < 0, (a.flags & MOE_F_CAUSAL) != 0, nullptr, nullptr};
   if (c.head_dim == 64) launch<64>(p, plan(c, b, a), static_cast<float*>(ws), s);
   else launch<128>(p, plan(c, b, a), static_cast<float*>(ws), s);
