@@ -92,14 +92,14 @@ def reference(m, xs):
     return (h + y)[0]
 
 
-def main():
+def main(argv=None):
     ap = argparse.ArgumentParser()
     ap.add_argument("--requests", type=int, default=16)
     ap.add_argument("--tokens", type=int, default=512, help="longest prompt")
     ap.add_argument("--steps", type=int, default=4, help="single-token steps after the prompts")
     ap.add_argument("--hidden", type=int, default=2048)
     ap.add_argument("--experts", type=int, default=128)
-    args = ap.parse_args()
+    args = ap.parse_args(argv)
     B, H = args.requests, args.hidden
     layer = Layer(H, heads=32, kv_heads=4, D=128, E=args.experts, F=768, k=8)
     g = torch.Generator(device="cuda").manual_seed(1)

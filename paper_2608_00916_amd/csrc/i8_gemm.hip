@@ -132,28 +132,44 @@ __global__ __launch_bounds__(C::kThreads) void k_i8_matmul(DenseArgs p) {
 }
 
 // ---------------------------------------------------------------- few rows
-// 16 columns per workgroup, its 8 waves taking the 64-byte slices of k in turn,
-// so that a CU has every byte of its weight rows in flight at once; the waves'
-// sums meet in LDS.  With kFused the rows of A are bf16, and every workgroup
-// rounds them to int8 in LDS itself: one launch, no trip through memory.
+// Tiles of 16 MT x 16 NT whose 8 waves take the 64-byte slices of k in turn:
+// every wave has operands of its own, so they go straight into registers, with
+// several slices of each wave in flight at once; the waves' sums meet in LDS.
+// Where tiles are few this beats the streamed tiles, whose steps follow each
+// other (512 x 1024 x 8192: 64 steps of 1 us).  With kFused the rows of A are
+// bf16, and every workgroup rounds them to int8 in LDS itself: one launch, no
+// trip through memory.
 constexpr int kFewWaves = 8;
 constexpr int kFusedRows = 16, kFusedBytes = 49152;
 
-// MT: 16-row blocks of A.
-template <int MT, bool kFused, bool F32>
+template <int MT, int NT, bool kFused, bool F32>
 __global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(DenseArgs p, const bf16_t* __restrict__ x, int64_t ldx) {
   extern __shared__ __attribute__((aligned(16))) int8_t a8[];  // kFused: [M][K + 16]
-  __shared__ i32x4 sums[kFewWaves][MT][64];
+  __shared__ i32x4 sums[kFewWaves][MT][NT][64];
   __shared__ float scales[kFusedRows];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, g = lane >> 4, i16 = lane & 15;
-  const int n0 = blockIdx.x * 16;
-  const int8_t* brow = p.b + static_cast<int64_t>(min(n0 + i16, p.N - 1)) * p.K;
-  constexpr int kAhead = 4;  // slices in flight per wave
-  const int slices = cdiv(p.K, 64);
-  uint4 b[kAhead];
-  auto load_b = [&](int s) { return *reinterpret_cast<const uint4*>(brow + min(s * 64 + g * 16, p.K - 16)); };
+  const int nt = cdiv(p.N, 16 * NT);
+  const int m0 = blockIdx.x / nt * (16 * MT), n0 = blockIdx.x % nt * (16 * NT);
+  const int8_t *arow[MT], *brow[NT];
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) b[i] = load_b(min(wv + i * kFewWaves, slices - 1));
+  for (int m = 0; m < MT; ++m) arow[m] = p.a + static_cast<int64_t>(min(m0 + m * 16 + i16, p.M - 1)) * p.K;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) brow[n] = p.b + static_cast<int64_t>(min(n0 + n * 16 + i16, p.N - 1)) * p.K;
+  constexpr int kAhead = NT == 1 ? 4 : 2;  // slices in flight per wave
+  const int slices = cdiv(p.K, 64);
+  uint4 b[kAhead][NT], a[kFused ? 1 : kAhead][MT];
+  // chunks past K are read from K's last one and cleared in A
+  auto load = [&](int s, int i) {
+    const int k = min(s, slices - 1) * 64 + g * 16, kk = min(k, p.K - 16);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) b[i][n] = *reinterpret_cast<const uint4*>(brow[n] + kk);
+    if constexpr (!kFused) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) a[i][m] = *reinterpret_cast<const uint4*>(arow[m] + kk);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(wv + i * kFewWaves, i);
   if constexpr (kFused) {
     for (int r = wv; r < p.M; r += kFewWaves) {
       const bf16_t* src = x + r * ldx;
@@ -166,9 +182,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(DenseArgs p, const bf
     }
     __syncthreads();
   }
-  i32x4 acc[MT];
+  i32x4 acc[MT][NT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) acc[m] = i32x4{0, 0, 0, 0};
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
   for (int s0 = wv; s0 < slices; s0 += kAhead * kFewWaves) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -176,25 +194,29 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(DenseArgs p, const bf
       const int k = s * 64 + g * 16;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const int row = m * 16 + i16;
-        uint4 a = make_uint4(0, 0, 0, 0);
-        if (row < p.M && k < p.K)
-          a = kFused ? *reinterpret_cast<const uint4*>(a8 + row * (p.K + 16) + k)
-                     : *reinterpret_cast<const uint4*>(p.a + static_cast<int64_t>(row) * p.K + k);
-        acc[m] = mfma_i8(b[i], a, acc[m]);
+        uint4 x8 = make_uint4(0, 0, 0, 0);
+        if constexpr (kFused) {
+          if (i16 < p.M && k < p.K) x8 = *reinterpret_cast<const uint4*>(a8 + i16 * (p.K + 16) + k);
+        } else {
+          if (k < p.K) x8 = a[i][m];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_i8(b[i][n], x8, acc[m][n]);
       }
-      b[i] = load_b(min(s + kAhead * kFewWaves, slices - 1));
+      load(s + kAhead * kFewWaves, i);
     }
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m) sums[wv][m][lane] = acc[m];
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sums[wv][m][n][lane] = acc[m][n];
   __syncthreads();
-  for (int i = threadIdx.x; i < MT * 256; i += 64 * kFewWaves) {
-    const int m = i >> 8, r = i >> 4 & 15, c = i & 15, row = m * 16 + r, col = n0 + c;
+  for (int i = threadIdx.x; i < MT * NT * 256; i += 64 * kFewWaves) {
+    const int c = i % (16 * NT), r = i / (16 * NT), row = m0 + r, col = n0 + c;
     if (row >= p.M || col >= p.N) continue;
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) sum += sums[w][m][(c >> 2) * 16 + r][c & 3];
+    for (int w = 0; w < kFewWaves; ++w) sum += sums[w][r >> 4][c >> 4][(c >> 2 & 3) * 16 + (r & 15)][c & 3];
     const float v = static_cast<float>(sum) * (kFused ? scales[row] : p.sa[row]) * p.sb[col];
     if (F32) static_cast<float*>(p.out)[row * p.ldo + col] = v;
     else static_cast<bf16_t*>(p.out)[row * p.ldo + col] = f2bf(v);
@@ -465,14 +487,12 @@ void launch_dense(const DenseArgs& p, bool f32, int per_cu, hipStream_t s) {
   else launch_dense<C, false, false>(p, per_cu, s);
 }
 
-constexpr int kFewRows = 128;
-
-template <int MT, bool kFused>
+template <int MT, int NT, bool kFused>
 void launch_few(const DenseArgs& p, const bf16_t* x, int64_t ldx, bool f32, hipStream_t s) {
-  const dim3 grid(cdiv(p.N, 16)), block(64 * kFewWaves);
+  const dim3 grid(cdiv(p.M, 16 * MT) * cdiv(p.N, 16 * NT)), block(64 * kFewWaves);
   const int lds = kFused ? p.M * (p.K + 16) : 0;
-  if (f32) hipLaunchKernelGGL((k_i8_few<MT, kFused, true>), grid, block, lds, s, p, x, ldx);
-  else hipLaunchKernelGGL((k_i8_few<MT, kFused, false>), grid, block, lds, s, p, x, ldx);
+  if (f32) hipLaunchKernelGGL((k_i8_few<MT, NT, kFused, true>), grid, block, lds, s, p, x, ldx);
+  else hipLaunchKernelGGL((k_i8_few<MT, NT, kFused, false>), grid, block, lds, s, p, x, ldx);
 }
 
 template <class C, template <class, bool> class Job, bool kGather>
@@ -494,9 +514,22 @@ void launch_down(const GroupedArgs& p, int rows_cap, int per_cu, hipStream_t s) 
   launch_grouped<C, DownJob, false>(p, rows_cap, p.F, cdiv(p.H, C::BN), per_cu, s);
 }
 
-// Few rows per expert: reading the weights bounds the products, and low tiles
-// keep two workgroups' copies in flight.
-bool few_rows(int rows_cap, int E) { return rows_cap <= 24ll * E; }
+// The lowest tile that runs in one round of two workgroups per CU, counting half
+// a part-filled row tile per expert; Low and Small also while most of a higher
+// tile would be empty.  us of the gate/up product as Low, Small, Tall (H 2048,
+// F 768; E x rows per expert): 8 x 256 21 24 29; 8 x 512 36 24 29; 8 x 1024 65
+// 43 39; 128 x 24 78 86 97; 128 x 64 107 95 102; 128 x 128 164 137 129; down:
+// 8 x 128 11 13 14; 16 x 128 19 14 17; 128 x 64 50 45 49; 128 x 512 328 230 211.
+enum class Rows { kLow, kSmall, kTall };
+
+Rows rows_of(int rows_cap, int E, int width) {
+  const auto one_round = [&](int bm, int bn) {
+    return (static_cast<double>(rows_cap) / bm + 0.5 * E) * cdiv(width, bn) < 2 * kCus;
+  };
+  if (rows_cap <= 24ll * E || one_round(Low::BM, Low::BN)) return Rows::kLow;
+  if (rows_cap <= 96ll * E || one_round(Small::BM, Small::BN)) return Rows::kSmall;
+  return Rows::kTall;
+}
 
 }  // namespace
 
@@ -504,12 +537,26 @@ hipError_t launch_i8_matmul(const int8_t* a, const float* sa, const int8_t* b, c
                             void* out, int64_t ldo, bool f32, hipStream_t s) {
   TraceScope trace_scope(K_I8_MATMUL, s);
   const DenseArgs p{a, sa, b, sb, M, N, K, out, ldo};
-  if (M <= 16) launch_few<1, false>(p, nullptr, 0, f32, s);
-  else if (M <= 32) launch_few<2, false>(p, nullptr, 0, f32, s);
-  else if (M <= 64) launch_few<4, false>(p, nullptr, 0, f32, s);
-  else if (M <= kFewRows) launch_few<8, false>(p, nullptr, 0, f32, s);
-  else if (static_cast<int64_t>(cdiv(M, 256)) * cdiv(N, 256) >= kCus) launch_dense<Tall>(p, f32, 1, s);
-  else launch_dense<Small>(p, f32, 2, s);
+  // Few tiles: 8 waves split k within a tile, up to one tile per CU (a weight
+  // for up to 64 rows: two).  us at K 8192, as 16 MT x 16, 32 x 64, 64 x 64 and
+  // streamed: 16 x 5120 16 21 28 62; 64 x 1024 20 25 34 50; 64 x 5120 39 26 34
+  // 64; 512 x 1024 - 26 35 59; 1024 x 1024 - 47 35 63; 128 x 16384 - 92 68 66.
+  // 64 x 64 against streamed at 512 x 1024: K 512 9.7 6.7, K 2048 13.2 15.6.
+  // Tall tiles gain from half a round on: 160 of them at K 2048 21 against 26.
+  const auto tiles = [&](int bm, int bn) { return static_cast<int64_t>(cdiv(M, bm)) * cdiv(N, bn); };
+  if (M <= 64 && cdiv(M, 16) * tiles(64, 16) <= 2 * kCus) {
+    if (M <= 16) launch_few<1, 1, false>(p, nullptr, 0, f32, s);
+    else if (M <= 32) launch_few<2, 1, false>(p, nullptr, 0, f32, s);
+    else launch_few<4, 1, false>(p, nullptr, 0, f32, s);
+  } else if (M <= 32 || tiles(32, 64) <= kCus) {
+    launch_few<2, 4, false>(p, nullptr, 0, f32, s);
+  } else if (K >= 2048 && tiles(64, 64) <= kCus) {
+    launch_few<4, 4, false>(p, nullptr, 0, f32, s);
+  } else if (tiles(256, 256) > kCus / 2) {
+    launch_dense<Tall>(p, f32, 1, s);
+  } else {
+    launch_dense<Small>(p, f32, 2, s);
+  }
   return hipGetLastError();
 }
 
@@ -517,7 +564,7 @@ bool launch_i8_linear_fused(const bf16_t* x, int64_t ldx, const int8_t* b, const
                             void* out, int64_t ldo, bool f32, hipStream_t s) {
   if (M > kFusedRows || static_cast<int64_t>(M) * (K + 16) > kFusedBytes) return false;
   TraceScope trace_scope(K_I8_MATMUL, s);
-  launch_few<1, true>(DenseArgs{nullptr, nullptr, b, sb, M, N, K, out, ldo}, x, ldx, f32, s);
+  launch_few<1, 1, true>(DenseArgs{nullptr, nullptr, b, sb, M, N, K, out, ldo}, x, ldx, f32, s);
   return true;
 }
 
@@ -525,8 +572,11 @@ hipError_t launch_i8_gateup(const I8Rows& r, const int8_t* x, const float* sx, c
                             const moe_i8_experts& w, int H, int F, int16_t* a, float* a_top, hipStream_t s) {
   TraceScope trace_scope(K_I8_GATEUP, s);
   const GroupedArgs p{r.offsets, r.E, x, sx, rows, w, H, F, a, a_top, nullptr};
-  if (few_rows(r.rows_cap, r.E)) launch_gateup<Low>(p, r.rows_cap, 2, s);
-  else launch_gateup<Tall>(p, r.rows_cap, 1, s);
+  switch (rows_of(r.rows_cap, r.E, F * 2)) {
+    case Rows::kLow: launch_gateup<Low>(p, r.rows_cap, 2, s); break;
+    case Rows::kSmall: launch_gateup<Small>(p, r.rows_cap, 2, s); break;
+    case Rows::kTall: launch_gateup<Tall>(p, r.rows_cap, 1, s); break;
+  }
   return hipGetLastError();
 }
 
@@ -534,8 +584,11 @@ hipError_t launch_i8_down(const I8Rows& r, const int8_t* a, const float* sa, con
                           bf16_t* o, hipStream_t s) {
   TraceScope trace_scope(K_I8_DOWN, s);
   const GroupedArgs p{r.offsets, r.E, a, sa, nullptr, w, H, F, nullptr, nullptr, o};
-  if (few_rows(r.rows_cap, r.E)) launch_down<Low>(p, r.rows_cap, 2, s);
-  else launch_down<Tall>(p, r.rows_cap, 1, s);
+  switch (rows_of(r.rows_cap, r.E, H)) {
+    case Rows::kLow: launch_down<Low>(p, r.rows_cap, 2, s); break;
+    case Rows::kSmall: launch_down<Small>(p, r.rows_cap, 2, s); break;
+    case Rows::kTall: launch_down<Tall>(p, r.rows_cap, 1, s); break;
+  }
   return hipGetLastError();
 }
 

@@ -137,6 +137,18 @@ def test_matmul_large(M, N, K, fp32):
     assert ((out.double() - ref).abs() <= ref.abs() * (4 * 2.0 ** -24 + (0 if fp32 else BF))).all()
 
 
+@pytest.mark.parametrize("M,N,K", [
+    (16, 9001, 144), (32, 20011, 208), (60, 5000, 1040), (100, 1999, 2064),  # 32 x 64 tiles
+    (1000, 1001, 2064), (70, 16100, 2048),                                  # 64 x 64
+    (300, 4099, 400), (700, 3001, 1040), (2000, 1504, 272),                 # streamed
+    (2500, 3300, 144), (2304, 4096, 384),                                   # and tall
+])
+@pytest.mark.parametrize("fp32", [False, True])
+def test_matmul_between(M, N, K, fp32):
+    """Every tile shape, ragged; sums are exact, so only the output's rounding is left."""
+    test_matmul_large(M, N, K, fp32)
+
+
 def test_matmul_full_range():
     """K products of 127 * 127 at the largest K: the sum needs 31 bits."""
     import torch
@@ -229,6 +241,16 @@ def test_experts(rows, counts, H, F):
     assert (first[r0:] == 5).all()  # rows past the counts are not written
 
 
+@pytest.mark.parametrize("rows,counts,H,F", [
+    (4500, [1401, 0, 2899, 200], 1024, 640),
+    (6144, [64] * 96, 256, 256),
+    (12000, [5001, 0, 6743, 200], 1024, 640),
+])
+def test_experts_many_rows(rows, counts, H, F):
+    """Tiles of 128 and of 256 rows, some part-filled."""
+    test_experts(rows, counts, H, F)
+
+
 def test_experts_rows_past_the_capacity_and_the_counts():
     import torch
     import paper_2608_00916_amd as moe
@@ -282,6 +304,12 @@ def test_infer_is_routing_experts_and_combine(T, H, E, F, k, masked):
     row, gate = v["row_of"].cpu().numpy(), host(v["gates"])
     ref = (gate[..., None] * host(o)[np.maximum(row, 0)] * (row >= 0)[..., None]).sum(1)
     assert (np.abs(got - ref) <= BF * SLACK * np.abs(ref) + 1e-6 * np.abs(ref).max()).all()
+
+
+@pytest.mark.parametrize("T,H,E,F", [(700, 512, 32, 384), (3000, 512, 32, 384)])
+def test_infer_many_rows(T, H, E, F):
+    """Rows of x taken by token, in tiles of 128 and of 256 rows."""
+    test_infer_is_routing_experts_and_combine(T, H, E, F, 8, False)
 
 
 # ------------------------------------------------------------------ tables
@@ -508,6 +536,25 @@ def test_long_keys_are_split_and_joined():
     attend(pg, [150, 2, 190], [5000, 9, 2600], 8)
 
 
+@pytest.mark.parametrize("heads", [5, 8])
+def test_long_keys_of_a_few_tokens(heads):
+    """17 to 32 rows of a request: registers only, with the keys split."""
+    say("long keys, few tokens", heads)
+    pg = Pages(gen(24), [5000, 9, 2600, 70], 32, 1, 128)
+    attend(pg, [4, 2, 3, 0], [5000, 9, 2600, 70], heads)
+    attend(pg, [4, 2, 3, 0], [5000, 9, 2600, 70], heads, causal=False, scale=0.3)
+
+
+@pytest.mark.parametrize("B", [64, 65, 100])
+def test_many_requests_of_many_tokens(B):
+    """Up to 64 requests are taken by their keys, more in their order."""
+    say("many requests of many tokens", B)
+    g = gen(25)
+    kv = g.integers(1, 150, B).tolist()
+    pg = Pages(g, kv, 16, 1, 64)
+    attend(pg, [int(g.integers(0, n + 1)) for n in kv], kv, 4)
+
+
 def test_rows_without_a_key():
     """More new tokens than the cache holds: the first see nothing, and are 0."""
     say("rows without a key")
@@ -633,3 +680,20 @@ def test_one_step_on_another_stream_and_in_a_graph():
         assert torch.equal(lin2.out, want)
         assert torch.equal(captured[0].k, eager[0].k) and torch.equal(captured[0].k_scale, eager[0].k_scale)
         assert torch.equal(captured[1], eager[1])
+
+
+def test_the_example():
+    """All operators together: prompts, then single tokens.  Each of the 6 roundings to 8 bits of
+    a step (4 operands, keys, values) is off by up to half a step of its largest value, under
+    0.5 / 127 of it: together under 2.4 percent of parts that add to x."""
+    import torch
+    import importlib.util
+    import os
+    say("example")
+    spec = importlib.util.spec_from_file_location("serve_int8", os.path.join(
+        os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_int8.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    err = ex.main(["--requests", "5", "--tokens", "40", "--steps", "2", "--hidden", "256", "--experts", "16"])
+    torch.cuda.synchronize()
+    assert err <= 0.05
