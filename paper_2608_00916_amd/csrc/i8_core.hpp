@@ -10,9 +10,10 @@
 // linear in the lanes, so the swizzle is applied to the global address.
 //
 // The B fragment is fed first, so a lane holds four consecutive fragment rows
-// of B.  Fragment n of a wave takes rows 4 FN (i / 4) + 4 n + i % 4 (i < 16):
-// lane l then holds C[m = l % 16][4 FN (l / 16) + 4 n + i], 4 FN consecutive
-// columns over its FN = 4 fragments, stored 16 bytes at a time.
+// of B.  Fragment n of a wave takes rows col(n) + 8 (i / 4) + i % 4 (i < 16):
+// lane l then holds C[m = l % 16][col(n) + 8 (l / 16) + i], two runs of 8
+// columns over its FN = 4 fragments; of either run the four lanes of a row
+// store 64 consecutive bytes of bf16.
 //
 // Two LDS stages: the copies of step k + 1 run under the products of step k,
 // and those of the next tile's first step under this tile's last one.  Loads
@@ -43,10 +44,27 @@ __device__ __forceinline__ i32x4 mfma_i8(const uint4& p, const uint4& q, i32x4 a
 
 // 16 bytes per lane from a buffer resource to LDS at base + 16 lane; offsets at
 // or past the resource's size read zeros (the check covers the per-lane offset
-// only, so all of the offset is in it).
-__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, int8_t* lds_base) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds_base), 16,
-                                           static_cast<int>(off), 0, 0, 0);
+// only, so all of the offset is in it).  The instructions are written out
+// because the compiler, which cannot tell the stages apart, makes every LDS
+// read wait for the copies that it knows of: the products then overlap with no
+// copy.  Their waits are wait_vm's below.  The nop covers the distance from a
+// VALU write of the resource's or base's registers, and from that of m0.
+__device__ __forceinline__ void copy_to_lds(i32x4 r, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds_base), "v"(off), "s"(r)
+               : "memory");
+}
+
+__device__ __forceinline__ void copy_to_lds(const int8_t* p, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(lds_base), "v"(p)
+               : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(int8_t* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int8_t*)(p)));
 }
 
 constexpr uint32_t kI8Oob = 0x80000000u;  // an offset past every resource
@@ -64,7 +82,10 @@ struct I8Source {
 template <int N>
 __device__ __forceinline__ void wait_vm() {
   static_assert(N < 64, "the counter has 6 bits");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  asm volatile("" ::: "memory");
+  // the builtin, so that the compiler too takes its own loads as done
+  __builtin_amdgcn_s_waitcnt((N & 15) | N >> 4 << 14 | 7 << 4 | 15 << 8);
+  asm volatile("" ::: "memory");
 }
 
 // All waves are here; LDS reads before it have returned (their products were
@@ -82,19 +103,19 @@ struct I8Tile {
   static constexpr int kWaves = WM * WN;
   static constexpr int kThreads = 64 * kWaves;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  static constexpr int kRun = 4 * FN;  // consecutive columns a lane holds
+  static constexpr int col(int n) { return (n >> 1) * 32 + (n & 1) * 4; }  // of a lane's four columns of fragment n
   static constexpr int kStage = (BM + BN) * kI8Step;
   static constexpr int kCopies = (BM + BN) / 8 / kWaves;  // of 8 rows, per wave and step
   static constexpr int kCopiesA = BM / 8 / kWaves;
   static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "rows must split evenly over the waves");
-  static_assert(FN == 4, "a lane holds 16 columns, and the B swizzle separates rows 16 apart");
+  static_assert(FN == 4, "a lane holds two runs of 8 columns");
 };
 
 // Chunk position of chunk c of row r of either operand.  LDS has 64 banks (256
 // bytes, two rows): the XOR separates the row pairs of one fragment.
 __device__ __forceinline__ int a_swizzle(int r, int c) { return c ^ ((r >> 1) & 7); }
-__device__ __forceinline__ int b_swizzle(int r, int c) {  // fragment rows: 4 together, 16 apart
-  return c ^ (((r >> 1) & 1) | (((r >> 4) & 3) << 1));
+__device__ __forceinline__ int b_swizzle(int r, int c) {  // fragment rows: 4 together, 8 apart
+  return c ^ (((r >> 1) & 1) | (((r >> 3) & 3) << 1));
 }
 
 // Work items of a persistent grid over n tiles.  Where the last, incomplete
@@ -123,14 +144,13 @@ struct Items {
 //   I8Source a(const Tile&)       the tile's rows of A
 //   I8Source b(const Tile&, int)  of B, part 0 .. kParts - 1: B row q is row
 //   int b_part(q), b_row(q)       b_row(q) of part b_part(q)
-//   void prefetch(const Tile&)    called before the tile's last step
+//   void prefetch(const Tile&)    called before the tile's first step: loads within the loop
+//                                 would make every round wait for its copies
 //   bool kSkip                    waves without a valid row skip the products
 //   void finish(const Tile&, acc) its results; waves without a valid row skip it
-//   bool whole(const Tile&)       every lane of this wave stores all its results:
-//                                 then finish issues kStores stores
 // kGather: rows of A through an index, at 64-bit offsets.
 template <class C, bool kTail, bool kGather, class Job>
-__device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st0, int8_t* st1) {
+__device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st) {
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wv / C::WN, wn = wv % C::WN;
   const int steps = cdiv(K, kI8Step);
@@ -151,21 +171,21 @@ __device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st
     }
   };
   auto rsrc = [&](const I8Source& x) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(x.base), 0, x.rows * K, 0x00020000);
+    const uint64_t p = reinterpret_cast<uint64_t>(x.base);
+    return i32x4{static_cast<int>(p), static_cast<int>(p >> 32 & 0xffff), x.rows * K, 0x00020000};
   };
-  auto load = [&](int kt, int8_t* st) {
+  auto load = [&](int kt, int8_t* to) {
     const bool part = kTail && (kt + 1) * kI8Step > K;
-    const __amdgpu_buffer_rsrc_t ra = rsrc(sa);
-    __amdgpu_buffer_rsrc_t rb[Job::kParts];
+    const i32x4 ra = rsrc(sa);
+    i32x4 rb[Job::kParts];
 #pragma unroll
     for (int q = 0; q < Job::kParts; ++q) rb[q] = rsrc(sb[q]);
 #pragma unroll
     for (int i = 0; i < C::kCopies; ++i) {
-      int8_t* dst = st + row0(i) * kI8Step;
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_address(to)) + row0(i) * kI8Step;
       if (i < C::kCopiesA) {
         if constexpr (kGather) {
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(gather[i] + kt * kI8Step),
-                                           (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+          copy_to_lds(gather[i] + kt * kI8Step, dst);
         } else {
           uint32_t off = static_cast<uint32_t>((lane >> 3) * K + a_chunk(i) + (row0(i) * K + kt * kI8Step));
           if (part && kt * kI8Step + a_chunk(i) >= K) off = kI8Oob;
@@ -182,17 +202,17 @@ __device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st
   };
   const int g = lane >> 4, i16 = lane & 15;
   i32x4 acc[C::FM][C::FN];
-  auto compute = [&](const int8_t* st) {
-    const int8_t* at = st + (wm * C::FM * 16 + i16) * kI8Step;
-    const int brow = C::kRun * (i16 >> 2) + (i16 & 3);
-    const int8_t* bt = st + (C::BM + wn * C::FN * 16 + brow) * kI8Step;
+  auto compute = [&](const int8_t* from) {
+    const int8_t* at = from + (wm * C::FM * 16 + i16) * kI8Step;
+    const int brow = 8 * (i16 >> 2) + (i16 & 3);
+    const int8_t* bt = from + (C::BM + wn * C::FN * 16 + brow) * kI8Step;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       uint4 b[C::FN];
       const int ca = a_swizzle(i16, s * 4 + g) * 16;
 #pragma unroll
       for (int n = 0; n < C::FN; ++n)
-        b[n] = *reinterpret_cast<const uint4*>(bt + n * 4 * kI8Step + b_swizzle(brow, s * 4 + g) * 16);
+        b[n] = *reinterpret_cast<const uint4*>(bt + C::col(n) * kI8Step + b_swizzle(brow, s * 4 + g) * 16);
 #pragma unroll
       for (int m = 0; m < C::FM; ++m) {
         const uint4 a = *reinterpret_cast<const uint4*>(at + m * 16 * kI8Step + ca);
@@ -221,49 +241,42 @@ __device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st
   int t = find(blockIdx.x, cur);
   if (t >= items) return;
   sources(cur);
-  load(0, st0);
+  load(0, st);
   wait_vm<0>();
+  int8_t *now = st, *then = st + C::kStage;
+  auto swap = [&] {
+    int8_t* x = now;
+    now = then;
+    then = x;
+  };
   while (true) {
-    typename Job::Tile next = cur;
-    int tn = items;
-    auto load_next = [&] {
-      tn = find(t + gridDim.x, next);
-      if (tn >= items) return;
-      sources(next);
-      load(0, st0);
-    };
     const bool live = !Job::kSkip || wm * C::FM * 16 < cur.rows;
 #pragma unroll
     for (int m = 0; m < C::FM; ++m)
 #pragma unroll
       for (int n = 0; n < C::FN; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
     lds_barrier();
-    for (int kt = 0;; kt += 2) {
-      if (kt + 1 < steps) load(kt + 1, st1);
-      else job.prefetch(cur);
-      if (live) compute(st0);
-      if (kt + 1 >= steps) break;
+    for (int kt = 0; kt + 1 < steps; ++kt) {
+      load(kt + 1, then);
+      if (live) compute(now);
       wait_vm<0>();
       lds_barrier();
-      if (kt + 2 < steps) {
-        load(kt + 2, st0);
-      } else {
-        job.prefetch(cur);
-        load_next();
-      }
-      if (live) compute(st1);
-      if (kt + 2 >= steps) break;
-      wait_vm<0>();
-      lds_barrier();
+      swap();
     }
-    if (steps & 1) {
-      lds_barrier();  // every wave is done with st0
-      load_next();
+    // The last step stands apart: loads into registers within the loop would
+    // make each of its rounds wait for its copies.
+    job.prefetch(cur);
+    typename Job::Tile next = cur;
+    const int tn = find(t + gridDim.x, next);
+    if (tn < items) {
+      sources(next);
+      load(0, then);
     }
+    if (live) compute(now);
+    wait_vm<0>();  // the scales and the copies, but not the stores that follow
     if (live) job.finish(cur, acc);
     if (tn >= items) break;
-    if (live && job.whole(cur)) wait_vm<Job::kStores>();
-    else wait_vm<0>();
+    swap();
     t = tn;
     cur = next;
   }

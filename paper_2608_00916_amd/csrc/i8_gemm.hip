@@ -57,7 +57,7 @@ struct DenseJob {
   static __device__ __forceinline__ int b_row(int q) { return q; }
   __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
   __device__ __forceinline__ int col0() const {
-    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * C::kRun;
+    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * 8;
   }
   __device__ __forceinline__ void prefetch(const Tile& t) {
 #pragma unroll
@@ -65,14 +65,11 @@ struct DenseJob {
     const int c = t.n0 + col0();
 #pragma unroll
     for (int n = 0; n < C::FN; ++n) {
-      if (kWide) sb[n] = *reinterpret_cast<const float4*>(p.sb + min(c + n * 4, p.N - 4));
-      else sb[n] = make_float4(p.sb[min(c + n * 4, p.N - 1)], p.sb[min(c + n * 4 + 1, p.N - 1)],
-                               p.sb[min(c + n * 4 + 2, p.N - 1)], p.sb[min(c + n * 4 + 3, p.N - 1)]);
+      const int cn = c + C::col(n);
+      if (kWide) sb[n] = *reinterpret_cast<const float4*>(p.sb + min(cn, p.N - 4));
+      else sb[n] = make_float4(p.sb[min(cn, p.N - 1)], p.sb[min(cn + 1, p.N - 1)], p.sb[min(cn + 2, p.N - 1)],
+                               p.sb[min(cn + 3, p.N - 1)]);
     }
-  }
-  static constexpr int kStores = C::FM * (F32 ? 4 : 2);
-  __device__ __forceinline__ bool whole(const Tile& t) const {
-    return kWide && t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16 && t.n0 + C::BN <= p.N;
   }
   __device__ __forceinline__ void finish(const Tile& t, const i32x4 (&acc)[C::FM][C::FN]) const {
     const int c = t.n0 + col0(), r0 = t.m0 + row0();
@@ -80,7 +77,7 @@ struct DenseJob {
     char* dst = static_cast<char*>(p.out) + (r0 * p.ldo + c) * kSize;
 #pragma unroll
     for (int m = 0; m < C::FM; ++m, dst += p.ldo * (16 * kSize)) {
-      float v[C::kRun];
+      float v[4 * C::FN];
 #pragma unroll
       for (int n = 0; n < C::FN; ++n) {
         v[4 * n] = static_cast<float>(acc[m][n][0]) * sa[m] * sb[n].x;
@@ -91,10 +88,10 @@ struct DenseJob {
       if constexpr (!kWide) {
         // rows of odd pitch: 64 consecutive columns of a row per store
         const int lane = threadIdx.x & 63, rows = p.M - (r0 + m * 16 - (lane & 15));
-        const int col = c - (lane >> 4) * C::kRun + lane;
+        const int col = c - (lane >> 4) * 8 + lane;
 #pragma unroll
         for (int n = 0; n < C::FN; ++n)
-          *reinterpret_cast<float4*>(swap + (lane & 15) * 64 + 4 * ((4 * (lane >> 4) + n) ^ (lane & 15))) =
+          *reinterpret_cast<float4*>(swap + (lane & 15) * 64 + 4 * ((2 * (lane >> 4) + C::col(n) / 4) ^ (lane & 15))) =
               make_float4(v[4 * n], v[4 * n + 1], v[4 * n + 2], v[4 * n + 3]);
         char* line = static_cast<char*>(p.out) + ((r0 + m * 16 - (lane & 15)) * p.ldo + col) * kSize;
         for (int r = 0; r < min(rows, 16); ++r, line += p.ldo * kSize) {
@@ -108,13 +105,13 @@ struct DenseJob {
       }
       if (r0 + m * 16 >= p.M) continue;
 #pragma unroll
-      for (int i = 0; i < C::kRun; i += 16 / kSize) {
-        if (c + i >= p.N) continue;
+      for (int i = 0; i < 4 * C::FN; i += 16 / kSize) {
+        if (c + C::col(i / 4) >= p.N) continue;
         uint4 w;
         if (F32) w = __builtin_bit_cast(uint4, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
         else w = make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
                             pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-        *reinterpret_cast<uint4*>(dst + i * kSize) = w;
+        *reinterpret_cast<uint4*>(dst + C::col(i / 4) * kSize) = w;
       }
     }
   }
@@ -122,13 +119,12 @@ struct DenseJob {
 
 template <class C, bool kTail, bool F32, bool kWide>
 __global__ __launch_bounds__(C::kThreads) void k_i8_matmul(DenseArgs p) {
-  __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
-  __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
+  __shared__ __attribute__((aligned(16))) int8_t st[2 * C::kStage];
   using Job = DenseJob<C, F32, kWide>;
   __shared__ __attribute__((aligned(16))) float swap[kWide ? 4 : C::kWaves * 16 * 64];
   const Items items(C::WM > 1, cdiv(p.M, C::BM) * cdiv(p.N, C::BN));
   Job job{p, items, swap + (kWide ? 0 : (threadIdx.x >> 6) * 16 * 64)};
-  i8_stream<C, kTail, false>(p.K, items.count(), job, st0, st1);
+  i8_stream<C, kTail, false>(p.K, items.count(), job, st);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -286,12 +282,12 @@ struct GroupedArgs {
   bf16_t* o;  // down out
 };
 
-// Gate and up columns side by side: a lane's first kRun / 2 columns are of
-// gate, the others the same columns of up.  A tile is BN / 2 columns of both;
+// Gate and up columns side by side: a lane's first run of 8 columns is of
+// gate, the other the same columns of up.  A tile is BN / 2 columns of both;
 // a wave's 32 columns of one row are one partial of the activation.
 template <class C, bool kGather>
 struct GateUpJob {
-  static constexpr int kHalf = C::kRun / 2, kPart = kI8Cols, kCols = C::BN / 2;
+  static constexpr int kHalf = 8, kPart = kI8Cols, kCols = C::BN / 2;
   struct Tile {
     int e, row, rows, col;
   };
@@ -322,11 +318,8 @@ struct GateUpJob {
   __device__ __forceinline__ I8Source b(const Tile& t, int part) const {
     return {(part ? p.w.w_up : p.w.w_gate) + (static_cast<int64_t>(t.e) * p.F + t.col) * p.H, kCols};
   }
-  static __device__ __forceinline__ int b_part(int q) { return q / kHalf & 1; }
-  static __device__ __forceinline__ int b_row(int q) {
-    const int r = q % (16 * C::FN);
-    return q / (16 * C::FN) * kPart + kHalf * (r / C::kRun) + r % kHalf;
-  }
+  static __device__ __forceinline__ int b_part(int q) { return q / kPart & 1; }
+  static __device__ __forceinline__ int b_row(int q) { return q / (2 * kPart) * kPart + q % kPart; }
   __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
   __device__ __forceinline__ int col0() const {
     return (threadIdx.x >> 6) % C::WN * kPart + ((threadIdx.x & 63) >> 4) * kHalf;
@@ -340,10 +333,6 @@ struct GateUpJob {
       sg[n] = *reinterpret_cast<const float4*>(p.w.s_gate + c + n * 4);
       su[n] = *reinterpret_cast<const float4*>(p.w.s_up + c + n * 4);
     }
-  }
-  static constexpr int kStores = 2 * C::FM;
-  __device__ __forceinline__ bool whole(const Tile& t) const {
-    return t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16;
   }
   // With G = s g, U = s u (s the row's scale): silu(G) U = s^2 g u / (1 + e^-G).
   // The factor s^2 is common to the row, so it is left to its largest value.
@@ -417,7 +406,7 @@ struct DownJob {
   static __device__ __forceinline__ int b_row(int q) { return q; }
   __device__ __forceinline__ int row0() const { return (threadIdx.x >> 6) / C::WN * C::FM * 16 + (threadIdx.x & 15); }
   __device__ __forceinline__ int col0() const {
-    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * C::kRun;
+    return (threadIdx.x >> 6) % C::WN * C::FN * 16 + ((threadIdx.x & 63) >> 4) * 8;
   }
   __device__ __forceinline__ void prefetch(const Tile& t) {
 #pragma unroll
@@ -425,15 +414,12 @@ struct DownJob {
 #pragma unroll
     for (int n = 0; n < C::FN; ++n)
       sw[n] = *reinterpret_cast<const float4*>(p.w.s_down + static_cast<int64_t>(t.e) * p.H +
-                                               min(t.col + col0() + n * 4, p.H - 4));
-  }
-  static constexpr int kStores = 2 * C::FM;
-  __device__ __forceinline__ bool whole(const Tile& t) const {
-    return t.rows >= row0() - (threadIdx.x & 15) + C::FM * 16 && t.col + C::BN <= p.H;
+                                               min(t.col + col0() + C::col(n), p.H - 4));
   }
   __device__ __forceinline__ void finish(const Tile& t, const i32x4 (&acc)[C::FM][C::FN]) const {
     const int c = t.col + col0();
-    if (c >= p.H) return;  // H is a multiple of 128: a lane's columns are all there or none is
+    // H is a multiple of 128: of a wave's 64 columns all are there or none is
+    if (c >= p.H) return;
 #pragma unroll
     for (int m = 0; m < C::FM; ++m) {
       const int r = row0() + m * 16;
@@ -442,7 +428,7 @@ struct DownJob {
 #pragma unroll
       for (int n = 0; n < C::FN; n += 2) {
         const auto f = [&](int nn, int i, float w) { return static_cast<float>(acc[m][nn][i]) * s[m] * w; };
-        *reinterpret_cast<uint4*>(dst + 4 * n) =
+        *reinterpret_cast<uint4*>(dst + C::col(n)) =
             make_uint4(pack_bf16x2(f(n, 0, sw[n].x), f(n, 1, sw[n].y)), pack_bf16x2(f(n, 2, sw[n].z), f(n, 3, sw[n].w)),
                        pack_bf16x2(f(n + 1, 0, sw[n + 1].x), f(n + 1, 1, sw[n + 1].y)),
                        pack_bf16x2(f(n + 1, 2, sw[n + 1].z), f(n + 1, 3, sw[n + 1].w)));
@@ -453,13 +439,12 @@ struct DownJob {
 
 template <class C, template <class, bool> class Job, bool kGather>
 __global__ __launch_bounds__(C::kThreads) void k_i8_grouped(GroupedArgs p, int K, int col_tiles) {
-  __shared__ __attribute__((aligned(16))) int8_t st0[C::kStage];
-  __shared__ __attribute__((aligned(16))) int8_t st1[C::kStage];
+  __shared__ __attribute__((aligned(16))) int8_t st[2 * C::kStage];
   __shared__ int first[MOE_MAX_EXPERTS + 1];
   count_row_tiles<C>(p.offsets, p.E, first);
   const Items items(C::WM > 1, __builtin_amdgcn_readfirstlane(first[p.E]) * col_tiles);
   Job<C, kGather> job{p, {p.offsets, first, p.E}, items};
-  i8_stream<C, false, kGather>(K, items.count(), job, st0, st1);
+  i8_stream<C, false, kGather>(K, items.count(), job, st);
 }
 
 constexpr int kCus = 256;
