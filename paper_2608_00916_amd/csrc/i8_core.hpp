@@ -17,12 +17,17 @@
 //
 // Two LDS stages: the copies of step k + 1 run under the products of step k,
 // and those of the next tile's first step under this tile's last one.  Loads
-// and stores share one in-order counter, so a tile's first step waits for all
-// but the stores of the tile before (whose number is known where the wave's
-// part of it is whole), and they have that step to drain.  What bounds it is the bytes a step must bring from L2
-// for its products, hence the 256 x 256 tile over 8 waves (128 x 64 each):
-// 8192^3 at 2370 TOPS; 128 x 256 reaches 1720, or 2000 with three stages, 128 x
-// 128 over 4 waves 1660.  More, shorter stages (64 bytes of k) are 5% slower.
+// and stores share one in-order counter: the copies of the next tile's first
+// step are waited for before this tile's stores, which then have that step to
+// drain.  What bounds it is the bytes a step must bring from L2 for its
+// products, hence the 256 x 256 tile over 8 waves (128 x 64 each): 4096 x 16384
+// x 8192 at 2540 TOPS (the tallest rate the power limit was seen to allow is
+// 2700), 128 x 128 tiles over 4 waves at 2080; at K 2048 2140 and 1800, where
+// the stores of all workgroups meet at the memory every 16 steps.  Measured and
+// not taken: four stages of 64 bytes of k (13% slower, twice the barriers), a
+// barrier within the step with the next fragments read under its last products
+// (the same), lines brought into L2 ahead of the copies (20% slower),
+// workgroups out of phase (the same), stores past the caches (the same).
 //
 // The copies are buffer loads whose resource ends with the operand's last row
 // in the tile: rows past it read zeros, and so do chunks past K, so no load

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(C::kThreads) void k_i8_matmul(DenseArgs p) {
 // every wave has operands of its own, so they go straight into registers, with
 // several slices of each wave in flight at once; the waves' sums meet in LDS.
 // Where tiles are few this beats the streamed tiles, whose steps follow each
-// other (512 x 1024 x 8192: 64 steps of 1 us).  With kFused the rows of A are
+// other (512 x 1024 x 8192: 64 steps of 0.6 us).  With kFused the rows of A are
 // bf16, and every workgroup rounds them to int8 in LDS itself: one launch, no
 // trip through memory.
 constexpr int kFewWaves = 8;
@@ -502,16 +502,16 @@ void launch_down(const GroupedArgs& p, int rows_cap, int per_cu, hipStream_t s) 
 // The lowest tile that runs in one round of two workgroups per CU, counting half
 // a part-filled row tile per expert; Low and Small also while most of a higher
 // tile would be empty.  us of the gate/up product as Low, Small, Tall (H 2048,
-// F 768; E x rows per expert): 8 x 256 21 24 29; 8 x 512 36 24 29; 8 x 1024 65
-// 43 39; 128 x 24 78 86 97; 128 x 64 107 95 102; 128 x 128 164 137 129; down:
-// 8 x 128 11 13 14; 16 x 128 19 14 17; 128 x 64 50 45 49; 128 x 512 328 230 211.
+// F 768; E x rows per expert): 8 x 200 18 19 22; 8 x 512 31 21 24; 8 x 1024 54
+// 37 35; 128 x 16 73 76 83; 128 x 64 99 86 92; 128 x 128 150 113 105; down: 8 x
+// 128 9 11 13; 16 x 200 17 13 17; 128 x 96 56 44 49; 128 x 512 306 202 173.
 enum class Rows { kLow, kSmall, kTall };
 
 Rows rows_of(int rows_cap, int E, int width) {
   const auto one_round = [&](int bm, int bn) {
     return (static_cast<double>(rows_cap) / bm + 0.5 * E) * cdiv(width, bn) < 2 * kCus;
   };
-  if (rows_cap <= 24ll * E || one_round(Low::BM, Low::BN)) return Rows::kLow;
+  if (rows_cap <= 16ll * E || one_round(Low::BM, Low::BN)) return Rows::kLow;
   if (rows_cap <= 96ll * E || one_round(Small::BM, Small::BN)) return Rows::kSmall;
   return Rows::kTall;
 }
@@ -524,20 +524,21 @@ hipError_t launch_i8_matmul(const int8_t* a, const float* sa, const int8_t* b, c
   const DenseArgs p{a, sa, b, sb, M, N, K, out, ldo};
   // Few tiles: 8 waves split k within a tile, up to one tile per CU (a weight
   // for up to 64 rows: two).  us at K 8192, as 16 MT x 16, 32 x 64, 64 x 64 and
-  // streamed: 16 x 5120 16 21 28 62; 64 x 1024 20 25 34 50; 64 x 5120 39 26 34
-  // 64; 512 x 1024 - 26 35 59; 1024 x 1024 - 47 35 63; 128 x 16384 - 92 68 66.
-  // 64 x 64 against streamed at 512 x 1024: K 512 9.7 6.7, K 2048 13.2 15.6.
-  // Tall tiles gain from half a round on: 160 of them at K 2048 21 against 26.
+  // streamed: 16 x 5120 16 21 28 40; 64 x 1024 20 25 33 39; 64 x 5120 39 25 33
+  // 40; 512 x 1024 - 26 34 40; 1024 x 1024 - 47 35 41; 128 x 16384 - 92 68 45.
+  // The longer K, the more: 512 x 1024 takes 9 13 13 at K 2048, 7 10 6 at 512.
+  // Tall tiles gain once there is one for every CU: 320 of them at K 2048 53
+  // against 54, 512 70 against 79, but 160 32 against 29.
   const auto tiles = [&](int bm, int bn) { return static_cast<int64_t>(cdiv(M, bm)) * cdiv(N, bn); };
   if (M <= 64 && cdiv(M, 16) * tiles(64, 16) <= 2 * kCus) {
     if (M <= 16) launch_few<1, 1, false>(p, nullptr, 0, f32, s);
     else if (M <= 32) launch_few<2, 1, false>(p, nullptr, 0, f32, s);
     else launch_few<4, 1, false>(p, nullptr, 0, f32, s);
-  } else if (M <= 32 || tiles(32, 64) <= kCus) {
+  } else if (M <= 32 || (K >= 1024 && tiles(32, 64) <= kCus)) {
     launch_few<2, 4, false>(p, nullptr, 0, f32, s);
-  } else if (K >= 2048 && tiles(64, 64) <= kCus) {
+  } else if (K >= 4096 && tiles(64, 64) <= kCus) {
     launch_few<4, 4, false>(p, nullptr, 0, f32, s);
-  } else if (tiles(256, 256) > kCus / 2) {
+  } else if (tiles(256, 256) >= kCus) {
     launch_dense<Tall>(p, f32, 1, s);
   } else {
     launch_dense<Small>(p, f32, 2, s);

@@ -139,9 +139,9 @@ def test_matmul_large(M, N, K, fp32):
 
 @pytest.mark.parametrize("M,N,K", [
     (16, 9001, 144), (32, 20011, 208), (60, 5000, 1040), (100, 1999, 2064),  # 32 x 64 tiles
-    (1000, 1001, 2064), (70, 16100, 2048),                                  # 64 x 64
+    (1000, 1001, 2064), (70, 16100, 2048), (1000, 1001, 4112), (70, 16100, 4096),  # 64 x 64 for the longer K
     (300, 4099, 400), (700, 3001, 1040), (2000, 1504, 272),                 # streamed
-    (2500, 3300, 144), (2304, 4096, 384),                                   # and tall
+    (2500, 3300, 144), (2304, 4096, 384), (4095, 4088, 144), (2304, 8192, 384),  # and tall for the last two
 ])
 @pytest.mark.parametrize("fp32", [False, True])
 def test_matmul_between(M, N, K, fp32):
