@@ -94,11 +94,17 @@ struct DenseJob {
           *reinterpret_cast<float4*>(swap + (lane & 15) * 64 + 4 * ((2 * (lane >> 4) + C::col(n) / 4) ^ (lane & 15))) =
               make_float4(v[4 * n], v[4 * n + 1], v[4 * n + 2], v[4 * n + 3]);
         char* line = static_cast<char*>(p.out) + ((r0 + m * 16 - (lane & 15)) * p.ldo + col) * kSize;
-        for (int r = 0; r < min(rows, 16); ++r, line += p.ldo * kSize) {
-          const float x = swap[r * 64 + (4 * ((lane >> 2) ^ r) | (lane & 3))];
-          if (col >= p.N) continue;
-          if (F32) *reinterpret_cast<float*>(line) = x;
-          else *reinterpret_cast<bf16_t*>(line) = f2bf(x);
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {  // eight reads under way at once
+          float x[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) x[r] = swap[(h + r) * 64 + (4 * ((lane >> 2) ^ (h + r)) | (lane & 3))];
+#pragma unroll
+          for (int r = 0; r < 8; ++r, line += p.ldo * kSize) {
+            if (h + r >= rows || col >= p.N) continue;
+            if (F32) *reinterpret_cast<float*>(line) = x[r];
+            else *reinterpret_cast<bf16_t*>(line) = f2bf(x[r]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);  // one row of fragments at a time: registers
         continue;
