@@ -4,7 +4,10 @@
 // Work is found from the packed row starts alone: a request with n rows
 // starting at row s gets the units floor(s / u) + c b, ... of a grid, which
 // never overlap the next request's because n rows need at most
-// floor(n / u) + c of them; a unit finds its request by binary search.
+// floor(n / u) + c of them; a unit finds its request by a search.  The calls of
+// single tokens are chains of dependent loads, so a search probes 64 places at
+// once (6 binary steps take 4 us, one of these 1), and block sizes, powers of
+// two, are shifts.
 #include "i8_round.hpp"
 #include "serve.hpp"
 #include "trace.hpp"
@@ -14,8 +17,8 @@ namespace moe {
 namespace {
 
 // ---------------------------------------------------------------- plan
-constexpr int kPlanPer = 16;                 // requests per thread and round
-constexpr int kPlanRound = 256 * kPlanPer;   // requests per round
+constexpr int kPlanPer = 16;                // requests per thread and round (1 for up to 256 requests)
+constexpr int kPlanMost = (1 << 30) - 1;    // longest request: sums of two fit in 32 bits
 
 // Largest b in [0, n) with at(b) <= x (at is non-decreasing, at(0) <= x).
 template <class At>
@@ -29,6 +32,22 @@ __device__ __forceinline__ int last_not_above(int n, int64_t x, At at) {
   return lo;
 }
 
+// The same by a whole wave, 64 places at a time.
+template <class At>
+__device__ __forceinline__ int wave_last_not_above(int n, int x, At at) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int stride = (hi - lo + 63) >> 6, m = lo + lane * stride;
+    const int below = __popcll(__ballot(m < hi && at(m) <= x));
+    lo += max(below - 1, 0) * stride;
+    hi = min(hi, lo + stride);
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int log2_of(int block_tokens) { return __ffs(block_tokens) - 1; }
+
 struct PlanArgs {
   moe_kv_plan_dims d;
   const int32_t *old_len, *new_len;
@@ -38,18 +57,25 @@ struct PlanArgs {
 };
 
 // Blocks the table of a request with `len` tokens holds, of W places.
-__device__ __forceinline__ int blocks_of(int len, int bt, int W) {
-  const int n = (len >> 4) / (bt >> 4) + (len % bt != 0);
-  return min(n, W);
+__device__ __forceinline__ int blocks_of(int len, int sh, int W) {
+  return min((len >> sh) + ((len & ((1 << sh) - 1)) != 0), W);
+}
+
+// Sum of two non-negative numbers, at most 2^31 - 1.
+__device__ __forceinline__ int add(int a, int b) {
+  return static_cast<int>(min(static_cast<uint32_t>(a) + static_cast<uint32_t>(b), 0x7fffffffu));
 }
 
 // Every workgroup scans all requests' lengths (8 bytes each, from L2) and
-// keeps the running sums of new tokens and of blocks taken in LDS, then
-// fills its share of the outputs: one launch, no order between workgroups.
+// keeps them and the running sums of new tokens and of blocks taken in LDS,
+// then fills its share of the outputs, four tokens a thread: one launch, no
+// order between workgroups.
+template <int kPer>
 __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
-  __shared__ int starts[kPlanRound + 1], needs[kPlanRound + 1];
+  constexpr int kRound = 256 * kPer;
+  __shared__ int starts[kRound + 1], needs[kRound + 1], olds[kRound];
   __shared__ int tmp[2][4];
-  const int B = p.d.B, T = p.d.T, W = p.d.W, bt = p.d.block_tokens;
+  const int B = p.d.B, T = p.d.T, W = p.d.W, sh = log2_of(p.d.block_tokens), bt = 1 << sh;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int n_free = min(max(*p.n_free, 0), p.d.free_cap);
   const int step = gridDim.x * 256, first = blockIdx.x * 256 + tid;
@@ -58,87 +84,103 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
     const int id = p.free_ids[n_free - 1 - j];
     return id >= 0 && id < p.d.n_blocks ? id : -1;
   };
+  auto len = [](int x) { return min(max(x, 0), kPlanMost); };
   int rows = 0, blocks = 0;  // of the rounds before
   int lost = 0;              // blocks past the table's width (thread's own share)
-  for (int b0 = 0; b0 < B; b0 += kPlanRound) {
-    int n[kPlanPer], nb[kPlanPer];
+  for (int b0 = 0; b0 < B; b0 += kRound) {
+    const int cnt = min(B - b0, kRound);
+    int n[kPer], nb[kPer], o[kPer];
     int sum_n = 0, sum_b = 0;
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) {
-      const int b = b0 + tid * kPlanPer + i;
-      const int o = b < B ? max(p.old_len[b], 0) : 0;
-      n[i] = b < B ? max(p.new_len[b], 0) : 0;
-      nb[i] = blocks_of(o + n[i], bt, W) - blocks_of(o, bt, W);
-      lost += blocks_of(o + n[i], bt, 0x7fffffff) - blocks_of(o + n[i], bt, W);
-      sum_n += n[i];
-      sum_b += nb[i];
+    for (int i = 0; i < kPer; ++i) {
+      const int b = min(tid * kPer + i, cnt - 1) + b0;
+      o[i] = len(p.old_len[b]);
+      n[i] = len(p.new_len[b]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (tid * kPer + i >= cnt) o[i] = n[i] = 0;
+      nb[i] = blocks_of(o[i] + n[i], sh, W) - blocks_of(o[i], sh, W);
+      lost = add(lost, blocks_of(o[i] + n[i], sh, 0x7fffffff) - blocks_of(o[i] + n[i], sh, W));
+      sum_n = add(sum_n, n[i]);
+      sum_b = add(sum_b, nb[i]);
     }
     int in = sum_n, ib = sum_b;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const int un = __shfl_up(in, off, 64), ub = __shfl_up(ib, off, 64);
-      in += lane >= off ? un : 0;
-      ib += lane >= off ? ub : 0;
+      in = add(in, lane >= off ? un : 0);
+      ib = add(ib, lane >= off ? ub : 0);
     }
+    // of the lanes before
+    int xn = __shfl_up(in, 1, 64), xb = __shfl_up(ib, 1, 64);
+    if (lane == 0) xn = xb = 0;
     __syncthreads();  // the round before is done with the shared arrays
     if (lane == 63) {
       tmp[0][wv] = in;
       tmp[1][wv] = ib;
     }
     __syncthreads();
-    int xn = rows + in - sum_n, xb = blocks + ib - sum_b;
     int all_n = rows, all_b = blocks;
+    xn = add(xn, rows);
+    xb = add(xb, blocks);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      xn += w < wv ? tmp[0][w] : 0;
-      xb += w < wv ? tmp[1][w] : 0;
-      all_n += tmp[0][w];
-      all_b += tmp[1][w];
+      xn = add(xn, w < wv ? tmp[0][w] : 0);
+      xb = add(xb, w < wv ? tmp[1][w] : 0);
+      all_n = add(all_n, tmp[0][w]);
+      all_b = add(all_b, tmp[1][w]);
     }
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) {
-      starts[tid * kPlanPer + i] = xn;
-      needs[tid * kPlanPer + i] = xb;
-      xn += n[i];
-      xb += nb[i];
+    for (int i = 0; i < kPer; ++i) {
+      starts[tid * kPer + i] = xn;
+      needs[tid * kPer + i] = xb;
+      olds[tid * kPer + i] = o[i];
+      xn = add(xn, n[i]);
+      xb = add(xb, nb[i]);
     }
-    const int cnt = min(B - b0, kPlanRound);
     __syncthreads();
     for (int i = first; i < cnt; i += step) {
-      const int b = b0 + i;
-      p.row_start[b] = starts[i];
-      p.kv_len[b] = max(p.old_len[b], 0) + max(p.new_len[b], 0);
+      p.row_start[b0 + i] = starts[i];
+      p.kv_len[b0 + i] = olds[i] + (kPer == 1 ? n[0] : len(p.new_len[b0 + i]));  // kPer 1: i = tid
     }
-    for (int64_t t = rows + first; t < min(all_n, T); t += step) {
-      const int i = last_not_above(cnt, t, [&](int m) { return starts[m]; });
-      const int b = b0 + i, o = max(p.old_len[b], 0);
-      const int pos = o + static_cast<int>(t) - starts[i];
-      const int at = pos / bt, have = blocks_of(o, bt, W);
-      int id = -1;
-      if (at < have) id = p.block_table[static_cast<int64_t>(b) * W + at];
-      else if (at < W) id = taken(needs[i] + at - have);
-      p.positions[t] = pos;
-      p.slots[t] = id >= 0 && id < p.d.n_blocks ? id * bt + pos % bt : -1;
-      p.seq[t] = b;
+    const int end = min(all_n, T);
+    for (int64_t t0 = rows + static_cast<int64_t>(first) * 4; t0 < end; t0 += static_cast<int64_t>(step) * 4) {
+      int i = last_not_above(cnt, t0, [&](int m) { return starts[m]; });
+      int seen = -1, id = -1;  // the place whose block is at hand
+      for (int t = static_cast<int>(t0); t < min(t0 + 4, static_cast<int64_t>(end)); ++t) {
+        while (i + 1 < cnt && starts[i + 1] <= t) ++i, seen = -1;
+        const int pos = olds[i] + t - starts[i], at = pos >> sh;
+        if (at != seen) {
+          const int have = blocks_of(olds[i], sh, W);
+          id = -1;
+          if (at < have) id = p.block_table[static_cast<int64_t>(b0 + i) * W + at];
+          else if (at < W) id = taken(needs[i] + at - have);
+          seen = at;
+        }
+        p.positions[t] = pos;
+        p.slots[t] = id >= 0 && id < p.d.n_blocks ? id * bt + (pos & (bt - 1)) : -1;
+        p.seq[t] = b0 + i;
+      }
     }
     for (int64_t j = blocks + first; j < all_b; j += step) {
       const int i = last_not_above(cnt, j, [&](int m) { return needs[m]; });
-      const int b = b0 + i, have = blocks_of(max(p.old_len[b], 0), bt, W);
-      p.block_table[static_cast<int64_t>(b) * W + have + (j - needs[i])] = taken(static_cast<int>(j));
+      const int have = blocks_of(olds[i], sh, W);
+      p.block_table[static_cast<int64_t>(b0 + i) * W + have + (j - needs[i])] = taken(static_cast<int>(j));
     }
     rows = all_n;
     blocks = all_b;
   }
   for (int64_t t = static_cast<int64_t>(rows) + first; t < T; t += step) p.positions[t] = p.slots[t] = p.seq[t] = -1;
   if (blockIdx.x != 0) return;
-  for (int m = 32; m >= 1; m >>= 1) lost += shfl_xor(lost, m);
+  for (int m = 32; m >= 1; m >>= 1) lost = add(lost, shfl_xor(lost, m));
   __syncthreads();
   if (lane == 0) tmp[0][wv] = lost;
   __syncthreads();
   if (tid == 0) {
     p.row_start[B] = rows;
     p.state[0] = max(n_free - blocks, 0);
-    p.state[1] = max(blocks - n_free, 0) + tmp[0][0] + tmp[0][1] + tmp[0][2] + tmp[0][3];
+    p.state[1] = add(max(blocks - n_free, 0), add(add(tmp[0][0], tmp[0][1]), add(tmp[0][2], tmp[0][3])));
   }
 }
 
@@ -156,14 +198,14 @@ __global__ __launch_bounds__(256) void k_kv_append(moe_kv_cache c, moe_kv_batch 
   constexpr int kMaxBlock = 128;
   __shared__ __attribute__((aligned(16))) int8_t tile[D * kMaxBlock];  // values only: [D][bt]
   __shared__ uint32_t tops[4];
-  const int bt = c.block_tokens, tid = threadIdx.x;
+  const int bt = c.block_tokens, sh = log2_of(bt), tid = threadIdx.x;
   auto start = [&](int b) { return min(max(bt_.row_start[b], 0), bt_.T); };
   const int u = blockIdx.x;
-  const int b = last_not_above(bt_.B, u, [&](int m) { return start(m) / bt + 2 * m; });
+  const int b = wave_last_not_above(bt_.B, u, [&](int m) { return (start(m) >> sh) + 2 * m; });
   const int s = start(b), n = start(b + 1) - s;
   const int old = bt_.kv_len[b] - n;
-  const int blk0 = max(old, 0) / bt;
-  const int blk = blk0 + u - (s / bt + 2 * b);
+  const int blk0 = max(old, 0) >> sh;
+  const int blk = blk0 + u - ((s >> sh) + 2 * b);
   // the request's new tokens that lie in this block: [p0, p1) of its positions
   const int p0 = max(max(old, 0), blk * bt), p1 = min(old + n, (blk + 1) * bt);
   if (n <= 0 || p0 >= p1 || blk >= bt_.W) return;
@@ -182,7 +224,7 @@ __global__ __launch_bounds__(256) void k_kv_append(moe_kv_cache c, moe_kv_batch 
   uint32_t m = 0;
   for (int t = tok; t < cnt; t += kTokens) m = max(m, top8(*reinterpret_cast<const uint4*>(src + t * ld + d0)));
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) m = max(m, static_cast<uint32_t>(shfl_xor(static_cast<int>(m), x)));
+  for (int o = 32; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(shfl_xor(static_cast<int>(m), o)));
   if ((tid & 63) == 0) tops[tid >> 6] = m;
   if (values && cnt < bt)  // a block's first tokens leave zeros behind them
     for (int i = tid * 16; i < D * bt; i += 256 * 16)
@@ -205,7 +247,7 @@ __global__ __launch_bounds__(256) void k_kv_append(moe_kv_cache c, moe_kv_batch 
     for (int i = tid; i < D * bt; i += 256)
       if ((i & (bt - 1)) < off) tile[i] = static_cast<int8_t>(round8(tile[i] * shrink));
   }
-  for (int t = tok; t < cnt; t += kTokens) {
+  for (int t = tok; t < cnt; t += kTokens) {  // from the caches: registers for 128 tokens cost more
     const uint4 x = *reinterpret_cast<const uint4*>(src + t * ld + d0);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     int q[8];
@@ -237,16 +279,16 @@ __global__ __launch_bounds__(256) void k_kv_read(moe_kv_cache c, int B, int W, c
                                                  const int32_t* __restrict__ kv_start, int total,
                                                  bf16_t* __restrict__ k_out, bf16_t* __restrict__ v_out) {
   __shared__ __attribute__((aligned(16))) int8_t tile[D][64 + 16];
-  const int bt = c.block_tokens, tid = threadIdx.x, h = blockIdx.y;
+  const int bt = c.block_tokens, sh = log2_of(bt), tid = threadIdx.x, h = blockIdx.y;
   auto start = [&](int b) { return min(max(kv_start[b], 0), total); };
   const int u = blockIdx.x;
-  const int b = last_not_above(B, u, [&](int m) { return start(m) / 64 + m; });
+  const int b = wave_last_not_above(B, u, [&](int m) { return start(m) / 64 + m; });
   const int s = start(b), n = start(b + 1) - s;
   const int t0 = (u - (s / 64 + b)) * 64;
   if (t0 >= n) return;
   const int32_t* table = block_table + static_cast<int64_t>(b) * W;
   auto block = [&](int t) {  // of token t, or -1
-    const int i = t / bt;
+    const int i = t >> sh;
     const int id = i < W ? table[i] : -1;
     return id >= 0 && id < c.n_blocks ? id : -1;
   };
@@ -260,7 +302,7 @@ __global__ __launch_bounds__(256) void k_kv_read(moe_kv_cache c, int B, int W, c
       uint4 x = make_uint4(0, 0, 0, 0);
       if (id >= 0)
         x = *reinterpret_cast<const uint4*>(c.v + (static_cast<int64_t>(id) * c.kv_heads + h) * bt * D + d * bt +
-                                            (t0 + t) % bt);
+                                            ((t0 + t) & (bt - 1)));
       *reinterpret_cast<uint4*>(&tile[d][t]) = x;
     }
     __syncthreads();
@@ -278,7 +320,7 @@ __global__ __launch_bounds__(256) void k_kv_read(moe_kv_cache c, int B, int W, c
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[j] = tile[d0 + j][t];
       } else {
-        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(c.k + at * bt * D + (t0 + t) % bt * D + d0);
+        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(c.k + at * bt * D + ((t0 + t) & (bt - 1)) * D + d0);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(q[2 * j] * sc, q[2 * j + 1] * sc);
@@ -298,9 +340,9 @@ hipError_t launch_kv_plan(const moe_kv_plan_dims& d, const int32_t* old_len, con
   const int work = d.T > d.B ? d.T : d.B;
   int grid = cdiv(work, 1024);
   grid = grid < 1 ? 1 : grid > 256 ? 256 : grid;
-  hipLaunchKernelGGL(k_kv_plan, dim3(grid), dim3(256), 0, s,
-                     PlanArgs{d, old_len, new_len, block_table, free_ids, n_free, row_start, kv_len, positions, slots,
-                              seq, state});
+  const PlanArgs p{d, old_len, new_len, block_table, free_ids, n_free, row_start, kv_len, positions, slots, seq, state};
+  if (d.B <= 256) hipLaunchKernelGGL(k_kv_plan<1>, dim3(grid), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(k_kv_plan<kPlanPer>, dim3(grid), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -43,6 +43,8 @@ def _rows(t, dtype=torch.bfloat16):
         raise ValueError("tensor must be on the GPU")
     if t.dtype != dtype:
         raise ValueError(f"tensor must be {dtype}, not {t.dtype}")
+    if t.is_contiguous() and t.shape[0]:
+        return t.data_ptr(), t.numel() // t.shape[0]
     n = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != n:
@@ -52,13 +54,14 @@ def _rows(t, dtype=torch.bfloat16):
 
 
 def _shape(name, t, shape):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:  # torch.Size compares as the tuple that it is
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
 
 
 def _s(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # the handle alone: a Stream object costs as much as the launch (3 us)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 

@@ -351,6 +351,31 @@ def test_plan_fewer_rows_than_tokens_and_a_bad_count():
     assert plan.state.tolist() == [0, 0] and t.tolist() == [[8, -1, -1, -1], [-1, 7, -1, -1]]
 
 
+@pytest.mark.parametrize("B", [3, 300])
+def test_plan_of_impossible_lengths(B):
+    """Lengths past 2^30 - 1 count as that, sums stop at 2^31 - 1, and nothing is written past the tables."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("plan impossible", B)
+    top, W = 2 ** 31 - 1, 4
+    old, new = np.zeros(B, np.int32), np.ones(B, np.int32)
+    old[1], new[1], new[2] = top, top, top
+    guard = torch.full((B + 2, W), 5, dtype=torch.int32, device="cuda")
+    t = guard[1:B + 1]
+    t.fill_(-1)
+    plan = moe.KVPlan(B, 40, W, 50, 16)
+    plan.build(i32(old), i32(new), t, dev(np.arange(50).astype(np.int32)), i32([50]))
+    most = 2 ** 30 - 1
+    starts = np.minimum(np.concatenate([[0], np.cumsum(np.minimum(new.astype(np.int64), most))]), top)
+    assert plan.row_start.tolist() == starts.tolist()
+    assert plan.kv_len.tolist() == (np.minimum(old, most) + np.minimum(new, most)).tolist()
+    assert plan.seq.tolist() == [0] + [1] * 39 and plan.slots[0] == 49 * 16
+    # request 1 is past its table already; request 2 takes all that its row holds
+    assert plan.slots[1:].tolist() == [-1] * 39 and t[1].tolist() == [-1] * W
+    assert t[2].tolist() == [48, 47, 46, 45]
+    assert (guard[0] == 5).all() and (guard[-1] == 5).all()
+
+
 # ------------------------------------------------------------------ the cache
 class Pages:
     """A cache on the GPU and the same blocks in numpy."""
