@@ -40,10 +40,8 @@ __global__ __launch_bounds__(256) void k_i8_quant_rows(const bf16_t* __restrict_
   if (lane == 0) scale[row] = r.scale;
 }
 
-// One wave per routed row: the row's largest magnitude is that of its
-// partials.  A value is a * (partial's largest / 32767), within 2^-16 of that
-// largest: 0.002 of a step of q at most, where the partial has the row's largest.
-__global__ __launch_bounds__(256) void k_i8_requant(const int16_t* __restrict__ a, const float* __restrict__ a_top,
+// One wave per routed row: the row's largest magnitude is that of its partials.
+__global__ __launch_bounds__(256) void k_i8_requant(const float* __restrict__ a, const float* __restrict__ a_top,
                                                     int rows, int F, const int32_t* __restrict__ n_valid,
                                                     int8_t* __restrict__ q, float* __restrict__ scale) {
   const int lane = threadIdx.x & 63;
@@ -55,15 +53,9 @@ __global__ __launch_bounds__(256) void k_i8_requant(const int16_t* __restrict__ 
   for (int i = lane; i < parts; i += 64) m = max(m, __float_as_uint(top[i]));
   const Rounder r(wave_umax(m));
   for (int c = lane * 8; c < F; c += 512) {
-    const uint4 v = *reinterpret_cast<const uint4*>(a + row * F + c);
-    const float step = top[c / kI8Cols] * (1.0f / 32767.0f);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    int b[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      b[2 * i] = r(static_cast<float>(static_cast<int16_t>(w[i] & 0xffff)) * step);
-      b[2 * i + 1] = r(static_cast<float>(static_cast<int16_t>(w[i] >> 16)) * step);
-    }
+    const float4 v = *reinterpret_cast<const float4*>(a + row * F + c);
+    const float4 w = *reinterpret_cast<const float4*>(a + row * F + c + 4);
+    const int b[8] = {r(v.x), r(v.y), r(v.z), r(v.w), r(w.x), r(w.y), r(w.z), r(w.w)};
     *reinterpret_cast<uint2*>(q + row * F + c) = make_uint2(pack4(b[0], b[1], b[2], b[3]), pack4(b[4], b[5], b[6], b[7]));
   }
   if (lane == 0) scale[row] = r.scale;
@@ -106,7 +98,7 @@ hipError_t launch_i8_quant_rows(const bf16_t* x, int64_t ldx, int rows, int K, c
   return hipGetLastError();
 }
 
-hipError_t launch_i8_requant(const int16_t* a, const float* a_top, int rows, int F, const int32_t* n_valid, int8_t* q,
+hipError_t launch_i8_requant(const float* a, const float* a_top, int rows, int F, const int32_t* n_valid, int8_t* q,
                              float* scale, hipStream_t s) {
   TraceScope trace_scope(K_I8_QUANT, s);
   hipLaunchKernelGGL(k_i8_requant, dim3(cdiv(rows, 4)), dim3(256), 0, s, a, a_top, rows, F, n_valid, q, scale);

@@ -16,8 +16,8 @@ namespace moe {
 hipError_t launch_i8_quant_rows(const bf16_t* x, int64_t ldx, int rows, int K, const int32_t* n_valid, int8_t* q,
                                 float* scale, hipStream_t s);
 // The same from the SwiGLU activation as the gate/up product leaves it: a
-// [rows, F] int16, a_top [rows, F / kI8Cols], value a * a_top / 32767.
-hipError_t launch_i8_requant(const int16_t* a, const float* a_top, int rows, int F, const int32_t* n_valid, int8_t* q,
+// [rows, F], a_top [rows, F / kI8Cols].
+hipError_t launch_i8_requant(const float* a, const float* a_top, int rows, int F, const int32_t* n_valid, int8_t* q,
                              float* scale, hipStream_t s);
 // w [E, K, N] bf16 -> q [E, N, K], scale [E, N].
 hipError_t launch_i8_quant_weight(const bf16_t* w, int E, int K, int N, int8_t* q, float* scale, hipStream_t s);
@@ -40,9 +40,9 @@ struct I8Rows {
 // Columns of one partial of the SwiGLU activation.
 constexpr int kI8Cols = 32;
 // A = silu(G) U of each routed row (x row rows[r], or r where rows is null),
-// as int16 of the largest value among each kI8Cols columns (a_top).
+// and the largest magnitude among each kI8Cols columns (a_top).
 hipError_t launch_i8_gateup(const I8Rows& r, const int8_t* x, const float* sx, const int32_t* rows,
-                            const moe_i8_experts& w, int H, int F, int16_t* a, float* a_top, hipStream_t s);
+                            const moe_i8_experts& w, int H, int F, float* a, float* a_top, hipStream_t s);
 // O = A W_down.
 hipError_t launch_i8_down(const I8Rows& r, const int8_t* a, const float* sa, const moe_i8_experts& w, int H, int F,
                           bf16_t* o, hipStream_t s);

@@ -59,7 +59,7 @@ LinearWs linear_layout(const moe_i8_dims* d, void* base) {
 
 // Scratch of the routed rows: the SwiGLU activation, its int8 rows.
 struct RowsWs {
-  int16_t* a;
+  float* a;
   float* a_top;
   int8_t* a8;
   float* sa;
@@ -67,7 +67,7 @@ struct RowsWs {
 
 RowsWs take_rows(Carve& c, size_t R, size_t F) {
   RowsWs w;
-  w.a = c.take<int16_t>(R * F);
+  w.a = c.take<float>(R * F);
   w.a_top = c.take<float>(R * (F / kI8Cols));
   w.a8 = c.take<int8_t>(R * F);
   w.sa = c.take<float>(R);

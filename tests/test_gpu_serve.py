@@ -251,6 +251,22 @@ def test_experts_many_rows(rows, counts, H, F):
     test_experts(rows, counts, H, F)
 
 
+@pytest.mark.parametrize("F", [128, 512])
+def test_experts_few_rows_round_as_the_64_bit_form(F):
+    """The activation is rounded to 8 bits once, from fp32: a step of one value is 2 / 127 of its
+    largest, and only values within 2^-20 of a boundary may take another, so what is left is the
+    output's rounding to bf16."""
+    import paper_2608_00916_amd as moe
+    say("experts i8 few rows", F)
+    for seed in range(12):
+        g = gen(100 + seed)
+        w8, w = expert_weights(g, 4, 128, F)
+        x = bf16(g.standard_normal((2, 128)))
+        got = host(moe.MoEExpertsI8(2, 128, 4, F).forward(x, i32([0, 1, 0, 1]), w8))
+        ref = np.concatenate([R.expert(host(x)[r:r + 1], w[0][e], w[1][e], w[2][e]) for r, e in ((0, 1), (1, 3))])
+        assert np.linalg.norm(got - ref) <= (BF + 0.0005) * np.linalg.norm(ref), seed
+
+
 def test_experts_rows_past_the_capacity_and_the_counts():
     import torch
     import paper_2608_00916_amd as moe
