@@ -376,7 +376,7 @@ typedef struct moe_kv_batch {
 
 /* Tables of one step, built on the device from request lengths: request b has
  * old_len[b] tokens in the cache and gets new_len[b] more (negative counts as
- * 0).  Blocks its table lacks are taken in request order from the top of the
+ * 0, and what exceeds 2^30 - 1 as that).  Blocks its table lacks are taken in request order from the top of the
  * stack free_ids[0 .. n_free).
  *   block_table [B, W]  the blocks taken are written (-1 once the stack is
  *                       empty), all other entries are left alone
