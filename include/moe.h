@@ -403,9 +403,10 @@ int moe_kv_append(const moe_kv_cache* c, const moe_kv_batch* b, const void* k, c
                   void* stream);
 
 /* Read the first kv_start[b + 1] - kv_start[b] tokens of each request back as
- * bf16 rows kv_start[b] .. (kv_start [B + 1] on the device, clamped to
- * [0, total]): k_out, v_out [total, kv_heads, head_dim].  Tokens without a
- * place read as 0. */
+ * bf16 rows kv_start[b] .. (kv_start [B + 1] on the device, non-decreasing,
+ * clamped to [0, total]): k_out, v_out [total, kv_heads, head_dim].  Tokens
+ * without a place read as 0; rows before kv_start[0] and from kv_start[B] on
+ * are not written. */
 int moe_kv_read(const moe_kv_cache* c, int32_t B, int32_t W, const int32_t* block_table, const int32_t* kv_start,
                 int32_t total, void* k_out, void* v_out, void* stream);
 

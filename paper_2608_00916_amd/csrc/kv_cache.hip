@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) void k_kv_read(moe_kv_cache c, int B, int W, c
   const int b = wave_last_not_above(B, u, [&](int m) { return start(m) / 64 + m; });
   const int s = start(b), n = start(b + 1) - s;
   const int t0 = (u - (s / 64 + b)) * 64;
-  if (t0 >= n) return;
+  if (t0 < 0 || t0 >= n) return;  // before the first request's rows, or none of this one
   const int32_t* table = block_table + static_cast<int64_t>(b) * W;
   auto block = [&](int t) {  // of token t, or -1
     const int i = t >> sh;
