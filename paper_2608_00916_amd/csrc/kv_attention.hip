@@ -707,8 +707,9 @@ constexpr int kFewItems = 3072, kFewLeast = 512;
 constexpr int kManyItems = 512, kManyLeast = 512;
 
 struct Plan {
-  bool many;  // some request may have more than `few_rows` rows
-  int units;  // row tiles of those
+  int64_t most;  // rows of a kv head that one request may have
+  bool many;     // more than `few_rows`
+  int units;     // row tiles of those
   int few_rows;
   Split few, rows;
 };
@@ -716,10 +717,11 @@ struct Plan {
 Plan plan(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
   const int64_t places = static_cast<int64_t>(b.W) * c.block_tokens;
   const int64_t max_kv = a.max_kv < places ? a.max_kv : places;
-  const int64_t group = a.heads / c.kv_heads, most = (a.max_q < b.T ? a.max_q : b.T) * group;
+  const int64_t group = a.heads / c.kv_heads;
   Plan p;
-  p.few_rows = most <= 16 ? 16 : 32;
-  p.many = most > p.few_rows;
+  p.most = (a.max_q < b.T ? a.max_q : b.T) * group;
+  p.few_rows = p.most <= 16 ? 16 : 32;
+  p.many = p.most > p.few_rows;
   p.units = static_cast<int>(b.T * group / kMany) + b.B;
   p.few = split(static_cast<int64_t>(b.B) * c.kv_heads, max_kv, kFewItems, kFewLeast);
   p.rows = split(static_cast<int64_t>(p.units) * c.kv_heads, max_kv, kManyItems, kManyLeast);
@@ -727,8 +729,9 @@ Plan plan(const moe_kv_cache& c, const moe_kv_batch& b, const moe_kv_attn& a) {
 }
 
 template <int D, int NB>
-void launch_few(AttnArgs p, const Split& sp, float* ws, hipStream_t s) {
+void launch_few(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
   constexpr int kRows = 16 * NB;
+  const Split& sp = pl.few;
   p.chunk = sp.chunk;
   p.chunks = sp.chunks;
   p.part_o = ws;
@@ -739,7 +742,7 @@ void launch_few(AttnArgs p, const Split& sp, float* ws, hipStream_t s) {
   }
   if (p.chunks > 1) {
     TraceScope trace_scope(K_KV_COMBINE, s);
-    const int rows = p.max_q * p.group < kRows ? p.max_q * p.group : kRows;
+    const int rows = pl.most < kRows ? static_cast<int>(pl.most) : kRows;
     hipLaunchKernelGGL((k_kv_combine<D, kRows>), dim3(p.b.B, p.c.kv_heads, rows), dim3(256), 0, s, p);
   }
 }
@@ -765,8 +768,8 @@ void launch(AttnArgs p, const Plan& pl, float* ws, hipStream_t s) {
       hipLaunchKernelGGL(k_kv_combine_rows<D>, dim3(pl.units, heads, kMany / 16), dim3(256), 0, s, q);
     }
   }
-  if (pl.few_rows == 16) launch_few<D, 1>(p, pl.few, ws, s);
-  else launch_few<D, 2>(p, pl.few, ws, s);
+  if (pl.few_rows == 16) launch_few<D, 1>(p, pl, ws, s);
+  else launch_few<D, 2>(p, pl, ws, s);
 }
 
 }  // namespace

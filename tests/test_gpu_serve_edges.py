@@ -4,7 +4,7 @@ that are replaced, operands at the ends of their types."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_serve import Pages, dev, gen, i32, say
+from tests.test_gpu_serve import Pages, attend, dev, gen, i32, say
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +27,13 @@ def test_read_into_rows_that_start_late(bt, first):
     for x, y in zip(got, want):
         assert torch.equal(x[first:first + total], y)
         assert (x[:first] == 9).all() and (x[first + total:] == 9).all()
+
+
+@pytest.mark.parametrize("max_q", [2 ** 29, 2 ** 29 + 1, 2 ** 31 - 1])
+def test_a_loose_max_q(max_q):
+    """max_q only bounds a request's new tokens: times the heads of a group it may pass 32 bits."""
+    say("loose max_q", max_q)
+    pg = Pages(gen(32), [5000, 9, 2600], 64, 1, 128)
+    attend(pg, [1, 1, 0], [5000, 9, 2600], 8, max_q=max_q)
+    attend(pg, [1, 2, 4], [5000, 9, 2600], 8, max_q=max_q)
+    attend(pg, [40, 2, 3], [5000, 9, 2600], 8, max_q=max_q)
