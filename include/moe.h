@@ -362,8 +362,11 @@ typedef struct moe_kv_cache {
 } moe_kv_cache;
 
 /* A batch of B requests whose new tokens are packed request after request
- * into T rows: request b has rows row_start[b] .. row_start[b + 1] (clamped to
- * [0, T]), the last of its kv_len[b] tokens.  Its token p lies in block
+ * into T rows: rows row_start[b] .. row_start[b + 1] (non-decreasing) are the
+ * last of request b's kv_len[b] tokens.  A row_start may pass T, as those of
+ * moe_kv_plan do when T is too small: kv_len then counts tokens that have no
+ * row, the rows there are keep their positions, and the tokens past them are
+ * not written and not seen.  Token p lies in block
  * block_table[b][p / block_tokens]; entries outside [0, n_blocks) and tokens
  * past W blocks have no place: they are not written, and no query sees them.
  * All three arrays are on the device. */
@@ -380,7 +383,8 @@ typedef struct moe_kv_batch {
  * stack free_ids[0 .. n_free).
  *   block_table [B, W]  the blocks taken are written (-1 once the stack is
  *                       empty), all other entries are left alone
- *   row_start [B + 1], kv_len [B]   as in moe_kv_batch (row_start not clamped)
+ *   row_start [B + 1], kv_len [B]   as in moe_kv_batch: of all new tokens, also
+ *                       where T is too small for them
  *   positions, slots, seq [T]       per packed token its position in its
  *                       request, block * block_tokens + offset (-1: no place)
  *                       and its request; -1 past the last token

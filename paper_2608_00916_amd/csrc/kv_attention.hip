@@ -93,7 +93,9 @@ __device__ __forceinline__ int row_start(const AttnArgs& p, int i) { return min(
 __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
   Request r;
   r.first = row_start(p, b);
-  const int all = max(row_start(p, b + 1) - r.first, 0), len = p.b.kv_len[b];
+  const int end = p.b.row_start[b + 1];
+  const int all = max(min(end, p.b.T) - r.first, 0);
+  const int len = max(p.b.kv_len[b], 0) - max(end - p.b.T, 0);  // without the tokens past the last row
   r.n = min(all, p.max_q);
   r.rows = r.n * p.group;
   r.kv = max(0, min(min(len, p.max_kv), p.b.W * p.c.block_tokens));

@@ -207,8 +207,8 @@ __global__ __launch_bounds__(256) void k_kv_append(moe_kv_cache c, moe_kv_batch 
   auto start = [&](int b) { return min(max(bt_.row_start[b], 0), bt_.T); };
   const int u = blockIdx.x;
   const int b = wave_last_not_above(bt_.B, u, [&](int m) { return (start(m) >> sh) + 2 * m; });
-  const int s = start(b), n = start(b + 1) - s;
-  const int old = bt_.kv_len[b] - n;
+  const int s = start(b), end = bt_.row_start[b + 1], n = min(max(end, 0), bt_.T) - s;
+  const int old = max(bt_.kv_len[b], 0) - max(end - bt_.T, 0) - n;  // kv_len counts the tokens past the last row too
   const int blk0 = max(old, 0) >> sh;
   const int blk = blk0 + u - ((s >> sh) + 2 * b);
   // the request's new tokens that lie in this block: [p0, p1) of its positions

@@ -4,7 +4,7 @@ that are replaced, operands at the ends of their types."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_serve import Pages, attend, dev, gen, i32, say
+from tests.test_gpu_serve import Pages, attend, bf16, dev, gen, i32, say
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,45 @@ def test_a_loose_max_q(max_q):
     attend(pg, [1, 1, 0], [5000, 9, 2600], 8, max_q=max_q)
     attend(pg, [1, 2, 4], [5000, 9, 2600], 8, max_q=max_q)
     attend(pg, [40, 2, 3], [5000, 9, 2600], 8, max_q=max_q)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("T", [0, 4, 5, 23, 24, 60])
+def test_fewer_rows_than_new_tokens(T, causal):
+    """Rows past T do not exist, and what there is of a request are its first new tokens: the cache
+    and the output are those of a batch that has only these."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("short T", T, causal)
+    g = gen(33)
+    bt, heads, D, W = 16, 2, 64, 8
+    old, new = [0, 35, 3, 20], [4, 20, 100, 1]
+    fit = np.clip(T - (np.cumsum(new) - new), 0, new)
+    kv = bf16(g.standard_normal((2, 140, heads, D)))
+    k, v = bf16(g.standard_normal((125, heads, D))), bf16(g.standard_normal((125, heads, D)))
+    q = bf16(2 * g.standard_normal((125, 4, D)))
+    free = dev(g.permutation(40).astype(np.int32))
+    got = []
+    for step in (np.array(new), fit):
+        cache = moe.KVCache(40, bt, heads, D)
+        cache.k.fill_(77), cache.v.fill_(-55), cache.k_scale.fill_(3.0), cache.v_scale.fill_(2.0)
+        table = i32(np.full((4, W), -1))
+        n_free = i32([40])
+        if sum(old):
+            plan = moe.KVPlan(4, sum(old), W, 40, bt)
+            plan.build(i32([0] * 4), i32(old), table, free, n_free)
+            cache.append(kv[0, :sum(old)], kv[1, :sum(old)], plan.row_start, plan.kv_len, table)
+            n_free = plan.state[:1].clone()
+        plan = moe.KVPlan(4, T, W, 40, bt)
+        plan.build(i32(old), i32(step), table, free, n_free)
+        cache.append(k[:T], v[:T], plan.row_start, plan.kv_len, table)
+        op = moe.KVAttention(cache, T, 4, 4, 100, W * bt, causal=causal)
+        op.out.fill_(3.0)
+        out = op.forward(q[:T], cache, table, plan.row_start, plan.kv_len).clone()
+        after = np.array(old) + fit
+        start = np.concatenate([[0], np.cumsum(after)])
+        ko, vo = (torch.empty((int(start[-1]), heads, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        cache.read(table, i32(start), ko, vo)
+        got.append((plan.positions.clone(), out, ko, vo))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
