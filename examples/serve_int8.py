@@ -72,8 +72,7 @@ class Server:
         a = attn.forward(q, self.cache, self.table, plan.row_start, plan.kv_len)
         h = x + out.forward(a.view(-1, m.heads * m.D))
         h = h + experts.forward(h, m.w_r, m.experts8)
-        self.length.copy_(plan.kv_len)
-        self.n_free.copy_(plan.state[:1])
+        self.length, self.n_free = plan.kv_len, plan.state[:1]  # the next step's, also where it has the same plan
         return h
 
 

@@ -388,7 +388,10 @@ typedef struct moe_kv_batch {
  *   positions, slots, seq [T]       per packed token its position in its
  *                       request, block * block_tokens + offset (-1: no place)
  *                       and its request; -1 past the last token
- *   state [2]           {blocks left on the stack, blocks that were missing} */
+ *   state [2]           {blocks left on the stack, blocks that were missing}
+ * A step's kv_len and state[0] are the next one's old_len and n_free: kv_len
+ * may be old_len or new_len itself, and state begin at n_free (one launch
+ * more).  Nothing else that is written may overlap what is read. */
 typedef struct moe_kv_plan_dims {
   int32_t B, T, W;      /* B, W >= 1, T >= 0 */
   int32_t n_blocks, block_tokens;

@@ -54,6 +54,7 @@ struct PlanArgs {
   int32_t* block_table;
   const int32_t *free_ids, *n_free;
   int32_t *row_start, *kv_len, *positions, *slots, *seq, *state;
+  bool in_place;  // kv_len or state is an input too: k_kv_plan_lengths writes them
 };
 
 // Blocks the table of a request with `len` tokens holds, of W places.
@@ -64,6 +65,23 @@ __device__ __forceinline__ int blocks_of(int len, int sh, int W) {
 // Sum of two non-negative numbers, at most 2^31 - 1.
 __device__ __forceinline__ int add(int a, int b) {
   return static_cast<int>(min(static_cast<uint32_t>(a) + static_cast<uint32_t>(b), 0x7fffffffu));
+}
+
+__device__ __forceinline__ int length(int x) { return min(max(x, 0), kPlanMost); }
+
+// Blocks that a request takes from the stack, and those past its table's width.
+struct Need {
+  int taken, lost;
+  __device__ __forceinline__ Need(int old, int fresh, int sh, int W) {
+    const int held = blocks_of(old + fresh, sh, W);
+    taken = held - blocks_of(old, sh, W);
+    lost = blocks_of(old + fresh, sh, 0x7fffffff) - held;
+  }
+};
+
+__device__ __forceinline__ void write_state(const PlanArgs& p, int n_free, int blocks, int lost) {
+  p.state[0] = max(n_free - blocks, 0);
+  p.state[1] = add(max(blocks - n_free, 0), lost);
 }
 
 // Every workgroup scans all requests' lengths (8 bytes each, from L2) and
@@ -85,7 +103,6 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
     const int id = p.free_ids[n_free - 1 - j];
     return id >= 0 && id < p.d.n_blocks ? id : -1;
   };
-  auto len = [](int x) { return min(max(x, 0), kPlanMost); };
   int rows = 0, blocks = 0;  // of the rounds before
   int lost = 0;              // blocks past the table's width (thread's own share)
   for (int b0 = 0; b0 < B; b0 += kRound) {
@@ -95,14 +112,15 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int b = min(tid * kPer + i, cnt - 1) + b0;
-      o[i] = len(p.old_len[b]);
-      n[i] = len(p.new_len[b]);
+      o[i] = length(p.old_len[b]);
+      n[i] = length(p.new_len[b]);
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if (tid * kPer + i >= cnt) o[i] = n[i] = 0;
-      nb[i] = blocks_of(o[i] + n[i], sh, W) - blocks_of(o[i], sh, W);
-      lost = add(lost, blocks_of(o[i] + n[i], sh, 0x7fffffff) - blocks_of(o[i] + n[i], sh, W));
+      const Need need(o[i], n[i], sh, W);
+      nb[i] = need.taken;
+      lost = add(lost, need.lost);
       sum_n = add(sum_n, n[i]);
       sum_b = add(sum_b, nb[i]);
     }
@@ -143,7 +161,8 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
     __syncthreads();
     for (int i = first; i < cnt; i += step) {
       p.row_start[b0 + i] = starts[i];
-      p.kv_len[b0 + i] = olds[i] + (kPer == 1 ? n[0] : len(p.new_len[b0 + i]));  // kPer 1: i = tid
+      if (!p.in_place)
+        p.kv_len[b0 + i] = olds[i] + (kPer == 1 ? n[0] : length(p.new_len[b0 + i]));  // kPer 1: i = tid
     }
     const int end = min(all_n, T);
     for (int64_t t0 = rows + static_cast<int64_t>(first) * 4; t0 < end; t0 += static_cast<int64_t>(step) * 4) {
@@ -180,9 +199,40 @@ __global__ __launch_bounds__(256) void k_kv_plan(PlanArgs p) {
   __syncthreads();
   if (tid == 0) {
     p.row_start[B] = rows;
-    p.state[0] = max(n_free - blocks, 0);
-    p.state[1] = add(max(blocks - n_free, 0), add(add(tmp[0][0], tmp[0][1]), add(tmp[0][2], tmp[0][3])));
+    if (!p.in_place) write_state(p, n_free, blocks, add(add(tmp[0][0], tmp[0][1]), add(tmp[0][2], tmp[0][3])));
   }
+}
+
+// kv_len and state, where one of them lies where old_len, new_len or n_free
+// does: k_kv_plan's workgroups read those in no order, so they are written
+// after it, by one workgroup whose threads read a request before they write it.
+constexpr int kLengthThreads = 1024;
+__global__ __launch_bounds__(kLengthThreads) void k_kv_plan_lengths(PlanArgs p) {
+  __shared__ int sums[2][kLengthThreads / 64];
+  const int sh = log2_of(p.d.block_tokens), tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  int blocks = 0, lost = 0;
+  for (int b = tid; b < p.d.B; b += kLengthThreads) {
+    const int old = length(p.old_len[b]), fresh = length(p.new_len[b]);
+    const Need need(old, fresh, sh, p.d.W);
+    blocks = add(blocks, need.taken);
+    lost = add(lost, need.lost);
+    p.kv_len[b] = old + fresh;
+  }
+  for (int m = 32; m >= 1; m >>= 1) {
+    blocks = add(blocks, shfl_xor(blocks, m));
+    lost = add(lost, shfl_xor(lost, m));
+  }
+  if (lane == 0) {
+    sums[0][wv] = blocks;
+    sums[1][wv] = lost;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  for (int w = 1; w < kLengthThreads / 64; ++w) {
+    blocks = add(blocks, sums[0][w]);
+    lost = add(lost, sums[1][w]);
+  }
+  write_state(p, min(max(*p.n_free, 0), p.d.free_cap), blocks, lost);
 }
 
 // ---------------------------------------------------------------- write
@@ -345,9 +395,12 @@ hipError_t launch_kv_plan(const moe_kv_plan_dims& d, const int32_t* old_len, con
   const int work = d.T > d.B ? d.T : d.B;
   int grid = cdiv(work, 1024);
   grid = grid < 1 ? 1 : grid > 256 ? 256 : grid;
-  const PlanArgs p{d, old_len, new_len, block_table, free_ids, n_free, row_start, kv_len, positions, slots, seq, state};
+  const PlanArgs p{d,      old_len,   new_len, block_table, free_ids,
+                   n_free, row_start, kv_len,  positions,   slots,
+                   seq,    state,     kv_len == old_len || kv_len == new_len || state == n_free};
   if (d.B <= 256) hipLaunchKernelGGL(k_kv_plan<1>, dim3(grid), dim3(256), 0, s, p);
   else hipLaunchKernelGGL(k_kv_plan<kPlanPer>, dim3(grid), dim3(256), 0, s, p);
+  if (p.in_place) hipLaunchKernelGGL(k_kv_plan_lengths, dim3(1), dim3(kLengthThreads), 0, s, p);
   return hipGetLastError();
 }
 

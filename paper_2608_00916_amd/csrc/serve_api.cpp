@@ -157,6 +157,12 @@ int expert_products(const I8Rows& rt, const int8_t* x8, const float* sx, const i
   return hip_status(e, "down");
 }
 
+// Whether n and m int32 at a and b share memory without being the same.
+bool shifted(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x != y && x < y + m * sizeof(int32_t) && y < x + n * sizeof(int32_t);
+}
+
 bool block_size_ok(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128; }
 
 int check_cache(const moe_kv_cache* c) {
@@ -325,6 +331,8 @@ int moe_kv_plan(const moe_kv_plan_dims* d, const int32_t* old_len, const int32_t
     return rc;
   if (d->T > 0)
     if (int rc = check_ptrs({{"positions", positions}, {"slots", slots}, {"seq", seq}})) return rc;
+  if (shifted(kv_len, d->B, old_len, d->B) || shifted(kv_len, d->B, new_len, d->B))
+    return fail(MOE_ERR_ARG, "kv_len overlaps old_len or new_len without being it");
   return hip_status(launch_kv_plan(*d, old_len, new_len, block_table, free_ids, n_free, row_start, kv_len, positions,
                                    slots, seq, state, static_cast<hipStream_t>(stream)),
                     "cache plan");

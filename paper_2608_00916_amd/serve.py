@@ -302,7 +302,8 @@ class KVPlan:
         self._b = [_p(t) for t in (self.row_start, self.kv_len, self.positions, self.slots, self.seq, self.state)]
 
     def build(self, old_len, new_len, block_table, free_ids, n_free, stream=None):
-        """Tables of this step; takes the blocks that the requests lack into block_table."""
+        """Tables of this step; takes the blocks that the requests lack into block_table.
+        The last step's kv_len and state[:1] may be passed as old_len and n_free."""
         d = self.d
         _shape("old_len", old_len, (d.B,))
         _shape("new_len", new_len, (d.B,))

@@ -79,3 +79,35 @@ def test_fewer_rows_than_new_tokens(T, causal):
         got.append((plan.positions.clone(), out, ko, vo))
     for x, y in zip(*got):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("B,W", [(3, 40), (256, 6), (700, 6), (9000, 5)])
+def test_plan_in_place(B, W):
+    """A step's lengths and stack are the next one's: passed as they are, the tables are those of copies."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("plan in place", B)
+    g = gen(34)
+    bt, n = 16, 5 * B + 50
+    free = dev(g.permutation(n).astype(np.int32))
+    steps = [g.integers(-1, 30, B) * (g.random(B) > 0.2) for _ in range(4)]
+    T = max(int(np.maximum(s, 0).sum()) for s in steps) + 3
+    a, b = (moe.KVPlan(B, T, W, n, bt) for _ in range(2))
+    ta, tb = (i32(np.full((B, W), -1)) for _ in range(2))
+    a.kv_len.zero_(), a.state.fill_(n)
+    length, n_free = i32(np.zeros(B)), i32([n])
+    for s in steps:
+        a.build(a.kv_len, i32(s), ta, free, a.state[:1])
+        b.build(length, i32(s), tb, free, n_free)
+        length, n_free = b.kv_len.clone(), b.state[:1].clone()
+        for name in ("row_start", "kv_len", "positions", "slots", "seq", "state"):
+            assert torch.equal(getattr(a, name), getattr(b, name)), name
+        assert torch.equal(ta, tb)
+    # the new tokens' own tensor may take the lengths as well
+    s = i32(steps[0])
+    want = moe.KVPlan(B, T, W, n, bt)
+    want.build(length, s, tb, free, n_free)
+    a.kv_len.copy_(s)
+    a.build(length, a.kv_len, ta, free, n_free)
+    for name in ("row_start", "kv_len", "positions", "slots", "seq", "state"):
+        assert torch.equal(getattr(a, name), getattr(want, name)), name
