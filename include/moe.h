@@ -395,7 +395,7 @@ typedef struct moe_kv_batch {
 typedef struct moe_kv_plan_dims {
   int32_t B, T, W;      /* B, W >= 1, T >= 0 */
   int32_t n_blocks, block_tokens;
-  int32_t free_cap;     /* entries of free_ids */
+  int32_t free_cap;     /* entries of free_ids (0: free_ids is not looked at) */
 } moe_kv_plan_dims;
 int moe_kv_plan(const moe_kv_plan_dims* d, const int32_t* old_len, const int32_t* new_len, int32_t* block_table,
                 const int32_t* free_ids, const int32_t* n_free, int32_t* row_start, int32_t* kv_len,

@@ -326,9 +326,10 @@ int moe_kv_plan(const moe_kv_plan_dims* d, const int32_t* old_len, const int32_t
     return fail(MOE_ERR_ARG, "n_blocks=%d or W=%d x block_tokens=%d exceeds 2^31 - 1 slots", d->n_blocks, d->W,
                 d->block_tokens);
   if (int rc = check_ptrs({{"old_len", old_len}, {"new_len", new_len}, {"block_table", block_table},
-                           {"free_ids", free_ids}, {"n_free", n_free}, {"row_start", row_start}, {"kv_len", kv_len},
-                           {"state", state}}))
+                           {"n_free", n_free}, {"row_start", row_start}, {"kv_len", kv_len}, {"state", state}}))
     return rc;
+  if (d->free_cap > 0)
+    if (int rc = check_ptrs({{"free_ids", free_ids}})) return rc;
   if (d->T > 0)
     if (int rc = check_ptrs({{"positions", positions}, {"slots", slots}, {"seq", seq}})) return rc;
   if (shifted(kv_len, d->B, old_len, d->B) || shifted(kv_len, d->B, new_len, d->B))

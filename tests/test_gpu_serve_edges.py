@@ -111,3 +111,16 @@ def test_plan_in_place(B, W):
     a.build(length, a.kv_len, ta, free, n_free)
     for name in ("row_start", "kv_len", "positions", "slots", "seq", "state"):
         assert torch.equal(getattr(a, name), getattr(want, name)), name
+
+
+def test_plan_from_an_empty_stack():
+    """No stack at all: requests that need no block go on, the others get none."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("plan without a stack")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    table = i32([[4, -1], [5, -1]])
+    plan = moe.KVPlan(2, 5, 2, 10, 16)
+    plan.build(i32([3, 15]), i32([2, 3]), table, none, i32([7]))
+    assert plan.slots.tolist() == [67, 68, 95, -1, -1] and plan.state.tolist() == [0, 1]
+    assert table.tolist() == [[4, -1], [5, -1]]

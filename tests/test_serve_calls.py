@@ -15,3 +15,15 @@ def test_plan_refuses_lengths_that_overlap_in_part():
             call("moe_kv_plan", _lib.MOE_ERR_ARG, ref(d), old, new, table, ids, n_free, start, at + shift, pos, slots, seq,
                  state, None)
             assert "overlaps" in _lib.lib().moe_last_error().decode()
+
+
+def test_plan_without_a_stack_needs_no_ids():
+    """The stack is looked at only where it has entries: what is refused here is `state`."""
+    for cap, name in ((0, "state"), (1, "free_ids")):
+        d = _lib.MoeKvPlanDims(1, 4, 4, 10, 16, cap)
+        args = [FAKE] * 11
+        args[3] = None
+        if cap == 0:
+            args[10] = None
+        call("moe_kv_plan", _lib.MOE_ERR_ARG, ref(d), *args, None)
+        assert _lib.lib().moe_last_error().decode().startswith(name)
