@@ -356,7 +356,7 @@ class KVAttention:
         cache = getattr(cache, "d", cache)
         D, bt = cache.head_dim, cache.block_tokens
         self.a = MoeKvAttn(heads, max_q, max_kv, D ** -0.5 if scale is None else scale, MOE_F_CAUSAL if causal else 0)
-        self.T, self.B = T, B
+        self.T, self.B, self.D = T, B, D
         nb = moe_kv_attention_workspace_bytes(cache, MoeKvBatch(B, T, -(-max_kv // bt), None, None, None), self.a)
         if nb == 0:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
@@ -369,7 +369,9 @@ class KVAttention:
         t = q.shape[0]
         if t > self.T or block_table.shape[0] != self.B:
             raise ValueError(f"{t} tokens of {block_table.shape[0]} requests, made for {self.T} of {self.B}")
-        _shape("q", q, (t, self.a.heads, cache.d.head_dim))
+        if cache.d.head_dim != self.D:
+            raise ValueError(f"cache has head_dim {cache.d.head_dim}, made for {self.D}")
+        _shape("q", q, (t, self.a.heads, self.D))
         check(lib().moe_kv_attention(_ref(cache.d), _ref(kv_batch(t, row_start, kv_len, block_table)), _ref(self.a),
                                      *_rows(q), *self._b, _s(stream)))
         return self.out if t == self.T else self.out[:t]

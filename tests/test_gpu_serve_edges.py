@@ -124,3 +124,20 @@ def test_plan_from_an_empty_stack():
     plan.build(i32([3, 15]), i32([2, 3]), table, none, i32([7]))
     assert plan.slots.tolist() == [67, 68, 95, -1, -1] and plan.state.tolist() == [0, 1]
     assert table.tolist() == [[4, -1], [5, -1]]
+
+
+def test_attention_over_another_cache():
+    """What is made for one cache takes another of its head size, and refuses the rest."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("attention over another cache")
+    wide, narrow = (Pages(gen(35), [100], 16, 2, D) for D in (128, 64))
+    op = moe.KVAttention(wide.cache, 1, 4, 1, 1, 100)
+    args = dev(narrow.table), i32([0, 1]), i32([100])
+    with pytest.raises(ValueError, match="head_dim"):
+        op.forward(bf16(gen(36).standard_normal((1, 4, 64))), narrow.cache, *args)
+    other = Pages(gen(37), [100], 32, 2, 128)
+    q = bf16(gen(38).standard_normal((1, 4, 128)))
+    got = op.forward(q, other.cache, dev(other.table), i32([0, 1]), i32([100]))
+    assert torch.equal(got, moe.KVAttention(other.cache, 1, 4, 1, 1, 100).forward(q, other.cache, dev(other.table),
+                                                                                 i32([0, 1]), i32([100])))
