@@ -293,7 +293,7 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
 #define MOE_F_OUT_FP32 8u /* moe_i8_dims: the output is fp32, else bf16 */
 #define MOE_F_CAUSAL 16u  /* moe_kv_attn: a token sees the keys up to its own position, else all */
 
-#define MOE_I8_MAX_K 131072 /* sums of K products of int8 stay below 2^31 */
+#define MOE_I8_MAX_K 131072 /* sums of K products of int8 are at most 2^31 in magnitude */
 
 /* Rows of x ([rows, K] bf16, row pitch ldx elements) as int8 rows: q [rows, K],
  * scale [rows].  rows >= 1; K a multiple of 16, at most MOE_I8_MAX_K; ldx >= K,

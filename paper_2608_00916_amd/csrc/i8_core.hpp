@@ -35,6 +35,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "moe.h"
 
 namespace moe {
 
@@ -46,6 +47,11 @@ __device__ __forceinline__ i32x4 mfma_i8(const uint4& p, const uint4& q, i32x4 a
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, p), __builtin_bit_cast(i32x4, q), acc, 0, 0,
                                                0);
 }
+
+// The one sum that leaves int32: MOE_I8_MAX_K products of -128 and -128 are 2^31,
+// which arrives as -2^31, a sum that no operands have.  2^31 - 1 is the same
+// number in fp32.
+__device__ __forceinline__ int unwrap(int sum) { return sum == INT32_MIN ? INT32_MAX : sum; }
 
 // 16 bytes per lane from a buffer resource to LDS at base + 16 lane; offsets at
 // or past the resource's size read zeros (the check covers the per-lane offset
@@ -152,6 +158,7 @@ struct Items {
 //   void prefetch(const Tile&)    called before the tile's first step: loads within the loop
 //                                 would make every round wait for its copies
 //   bool kSkip                    waves without a valid row skip the products
+//   bool kAnyInt8                 operands may hold -128 (else -127 .. 127)
 //   void finish(const Tile&, acc) its results; waves without a valid row skip it
 // kGather: rows of A through an index, at 64-bit offsets.
 template <class C, bool kTail, bool kGather, class Job>
@@ -279,6 +286,16 @@ __device__ __forceinline__ void i8_stream(int K, int items, Job& job, int8_t* st
     }
     if (live) compute(now);
     wait_vm<0>();  // the scales and the copies, but not the stores that follow
+    if constexpr (Job::kAnyInt8) {
+      if (K == MOE_I8_MAX_K) {
+#pragma unroll
+        for (int m = 0; m < C::FM; ++m)
+#pragma unroll
+          for (int n = 0; n < C::FN; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][n][i] = unwrap(acc[m][n][i]);
+      }
+    }
     if (live) job.finish(cur, acc);
     if (tn >= items) break;
     swap();

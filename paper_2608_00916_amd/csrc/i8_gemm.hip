@@ -46,7 +46,7 @@ struct DenseJob {
     return {m0, in / h * C::BN, min(half < 0 ? C::BM : C::BM / 2, p.M - m0)};
   }
   static constexpr int kParts = 1;
-  static constexpr bool kSkip = C::WM > 1;
+  static constexpr bool kSkip = C::WM > 1, kAnyInt8 = true;
   __device__ __forceinline__ I8Source a(const Tile& t) const {
     return {p.a + static_cast<int64_t>(t.m0) * p.K, t.rows};
   }
@@ -216,10 +216,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(DenseArgs p, const bf
   for (int i = threadIdx.x; i < MT * NT * 256; i += 64 * kFewWaves) {
     const int c = i % (16 * NT), r = i / (16 * NT), row = m0 + r, col = n0 + c;
     if (row >= p.M || col >= p.N) continue;
-    int sum = 0;
+    uint32_t sum = 0;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) sum += sums[w][r >> 4][c >> 4][(c >> 2 & 3) * 16 + (r & 15)][c & 3];
-    const float v = static_cast<float>(sum) * (kFused ? scales[row] : p.sa[row]) * p.sb[col];
+    const float v = static_cast<float>(unwrap(static_cast<int>(sum))) * (kFused ? scales[row] : p.sa[row]) * p.sb[col];
     if (F32) static_cast<float*>(p.out)[row * p.ldo + col] = v;
     else static_cast<bf16_t*>(p.out)[row * p.ldo + col] = f2bf(v);
   }
@@ -315,7 +315,7 @@ struct GateUpJob {
     return x;
   }
   static constexpr int kParts = 2;  // gate, up
-  static constexpr bool kSkip = C::WM > 1;
+  static constexpr bool kSkip = C::WM > 1, kAnyInt8 = false;  // rows rounded here
   __device__ __forceinline__ int64_t source(int row) const { return kGather ? p.rows[row] : row; }
   __device__ __forceinline__ I8Source a(const Tile& t) const {
     if (kGather) return {p.x, t.rows, p.rows + t.row};
@@ -399,7 +399,7 @@ struct DownJob {
     return x;
   }
   static constexpr int kParts = 1;
-  static constexpr bool kSkip = C::WM > 1;
+  static constexpr bool kSkip = C::WM > 1, kAnyInt8 = false;  // rows rounded here
   __device__ __forceinline__ I8Source a(const Tile& t) const {
     return {p.x + static_cast<int64_t>(t.row) * p.F, t.rows};
   }

@@ -141,3 +141,23 @@ def test_attention_over_another_cache():
     got = op.forward(q, other.cache, dev(other.table), i32([0, 1]), i32([100]))
     assert torch.equal(got, moe.KVAttention(other.cache, 1, 4, 1, 1, 100).forward(q, other.cache, dev(other.table),
                                                                                  i32([0, 1]), i32([100])))
+
+
+@pytest.mark.parametrize("M,N", [(1, 5), (20, 40), (33, 40), (300, 500), (1000, 1001), (2000, 1500), (4096, 4104)])
+def test_matmul_of_the_lowest_values(M, N):
+    """-128 in both operands at the largest K: the sum is 2^31 itself.  Every tile shape."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("i8 matmul lowest", M, N)
+    K = moe._lib.MOE_I8_MAX_K
+    a = torch.full((M, K), -128, dtype=torch.int8, device="cuda")
+    b = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    b[1], b[2] = 127, 0
+    b[0, 5] = -127
+    one = torch.ones(max(M, N), device="cuda")
+    want = torch.full((N,), 2.0 ** 31, device="cuda")
+    want[0], want[1], want[2] = 2.0 ** 31 - 128, -128.0 * 127 * K, 0
+    for fp32 in (True, False):
+        out = torch.empty((M, N), dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
+        moe.moe_i8_matmul(a, one[:M], b, one[:N], out)
+        assert (out == want.to(out.dtype)).all()
