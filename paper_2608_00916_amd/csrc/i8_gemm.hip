@@ -340,7 +340,8 @@ struct GateUpJob {
       su[n] = *reinterpret_cast<const float4*>(p.w.s_up + c + n * 4);
     }
   }
-  // With G = s g, U = s u (s the row's scale): silu(G) U = s^2 g u / (1 + e^-G).
+  // With G = s g, U = s u (s the row's scale): silu(G) U = s g / (1 + e^-G) s u,
+  // the gate closed first: G U may pass fp32 where silu(G) is 0.
   // It is left in fp32: in 16 bits, each with its partial's scale, one value in
   // 1000 came out a step of its 8 bits away, which rows of few columns show
   // (0.004 of the output against 0.0017; 3 percent faster at 65536 rows).
@@ -361,7 +362,7 @@ struct GateUpJob {
           const float gate = static_cast<float>(acc[m][n][i]) * g4[i];
           const float up = static_cast<float>(acc[m][n + C::FN / 2][i]) * u4[i];
           const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(gate * e));
-          v[4 * n + i] = gate * s[m] * (up * s[m]) * sig;
+          v[4 * n + i] = gate * s[m] * sig * (up * s[m]);
           top = max(top, __float_as_uint(v[4 * n + i]) & 0x7fffffffu);
         }
       }

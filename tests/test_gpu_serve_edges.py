@@ -4,7 +4,8 @@ that are replaced, operands at the ends of their types."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_serve import Pages, attend, bf16, dev, gen, i32, say
+from tests import serve_ref as R
+from tests.test_gpu_serve import Pages, attend, bf16, dev, gen, host, i32, say
 
 pytestmark = pytest.mark.gpu
 
@@ -161,3 +162,28 @@ def test_matmul_of_the_lowest_values(M, N):
         out = torch.empty((M, N), dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda")
         moe.moe_i8_matmul(a, one[:M], b, one[:N], out)
         assert (out == want.to(out.dtype)).all()
+
+
+@pytest.mark.parametrize("rows", [3, 200, 3000])
+def test_experts_closed_gates_of_huge_values(rows):
+    """silu(G) U is 0 where the gate is far below 0, also where G U passes fp32."""
+    import paper_2608_00916_amd as moe
+    say("experts closed gates", rows)
+    g = gen(39)
+    H = F = 128
+    x = bf16(np.abs(g.standard_normal((rows, H))) * 1e10)
+    w = [g.integers(-127, 128, s).astype(np.int8) for s in ((1, F, H), (1, F, H), (1, H, F))]
+    s = [np.full(n, 1.0, np.float32) for n in ((1, F), (1, F), (1, H))]
+    w[0][:, 1::2] = -np.abs(w[0][:, 1::2])  # these gates are closed
+    w[0][:, ::2] = 0
+    w[0][:, ::2, 0] = 1
+    s[0][:, 1::2] = 1e10
+    s[1][:, 1::2] = 1e20
+    s[0][:, ::2] = s[1][:, ::2] = 1e-12
+    w8 = moe.i8_weights(*(dev(t) for p in zip(w, s) for t in p))
+    got = host(moe.MoEExpertsI8(rows, H, 1, F).forward(x, i32([rows]), w8))
+    assert np.isfinite(got).all()
+    v = [t[0].astype(np.float64) * sc[0].astype(np.float64)[:, None] for t, sc in zip(w, s)]
+    v[0], v[1], v[2] = v[0][::2], v[1][::2], v[2][:, ::2]
+    ref = R.expert(host(x), *v)
+    assert np.linalg.norm(got - ref) <= (2.0 ** -8 + 0.0005) * np.linalg.norm(ref)
