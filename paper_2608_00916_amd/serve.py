@@ -69,6 +69,28 @@ def _ws(n, device):
     return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
 
 
+class _Held:
+    """Buffers whose pointers are taken and checked once, by _take, and not at
+    every call; replacing one takes them again (or, refused, leaves it)."""
+
+    def __setattr__(self, name, value):
+        d = self.__dict__
+        old = d.get(name)
+        d[name] = value
+        if isinstance(old, torch.Tensor) and "_b" in d:
+            try:
+                self._take()
+            except (ValueError, AttributeError):
+                d[name] = old
+                raise
+
+
+def _take_ws(ws, nb):
+    if ws.numel() * ws.element_size() < nb:
+        raise ValueError(f"ws has less than {nb} bytes")
+    return _p(ws), nb
+
+
 # ------------------------------------------------------------------ int8 products
 def i8_dims(M, N, K, out_fp32=False) -> MoeI8Dims:
     return MoeI8Dims(M, N, K, MOE_F_OUT_FP32 if out_fp32 else 0)
@@ -131,13 +153,12 @@ def moe_i8_linear(d, x, b, b_scale, out, ws, stream=None):
                               ws.numel(), _s(stream)))
 
 
-class I8Linear:
+class I8Linear(_Held):
     """A projection with int8 weights [N, K] (moe_i8_quant_weight) for up to M
     rows: the caller-side workspace and output."""
 
     def __init__(self, M, weight, scale, out_fp32=False):
         N, K = weight.shape
-        _shape("scale", scale, (N,))
         self.weight, self.scale = weight, scale
         self.d = i8_dims(M, N, K, out_fp32)
         nb = moe_i8_linear_workspace_bytes(self.d)
@@ -145,8 +166,17 @@ class I8Linear:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, weight.device)
         self.out = torch.empty((M, N), dtype=torch.float32 if out_fp32 else torch.bfloat16, device=weight.device)
-        # pointers of what it owns, checked once
-        self._b = _p(weight, torch.int8), _p(scale, torch.float32), _p(self.out), N, _p(self.ws), nb
+        self._nb = nb
+        self._take()
+
+    def _take(self):
+        d = self.d
+        _shape("weight", self.weight, (d.N, d.K))
+        _shape("scale", self.scale, (d.N,))
+        _shape("out", self.out, (d.M, d.N))
+        self._b = (_p(self.weight, torch.int8), _p(self.scale, torch.float32),
+                   _p(self.out, torch.float32 if d.flags & MOE_F_OUT_FP32 else torch.bfloat16), d.N,
+                   *_take_ws(self.ws, self._nb))
 
     def forward(self, x, stream=None):
         """The product of x [m, K], m <= M (rows may be strided); a view of the output's first m rows."""
@@ -199,7 +229,7 @@ def moe_infer_i8(d, x, w_r, w: MoeI8Experts, token_mask, y, ws, stream=None):
                              _p(y, torch.bfloat16), _p(ws), ws.numel(), _s(stream)))
 
 
-class MoEExpertsI8:
+class MoEExpertsI8(_Held):
     """Caller-side buffers of one rank's local experts in 8 bits, forward only."""
 
     def __init__(self, rows, H, E, F, device="cuda"):
@@ -209,7 +239,12 @@ class MoEExpertsI8:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, device)
         self.o = torch.empty((rows, H), dtype=torch.bfloat16, device=device)
-        self._b = _p(self.o), _p(self.ws), nb  # pointers of what it owns
+        self._nb = nb
+        self._take()
+
+    def _take(self):
+        _shape("o", self.o, (self.d.rows, self.d.H))
+        self._b = _p(self.o, torch.bfloat16), *_take_ws(self.ws, self._nb)
 
     def forward(self, xp, counts, w: MoeI8Experts, stream=None):
         d = self.d
@@ -288,7 +323,7 @@ def moe_kv_attention(cache: MoeKvCache, batch: MoeKvBatch, a: MoeKvAttn, q, out,
     check(lib().moe_kv_attention(_ref(cache), _ref(batch), _ref(a), pq, ldq, po, ldo, _p(ws), ws.numel(), _s(stream)))
 
 
-class KVPlan:
+class KVPlan(_Held):
     """Buffers of one step's tables for B requests of up to W blocks, up to T packed new tokens."""
 
     def __init__(self, B, T, W, n_blocks, block_tokens, device="cuda"):
@@ -299,7 +334,16 @@ class KVPlan:
 
         self.row_start, self.kv_len, self.state = ints(B + 1), ints(B), ints(2)
         self.positions, self.slots, self.seq = ints(T), ints(T), ints(T)
-        self._b = [_p(t) for t in (self.row_start, self.kv_len, self.positions, self.slots, self.seq, self.state)]
+        self._take()
+
+    def _take(self):
+        d, held = self.d, []
+        for name, n in (("row_start", d.B + 1), ("kv_len", d.B), ("positions", d.T), ("slots", d.T), ("seq", d.T),
+                        ("state", 2)):
+            t = getattr(self, name)
+            _shape(name, t, (n,))
+            held.append(_p(t, torch.int32))
+        self._b = held
 
     def build(self, old_len, new_len, block_table, free_ids, n_free, stream=None):
         """Tables of this step; takes the blocks that the requests lack into block_table.
@@ -313,7 +357,7 @@ class KVPlan:
         moe_kv_plan(d, old_len, new_len, block_table, free_ids, n_free, *self._b, stream)
 
 
-class KVCache:
+class KVCache(_Held):
     """A paged cache of keys and values in 8 bits with a scale for each block and head."""
 
     def __init__(self, n_blocks, block_tokens, kv_heads, head_dim, device="cuda"):
@@ -330,13 +374,21 @@ class KVCache:
         return c
 
     def _own(self, k, v, k_scale, v_scale):
-        n, heads, bt, D = k.shape
-        _shape("v", v, (n, heads, D, bt))
-        _shape("k_scale", k_scale, (n, heads))
-        _shape("v_scale", v_scale, (n, heads))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.d = MoeKvCache(n, bt, heads, D, _p(k, torch.int8), _p(v, torch.int8), _p(k_scale, torch.float32),
-                            _p(v_scale, torch.float32))
+        n, heads, bt, D = k.shape
+        self.d = MoeKvCache(n, bt, heads, D, None, None, None, None)
+        self._take()
+
+    def _take(self):
+        d = self.d
+        n, heads, bt, D = d.n_blocks, d.kv_heads, d.block_tokens, d.head_dim
+        _shape("k", self.k, (n, heads, bt, D))
+        _shape("v", self.v, (n, heads, D, bt))
+        _shape("k_scale", self.k_scale, (n, heads))
+        _shape("v_scale", self.v_scale, (n, heads))
+        self._b = (_p(self.k, torch.int8), _p(self.v, torch.int8), _p(self.k_scale, torch.float32),
+                   _p(self.v_scale, torch.float32))
+        d.k, d.v, d.k_scale, d.v_scale = self._b
 
     def append(self, k, v, row_start, kv_len, block_table, stream=None):
         """Write the packed new keys and values ([T, kv_heads, head_dim], rows may be strided)."""
@@ -348,7 +400,7 @@ class KVCache:
         return k_out, v_out
 
 
-class KVAttention:
+class KVAttention(_Held):
     """Caller-side buffers of the attention of up to T packed new tokens (at most
     max_q of one request) of B requests over a cache of up to max_kv tokens each."""
 
@@ -362,7 +414,12 @@ class KVAttention:
             raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
         self.ws = _ws(nb, device)
         self.out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=device)
-        self._b = _p(self.out), heads * D, _p(self.ws), nb  # of what it owns
+        self._nb = nb
+        self._take()
+
+    def _take(self):
+        _shape("out", self.out, (self.T, self.a.heads, self.D))
+        self._b = _p(self.out, torch.bfloat16), self.a.heads * self.D, *_take_ws(self.ws, self._nb)
 
     def forward(self, q, cache: KVCache, block_table, row_start, kv_len, stream=None):
         """Attention of the packed queries q [t, heads, head_dim], t <= T (rows may be strided)."""

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import serve_ref as R
-from tests.test_gpu_serve import Pages, attend, bf16, dev, gen, host, i32, say
+from tests.test_gpu_serve import Pages, attend, bf16, dev, gen, host, i32, int8_rows, say
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +187,52 @@ def test_experts_closed_gates_of_huge_values(rows):
     v[0], v[1], v[2] = v[0][::2], v[1][::2], v[2][:, ::2]
     ref = R.expert(host(x), *v)
     assert np.linalg.norm(got - ref) <= (2.0 ** -8 + 0.0005) * np.linalg.norm(ref)
+
+
+def test_buffers_may_be_replaced():
+    """The classes run on the tensors they hold at the time of the call."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("buffers replaced")
+    g = gen(40)
+    (w, s), (w2, s2) = ([dev(t) for t in int8_rows(g, 64, 128)] for _ in range(2))
+    x = bf16(g.standard_normal((5, 128)))
+    lin = moe.I8Linear(5, w, s)
+    lin.forward(x)
+    lin.weight, lin.scale = w2, s2
+    first, lin.out = lin.out, torch.empty_like(lin.out)
+    want = moe.I8Linear(5, w2, s2).forward(x)
+    assert torch.equal(lin.forward(x), want) and not torch.equal(first, want)
+    with pytest.raises(ValueError):
+        lin.weight = w2[:32]
+    with pytest.raises(ValueError):
+        lin.scale = s2.double()
+    assert torch.equal(lin.forward(x), want)
+
+    pg, other = (Pages(gen(n), [50], 16, 2, 64) for n in (41, 42))
+    q = bf16(g.standard_normal((1, 4, 64)))
+    at = dev(other.table), i32([0, 1]), i32([50])
+    want = moe.KVAttention(other.cache, 1, 4, 1, 1, 50).forward(q, other.cache, *at)
+    op = moe.KVAttention(pg.cache, 1, 4, 1, 1, 50)
+    cache = pg.cache
+    cache.k, cache.v, cache.k_scale, cache.v_scale = (getattr(other.cache, n) for n in ("k", "v", "k_scale", "v_scale"))
+    op.out, op.ws = torch.empty_like(op.out), torch.empty_like(op.ws)
+    assert torch.equal(op.forward(q, cache, *at), want)
+    with pytest.raises(ValueError):
+        cache.v = cache.v[:1]
+    with pytest.raises(ValueError):
+        op.ws = op.ws[:16]
+    assert torch.equal(op.forward(q, cache, *at), want)
+
+    ex = moe.MoEExpertsI8(4, 128, 1, 128)
+    t = [dev(y) for shape in ((128, 128),) * 3 for y in int8_rows(g, *shape)]
+    w8 = moe.i8_weights(*(y[None] for y in t))
+    x = bf16(g.standard_normal((4, 128)))
+    want = ex.forward(x, i32([4]), w8).clone()
+    ex.o = torch.zeros_like(ex.o)
+    assert torch.equal(ex.forward(x, i32([4]), w8), want)
+
+    plan = moe.KVPlan(2, 3, 2, 10, 16)
+    plan.slots = torch.full_like(plan.slots, 9)
+    plan.build(i32([0, 0]), i32([1, 1]), i32([[-1, -1]] * 2), i32([4, 5]), i32([2]))
+    assert plan.slots.tolist() == [80, 64, -1]
