@@ -26,7 +26,7 @@ _ref = ctypes.byref
 
 
 def _p(t, dtype=None):
-    if t is None or type(t) is int:  # a pointer checked before
+    if t is None:
         return t
     if not t.is_cuda:
         raise ValueError("tensor must be on the GPU")
@@ -56,6 +56,13 @@ def _rows(t, dtype=torch.bfloat16):
 def _shape(name, t, shape):
     if t.shape != shape:  # torch.Size compares as the tuple that it is
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
+def _least(**sizes):
+    """Refuses tensors of fewer elements than the call will read or write: name=(tensor, elements)."""
+    for name, (t, n) in sizes.items():
+        if t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} elements of {n}")
 
 
 def _s(stream):
@@ -144,8 +151,9 @@ def moe_i8_linear_workspace_bytes(d: MoeI8Dims) -> int:
 
 
 def moe_i8_linear(d, x, b, b_scale, out, ws, stream=None):
-    px, ldx = _rows(x)
     _shape("x", x, (d.M, d.K))
+    _least(b=(b, d.N * d.K), b_scale=(b_scale, d.N))
+    px, ldx = _rows(x)
     if (out.dtype == torch.float32) != bool(d.flags & MOE_F_OUT_FP32):
         raise ValueError(f"out is {out.dtype}, which the dims do not say")
     po, ldo = _out_rows(out, d.M, d.N)
@@ -207,7 +215,7 @@ def i8_weights(w_gate, s_gate, w_up, s_up, w_down, s_down) -> MoeI8Experts:
 
 
 def _check_weights(w, E, H, F):
-    if w.shape != (E, H, F):
+    if getattr(w, "shape", (E, H, F)) != (E, H, F):  # a descriptor made by hand has none
         raise ValueError(f"weights of E, H, F = {w.shape}, not {(E, H, F)}")
 
 
@@ -216,6 +224,8 @@ def moe_experts_i8_workspace_bytes(d: MoeExpertsDims) -> int:
 
 
 def moe_experts_i8(d, xp, counts, w: MoeI8Experts, o, ws, stream=None):
+    _check_weights(w, d.E, d.H, d.F)
+    _least(xp=(xp, d.rows * d.H), counts=(counts, d.E), o=(o, d.rows * d.H))
     check(lib().moe_experts_i8(_ref(d), _p(xp, torch.bfloat16), _p(counts, torch.int32), _ref(w),
                                _p(o, torch.bfloat16), _p(ws), ws.numel(), _s(stream)))
 
@@ -225,6 +235,10 @@ def moe_infer_i8_workspace_bytes(d: MoeDims) -> int:
 
 
 def moe_infer_i8(d, x, w_r, w: MoeI8Experts, token_mask, y, ws, stream=None):
+    _check_weights(w, d.E, d.H, d.F)
+    _least(x=(x, d.T * d.H), w_r=(w_r, d.H * d.E), y=(y, d.T * d.H))
+    if token_mask is not None:
+        _least(token_mask=(token_mask, d.T))
     check(lib().moe_infer_i8(_ref(d), _p(x, torch.bfloat16), _p(w_r, torch.bfloat16), _ref(w), _p(token_mask),
                              _p(y, torch.bfloat16), _p(ws), ws.numel(), _s(stream)))
 
@@ -269,7 +283,6 @@ class MoEInferI8:
 
     def forward(self, x, w_r, w: MoeI8Experts, token_mask=None, stream=None):
         d = self.d
-        _check_weights(w, d.E, d.H, d.F)
         _shape("x", x, (d.T, d.H))
         _shape("w_r", w_r, (d.H, d.E))
         moe_infer_i8(d, x, w_r, w, token_mask, self.y, self.ws, stream)
@@ -279,10 +292,19 @@ class MoEInferI8:
 # ------------------------------------------------------------------ the paged cache
 def moe_kv_plan(d, old_len, new_len, block_table, free_ids, n_free, row_start, kv_len, positions, slots, seq, state,
                 stream=None):
+    _least(old_len=(old_len, d.B), new_len=(new_len, d.B), block_table=(block_table, d.B * d.W),
+           free_ids=(free_ids, d.free_cap), n_free=(n_free, 1), row_start=(row_start, d.B + 1), kv_len=(kv_len, d.B),
+           positions=(positions, d.T), slots=(slots, d.T), seq=(seq, d.T), state=(state, 2))
+    i32 = torch.int32
+    _plan(d, old_len, new_len, block_table, free_ids, n_free,
+          [_p(t, i32) for t in (row_start, kv_len, positions, slots, seq, state)], stream)
+
+
+def _plan(d, old_len, new_len, block_table, free_ids, n_free, written, stream):
+    """The call, on pointers of what it writes but for the table."""
     i32 = torch.int32
     check(lib().moe_kv_plan(_ref(d), _p(old_len, i32), _p(new_len, i32), _p(block_table, i32), _p(free_ids, i32),
-                            _p(n_free, i32), _p(row_start, i32), _p(kv_len, i32), _p(positions, i32), _p(slots, i32),
-                            _p(seq, i32), _p(state, i32), _s(stream)))
+                            _p(n_free, i32), *written, _s(stream)))
 
 
 def kv_batch(T, row_start, kv_len, block_table) -> MoeKvBatch:
@@ -354,7 +376,7 @@ class KVPlan(_Held):
         _shape("block_table", block_table, (d.B, d.W))
         _shape("n_free", n_free, (1,))
         d.free_cap = free_ids.numel()
-        moe_kv_plan(d, old_len, new_len, block_table, free_ids, n_free, *self._b, stream)
+        _plan(d, old_len, new_len, block_table, free_ids, n_free, self._b, stream)
 
 
 class KVCache(_Held):
