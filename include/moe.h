@@ -287,6 +287,15 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
  *   q_k = rint(127 x_k / a), a = max |x_k|, and the scale s = a / 127,
  * so x ~ s q.  A row of zeros has s = 0; a row with an infinity or NaN has
  * s = NaN and q = 0, so everything computed from it is NaN.
+ *
+ * What is held in fewer bits than fp32 beside the int8 rows and bf16 outputs:
+ *   - softmax weights enter the product with the values in fp16, times 2^7 to
+ *     2^15 against the largest: 2^-11 of each, and those below 2^-32 of the
+ *     largest are 0 there (the sum they are divided by is of the fp32 weights);
+ *   - queries are fp16 over a power of two per row: exact but for elements under
+ *     2^-17 of the row's largest, which are off by 2^-25 of it at most;
+ *   - exponentials and the reciprocals of the sigmoid and of value scales are
+ *     the hardware's, within an ulp or two of fp32.
  */
 
 /* flags (moe_i8_dims.flags, moe_kv_attn.flags) */
@@ -403,8 +412,10 @@ int moe_kv_plan(const moe_kv_plan_dims* d, const int32_t* old_len, const int32_t
 
 /* Write the batch's new keys and values (k, v: T rows of [kv_heads, head_dim]
  * bf16, row pitch ld elements, a multiple of 8) into their blocks.  A block's
- * scale is that of the largest value written to it since its first token: it
- * only grows, and the tokens it already holds are rounded again when it does.
+ * scale is that of the largest value written to it since its first token
+ * (largest / 127 in fp32): it only grows, and the tokens it already holds are
+ * rounded again when it does.  A value is rounded as rint(x / scale) in fp32,
+ * with the scale as it is stored.
  * A non-finite key or value makes the scale of its block and head NaN. */
 int moe_kv_append(const moe_kv_cache* c, const moe_kv_batch* b, const void* k, const void* v, int64_t ld,
                   void* stream);
@@ -420,7 +431,7 @@ int moe_kv_read(const moe_kv_cache* c, int32_t B, int32_t W, const int32_t* bloc
 /* Attention of the batch's new tokens over their requests' cache: per head
  *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale <q, k_j>),
  * over the keys the token sees (none: out = 0).  Query head i reads kv head
- * i / (heads / kv_heads).
+ * i / (heads / kv_heads).  Rows of no request are not written.
  *   q, out  T rows of [heads, head_dim] bf16, row pitches ldq and ldo elements (multiples of 8) */
 typedef struct moe_kv_attn {
   int32_t heads;  /* a multiple of kv_heads */
