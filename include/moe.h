@@ -291,7 +291,7 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
  * What is held in fewer bits than fp32 beside the int8 rows and bf16 outputs:
  *   - softmax weights enter the product with the values in fp16, times 2^7 to
  *     2^15 against the largest: 2^-11 of each, and those below 2^-32 of the
- *     largest are 0 there (the sum they are divided by is of the fp32 weights);
+ *     largest may be 0 there (the sum they are divided by is of the fp32 weights);
  *   - queries are fp16 over a power of two per row: exact but for elements under
  *     2^-17 of the row's largest, which are off by 2^-25 of it at most;
  *   - exponentials and the reciprocals of the sigmoid and of value scales are

@@ -19,11 +19,12 @@
 // and those of the next tile's first step under this tile's last one.  Loads
 // and stores share one in-order counter: the copies of the next tile's first
 // step are waited for before this tile's stores, which then have that step to
-// drain.  What bounds it is the bytes a step must bring from L2 for its
-// products, hence the 256 x 256 tile over 8 waves (128 x 64 each): 4096 x 16384
-// x 8192 at 2540 TOPS (the tallest rate the power limit was seen to allow is
-// 2700), 128 x 128 tiles over 4 waves at 2080; at K 2048 2140 and 1800, where
-// the stores of all workgroups meet at the memory every 16 steps.  Measured and
+// drain.  A taller tile brings fewer bytes from L2 per product, hence the 256 x
+// 256 tile over 8 waves (128 x 64 each): 4096 x 16384 x 8192 at 2570 TOPS, 128
+// x 128 tiles over 4 waves at 2080; at K 2048 2200 and 1840, where the stores of
+// all workgroups meet at the memory every 16 steps.  At 8192 x 5120 x 2048 the
+// matrix cores are busy 43% of the time, and waves wait 40% of theirs, for
+// copies and at the barrier; LDS (16%) and VALU (22%) have room.  Measured and
 // not taken: four stages of 64 bytes of k (13% slower, twice the barriers), a
 // barrier within the step with the next fragments read under its last products
 // (the same), lines brought into L2 ahead of the copies (20% slower),

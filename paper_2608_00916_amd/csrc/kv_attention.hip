@@ -261,7 +261,10 @@ __device__ __forceinline__ bf16_t* out_row(const AttnArgs& p, const Request& rq,
 // Factor that turns a row's sums into its output (0 for a row without a key).
 __device__ __forceinline__ float normaliser(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-// NB blocks of 16 rows.
+// NB blocks of 16 rows.  64 single tokens over up to 32768 keys (32 / 4 heads of
+// 128): 250 us, 5.2 TB/s of HBM reads, a copy's rate.  The registers of 32 rows
+// leave one wave a SIMD instead of two: 64 x 4 tokens over 4096 keys 104 us, 64
+// x 1 49.
 template <int D, int NB>
 __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
   constexpr int kP = D / 64, kDt = D / 16;
@@ -406,7 +409,10 @@ __global__ __launch_bounds__(256) void k_kv_attention(AttnArgs p) {
   }
 }
 
-// NB 16-row blocks per wave.
+// NB 16-row blocks per wave.  16 x 512 tokens over up to 4096 keys (32 / 4 heads
+// of 128): 254 us.  VALU instructions (conversion, softmax) issue for 49% of the
+// SIMDs' cycles and matrix instructions for 30%, with under 2 waves a SIMD to
+// overlap them; LDS is read 31% of the time, HBM is idle (0.6 TB/s).
 template <int D, int NB>
 __global__ __launch_bounds__(64 * kMany / 16 / NB, NB == 1 ? 4 : 2) void k_kv_attention_rows(AttnArgs p) {
   constexpr int kThreads = 64 * kMany / 16 / NB;
