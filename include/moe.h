@@ -292,6 +292,7 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
  *   - softmax weights enter the product with the values in fp16, times 2^7 to
  *     2^15 against the largest: 2^-11 of each, and those below 2^-32 of the
  *     largest may be 0 there (the sum they are divided by is of the fp32 weights);
+ *     scales of values below 2^-80 count as that there;
  *   - queries are fp16 over a power of two per row: exact but for elements under
  *     2^-17 of the row's largest, which are off by 2^-25 of it at most;
  *   - exponentials and the reciprocals of the sigmoid and of value scales are

@@ -32,7 +32,9 @@ constexpr int kTile = 64;  // tokens per step
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kBoostLog2 = 7.0f;     // weights of the maximum are 2^7 ...
 constexpr float kSlack = 8.0f;         // ... and at most 2^15: fp16 ends at 2^16
-constexpr float kMinScale = 0x1p-100f;  // of values: a block of zeros has scale 0
+// Least scale of values (a block of zeros has 0): 2^30 weights of 2^15 over it,
+// the most that a sum can hold, stay in fp32.
+constexpr float kMinScale = 0x1p-80f;
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));

@@ -236,3 +236,28 @@ def test_buffers_may_be_replaced():
     plan.slots = torch.full_like(plan.slots, 9)
     plan.build(i32([0, 0]), i32([1, 1]), i32([[-1, -1]] * 2), i32([4, 5]), i32([2]))
     assert plan.slots.tolist() == [80, 64, -1]
+
+
+def test_attention_over_many_keys_without_values():
+    """70000 keys whose values are all 0 before a block with values: the sum of their weights, which
+    grow after the first block, stays in fp32."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("zero values")
+    L, bt, D, T, heads = 70016, 64, 64, 4096, 16
+    n = L // bt
+    cache = moe.KVCache(n, bt, 1, D)
+    cache.k[1:] = 127
+    cache.k_scale.fill_(1 / 127)
+    cache.v[-1] = dev(gen(43).integers(-127, 128, (1, D, bt)).astype(np.int8))
+    cache.v_scale[-1] = 0.01
+    q = torch.full((T, heads, D), 1 / 16, dtype=torch.bfloat16, device="cuda")
+    scale = 5.4 * 16 / D  # scores 0 in the first block, 5.4 from there on: below 8 in base 2
+    table, kv = i32(np.arange(n)[None]), i32([L])
+    v = host(cache.v[-1, 0]) * 0.01
+    want = v.sum(1) / (L - bt + bt * np.exp(-5.4))
+    for t, h in ((T, heads), (1, heads), (1, 4), (2, heads)):
+        op = moe.KVAttention(cache, t, h, 1, t, L, causal=False, scale=scale)
+        got = host(op.forward(q[:t, :h], cache, table, i32([0, t]), kv))
+        bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * np.abs(v).sum(1) / (L - bt)
+        assert (np.abs(got - want) <= bound * 1.01).all(), (t, h)
