@@ -445,6 +445,98 @@ size_t moe_kv_attention_workspace_bytes(const moe_kv_cache* c, const moe_kv_batc
 int moe_kv_attention(const moe_kv_cache* c, const moe_kv_batch* b, const moe_kv_attn* a, const void* q, int64_t ldq,
                      void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------ a decoding step
+ * What a step needs around the products and the attention: the sum with the
+ * residual and its norm (with a backward, for training), the expert layer for
+ * a few tokens, and the next token from the logits. */
+
+/* Root-mean-square norm of rows, of their sum with a residual where there is
+ * one:
+ *   h = bf16(x + residual),  s = 1 / sqrt(mean_c h^2 + eps),  v = h s w (fp32),
+ *   y = bf16(v),  q, scale = the int8 rows of v.
+ * The norm is that of the sum as stored.  A row whose squares pass fp32 has
+ * s = 0; one with an infinity or NaN holds NaN where that was times s, and as
+ * an int8 row its scale is NaN. */
+#define MOE_NORM_MAX_H 32768
+typedef struct moe_norm_dims {
+  int32_t T, H;   /* T >= 1 rows of H: a multiple of 8 (of 16 for int8 rows), at most MOE_NORM_MAX_H */
+  uint32_t flags; /* MOE_F_DW_FP32: the backward's dw is fp32, else bf16 */
+  float eps;      /* a positive normal number */
+} moe_norm_dims;
+
+/*   x         [T, H] bf16, row pitch ldx elements (a multiple of 8)
+ *   residual  the same with ldr, or NULL (ldr is ignored)
+ *   w         [H] bf16
+ *   h         [T, H] bf16 or NULL; NULL without a residual
+ *   y         [T, H] bf16 or NULL
+ *   q, scale  [T, H] int8 and [T], or both NULL; y or q is given
+ * h or y may be x or residual itself where that has pitch H; apart from this
+ * nothing that is written may overlap anything else. */
+int moe_norm_fwd(const moe_norm_dims* d, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w,
+                 void* h, void* y, int8_t* q, float* scale, void* stream);
+
+/* Backward.  With n = h s and g = dy w:
+ *   dx = s (g - n mean_c(g n)) + dh,  dw = sum_t dy n
+ * dx is the gradient of x and of the residual alike.
+ *   h   the rows that were normed (the stored sum; x without a residual), pitch ldh
+ *   dy  [T, H] bf16, pitch lddy;  dh the gradient that reaches h past the norm, pitch lddh, or NULL
+ *   dx  [T, H] bf16; may be dy or dh itself where that has pitch H, else overlaps nothing
+ *   dw  [H] bf16, or fp32 with MOE_F_DW_FP32; overwritten
+ *   ws  moe_norm_bwd_workspace_bytes(d) bytes of scratch */
+size_t moe_norm_bwd_workspace_bytes(const moe_norm_dims* d);
+int moe_norm_bwd(const moe_norm_dims* d, const void* h, int64_t ldh, const void* w, const void* dy, int64_t lddy,
+                 const void* dh, int64_t lddh, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* moe_infer for at most MOE_DECODE_MAX_T tokens: the same layer with the same
+ * selection and gates, bit for bit, in tiles for few rows.  G, U and O stay
+ * fp32, only A is rounded to bf16 between the products, so Y is closer to the
+ * equations than moe_infer's and not its bits.  Arguments and flags as
+ * moe_infer.
+ *   ws  moe_decode_workspace_bytes(d) bytes of scratch */
+#define MOE_DECODE_MAX_T 64
+size_t moe_decode_workspace_bytes(const moe_dims* d);
+int moe_decode(const moe_dims* d, const void* x, const void* w_r, const void* w_gate, const void* w_up,
+               const void* w_down, const uint8_t* token_mask, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* The same with the experts in 8 bits, as in moe_infer_i8 (O stays fp32).
+ *   ws  moe_decode_i8_workspace_bytes(d) bytes of scratch */
+size_t moe_decode_i8_workspace_bytes(const moe_dims* d);
+int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i8_experts* w, const uint8_t* token_mask,
+                  void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* The next token of each of B rows of V logits, from a given number u in [0, 1)
+ * per row.  Larger logits come first, equal ones by lower index.
+ *   weights  e^((logit - largest) / temperature), held to 2^-43
+ *   top_k    the first top_k stay; 0 or less, or V or more: all
+ *   top_p    of those the shortest prefix whose weights reach top_p of their
+ *            sum stays, one at least; 1 or more: all
+ *   min_p    of those the weights of at least min_p times the largest stay
+ *            (more than 1 counts as 1); 0 or less: all
+ *   token    of what stays the lowest index at which the running sum of
+ *            weights, in index order, passes u times their sum
+ * A temperature of 0 or less (or NaN) takes the first in the order.  NaN in
+ * top_p or min_p turns that filter off; u below 0 or NaN counts as 0, u of 1
+ * and more takes the last.  A logit of -infinity or NaN is never taken; +infinity
+ * leaves only its like.  A row without a logit to take has token -1 and
+ * logprob -infinity. */
+#define MOE_SAMPLE_MAX_V 1048576
+typedef struct moe_sample_dims {
+  int32_t B, V;   /* 1 <= B <= 65535, 1 <= V <= MOE_SAMPLE_MAX_V */
+  uint32_t flags; /* MOE_F_LOGITS_FP32 */
+} moe_sample_dims;
+#define MOE_F_LOGITS_FP32 32u /* moe_sample_dims: the logits are fp32, else bf16 */
+
+/*   logits       [B, V], row pitch ld >= V elements
+ *   temperature, top_p, min_p  [B] fp32, top_k [B] int32, each on the device, or NULL: off (temperature: 1)
+ *   u            [B] fp32
+ *   token        [B] int32
+ *   logprob      [B] fp32 or NULL: log of the token's share of the weights that stay (0 at temperature 0)
+ *   ws           moe_sample_workspace_bytes(d) bytes of scratch */
+size_t moe_sample_workspace_bytes(const moe_sample_dims* d);
+int moe_sample(const moe_sample_dims* d, const void* logits, int64_t ld, const float* temperature,
+               const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,
+               float* logprob, void* ws, size_t ws_bytes, void* stream);
+
 /* Per-kernel timing.  With tracing on, every kernel the library launches is
  * bracketed by two HIP events recorded on its launch stream (no host
  * synchronisation at launch time).  moe_trace_read waits for the recorded

@@ -17,6 +17,8 @@ from ._lib import (MOE_F_DW_FP32, MOE_F_MASK, MOE_F_RECOMPUTE, MOE_MAX_EXPERTS, 
                    MoeError, MoeExpertsDims, MoeExpertsSavedView, MoeLora, MoeSavedView, check, lib)
 from . import serve
 from .serve import *  # noqa: F401,F403  the 8-bit serving operators
+from . import step
+from .step import *  # noqa: F401,F403  norms, the experts for a few tokens, sampling
 
 __all__ = [
     "dims", "experts_dims", "moe_saved_bytes", "moe_fwd_workspace_bytes",
@@ -27,7 +29,7 @@ __all__ = [
     "moe_experts_fwd", "moe_experts_bwd", "moe_last_error", "moe_version",
     "moe_trace_enable", "moe_trace_read", "MoEBlock", "MoEExperts", "MoeError", "MOE_F_MASK", "MOE_F_DW_FP32",
     "MOE_F_RECOMPUTE",
-    "MOE_MAX_EXPERTS", "MOE_MAX_TOPK", *serve.__all__,
+    "MOE_MAX_EXPERTS", "MOE_MAX_TOPK", *serve.__all__, *step.__all__,
 ]
 
 

@@ -24,7 +24,11 @@ MOE_F_DW_FP32 = 2
 MOE_F_RECOMPUTE = 4
 MOE_F_OUT_FP32 = 8
 MOE_F_CAUSAL = 16
+MOE_F_LOGITS_FP32 = 32
 MOE_I8_MAX_K = 131072
+MOE_NORM_MAX_H = 32768
+MOE_DECODE_MAX_T = 64
+MOE_SAMPLE_MAX_V = 1 << 20
 MOE_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = (
@@ -36,6 +40,8 @@ EXPORTS = (
     "moe_i8_quant_rows", "moe_i8_quant_weight", "moe_i8_matmul", "moe_i8_linear_workspace_bytes", "moe_i8_linear",
     "moe_experts_i8_workspace_bytes", "moe_experts_i8", "moe_infer_i8_workspace_bytes", "moe_infer_i8",
     "moe_kv_plan", "moe_kv_append", "moe_kv_read", "moe_kv_attention_workspace_bytes", "moe_kv_attention",
+    "moe_norm_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd", "moe_decode_workspace_bytes", "moe_decode",
+    "moe_decode_i8_workspace_bytes", "moe_decode_i8", "moe_sample_workspace_bytes", "moe_sample",
     "moe_trace_enable", "moe_trace_read", "moe_trace_name",
     "moe_last_error", "moe_version",
 )
@@ -96,6 +102,14 @@ class MoeKvAttn(ctypes.Structure):
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
+class MoeNormDims(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("flags", ctypes.c_uint32), ("eps", ctypes.c_float)]
+
+
+class MoeSampleDims(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("V", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
 class MoeError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{msg} (code {code})")
@@ -122,6 +136,7 @@ def lib() -> ctypes.CDLL:
     I, I64 = ctypes.c_int32, ctypes.c_int64
     QD, QW = ctypes.POINTER(MoeI8Dims), ctypes.POINTER(MoeI8Experts)
     KC, KB, KA = ctypes.POINTER(MoeKvCache), ctypes.POINTER(MoeKvBatch), ctypes.POINTER(MoeKvAttn)
+    ND, SD = ctypes.POINTER(MoeNormDims), ctypes.POINTER(MoeSampleDims)
     sig = {
         "moe_saved_bytes": (S, [D]),
         "moe_fwd_workspace_bytes": (S, [D]),
@@ -156,6 +171,15 @@ def lib() -> ctypes.CDLL:
         "moe_kv_read": (ctypes.c_int, [KC, I, I, P, P, I, P, P, P]),
         "moe_kv_attention_workspace_bytes": (S, [KC, KB, KA]),
         "moe_kv_attention": (ctypes.c_int, [KC, KB, KA, P, I64, P, I64, P, S, P]),
+        "moe_norm_fwd": (ctypes.c_int, [ND, P, I64, P, I64, P, P, P, P, P, P]),
+        "moe_norm_bwd_workspace_bytes": (S, [ND]),
+        "moe_norm_bwd": (ctypes.c_int, [ND, P, I64, P, P, I64, P, I64, P, P, P, S, P]),
+        "moe_decode_workspace_bytes": (S, [D]),
+        "moe_decode": (ctypes.c_int, [D, P, P, P, P, P, P, P, P, S, P]),
+        "moe_decode_i8_workspace_bytes": (S, [D]),
+        "moe_decode_i8": (ctypes.c_int, [D, P, P, QW, P, P, P, S, P]),
+        "moe_sample_workspace_bytes": (S, [SD]),
+        "moe_sample": (ctypes.c_int, [SD, P, I64, P, P, P, P, P, P, P, P, S, P]),
         "moe_trace_enable": (ctypes.c_int, [ctypes.c_int]),
         "moe_trace_read": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double),
                                           ctypes.POINTER(ctypes.c_int32), ctypes.c_int]),

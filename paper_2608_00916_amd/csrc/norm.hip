@@ -1,0 +1,328 @@
+// Sum of a row with the residual, its root-mean-square norm in bf16 and in
+// int8 rows, and the backward.  Memory bounds all of it: every value is read
+// once into registers, reduced there, and written once.
+//
+//   h = bf16(x + r),  s = (mean h^2 + eps)^(-1/2),  y = h s w
+//
+// The norm is that of the sum as it is stored, so that the backward, which has
+// the stored one, differentiates exactly what the forward computed.  Sums,
+// statistics and products are fp32; the int8 rows are those of the fp32
+// product, which meets no bf16 on its way.
+#include <algorithm>
+
+#include "i8_round.hpp"
+#include "step.hpp"
+#include "trace.hpp"
+
+namespace moe {
+
+namespace {
+
+__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+  f[0] = lo_bf(v.x), f[1] = hi_bf(v.x), f[2] = lo_bf(v.y), f[3] = hi_bf(v.y);
+  f[4] = lo_bf(v.z), f[5] = hi_bf(v.z), f[6] = lo_bf(v.w), f[7] = hi_bf(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// A row belongs to WAVES waves, VEC 16-byte vectors per lane, so a row of up
+// to 2048 columns is one wave's (no barrier), one of up to 8192 four waves'
+// and the longest, 32768, sixteen waves'.
+template <int WAVES>
+constexpr int kRowThreads = WAVES * kWave;
+// Waves of a workgroup: several rows where a row is one wave's.
+template <int WAVES>
+constexpr int kFwdRows = WAVES == 1 ? 4 : 1;
+template <int WAVES>
+constexpr int kBwdRows = WAVES == 1 ? 8 : WAVES == 4 ? 2 : 1;
+
+// Sum (or largest) over a row's waves; every lane gets it.  `red` is this
+// row's and this call's own, so no barrier follows the read.
+template <int WAVES>
+__device__ __forceinline__ float row_sum(float v, float* red, int wave) {
+  v = wave_sum(v);
+  if constexpr (WAVES == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[wave] = v;
+  __syncthreads();
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) t += red[i];
+  return t;
+}
+template <int WAVES>
+__device__ __forceinline__ uint32_t row_umax(uint32_t v, uint32_t* red, int wave) {
+  v = wave_umax(v);
+  if constexpr (WAVES == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[wave] = v;
+  __syncthreads();
+  uint32_t t = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) t = max(t, red[i]);
+  return t;
+}
+
+template <int WAVES, int VEC>
+__global__ __launch_bounds__(kRowThreads<WAVES>* kFwdRows<WAVES>) void k_norm_fwd(NormFwd a) {
+  __shared__ float sums[WAVES];
+  __shared__ uint32_t tops[WAVES];
+  const int in_row = threadIdx.x % kRowThreads<WAVES>, wave = in_row >> 6;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kFwdRows<WAVES> + threadIdx.x / kRowThreads<WAVES>;
+  if (row >= a.T) return;  // whole waves, and only where a row is one wave's
+  const int H = a.H;
+  uint4 held[VEC];
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+    held[i] = c < H ? *reinterpret_cast<const uint4*>(a.x + row * a.ldx + c) : make_uint4(0, 0, 0, 0);
+  }
+  if (a.r != nullptr) {
+    uint4 res[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+      res[i] = c < H ? *reinterpret_cast<const uint4*>(a.r + row * a.ldr + c) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      float f[8], g[8];
+      unpack8(held[i], f);
+      unpack8(res[i], g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] += g[j];
+      held[i] = pack8(f);
+      const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+      if (a.h != nullptr && c < H) *reinterpret_cast<uint4*>(a.h + row * H + c) = held[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    float f[8];
+    unpack8(held[i], f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq = fmaf(f[j], f[j], sq);
+  }
+  uint4 wv[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+    wv[i] = c < H ? *reinterpret_cast<const uint4*>(a.w + c) : make_uint4(0, 0, 0, 0);
+  }
+  const float s = 1.0f / sqrtf(row_sum<WAVES>(sq, sums, wave) / static_cast<float>(H) + a.eps);
+  float v[VEC][8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    float f[8], w[8];
+    unpack8(held[i], f);
+    unpack8(wv[i], w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[i][j] = f[j] * s * w[j];
+      top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    }
+    const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+    if (a.y != nullptr && c < H) *reinterpret_cast<uint4*>(a.y + row * H + c) = pack8(v[i]);
+  }
+  if (a.q == nullptr) return;
+  const Rounder r(row_umax<WAVES>(top, tops, wave));
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int c = (i * kRowThreads<WAVES> + in_row) * 8;
+    if (c < H)
+      *reinterpret_cast<uint2*>(a.q + row * H + c) =
+          make_uint2(pack4(r(v[i][0]), r(v[i][1]), r(v[i][2]), r(v[i][3])),
+                     pack4(r(v[i][4]), r(v[i][5]), r(v[i][6]), r(v[i][7])));
+  }
+  if (in_row == 0) a.scale[row] = r.scale;
+}
+
+// Backward.  With n = h s and g = dy w,
+//   dx = s (g - n mean(g n)) + dh,   dw = sum_t dy n.
+// Both means of a row come from one pass over its registers.  A workgroup
+// takes rows blockIdx.x, + gridDim.x, ... (times its rows at a time) and keeps
+// its share of dw in registers; the shares are added in a fixed order by
+// k_norm_dw, so dw does not depend on timing.
+template <int WAVES, int VEC>
+__global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bwd(NormBwd a) {
+  constexpr int ROWS = kBwdRows<WAVES>, RT = kRowThreads<WAVES>;
+  __shared__ float2 sums[2][ROWS][WAVES];
+  extern __shared__ float dws[];  // H floats where a workgroup has more than one row at a time
+  const int in_row = threadIdx.x % RT, wave = in_row >> 6, slot = threadIdx.x / RT;
+  const int H = a.H;
+  const float inv_h = 1.0f / static_cast<float>(H);
+  float acc[VEC][8];
+  uint4 wv[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int c = (i * RT + in_row) * 8;
+    wv[i] = c < H ? *reinterpret_cast<const uint4*>(a.w + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = 0.0f;
+  }
+  int turn = 0;
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * ROWS; base < a.T; base += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const int64_t row = base + slot;
+    const bool on = row < a.T;  // the loop's trips are the workgroup's, its barrier is met by all
+    uint4 hv[VEC], dv[VEC], uv[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (i * RT + in_row) * 8;
+      const bool in = on && c < H;
+      hv[i] = in ? *reinterpret_cast<const uint4*>(a.h + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
+      dv[i] = in ? *reinterpret_cast<const uint4*>(a.dy + row * a.lddy + c) : make_uint4(0, 0, 0, 0);
+      uv[i] = in && a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
+    }
+    float sq = 0.0f, gh = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      float h[8], d[8], w[8];
+      unpack8(hv[i], h);
+      unpack8(dv[i], d);
+      unpack8(wv[i], w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sq = fmaf(h[j], h[j], sq);
+        gh = fmaf(d[j] * w[j], h[j], gh);
+      }
+    }
+    sq = wave_sum(sq);
+    gh = wave_sum(gh);
+    if constexpr (WAVES > 1) {
+      // two sets of sums in turn: a set is written again only after the other's barrier
+      if ((threadIdx.x & 63) == 0) sums[turn][slot][wave] = make_float2(sq, gh);
+      __syncthreads();
+      sq = gh = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        sq += sums[turn][slot][i].x;
+        gh += sums[turn][slot][i].y;
+      }
+      turn ^= 1;
+    }
+    const float s = 1.0f / sqrtf(sq * inv_h + a.eps);
+    const float c1 = gh * inv_h * s * s;  // mean(g n) s: what a unit of h takes off g
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (i * RT + in_row) * 8;
+      if (!on || c >= H) continue;
+      float h[8], d[8], w[8], u[8];
+      unpack8(hv[i], h);
+      unpack8(dv[i], d);
+      unpack8(wv[i], w);
+      unpack8(uv[i], u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        acc[i][j] = fmaf(d[j], h[j] * s, acc[i][j]);
+        u[j] = fmaf(s, fmaf(-h[j], c1, d[j] * w[j]), u[j]);
+      }
+      *reinterpret_cast<uint4*>(a.dx + row * H + c) = pack8(u);
+    }
+  }
+  float* part = a.part + static_cast<int64_t>(blockIdx.x) * H;
+  if constexpr (ROWS > 1) {
+    for (int k = 0; k < ROWS; ++k) {  // the rows' shares one after another
+      if (k > 0) __syncthreads();
+      if (slot != k) continue;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int c = (i * RT + in_row) * 8;
+        if (c >= H) continue;
+        float* at = k + 1 < ROWS ? dws + c : part + c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) at[j] = k == 0 ? acc[i][j] : dws[c + j] + acc[i][j];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (i * RT + in_row) * 8;
+      if (c >= H) continue;
+      *reinterpret_cast<float4*>(part + c) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      *reinterpret_cast<float4*>(part + c + 4) = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+    }
+  }
+}
+
+// dw[c] = sum of the workgroups' shares: 16 runs of them, each in order, then
+// the runs in order.
+__global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ part, int n, int H, void* __restrict__ dw,
+                                                  bool fp32) {
+  __shared__ float red[16][64];
+  const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane;
+  const int per = cdiv(n, 16), first = run * per, last = min(n, first + per);
+  float t = 0.0f;
+  if (c < H) {
+#pragma unroll 8
+    for (int i = first; i < last; ++i) t += part[static_cast<int64_t>(i) * H + c];
+  }
+  red[run][lane] = t;
+  __syncthreads();
+  if (run != 0 || c >= H) return;
+  t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t += red[i][lane];
+  if (fp32) static_cast<float*>(dw)[c] = t;
+  else static_cast<bf16_t*>(dw)[c] = f2bf(t);
+}
+
+// Waves of a row by its length.
+int row_waves(int H) { return H <= 2048 ? 1 : H <= 8192 ? 4 : 16; }
+
+template <int WAVES, int VEC>
+void start_fwd(const NormFwd& a, hipStream_t s) {
+  constexpr int rows = kFwdRows<WAVES>;
+  hipLaunchKernelGGL((k_norm_fwd<WAVES, VEC>), dim3(cdiv(a.T, rows)), dim3(kRowThreads<WAVES> * rows), 0, s, a);
+}
+template <int WAVES, int VEC>
+void start_bwd(const NormBwd& a, hipStream_t s) {
+  constexpr int rows = kBwdRows<WAVES>;
+  hipLaunchKernelGGL((k_norm_bwd<WAVES, VEC>), dim3(norm_bwd_parts(a.T, a.H)), dim3(kRowThreads<WAVES> * rows),
+                     rows > 1 ? a.H * sizeof(float) : 0, s, a);
+}
+
+}  // namespace
+
+#define MOE_NORM_ROWS(START, A, S)                                 \
+  do {                                                             \
+    const int waves = row_waves((A).H), vec = cdiv((A).H, waves * 512); \
+    if (waves == 1) {                                              \
+      if (vec == 1) START<1, 1>(A, S);                             \
+      else if (vec == 2) START<1, 2>(A, S);                        \
+      else if (vec == 3) START<1, 3>(A, S);                        \
+      else START<1, 4>(A, S);                                      \
+    } else if (waves == 4) {                                       \
+      if (vec == 2) START<4, 2>(A, S);                             \
+      else if (vec == 3) START<4, 3>(A, S);                        \
+      else START<4, 4>(A, S);                                      \
+    } else {                                                       \
+      if (vec == 2) START<16, 2>(A, S);                            \
+      else if (vec == 3) START<16, 3>(A, S);                       \
+      else START<16, 4>(A, S);                                     \
+    }                                                              \
+  } while (0)
+
+hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t s) {
+  TraceScope trace_scope(K_NORM_FWD, s);
+  MOE_NORM_ROWS(start_fwd, a, s);
+  return hipGetLastError();
+}
+
+// Workgroups of the backward, hence shares of dw: enough to fill the chip, few
+// enough that adding them costs little.
+int norm_bwd_parts(int T, int H) {
+  const int waves = row_waves(H), rows = waves == 1 ? kBwdRows<1> : waves == 4 ? kBwdRows<4> : kBwdRows<16>;
+  return std::min(cdiv(T, rows), 512);
+}
+
+hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s) {
+  TraceScope trace_scope(K_NORM_BWD, s);
+  MOE_NORM_ROWS(start_bwd, a, s);
+  hipLaunchKernelGGL(k_norm_dw, dim3(cdiv(a.H, 64)), dim3(1024), 0, s, a.part, norm_bwd_parts(a.T, a.H), a.H, a.dw,
+                     a.dw_fp32);
+  return hipGetLastError();
+}
+
+}  // namespace moe

@@ -1,0 +1,76 @@
+// Internal launchers of a decoding step's kernels around attention and the
+// products: norms, the expert layer for a few tokens, token sampling (host
+// side).  Not part of the C ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.hpp"
+#include "moe.h"
+
+namespace moe {
+
+// ---- residual sum and root-mean-square norm (norm.hip)
+struct NormFwd {
+  const bf16_t *x, *r;  // r null: no residual
+  int64_t ldx, ldr;
+  const bf16_t* w;
+  bf16_t *h, *y;  // either may be null
+  int8_t* q;      // may be null
+  float* scale;
+  int T, H;
+  float eps;
+};
+hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t s);
+
+struct NormBwd {
+  const bf16_t *h, *dy, *dh;  // dh null: no gradient of the sum from elsewhere
+  int64_t ldh, lddy, lddh;
+  const bf16_t* w;
+  bf16_t* dx;
+  void* dw;  // fp32 or bf16
+  bool dw_fp32;
+  float* part;  // norm_bwd_parts(T, H) rows of H
+  int T, H;
+  float eps;
+};
+int norm_bwd_parts(int T, int H);
+hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s);
+
+// ---- the expert layer for a few tokens (decode.hip)
+constexpr int kDecodeMaxT = MOE_DECODE_MAX_T;
+
+// Routing of T <= kDecodeMaxT tokens: topk_idx, gates [T, k], counts [E].  A
+// routed row is named by its slot t k + j.
+struct DecodeRows {
+  const int32_t *topk_idx, *counts;
+  int T, H, E, F, k;
+};
+// a [T k, F] = SwiGLU of the slots' tokens through their experts.
+hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,
+                                bf16_t* a, hipStream_t s);
+hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const float* sx, const moe_i8_experts& w,
+                                   float* a, hipStream_t s);
+// o [T k, H] = a W_down.
+hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const bf16_t* w_down, float* o, hipStream_t s);
+hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, const moe_i8_experts& w, float* o, hipStream_t s);
+// y [T, H] = sum_j gates o.
+hipError_t launch_decode_combine(const DecodeRows& r, const float* gates, const float* o, bf16_t* y, hipStream_t s);
+
+// ---- token sampling (sample.hip)
+struct SampleArgs {
+  const void* logits;
+  int64_t ld;
+  bool fp32;
+  int B, V;
+  const float *temperature, *top_p, *min_p;  // any may be null: off
+  const int32_t* top_k;
+  const float* u;
+  int32_t* token;
+  float* logprob;  // may be null
+};
+size_t sample_ws(int B, int V);
+hipError_t launch_sample(const SampleArgs& a, void* ws, hipStream_t s);
+
+}  // namespace moe

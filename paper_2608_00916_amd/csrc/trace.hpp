@@ -42,6 +42,12 @@ enum KernelId {
   K_KV_READ,
   K_KV_ATTENTION,
   K_KV_COMBINE,
+  K_NORM_FWD,
+  K_NORM_BWD,
+  K_DECODE_GATEUP,
+  K_DECODE_DOWN,
+  K_DECODE_COMBINE,
+  K_SAMPLE,
   K_NUM_KERNELS
 };
 

@@ -1,0 +1,528 @@
+"""GPU tests of a decoding step's operators against plain 64-bit forms.
+
+Tolerances, from the formats.  A bf16 output is off by 2^-8 of itself (half a
+step).  A row's sum of squares takes at most 32 additions per lane and 16 over
+lanes and waves, 2^-24 each, so the factor 1 / rms is off by under 2^-18; dw
+sums at most 100 terms in a row, 2^-17.  An int8 row's value is off by half its
+scale.  The expert layer's activation is rounded to bf16 (2^-8 of each) between
+the products; its int8 form is held as in the other 8-bit tests (0.6% of the
+output's norm).  A token is exact; its log probability is rounded to fp32, and
+the weights behind it are held to 2^-43 each."""
+import numpy as np
+import pytest
+
+from tests import step_ref as R
+
+pytestmark = pytest.mark.gpu
+
+BF, SUM = 2.0 ** -8, 2.0 ** -17
+SLACK = 1.02
+
+
+def gen(seed):
+    return np.random.default_rng(seed)
+
+
+def bf16(x):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda().to(torch.bfloat16)
+
+
+def dev(x, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def near(got, want, tol, what):
+    err = np.abs(host(got) - want)
+    bad = ~(err <= tol)
+    assert not bad.any(), (what, float((err / np.maximum(tol, 1e-300)).max()), int(bad.sum()))
+
+
+# ------------------------------------------------------------------ norms
+LENGTHS = [(1, 16), (1, 2048), (5, 128), (130, 640), (3, 1024), (2, 1552), (7, 2064), (2, 5120), (3, 8192), (2, 8208),
+           (1, 17536), (2, 32768), (4097, 512)]
+
+
+def check_int8(q, scale, v, what):
+    top = np.abs(v).max(-1)
+    near(scale, top / 127, SUM * top / 127, what + " scale")
+    near(q.double() * scale.double()[:, None], v, 0.5 * SLACK * top[:, None] / 127 + 2 * SUM * np.abs(v), what)
+
+
+@pytest.mark.parametrize("T,H", LENGTHS)
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm(T, H, residual):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm", T, H, residual)
+    g = gen(T + H)
+    x, r = bf16(g.standard_normal((T, H))), bf16(2 * g.standard_normal((T, H)))
+    x[:, ::7] *= 30
+    w = bf16(1 + 0.2 * g.standard_normal(H))
+    op = moe.RMSNorm(T, w, eps=1e-5, out="both")
+    h, y, q, scale = op.forward(x, r if residual else None)
+    stored = (x.float() + r.float()).bfloat16() if residual else x
+    assert (h is None) != residual
+    if residual:
+        assert torch.equal(h, stored)
+    v, _ = R.norm(host(stored), host(w), 1e-5)
+    near(y, v, (BF + SUM) * np.abs(v), "y")
+    check_int8(q, scale, v, "q")
+    # one output alone, fewer rows, the same bits
+    for out in ("bf16", "i8"):
+        one = moe.RMSNorm(T + 3, w, eps=1e-5, out=out).forward(x, r if residual else None)
+        for a, b in zip(one, (h, y if out == "bf16" else None, q if out == "i8" else None, scale if out == "i8" else None)):
+            assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+
+
+def test_norm_strides_and_places():
+    """Rows apart, and sums and norms written over their inputs."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm strides")
+    g = gen(3)
+    for H in (264, 4104):
+        big = bf16(g.standard_normal((9, 3, H)))
+        x, r = big[:, 1], big[:, 2]
+        w = bf16(g.standard_normal(H))
+        d = moe.norm_dims(9, H)
+        h, y = (torch.empty((9, H), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        moe.moe_norm_fwd(d, x, r, w, h=h, y=y)
+        v, _ = R.norm(host((x.float() + r.float()).bfloat16()), host(w), 1e-6)
+        near(y, v, (BF + SUM) * np.abs(v), "strided")
+        a, b = x.contiguous(), r.contiguous()
+        moe.moe_norm_fwd(d, a, b, w, h=b, y=a)
+        assert torch.equal(a, y) and torch.equal(b, h)
+        a = x.contiguous()
+        moe.moe_norm_fwd(d, a, None, w, y=a)
+        moe.moe_norm_fwd(d, x, None, w, y=y)
+        assert torch.equal(a, y)
+
+
+@pytest.mark.parametrize("H", [64, 4096])
+def test_norm_extremes(H):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm extremes", H)
+    x = torch.ones((6, H), dtype=torch.bfloat16, device="cuda")
+    x[0] = 0
+    x[1, 3] = float("inf")
+    x[2, 5] = float("nan")
+    x[3] = 1e-30
+    x[4] = 1e15
+    w = torch.full((H,), 2.0, dtype=torch.bfloat16, device="cuda")
+    _, y, q, scale = moe.RMSNorm(6, w, eps=1e-6, out="both").forward(x)
+    y, q, scale = host(y), host(q), host(scale)
+    assert (y[0] == 0).all() and (q[0] == 0).all() and scale[0] == 0
+    assert np.isnan(y[1, 3]) and (np.delete(y[1], 3) == 0).all()
+    assert np.isnan(y[2]).all()
+    assert np.isnan(scale[1]) and np.isnan(scale[2]) and (q[1:3] == 0).all()
+    assert np.allclose(y[3], 2e-30 / 1e-3, rtol=2 * BF) and (q[3:] == 127).all()
+    assert (y[4] == 2).all() and (y[5] == 2).all() and np.allclose(scale[4:], 2 / 127, rtol=1e-5)
+
+
+@pytest.mark.parametrize("T,H,dh,fp32", [(1, 8, True, True), (2, 136, False, False), (300, 640, False, False),
+                                         (513, 2048, True, True), (65, 2056, True, False), (33, 8192, False, True),
+                                         (9, 8200, True, True), (5, 20000, True, False), (4, 32768, False, True),
+                                         (5000, 256, True, True), (1025, 1024, True, True), (700, 1536, True, True)])
+def test_norm_backward(T, H, dh, fp32):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm backward", T, H, dh, fp32)
+    g = gen(T * H)
+    h, dy, u = (bf16(g.standard_normal((T, H))) for _ in range(3))
+    w = bf16(1 + 0.2 * g.standard_normal(H))
+    op = moe.RMSNorm(T, w, eps=1e-5, dw_fp32=fp32, backward=True)
+    dx, dw = op.backward(h, dy, u if dh else None)
+    rx, rw, mx, mw = R.norm_bwd(host(h), host(w), host(dy), host(u) if dh else 0.0, 1e-5)
+    near(dx, rx, BF * np.abs(rx) + 4 * SUM * mx, "dx")
+    near(dw, rw, (0 if fp32 else BF) * np.abs(rw) + 2 * SUM * mw, "dw")
+    a, b = dx.clone(), dw.clone()
+    dx, dw = op.backward(h, dy, u if dh else None)
+    assert torch.equal(a, dx) and torch.equal(b, dw)
+    if dh:  # in place, and from rows apart
+        d = moe.norm_dims(T, H, 1e-5, fp32)
+        wide = torch.stack([h, dy, u], 1)
+        out = u.clone()
+        moe.moe_norm_bwd(d, wide[:, 0], w, wide[:, 1], out, out, dw, op.ws)
+        assert torch.equal(out, a) and torch.equal(dw, b)
+
+
+def test_norm_backward_against_differences():
+    """The kernels' gradients against differences of the 64-bit norm along random directions."""
+    import paper_2608_00916_amd as moe
+    say("norm differences")
+    T, H, eps = 7, 768, 1e-5
+    g = gen(11)
+    h, dy, u, w = (bf16(g.standard_normal(s)) for s in ((T, H), (T, H), (T, H), (H,)))
+    dx, dw = moe.RMSNorm(T, w, eps=eps, dw_fp32=True, backward=True).backward(h, dy, u)
+    H0, W0, D, U = host(h), host(w), host(dy), host(u)
+
+    def loss(h, w):
+        return (R.norm(h, w, eps)[0] * D).sum() + (h * U).sum()
+
+    for i in range(4):
+        a, b = g.standard_normal((T, H)), g.standard_normal(H)
+        diff = (loss(H0 + 1e-5 * a, W0 + 1e-5 * b) - loss(H0 - 1e-5 * a, W0 - 1e-5 * b)) / 2e-5
+        got = (host(dx) * a).sum() + (host(dw) * b).sum()
+        # each dx is off by 2^-8 of itself at most; the sums of squares of 1e-10 beside that do not count
+        assert abs(got - diff) <= SLACK * BF * (np.abs(host(dx)) * np.abs(a)).sum() + 1e-4
+
+
+# ------------------------------------------------------------------ the expert layer for a few tokens
+DECODE = [(1, 128, 8, 128, 1), (1, 2048, 128, 768, 8), (2, 256, 8, 384, 8), (16, 512, 16, 256, 2), (17, 384, 8, 128, 3),
+          (33, 128, 16, 640, 4), (64, 1152, 8, 128, 8), (64, 128, 256, 128, 6), (5, 4096, 8, 1280, 2), (3, 256, 32, 2176, 32),
+          (31, 640, 40, 384, 5)]
+
+
+def layer(T, H, E, F, k, seed=0):
+    """Tokens whose selection is clear, and weights; (tensors, host copies)."""
+    g = gen(T + H + E + F + k + seed)
+    w_r = bf16(0.1 * g.standard_normal((H, E)))
+    x = bf16(g.standard_normal((2 * T + 8, H)))
+    idx, gates, gap = R.route(host(x), host(w_r), k)
+    at = np.nonzero(gap > 1e-3)[0][:T]
+    assert len(at) == T
+    # equal gates' order does not matter: y sums over the slots
+    t = dict(x=x[at].contiguous(), w_r=w_r)
+    for n, (K, N) in dict(w_gate=(H, F), w_up=(H, F), w_down=(F, H)).items():
+        t[n] = bf16(g.standard_normal((E, K, N)) * K ** -0.5)
+    return t, idx[at], gates[at]
+
+
+def eight(t):
+    """The weights in int8: (descriptor, what they stand for)."""
+    import paper_2608_00916_amd as moe
+    q = [moe.moe_i8_quant_weight(t[n]) for n in ("w_gate", "w_up", "w_down")]
+    stand = [(a.double() * s.double()[..., None]).transpose(1, 2) for a, s in q]
+    return moe.i8_weights(*(p for m in q for p in m)), stand
+
+
+def check_layer(y, t, idx, gates, stand=None, on=None):
+    x = host(t["x"])
+    if on is not None:
+        gates = gates * on[:, None]
+    if stand is None:
+        want, mag = R.experts(x, idx, gates, lambda e: [host(t[n][e]) for n in ("w_gate", "w_up", "w_down")])
+        near(y, want, SLACK * BF * (mag + np.abs(want)), "y")
+        rel = 2 * BF
+    else:
+        want, _ = R.experts(x, idx, gates, lambda e: [host(s[e]) for s in stand], i8=True)
+        rel = 0.006 + BF
+    if np.linalg.norm(want) > 0:
+        assert np.linalg.norm(host(y) - want) <= rel * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("T,H,E,F,k", DECODE)
+def test_decode(T, H, E, F, k):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode", T, H, E, F, k)
+    t, idx, gates = layer(T, H, E, F, k)
+    args = [t[n] for n in ("w_r", "w_gate", "w_up", "w_down")]
+    op = moe.MoEDecode(T, H, E, F, k)
+    y = op.forward(t["x"], *args).clone()
+    check_layer(y, t, idx, gates)
+    assert torch.equal(op.forward(t["x"], *args), y)
+    # beside moe_infer, which rounds G, U, A and O to bf16 on its way
+    z = moe.MoEInfer(T, H, E, F, k).forward(t["x"], *args)
+    assert float((y.float() - z.float()).norm() / z.float().norm()) < 5 * BF
+    # a token's output does not depend on the tokens beside it beyond the tiles' order
+    one = moe.MoEDecode(T + 1 if T < 64 else T, H, E, F, k).forward(t["x"][-1:], *args)
+    assert float((one.float() - y[-1:].float()).norm() / y[-1:].float().norm()) < 2 * BF
+
+
+@pytest.mark.parametrize("T,H,E,F,k", DECODE)
+def test_decode_i8(T, H, E, F, k):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode i8", T, H, E, F, k)
+    t, idx, gates = layer(T, H, E, F, k)
+    w, stand = eight(t)
+    op = moe.MoEDecodeI8(T, H, E, F, k)
+    y = op.forward(t["x"], t["w_r"], w).clone()
+    check_layer(y, t, idx, gates, stand)
+    assert torch.equal(op.forward(t["x"], t["w_r"], w), y)
+    z = moe.MoEInferI8(T, H, E, F, k).forward(t["x"], t["w_r"], w)
+    assert float((y.float() - z.float()).norm() / z.float().norm()) < 0.006 + 2 * BF
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("on", [[1, 0, 1, 1, 0], [0] * 5, [0] * 4 + [1], [1] * 20 + [0] * 20 + [1]])
+def test_decode_masks(i8, on):
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode masks", i8, on)
+    T = len(on)
+    t, idx, gates = layer(T, 256, 16, 128, 4)
+    on = np.array(on)
+    for dtype in (torch.uint8, torch.bool):
+        mask = dev(on).to(dtype)
+        if i8:
+            w, stand = eight(t)
+            y = moe.MoEDecodeI8(T, 256, 16, 128, 4, mask=True).forward(t["x"], t["w_r"], w, mask)
+        else:
+            stand = None
+            op = moe.MoEDecode(T, 256, 16, 128, 4, mask=True)
+            y = op.forward(t["x"], *(t[n] for n in ("w_r", "w_gate", "w_up", "w_down")), mask)
+        check_layer(y, t, idx, gates, stand, on)
+        assert (host(y)[on == 0] == 0).all()
+
+
+def test_decode_far_weights():
+    """Experts past 2^32 bytes of a matrix: the last ones are picked."""
+    import torch
+    import paper_2608_00916_amd as moe
+    T, H, E, F, k = 2, 16384, 16, 8320, 2
+    say("decode far", H, E, F)
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def normal(*shape, std=1.0):
+        return torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(0, std, generator=g)
+
+    x = normal(T, H)
+    w_r = torch.zeros((H, E), dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 1
+    w_r[0, 15], w_r[0, 14] = 3, 2
+    w = [normal(E, H, F, std=H ** -0.5), normal(E, H, F, std=H ** -0.5), normal(E, F, H, std=F ** -0.5)]
+    assert w[0][0].numel() * 14 * 2 > 2 ** 31
+    y = moe.MoEDecode(T, H, E, F, k).forward(x, w_r, *w)
+    gates = torch.softmax(torch.tensor([3.0, 2.0], dtype=torch.float64, device="cuda"), 0)
+    want = 0
+    for j, e in enumerate((15, 14)):
+        a, b = x.float() @ w[0][e].float(), x.float() @ w[1][e].float()
+        want = want + gates[j] * ((torch.nn.functional.silu(a) * b) @ w[2][e].float()).double()
+    assert float((y.double() - want).norm() / want.norm()) < 2 * BF
+
+
+# ------------------------------------------------------------------ sampling
+def rows_of(B, V, seed, fp32):
+    import torch
+    g = gen(seed)
+    x = 2.5 * g.standard_normal((B, V))
+    for b in range(B):
+        x[b, g.integers(0, V, 8)] += 8 * g.random(8)
+    t = dev(x.astype(np.float32))
+    return t if fp32 else t.to(torch.bfloat16)
+
+
+def check_tokens(logits, u, got, **settings):
+    token, logprob = got[0].cpu().numpy(), host(got[1])
+    rows, V = host(logits), logits.shape[1]
+    for b in range(len(rows)):
+        s = {n: (v[b].item() if n != "top_k" else int(v[b])) for n, v in settings.items() if v is not None}
+        i, lp = R.sample(rows[b], u[b].item(), **s)
+        assert token[b] == i, (b, token[b], i, s, u[b].item())
+        tol = 2.0 ** -24 * abs(lp) + V * 2.0 ** -43
+        assert logprob[b] == lp or abs(logprob[b] - lp) <= tol, (b, logprob[b], lp)
+
+
+VOCABS = [1, 2, 7, 1000, 4099, 16377, 16378, 50001, 131072]
+
+
+@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("fp32", [True, False])
+def test_sample(V, fp32):
+    import torch
+    import paper_2608_00916_amd as moe
+    B = 12
+    say("sample", V, fp32)
+    logits = rows_of(B, V, V, fp32)
+    g = gen(V + 1)
+    u = dev(g.random(B).astype(np.float32))
+    op = moe.Sampler(B + 1, V)
+    off = dict(temperature=None, top_k=None, top_p=None, min_p=None)
+    full = lambda v, dtype=np.float32: dev(np.full(B, v, dtype))  # noqa: E731
+    for s in (dict(), dict(temperature=full(0.0)), dict(temperature=full(0.7)), dict(top_k=full(1, np.int32)),
+              dict(top_k=full(50, np.int32), temperature=full(1.5)), dict(top_k=full(3000, np.int32)),
+              dict(top_p=full(0.9)), dict(top_p=full(0.0)), dict(top_p=full(0.999), temperature=full(2.0)),
+              dict(min_p=full(0.05)), dict(min_p=full(1.5)), dict(min_p=full(1e-6)),
+              dict(top_k=full(40, np.int32), top_p=full(0.8), min_p=full(0.02), temperature=full(0.9)),
+              dict(top_k=full(2500, np.int32), top_p=full(0.7)),
+              dict(temperature=dev(g.choice([0, 0.5, 1, 2], B).astype(np.float32)),
+                   top_k=dev(g.choice([-1, 0, 1, 5, 100, 1000, V, V + 5], B).astype(np.int32)),
+                   top_p=dev(g.choice([0.3, 0.95, 1, 1.5], B).astype(np.float32)),
+                   min_p=dev(g.choice([-1, 0, 0.01, 0.2], B).astype(np.float32)))):
+        say("  ", {n: v[:4].tolist() for n, v in s.items()})
+        check_tokens(logits, u, op.forward(logits, u, **{**off, **s}), **s)
+
+
+@pytest.mark.parametrize("V,pad,fp32", [(5, 6, True), (1001, 1002, False), (8193, 8200, True), (20011, 20012, False)])
+def test_sample_rows_apart(V, pad, fp32):
+    """Rows that do not begin on 16 bytes, with larger logits between them."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("sample strides", V, pad, fp32)
+    B = 9
+    wide = torch.full((B, pad), 100.0, device="cuda", dtype=torch.float32 if fp32 else torch.bfloat16)
+    wide[:, :V] = rows_of(B, V, V, fp32)
+    logits = wide[:, :V]
+    u = dev(gen(0).random(B).astype(np.float32))
+    op = moe.Sampler(B, V)
+    p = dev(np.full(B, 0.8, np.float32))
+    for s in (dict(), dict(top_p=p), dict(top_k=dev(np.full(B, 4, np.int32))), dict(temperature=0 * p)):
+        check_tokens(logits, u, op.forward(logits, u, **s), **s)
+
+
+def test_sample_equal_and_missing_logits():
+    import torch
+    import paper_2608_00916_amd as moe
+    say("sample ties and masks")
+    inf = float("inf")
+    for V in (100, 16000, 70000):
+        rows = np.zeros((10, V), np.float32)
+        rows[1, V // 2:] = -inf
+        rows[2] = -inf
+        rows[3] = -inf
+        rows[3, V - 1] = -3.4e38
+        rows[4] = np.nan
+        rows[5, 7] = inf
+        rows[5, V - 3] = inf
+        rows[5, 3] = np.nan
+        rows[6] = -3.4028235e38  # masked with the type's lowest value, all of it
+        rows[7] = -3.4028235e38
+        rows[7, 11] = 5.0
+        rows[8] = np.where(np.arange(V) % 3 == 0, 1.0, -inf)
+        rows[9] = 1e30 * np.where(np.arange(V) % 2 == 0, 1, -1)
+        logits = dev(rows)
+        B = len(rows)
+        u = dev(gen(V).random(B).astype(np.float32))
+        op = moe.Sampler(B, V)
+        half, k = dev(np.full(B, 0.5, np.float32)), dev(np.full(B, min(V - 1, 6000), np.int32))
+        for s in (dict(), dict(temperature=0 * half), dict(top_p=half), dict(top_k=k), dict(min_p=half),
+                  dict(top_k=k, top_p=half, min_p=half, temperature=half)):
+            say("  ", V, list(s))
+            check_tokens(logits, u, op.forward(logits, u, **s), **s)
+
+
+def test_sample_odd_settings():
+    """Numbers outside the settings' ranges mean what the header says."""
+    import paper_2608_00916_amd as moe
+    say("sample odd settings")
+    V, nan, inf = 3000, float("nan"), float("inf")
+    row = rows_of(1, V, 9, True)
+    cases = [(nan, 1.0, 0, 1.0, 0.0), (-1.0, 1.0, 0, 1.0, 0.0), (0.5, inf, 0, 1.0, 0.0), (0.5, nan, 0, 1.0, 0.0),
+             (0.5, -2.0, 0, 1.0, 0.0), (0.5, 1.0, -5, nan, nan), (0.5, 1.0, 10, -1.0, 7.0), (1.0, 1.0, 0, 1.0, 0.0),
+             (2.0, 1.0, 7, 0.9, 0.0), (inf, 1.0, 0, 0.5, 0.0), (0.3, 1e-30, 0, 0.9, 0.1), (0.3, 1e-42, 0, 1.0, 0.0)]
+    cols = list(zip(*cases))
+    u, t, p, m = (dev(np.array(cols[i], np.float32)) for i in (0, 1, 3, 4))
+    k = dev(np.array(cols[2], np.int32))
+    B = len(cases)
+    got = moe.Sampler(B, V).forward(row.expand(B, V).contiguous(), u, t, k, p, m)
+    r = host(row)[0]
+    for b, (uu, tt, kk, pp, mm) in enumerate(cases):
+        tt = 0.0 if np.isnan(tt) else float(np.float32(tt))
+        i, lp = R.sample(r, float(np.float32(uu)), tt, kk, 1.0 if np.isnan(pp) else float(np.float32(pp)), 0.0 if np.isnan(mm) else float(np.float32(mm)))
+        assert int(got[0][b]) == i, (b, cases[b])
+        assert abs(float(got[1][b]) - lp) <= 2.0 ** -24 * abs(lp) + V * 2.0 ** -43
+
+
+def test_sample_largest():
+    import paper_2608_00916_amd as moe
+    V = 1 << 20
+    say("sample largest", V)
+    logits = rows_of(3, V, 1, True)
+    logits[2] = 0.25
+    u = dev(np.array([0.3, 0.9999, 0.6], np.float32))
+    op = moe.Sampler(3, V)
+    p, k = dev(np.full(3, 0.4, np.float32)), dev(np.full(3, 500, np.int32))
+    for s in (dict(), dict(top_p=p), dict(top_k=k)):
+        check_tokens(logits, u, op.forward(logits, u, **s), **s)
+
+
+# ------------------------------------------------------------------ streams, graphs, together
+def test_step_on_a_stream_and_in_a_graph():
+    """Norm, expert layer, norm, head product and choice of the token as one step: on a
+    stream of its own, captured once and replayed with new inputs."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("step")
+    T, H, E, F, k, V = 6, 512, 16, 256, 4, 3001
+    t, _, _ = layer(T, H, E, F, k)
+    g = gen(2)
+    w = bf16(1 + 0.1 * g.standard_normal(H))
+    head, sh = moe.moe_i8_quant_weight(bf16(0.05 * g.standard_normal((H, V))))
+    w8, _ = eight(t)
+    n1, n2 = moe.RMSNorm(T, w), moe.RMSNorm(T, w, out="i8")
+    experts, experts8, sampler = moe.MoEDecode(T, H, E, F, k), moe.MoEDecodeI8(T, H, E, F, k), moe.Sampler(T, V)
+    logits = torch.empty((T, V), device="cuda")
+    temp, p = dev(np.full(T, 0.8, np.float32)), dev(np.full(T, 0.9, np.float32))
+    x, r, u = t["x"].clone(), t["x"].flip(0).contiguous(), dev(g.random(T).astype(np.float32))
+
+    def step():
+        h, y, _, _ = n1.forward(x, r)
+        e = experts.forward(y, t["w_r"], t["w_gate"], t["w_up"], t["w_down"])
+        _, _, q, s = n2.forward(e, h)
+        e8 = experts8.forward(y, t["w_r"], w8)
+        moe.moe_i8_matmul(q, s, head, sh, logits)
+        return (*sampler.forward(logits, u, temperature=temp, top_p=p), e, e8, logits)
+
+    want = [o.clone() for o in step()]
+    check_tokens(logits, u, want, temperature=temp, top_p=p)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(4):
+        x.copy_(bf16(g.standard_normal((T, H))))
+        u.copy_(dev(g.random(T).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [o.clone() for o in outs]
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, eager)), i
+
+
+def test_norms_train_around_the_block():
+    """A pre-norm layer's gradients: x -> x + block(norm(x)), through moe_fwd, moe_bwd and
+    the norm's backward, against 64-bit differences along random directions."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm and block")
+    T, H, E, F, k = 40, 128, 8, 128, 2
+    t, _, _ = layer(T, H, E, F, k, seed=3)
+    g = gen(8)
+    w = bf16(1 + 0.1 * g.standard_normal(H))
+    # tokens whose selection holds along the differences
+    x = t["x"]
+    n, blk = moe.RMSNorm(T, w, dw_fp32=True, backward=True), moe.MoEBlock(T, H, E, F, k)
+    args = [t[m] for m in ("w_r", "w_gate", "w_up", "w_down")]
+    _, y, _, _ = n.forward(x)
+    blk.forward(y, *args)
+    dout = bf16(g.standard_normal((T, H)))
+    dy = blk.backward(y, *args, dout)[0]
+    dx, dw = n.backward(x, dy, dout)
+    X, W, D = host(x), host(w), host(dout)
+    idx, _, gap = R.route(R.norm(X, W, 1e-6)[0], host(t["w_r"]), k)
+    assert gap.min() > 1e-3
+
+    def loss(x, w):
+        v, _ = R.norm(x, w, 1e-6)
+        z = np.take_along_axis(v @ host(t["w_r"]), idx, -1)
+        p = np.exp(z - z.max(-1, keepdims=True))
+        out, _ = R.experts(v, idx, p / p.sum(-1, keepdims=True), lambda e: [host(t[m][e]) for m in ("w_gate", "w_up", "w_down")])
+        return ((x + out) * D).sum()
+
+    for _ in range(3):
+        a, b = g.standard_normal((T, H)), g.standard_normal(H)
+        diff = (loss(X + 1e-5 * a, W + 1e-5 * b) - loss(X - 1e-5 * a, W - 1e-5 * b)) / 2e-5
+        got = (host(dx) * a).sum() + (host(dw) * b).sum()
+        # the block's gradients hold to 2e-2 of the largest; along a random direction errors add up in squares
+        size = np.linalg.norm(host(dx)) + np.linalg.norm(host(dw))
+        assert abs(got - diff) <= 2e-2 * 3 * size
