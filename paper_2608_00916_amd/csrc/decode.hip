@@ -1,9 +1,9 @@
 // The expert layer for a few tokens.  Reading the weights of the experts that
 // the tokens picked bounds it: at one token and top-8 of a 30B-A3B model 75 MB
 // in bf16 for 75 MFLOP.  So every weight goes from memory straight into the
-// registers of the one wave that multiplies it, in wide loads with many of
-// them in flight, and the K axis is split over a workgroup's waves until the
-// few (expert, columns) tiles fill the chip.
+// registers of the one wave that multiplies it, in whole 128-byte lines and
+// with as many of them in flight as registers hold, and the K axis is split
+// over a workgroup's waves until the (expert, columns) tiles fill the chip.
 //
 // A workgroup takes one used expert and a tile of columns, finds the expert's
 // rows (at most one per token) from the selection by itself, and multiplies
@@ -15,128 +15,256 @@
 #include "i8_core.hpp"
 #include "i8_round.hpp"
 #include "step.hpp"
+#include "topk.hpp"
 #include "trace.hpp"
 
 namespace moe {
 
 namespace {
 
-// The slots of the blockIdx.y-th used expert in token order; false where there
-// are fewer used experts.  One wave finds them; ends with a barrier.
-struct Rows {
-  int32_t slot[kDecodeMaxT];
-  int expert, n;
-};
-__device__ __forceinline__ bool find_rows(const DecodeRows& r, Rows& rows) {
-  if (threadIdx.x < kWave) {
-    const int lane = threadIdx.x;
-    int e = -1, before = 0;
-    const int want = blockIdx.y;
-    for (int m = 0; m < r.E; m += kWave) {
-      const unsigned long long used = __ballot(m + lane < r.E && r.counts[min(m + lane, r.E - 1)] > 0);
-      const int n = __popcll(used);
-      if (e < 0 && want < before + n) {
-        unsigned long long u = used;
-        for (int i = before; i < want; ++i) u &= u - 1ull;
-        e = m + __builtin_ctzll(u);
-      }
-      before += n;
+// ---- router
+// Logits in the router's own order of summation, so that the selection is
+// moe_infer's bit for bit: range s of K goes through the same instructions in
+// the same order into plane s of part [kRouterSplits, T, E].  A wave takes
+// one range, 32 experts and 16 tokens, its loads all issued ahead of the
+// products; the workgroup's four waves are the ranges.  Further workgroups
+// round the tokens to int8 rows (q null: none), work that needs no launch of its own.
+constexpr int kRouterCols = 32;
+__global__ __launch_bounds__(kRouterSplits* kWave) void k_decode_router(const bf16_t* __restrict__ x,
+                                                                        const bf16_t* __restrict__ w_r, int T, int H,
+                                                                        int E, float* __restrict__ part,
+                                                                        int32_t* __restrict__ counts,
+                                                                        int8_t* __restrict__ q, float* __restrict__ sx) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int cols = cdiv(E, kRouterCols), tiles = cols * cdiv(T, 16);
+  if (static_cast<int>(blockIdx.x) >= tiles) {  // a token's int8 row per wave
+    const int t = (blockIdx.x - tiles) * kRouterSplits + wave;
+    if (t >= T) return;
+    const bf16_t* src = x + static_cast<int64_t>(t) * H;
+    uint32_t m = 0;
+    for (int c = lane * 8; c < H; c += 512) m = max(m, top8(*reinterpret_cast<const uint4*>(src + c)));
+    const Rounder r(wave_umax(m));
+    for (int c = lane * 8; c < H; c += 512)
+      *reinterpret_cast<uint2*>(q + static_cast<int64_t>(t) * H + c) = quant8(*reinterpret_cast<const uint4*>(src + c), r);
+    if (lane == 0) sx[t] = r.scale;
+    return;
+  }
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < E; i += blockDim.x) counts[i] = 0;
+  const int e0 = blockIdx.x % cols * kRouterCols + (lane & 15) * 2, t = blockIdx.x / cols * 16 + (lane & 15);
+  const int quad = (lane >> 4) * 8;
+  const int range = router_range(H), k0 = min(H, wave * range), k1 = min(H, k0 + range);
+  const bool in_e = e0 < E, in_t = t < T;  // E is even
+  f32x4 acc[2] = {};
+  constexpr int U = 8;
+  for (int k = k0; k < k1; k += U * 32) {
+    uint32_t w[U][8];
+    uint4 xv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = k + u * 32 + quad;
+      const bool in = k + u * 32 < k1;
+      xv[u] = in && in_t ? *reinterpret_cast<const uint4*>(x + static_cast<int64_t>(t) * H + at) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        w[u][r] = in && in_e ? *reinterpret_cast<const uint32_t*>(w_r + static_cast<int64_t>(at + r) * E + e0) : 0u;
     }
-    int slot = -1;
-    if (e >= 0 && lane < r.T)
-      for (int j = 0; j < r.k; ++j)
-        if (r.topk_idx[lane * r.k + j] == e) slot = lane * r.k + j;
-    const unsigned long long has = __ballot(slot >= 0);
-    if (slot >= 0) rows.slot[__popcll(has & ((1ull << lane) - 1ull))] = slot;
-    if (lane == 0) {
-      rows.expert = e;
-      rows.n = __popcll(has);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k + u * 32 >= k1) break;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          c[i] = __builtin_amdgcn_perm(w[u][2 * i + 1], w[u][2 * i], p ? 0x07060302u : 0x05040100u);
+        acc[p] = mfma16x16x32(make_uint4(c[0], c[1], c[2], c[3]), xv[u], acc[p]);
+      }
     }
   }
+  // lane l holds experts 2 (4 (l / 16) + i) + p of the tile for token l % 16
+  if (!in_t) return;
+  float* out = part + (static_cast<int64_t>(wave) * T + t) * E;
+  const int first = blockIdx.x % cols * kRouterCols + 8 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (first + 2 * i < E) *reinterpret_cast<float2*>(out + first + 2 * i) = make_float2(acc[0][i], acc[1][i]);
+}
+
+// ---- which rows a workgroup has
+struct Rows {
+  int32_t slot[kDecodeMaxT];  // of the expert, in token order
+  int expert, n;
+};
+// The blockIdx.y-th used expert and its slots; one wave finds them.
+__device__ __forceinline__ void find_rows(const DecodeRows& r, const int32_t* counts, const int32_t* topk_idx, Rows& rows) {
+  const int lane = threadIdx.x;
+  if (r.T == 1) {  // the slots are the experts
+    if (lane == 0) {
+      rows.slot[0] = blockIdx.y;
+      rows.expert = topk_idx[blockIdx.y];
+      rows.n = 1;
+    }
+    return;
+  }
+  int e = -1, before = 0;
+  const int want = blockIdx.y;
+  for (int m = 0; m < r.E; m += kWave) {
+    const unsigned long long used = __ballot(m + lane < r.E && counts[min(m + lane, r.E - 1)] > 0);
+    const int n = __popcll(used);
+    if (e < 0 && want < before + n) {
+      unsigned long long u = used;
+      for (int i = before; i < want; ++i) u &= u - 1ull;
+      e = m + __builtin_ctzll(u);
+    }
+    before += n;
+  }
+  int slot = -1;
+  if (e >= 0 && lane < r.T)
+    for (int j = 0; j < r.k; ++j)
+      if (topk_idx[lane * r.k + j] == e) slot = lane * r.k + j;
+  const unsigned long long has = __ballot(slot >= 0);
+  if (slot >= 0) rows.slot[__popcll(has & ((1ull << lane) - 1ull))] = slot;
+  if (lane == 0) {
+    rows.expert = e;
+    rows.n = __popcll(has);
+  }
+}
+__device__ __forceinline__ bool read_rows(const DecodeRows& r, Rows& rows) {
+  if (threadIdx.x < kWave) find_rows(r, r.counts, r.topk_idx, rows);
   __syncthreads();
   return rows.expert >= 0;
 }
 
-// CW neighbouring bf16 of a weight row.
-template <int CW>
-struct Vec;
-template <>
-struct Vec<2> {
-  using T = uint32_t;
+// Selection of up to kFusedT tokens by every workgroup of the gate/up product
+// for itself, a wave per token, instead of a launch between the router and it;
+// the first workgroup leaves it for the launches after.
+constexpr int kFusedT = 8;
+struct Selection {
+  int32_t idx[kFusedT * MOE_MAX_TOPK];
+  float gates[kFusedT * MOE_MAX_TOPK];
+  int32_t counts[MOE_MAX_EXPERTS];
 };
-template <>
-struct Vec<4> {
-  using T = uint2;
-};
-__device__ __forceinline__ uint32_t word(uint32_t v, int) { return v; }
-__device__ __forceinline__ uint32_t word(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
+template <int PL>
+__device__ __forceinline__ void select_token(const DecodeRows& r, int t, Selection& sel) {
+  const int lane = threadIdx.x & 63;
+  float val[PL];
+  uint32_t key[PL];
+#pragma unroll
+  for (int m = 0; m < PL; ++m) {
+    const int e = lane + kWave * m;
+    float v[kRouterSplits];
+#pragma unroll
+    for (int s = 0; s < kRouterSplits; ++s) v[s] = e < r.E ? r.part[(static_cast<int64_t>(s) * r.T + t) * r.E + e] : 0.0f;
+    val[m] = v[0];
+#pragma unroll
+    for (int s = 1; s < kRouterSplits; ++s) val[m] += v[s];
+    key[m] = e < r.E ? max(order_key(val[m]), 1u) : 0u;
+  }
+  topk_select<PL>(val, key, r.k, lane, sel.idx + t * r.k, sel.gates + t * r.k, sel.counts);
+}
+__device__ __forceinline__ bool select_rows(const DecodeRows& r, Selection& sel, Rows& rows) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  for (int i = tid; i < r.E; i += blockDim.x) sel.counts[i] = 0;
+  __syncthreads();
+  for (int t = wave; t < r.T; t += blockDim.x / kWave) {
+    if (r.mask != nullptr && r.mask[t] == 0) {
+      if ((tid & 63) < r.k) {
+        sel.idx[t * r.k + (tid & 63)] = -1;
+        sel.gates[t * r.k + (tid & 63)] = 0.0f;
+      }
+    } else if (r.E <= kWave) {
+      select_token<1>(r, t, sel);
+    } else if (r.E <= 2 * kWave) {
+      select_token<2>(r, t, sel);
+    } else {
+      select_token<4>(r, t, sel);
+    }
+  }
+  __syncthreads();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+    for (int i = tid; i < r.T * r.k; i += blockDim.x) {
+      r.topk_idx[i] = sel.idx[i];
+      r.gates[i] = sel.gates[i];
+    }
+    for (int i = tid; i < r.E; i += blockDim.x) r.counts[i] = sel.counts[i];
+  }
+  if (tid < kWave) find_rows(r, sel.counts, sel.idx, rows);
+  __syncthreads();
+  return rows.expert >= 0;
+}
 
-// Two rows' bf16 at the same column (the low or the high half of a word) side by side.
-__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-
-// Eight consecutive K rows of a lane's CW columns -> the matrix instruction's
-// operand for column p of each lane: eight K values of one column.
-template <int CW>
-__device__ __forceinline__ uint4 column(const typename Vec<CW>::T (&v)[8], int p) {
+// ---- bf16 products
+// Eight K rows of a lane's four columns -> the matrix instruction's operand
+// for column p of each lane: eight K values of one column.
+__device__ __forceinline__ uint4 column(const uint2 (&v)[8], int p) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t a = word(v[2 * i], p >> 1), b = word(v[2 * i + 1], p >> 1);
-    w[i] = p & 1 ? highs(a, b) : lows(a, b);
+    const uint32_t a = p < 2 ? v[2 * i].x : v[2 * i].y, b = p < 2 ? v[2 * i + 1].x : v[2 * i + 1].y;
+    w[i] = __builtin_amdgcn_perm(b, a, p & 1 ? 0x07060302u : 0x05040100u);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ uint2 stream8(const bf16_t* p) {
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p)));
+}
 
-// Products of up to 16 NT rows (bf16, K-contiguous, row pitch K, row id
-// row_of[i]) with NB column-contiguous matrices [K, N] at columns c0 .. c0 +
-// 16 CW, the K axis split over the workgroup's WAVES waves, 32 at a time.
-// Lane l holds columns c0 + CW (l % 16) + p: a load of CW columns per lane
-// brings four rows of 32 CW bytes each.
-template <int NT, int CW, int NB, int WAVES, int U>
-__device__ __forceinline__ void few_rows(const bf16_t* __restrict__ x, const int (&row)[NT], const bf16_t* const (&b)[NB],
-                                         int K, int N, f32x4 (&acc)[NT][NB][CW]) {
-  using V = typename Vec<CW>::T;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Columns of a tile: lane l holds columns 4 (l % 16) + p, so a load of 8 bytes
+// a lane brings four rows of a whole 128-byte line.  Two columns a lane, half
+// lines, reached 3.2 TB/s where these reach 5.6 (16 tokens).
+constexpr int kCols = 64;
+
+// Products of 16 NT rows with NB column-contiguous matrices [K, N] at their
+// pointers' columns, steps s0, s0 + stride, ... < s1 of 32 k, U of them in
+// flight.  get(t, k, parts) gives the PARTS summands of row tile t's operand;
+// begin() comes after the first weights' loads and before the first get.
+template <int NT, int NB, int PARTS, int U, class Begin, class Get>
+__device__ __forceinline__ void few_rows(const bf16_t* const (&b)[NB], int N, int s0, int s1, int stride, Begin& begin,
+                                         const Get& get, f32x4 (&acc)[NT][NB][4]) {
+  const int lane = threadIdx.x & 63;
   const int quad = (lane >> 4) * 8;
-  const int steps = K / 32;
-  const int64_t col = (lane & 15) * CW;
-  auto batch = [&](int s0, auto count) {
+  const int64_t col = (lane & 15) * 4;
+  auto batch = [&](int s, auto count) {
     constexpr int n = decltype(count)::value;
-    V v[n][NB][8];
-    uint4 xv[n][NT];
+    uint2 v[n][NB][8];
+    uint4 xv[n][NT][PARTS];
 #pragma unroll
     for (int u = 0; u < n; ++u) {
-      const int k = (s0 + u * WAVES) * 32 + quad;
+      const int k = (s + u * stride) * 32 + quad;
 #pragma unroll
       for (int m = 0; m < NB; ++m)
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-          v[u][m][r] = *reinterpret_cast<const V*>(b[m] + static_cast<int64_t>(k + r) * N + col);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        xv[u][t] = row[t] >= 0 ? *reinterpret_cast<const uint4*>(x + static_cast<int64_t>(row[t]) * K + k) : make_uint4(0, 0, 0, 0);
+        for (int r = 0; r < 8; ++r) v[u][m][r] = stream8(b[m] + static_cast<int64_t>(k + r) * N + col);
     }
+    begin();
+#pragma unroll
+    for (int u = 0; u < n; ++u)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) get(t, (s + u * stride) * 32 + quad, xv[u][t]);
 #pragma unroll
     for (int u = 0; u < n; ++u)
 #pragma unroll
       for (int m = 0; m < NB; ++m)
 #pragma unroll
-        for (int p = 0; p < CW; ++p) {
-          const uint4 w = column<CW>(v[u][m], p);
+        for (int p = 0; p < 4; ++p) {
+          const uint4 w = column(v[u][m], p);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) acc[t][m][p] = mfma16x16x32(xv[u][t], w, acc[t][m][p]);
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) acc[t][m][p] = mfma16x16x32(xv[u][t][i], w, acc[t][m][p]);
         }
   };
-  int s = wave;
-  for (; s + (U - 1) * WAVES < steps; s += U * WAVES) batch(s, std::integral_constant<int, U>{});
-  for (; s < steps; s += WAVES) batch(s, std::integral_constant<int, 1>{});
+  int s = s0;
+  for (; s + (U - 1) * stride < s1; s += U * stride) batch(s, std::integral_constant<int, U>{});
+  for (; s < s1; s += stride) batch(s, std::integral_constant<int, 1>{});
 }
 
 // Sum over the waves of one row tile's products, which each holds per lane as
 // f32x4 (or i32x4): element i of lane l, fragment f.  `red` has
 // WAVES * FRAGS * 256 entries.
-template <int WAVES, int FRAGS, class V4, class S>
+template <int FRAGS, class V4, class S>
 __device__ __forceinline__ void put_parts(const V4 (&part)[FRAGS], S* red) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -149,232 +277,320 @@ __device__ __forceinline__ S sum_parts(const S* red, int f, int at) {
   for (int w = 0; w < WAVES; ++w) t += red[(w * FRAGS + f) * 256 + at];
   return t;
 }
+// Row and column (of 64, or of 16) of entry `at` of fragment p.
+__device__ __forceinline__ int entry_row(int at) { return 4 * (at >> 6) + (at & 3); }
+__device__ __forceinline__ int entry_lane(int at) { return (at >> 2) & 15; }
+
+// The activation as two bf16: the product with the second adds what the first
+// leaves out, so A enters the down product to 2^-17 of itself, at the price of
+// one more matrix instruction under the same weights.
+__device__ __forceinline__ void split_bf16(float v, bf16_t& hi, bf16_t& lo) {
+  hi = f2bf(v);
+  const float d = v - bf2f(hi);
+  lo = fabsf(d) < INFINITY ? f2bf(d) : 0;  // infinities and NaN are the first's alone
+}
 
 // Waves per workgroup: the gate/up product splits a long K (H), the down
 // product a shorter one (F).
 constexpr int kUpWaves = 8, kDownWaves = 4;
 
-template <int NT, int CW>
-__global__ __launch_bounds__(kUpWaves* kWave) void k_decode_gateup(DecodeRows r, const bf16_t* __restrict__ x,
-                                                                   const bf16_t* __restrict__ w_gate,
-                                                                   const bf16_t* __restrict__ w_up,
-                                                                   bf16_t* __restrict__ a) {
-  __shared__ Rows rows;
-  __shared__ float red[kUpWaves * 2 * CW * 256];
-  if (!find_rows(r, rows)) return;
-  const int lane = threadIdx.x & 63, n = rows.n;
-  int token[NT];
+// gridDim.z ranges of K: 1 where the tiles fill the chip, and the activation
+// is written; else a range's G and U are, and the down product adds them up.
+template <int NT>
+__device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ x,
+                                             const bf16_t* const (&b)[2], bf16_t* __restrict__ a, float* __restrict__ gu,
+                                             float* red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n;
+  const bf16_t* xr[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int i = t * 16 + (lane & 15);
-    token[t] = i < n ? rows.slot[i] / r.k : -1;
+    const int i = first + t * 16 + (lane & 15);
+    xr[t] = i < n ? x + static_cast<int64_t>(rows.slot[i] / r.k) * r.H : nullptr;
   }
-  const int64_t base = static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * (16 * CW);
-  const bf16_t* const b[2] = {w_gate + base, w_up + base};
-  f32x4 acc[NT][2][CW] = {};
-  few_rows<NT, CW, 2, kUpWaves, NT == 1 ? 4 / (CW / 2) : 2>(x, token, b, r.H, r.F, acc);
+  auto get = [&](int t, int k, uint4 (&v)[1]) {
+    v[0] = xr[t] != nullptr ? *reinterpret_cast<const uint4*>(xr[t] + k) : make_uint4(0, 0, 0, 0);
+  };
+  f32x4 acc[NT][2][4] = {};
+  auto begin = [] {};
+  few_rows<NT, 2, 1, NT == 1 ? 2 : 1>(b, r.F, blockIdx.z * kUpWaves + wave, r.H / 32, gridDim.z * kUpWaves, begin, get, acc);
+  const int64_t R = static_cast<int64_t>(r.T) * r.k;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    if (t * 16 >= n) break;
-    if (t > 0) __syncthreads();
-    f32x4 part[2 * CW];
+    if (first + t * 16 >= n) break;
+    __syncthreads();  // the last tile has been read
+    f32x4 part[8];
 #pragma unroll
-    for (int f = 0; f < 2 * CW; ++f) part[f] = acc[t][f / CW][f % CW];
-    put_parts<kUpWaves, 2 * CW>(part, red);
+    for (int f = 0; f < 8; ++f) part[f] = acc[t][f / 4][f % 4];
+    put_parts(part, red);
     __syncthreads();
-    for (int i = threadIdx.x; i < CW * 256; i += kUpWaves * kWave) {
-      const int p = i >> 8, at = i & 255, l = at >> 2, m = t * 16 + 4 * (l >> 4) + (at & 3);
+    for (int i = threadIdx.x; i < 4 * 256; i += kUpWaves * kWave) {
+      const int p = i >> 8, at = i & 255, m = first + t * 16 + entry_row(at);
       if (m >= n) continue;
-      const float g = sum_parts<kUpWaves, 2 * CW>(red, p, at), u = sum_parts<kUpWaves, 2 * CW>(red, CW + p, at);
-      // the one rounding between the products: the down product's operand is bf16
-      a[static_cast<int64_t>(rows.slot[m]) * r.F + blockIdx.x * (16 * CW) + (l & 15) * CW + p] = f2bf(silu_f(g) * u);
+      const float g = sum_parts<kUpWaves, 8>(red, p, at), u = sum_parts<kUpWaves, 8>(red, 4 + p, at);
+      const int64_t to = static_cast<int64_t>(rows.slot[m]) * r.F + blockIdx.x * kCols + entry_lane(at) * 4 + p;
+      if (gridDim.z == 1) {
+        split_bf16(silu_f(g) * u, a[to], a[to + R * r.F]);
+      } else {
+        gu[to + 2 * blockIdx.z * R * r.F] = g;
+        gu[to + (2 * blockIdx.z + 1) * R * r.F] = u;
+      }
     }
   }
 }
 
-template <int NT, int CW>
-__global__ __launch_bounds__(kDownWaves* kWave) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
+template <bool FUSED>
+__global__ __launch_bounds__(kUpWaves* kWave, 4) void k_decode_gateup(DecodeRows r, const bf16_t* __restrict__ x,
+                                                                   const bf16_t* __restrict__ w_gate,
+                                                                   const bf16_t* __restrict__ w_up,
+                                                                   bf16_t* __restrict__ a, float* __restrict__ gu) {
+  __shared__ Rows rows;
+  __shared__ float red[kUpWaves * 8 * 256];
+  if constexpr (FUSED) {
+    __shared__ Selection sel;
+    if (!select_rows(r, sel, rows)) return;
+  } else {
+    if (!read_rows(r, rows)) return;
+  }
+  const int64_t base = static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * kCols;
+  const bf16_t* const b[2] = {w_gate + base, w_up + base};
+  // more than 16 rows in pairs of tiles: what comes in again then is few experts' weights
+  if (FUSED || rows.n <= 16) {
+    gateup_tiles<1>(r, rows, 0, x, b, a, gu, red);
+  } else {
+    for (int t = 0; t < rows.n; t += 32) gateup_tiles<2>(r, rows, t, x, b, a, gu, red);
+  }
+}
+
+// The activation comes from a, or (RANGES) from LDS, act [rows][2][F].
+template <int NT, bool RANGES>
+__device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ a,
+                                           const float* __restrict__ gu, const bf16_t* const (&b)[1],
+                                           float* __restrict__ o, bf16_t* act, float* red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n;
+  const int64_t RF = static_cast<int64_t>(r.T) * r.k * r.F;
+  int64_t row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int i = first + t * 16 + (lane & 15);
+    row[t] = i >= n ? -1 : RANGES ? 2 * i * r.F : static_cast<int64_t>(rows.slot[i]) * r.F;
+  }
+  auto get = [&](int t, int k, uint4 (&v)[2]) {
+    v[0] = v[1] = make_uint4(0, 0, 0, 0);
+    if (row[t] < 0) return;
+    const bf16_t* src = (RANGES ? act : a) + row[t] + k;
+    v[0] = *reinterpret_cast<const uint4*>(src);
+    v[1] = *reinterpret_cast<const uint4*>(src + (RANGES ? r.F : RF));
+  };
+  // the ranges' sums and SwiGLU, under the first weights' way here
+  bool begun = false;
+  auto begin = [&] {
+    if (!RANGES || begun) return;
+    begun = true;
+    for (int i = threadIdx.x; i < n * r.F; i += kDownWaves * kWave) {
+      const int m = i / r.F, c = i % r.F;
+      const float* src = gu + static_cast<int64_t>(rows.slot[m]) * r.F + c;
+      const float g = src[0] + src[2 * RF], u = src[RF] + src[3 * RF];
+      split_bf16(silu_f(g) * u, act[2 * m * r.F + c], act[(2 * m + 1) * r.F + c]);
+    }
+    __syncthreads();
+  };
+  f32x4 acc[NT][1][4] = {};
+  few_rows<NT, 1, 2, NT == 1 ? 2 : 1>(b, r.H, wave, r.F / 32, kDownWaves, begin, get, acc);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (first + t * 16 >= n) break;
+    __syncthreads();  // the last tile has been read
+    put_parts(acc[t][0], red);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * 256; i += kDownWaves * kWave) {
+      const int p = i >> 8, at = i & 255, m = first + t * 16 + entry_row(at);
+      if (m < n)
+        o[static_cast<int64_t>(rows.slot[m]) * r.H + blockIdx.x * kCols + entry_lane(at) * 4 + p] =
+            sum_parts<kDownWaves, 4>(red, p, at);
+    }
+  }
+}
+
+template <bool RANGES>
+__global__ __launch_bounds__(kDownWaves* kWave, 5) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
+                                                                   const float* __restrict__ gu,
                                                                    const bf16_t* __restrict__ w_down,
                                                                    float* __restrict__ o) {
   __shared__ Rows rows;
-  __shared__ float red[kDownWaves * CW * 256];
-  if (!find_rows(r, rows)) return;
-  const int lane = threadIdx.x & 63, n = rows.n;
-  int row[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int i = t * 16 + (lane & 15);
-    row[t] = i < n ? rows.slot[i] : -1;
-  }
-  const bf16_t* const b[1] = {w_down + static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * (16 * CW)};
-  f32x4 acc[NT][1][CW] = {};
-  few_rows<NT, CW, 1, kDownWaves, NT == 1 ? 6 / (CW / 2) : 2>(a, row, b, r.F, r.H, acc);
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (t * 16 >= n) break;
-    if (t > 0) __syncthreads();
-    put_parts<kDownWaves, CW>(acc[t][0], red);
-    __syncthreads();
-    for (int i = threadIdx.x; i < CW * 256; i += kDownWaves * kWave) {
-      const int p = i >> 8, at = i & 255, l = at >> 2, m = t * 16 + 4 * (l >> 4) + (at & 3);
-      if (m < n)
-        o[static_cast<int64_t>(rows.slot[m]) * r.H + blockIdx.x * (16 * CW) + (l & 15) * CW + p] =
-            sum_parts<kDownWaves, CW>(red, p, at);
-    }
+  __shared__ float red[kDownWaves * 4 * 256];
+  if (!read_rows(r, rows)) return;
+  const bf16_t* const b[1] = {w_down + static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * kCols};
+  extern __shared__ bf16_t act[];
+  if (RANGES || rows.n <= 16) {
+    down_tiles<1, RANGES>(r, rows, 0, a, gu, b, o, act, red);
+  } else {
+    for (int t = 0; t < rows.n; t += 32) down_tiles<2, RANGES>(r, rows, t, a, gu, b, o, act, red);
   }
 }
 
 // ---- int8 weights.  They are K-contiguous: lane l reads 16 bytes of channel
-// l % 16, the instruction's operand as it is, and two loads a whole 128-byte line.
-template <int NT>
-__global__ __launch_bounds__(kUpWaves* kWave) void k_decode_gateup_i8(DecodeRows r, const int8_t* __restrict__ x,
-                                                                      const float* __restrict__ sx, moe_i8_experts w,
-                                                                      float* __restrict__ a) {
-  __shared__ Rows rows;
-  __shared__ int red[kUpWaves * 2 * 256];
-  if (!find_rows(r, rows)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, H = r.H;
-  const int64_t channel = static_cast<int64_t>(rows.expert) * r.F + blockIdx.x * 16;
-  const int quad = (lane >> 4) * 16;
-  const int8_t* const wg = w.w_gate + (channel + (lane & 15)) * H + quad;
-  const int8_t* const wu = w.w_up + (channel + (lane & 15)) * H + quad;
-  const int8_t* xr[NT];
+// l % 16, the instruction's operand as it is, and two loads a whole 128-byte
+// line (loads with the non-temporal policy lost its second half: 4.1 TB/s
+// against 5.5 at 16 tokens).
+
+// Products of 16 NT int8 rows with 16 channels of NB matrices (pointers at the
+// lane's channel and quarter), units u0, u0 + stride, ... < u1 of 128 k, U of them in flight.
+template <int NT, int NB, int U>
+__device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const int8_t* const (&x)[NT], int u0, int u1,
+                                            int stride, i32x4 (&acc)[NT][NB]) {
+  auto batch = [&](int unit, auto count) {
+    constexpr int n = decltype(count)::value;
+    uint4 w[n][2][NB], v[n][2][NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int i = t * 16 + (lane & 15);
-    xr[t] = i < n ? x + static_cast<int64_t>(rows.slot[i] / r.k) * H + quad : nullptr;
-  }
-  i32x4 acc[NT][2] = {};
-  auto batch = [&](int unit, auto count) {  // units of 128 k, kUpWaves apart
-    constexpr int m = decltype(count)::value;
-    uint4 g[m][2], u[m][2], v[m][2][NT];
-#pragma unroll
-    for (int i = 0; i < m; ++i)
+    for (int i = 0; i < n; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int k = (unit + i * kUpWaves) * 128 + h * 64;
-        g[i][h] = *reinterpret_cast<const uint4*>(wg + k);
-        u[i][h] = *reinterpret_cast<const uint4*>(wu + k);
+        const int k = (unit + i * stride) * 128 + h * 64;
+#pragma unroll
+        for (int m = 0; m < NB; ++m) w[i][h][m] = *reinterpret_cast<const uint4*>(b[m] + k);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-          v[i][h][t] = xr[t] != nullptr ? *reinterpret_cast<const uint4*>(xr[t] + k) : make_uint4(0, 0, 0, 0);
+          v[i][h][t] = x[t] != nullptr ? *reinterpret_cast<const uint4*>(x[t] + k) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
-    for (int i = 0; i < m; ++i)
+    for (int i = 0; i < n; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc[t][0] = mfma_i8(v[i][h][t], g[i][h], acc[t][0]);
-          acc[t][1] = mfma_i8(v[i][h][t], u[i][h], acc[t][1]);
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < NB; ++m) acc[t][m] = mfma_i8(v[i][h][t], w[i][h][m], acc[t][m]);
   };
-  const int units = H / 128;
-  int unit = wave;
-  for (; unit + kUpWaves < units; unit += 2 * kUpWaves) batch(unit, std::integral_constant<int, 2>{});
-  if (unit < units) batch(unit, std::integral_constant<int, 1>{});
+  int unit = u0;
+  for (; unit + (U - 1) * stride < u1; unit += U * stride) batch(unit, std::integral_constant<int, U>{});
+  for (; unit < u1; unit += stride) batch(unit, std::integral_constant<int, 1>{});
+}
+
+// Short workgroups that many fit a compute unit: two waves and one unit of k
+// in flight in each reached 5.5 TB/s at 16 tokens, eight waves 4.2.
+constexpr int kUpWaves8 = 2, kDownWaves8 = 4;
+
+template <int NT>
+__device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows& rows, int first,
+                                                const int8_t* __restrict__ x, const float* __restrict__ sx,
+                                                const moe_i8_experts& w, float* __restrict__ a, int* red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, H = r.H;
+  const int64_t channel = static_cast<int64_t>(rows.expert) * r.F + blockIdx.x * 16;
+  const int quad = (lane >> 4) * 16;
+  const int64_t at = (channel + (lane & 15)) * H + quad;
+  const int8_t* const b[2] = {w.w_gate + at, w.w_up + at};
+  const int8_t* xr[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    if (t * 16 >= n) break;
-    if (t > 0) __syncthreads();
-    put_parts<kUpWaves, 2>(acc[t], red);
+    const int i = first + t * 16 + (lane & 15);
+    xr[t] = i < n ? x + static_cast<int64_t>(rows.slot[i] / r.k) * H + quad : nullptr;
+  }
+  i32x4 acc[NT][2] = {};
+  few_rows_i8<NT, 2, 1>(b, xr, wave, H / 128, kUpWaves8, acc);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (first + t * 16 >= n) break;
+    __syncthreads();  // the last tile has been read
+    put_parts(acc[t], red);
     __syncthreads();
-    const int at = threadIdx.x, l = at >> 2, m = t * 16 + 4 * (l >> 4) + (at & 3), c = l & 15;
-    if (at < 256 && m < n) {
+    for (int i = threadIdx.x; i < 256; i += kUpWaves8 * kWave) {
+      const int m = first + t * 16 + entry_row(i), c = entry_lane(i);
+      if (m >= n) continue;
       const float s = sx[rows.slot[m] / r.k];
-      const float g = static_cast<float>(unwrap(sum_parts<kUpWaves, 2>(red, 0, at))) * s * w.s_gate[channel + c];
-      const float u = static_cast<float>(unwrap(sum_parts<kUpWaves, 2>(red, 1, at))) * s * w.s_up[channel + c];
+      const float g = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 0, i))) * s * w.s_gate[channel + c];
+      const float u = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 1, i))) * s * w.s_up[channel + c];
       a[static_cast<int64_t>(rows.slot[m]) * r.F + blockIdx.x * 16 + c] = silu_f(g) * u;
     }
   }
 }
 
-// O = A W_down, 64 channels per workgroup, 16 per wave.  The activation's rows
-// are rounded to int8 by every workgroup for itself (from L2): their largest
-// magnitudes first, then kChunk columns at a time into LDS, while the chunk's
-// weights are on their way into registers.
-constexpr int kDownChunk = 1024, kDownUnits = kDownChunk / 128;
-constexpr int kDownPitch = kDownChunk + 16;  // 16 rows of one fragment read in distinct banks
-
-__global__ __launch_bounds__(kDownWaves* kWave) void k_decode_down_i8(DecodeRows r, const float* __restrict__ a,
-                                                                      moe_i8_experts w, float* __restrict__ o) {
+template <bool FUSED>
+__global__ __launch_bounds__(kUpWaves8* kWave, 6) void k_decode_gateup_i8(DecodeRows r, const int8_t* __restrict__ x,
+                                                                       const float* __restrict__ sx, moe_i8_experts w,
+                                                                       float* __restrict__ a) {
   __shared__ Rows rows;
-  __shared__ uint32_t tops[kDecodeMaxT];
-  __shared__ __attribute__((aligned(16))) int8_t a8[16 * kDownPitch];
-  if (!find_rows(r, rows)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, F = r.F;
-  for (int i = wave; i < n; i += kDownWaves) {
-    const float* src = a + static_cast<int64_t>(rows.slot[i]) * F;
-    uint32_t m = 0;
-    for (int c = lane * 2; c < F; c += 128) {
-      const float2 v = *reinterpret_cast<const float2*>(src + c);
-      m = max(m, max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu));
-    }
-    m = wave_umax(m);
-    if (lane == 0) tops[i] = m;
+  __shared__ int red[kUpWaves8 * 2 * 256];
+  if constexpr (FUSED) {
+    __shared__ Selection sel;
+    if (!select_rows(r, sel, rows)) return;
+  } else {
+    if (!read_rows(r, rows)) return;
   }
-  const int64_t channel = static_cast<int64_t>(rows.expert) * r.H + blockIdx.x * 64 + wave * 16;
-  const int quad = (lane >> 4) * 16;
-  const int8_t* const wd = w.w_down + (channel + (lane & 15)) * F + quad;
-  constexpr int kTiles = kDecodeMaxT / 16;
-  i32x4 acc[kTiles] = {};
-  for (int k0 = 0; k0 < F; k0 += kDownChunk) {
-    uint4 v[kDownUnits][2];
-#pragma unroll
-    for (int i = 0; i < kDownUnits; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = k0 + i * 128 + h * 64;
-        v[i][h] = k < F ? *reinterpret_cast<const uint4*>(wd + k) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      if (t * 16 >= n) break;
-      __syncthreads();  // the tops are there, the last tile has been read
-      for (int i = wave; i < 16; i += kDownWaves) {
-        const int m = t * 16 + i;
-        const Rounder rd(m < n ? tops[m] : 0u);
-        const float* src = m < n ? a + static_cast<int64_t>(rows.slot[m]) * F : nullptr;
-        for (int c = lane * 4; c < kDownChunk; c += 256) {
-          float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (src != nullptr && k0 + c < F) f = *reinterpret_cast<const float4*>(src + k0 + c);
-          *reinterpret_cast<uint32_t*>(a8 + i * kDownPitch + c) = pack4(rd(f.x), rd(f.y), rd(f.z), rd(f.w));
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kDownUnits; ++i) {
-        if (k0 + i * 128 >= F) break;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          acc[t] = mfma_i8(*reinterpret_cast<const uint4*>(a8 + (lane & 15) * kDownPitch + i * 128 + h * 64 + quad),
-                           v[i][h], acc[t]);
-      }
-    }
-  }
-  const float sd = w.s_down[channel + (lane & 15)];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    if (t * 16 >= n) break;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int m = t * 16 + 4 * (lane >> 4) + i;
-      if (m < n)
-        o[static_cast<int64_t>(rows.slot[m]) * r.H + blockIdx.x * 64 + wave * 16 + (lane & 15)] =
-            static_cast<float>(unwrap(acc[t][i])) * Rounder(tops[m]).scale * sd;
-    }
+  if (FUSED || rows.n <= 16) {
+    gateup_tiles_i8<1>(r, rows, 0, x, sx, w, a, red);
+  } else {
+    for (int t = 0; t < rows.n; t += 32) gateup_tiles_i8<2>(r, rows, t, x, sx, w, a, red);
   }
 }
 
-// y[t] = sum_j g o, in slot order; 0 for a token without rows.
-__global__ __launch_bounds__(256) void k_decode_combine(DecodeRows r, const float* __restrict__ gates,
-                                                        const float* __restrict__ o, bf16_t* __restrict__ y) {
+// The activation's rows as int8 rows, a wave per slot.
+__global__ __launch_bounds__(256) void k_decode_requant(DecodeRows r, const float* __restrict__ a, int8_t* __restrict__ q,
+                                                        float* __restrict__ scale) {
+  const int lane = threadIdx.x & 63, slot = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (slot >= r.T * r.k || r.topk_idx[slot] < 0) return;
+  const float* src = a + static_cast<int64_t>(slot) * r.F;
+  uint32_t m = 0;
+  for (int c = lane * 4; c < r.F; c += 256) {
+    const uint4 v = *reinterpret_cast<const uint4*>(src + c);
+    m = max(max(m, max(v.x & 0x7fffffffu, v.y & 0x7fffffffu)), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
+  }
+  const Rounder rd(wave_umax(m));
+  for (int c = lane * 4; c < r.F; c += 256) {
+    const float4 v = *reinterpret_cast<const float4*>(src + c);
+    *reinterpret_cast<uint32_t*>(q + static_cast<int64_t>(slot) * r.F + c) = pack4(rd(v.x), rd(v.y), rd(v.z), rd(v.w));
+  }
+  if (lane == 0) scale[slot] = rd.scale;
+}
+
+// O = A W_down: 16 channels per wave, all of F, so no sum over waves.
+template <int NT>
+__device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& rows, int first,
+                                              const int8_t* __restrict__ a, const float* __restrict__ sa,
+                                              const moe_i8_experts& w, float* __restrict__ o) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, F = r.F;
+  const int column = (blockIdx.x * kDownWaves8 + wave) * 16 + (lane & 15);
+  const int64_t channel = static_cast<int64_t>(rows.expert) * r.H + column;
+  const int quad = (lane >> 4) * 16;
+  const int8_t* const b[1] = {w.w_down + channel * F + quad};
+  const int8_t* ar[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int i = first + t * 16 + (lane & 15);
+    ar[t] = i < n ? a + static_cast<int64_t>(rows.slot[i]) * F + quad : nullptr;
+  }
+  i32x4 acc[NT][1] = {};
+  few_rows_i8<NT, 1, 2>(b, ar, 0, F / 128, 1, acc);
+  const float sd = w.s_down[channel];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = first + t * 16 + 4 * (lane >> 4) + i;
+      if (m < n)
+        o[static_cast<int64_t>(rows.slot[m]) * r.H + column] = static_cast<float>(unwrap(acc[t][0][i])) * sa[rows.slot[m]] * sd;
+    }
+}
+
+__global__ __launch_bounds__(kDownWaves8* kWave, 6) void k_decode_down_i8(DecodeRows r, const int8_t* __restrict__ a,
+                                                                       const float* __restrict__ sa, moe_i8_experts w,
+                                                                       float* __restrict__ o) {
+  __shared__ Rows rows;
+  if (!read_rows(r, rows)) return;
+  if (rows.n <= 16) {
+    down_tiles_i8<1>(r, rows, 0, a, sa, w, o);
+  } else {
+    for (int t = 0; t < rows.n; t += 32) down_tiles_i8<2>(r, rows, t, a, sa, w, o);
+  }
+}
+
+// y[t] = sum_j gates o, in slot order; 0 for a token without rows.
+__global__ __launch_bounds__(256) void k_decode_combine(DecodeRows r, const float* __restrict__ o, bf16_t* __restrict__ y) {
   const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= r.H) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (r.topk_idx[t * r.k] >= 0)
     for (int j = 0; j < r.k; ++j) {
-      const float g = gates[t * r.k + j];
+      const float g = r.gates[t * r.k + j];
       const float4 v = *reinterpret_cast<const float4*>(o + static_cast<int64_t>(t * r.k + j) * r.H + c);
       s.x = fmaf(g, v.x, s.x), s.y = fmaf(g, v.y, s.y), s.z = fmaf(g, v.z, s.z), s.w = fmaf(g, v.w, s.w);
     }
@@ -386,52 +602,72 @@ int slots(const DecodeRows& r) { return std::min(r.E, r.T * r.k); }
 
 }  // namespace
 
-// Row tiles of 16 that one expert may have: 1, 2 or 4.
-#define MOE_DECODE_TILES(T, CALL) \
-  do {                            \
-    if ((T) <= 16) CALL(1);       \
-    else if ((T) <= 32) CALL(2);  \
-    else CALL(4);                 \
-  } while (0)
+// Whether the selection is made by the gate/up product.
+bool decode_fused(int T) { return T <= kFusedT; }
 
-hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,
-                                bf16_t* a, hipStream_t s) {
-  TraceScope trace_scope(K_DECODE_GATEUP, s);
-#define MOE_CALL(NT) \
-  hipLaunchKernelGGL((k_decode_gateup<NT, 2>), dim3(r.F / 32, slots(r)), dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a)
-  MOE_DECODE_TILES(r.T, MOE_CALL);
-#undef MOE_CALL
+// Ranges of K of the bf16 gate/up product: two where few tokens leave its
+// tiles fewer than the chip's 256 compute units.  The down product then holds
+// the rows of an expert in LDS, at most 64 KB: with T k < E they are at most
+// the grid's slots, hence slots F < 256 kCols values, and else E >= 8 slots
+// leave F < 32 kCols for at most kFusedT rows.
+int decode_ranges(int T, int E, int F, int k) {
+  return decode_fused(T) && F / kCols * std::min(E, T * k) < 256 ? 2 : 1;
+}
+
+hipError_t launch_decode_router(const DecodeRows& r, const bf16_t* x, const bf16_t* w_r, int8_t* q, float* sx,
+                                hipStream_t s) {
+  TraceScope trace_scope(K_DECODE_ROUTER, s);
+  const int tiles = cdiv(r.E, kRouterCols) * cdiv(r.T, 16), more = q != nullptr ? cdiv(r.T, kRouterSplits) : 0;
+  hipLaunchKernelGGL(k_decode_router, dim3(tiles + more), dim3(kRouterSplits * kWave), 0, s, x, w_r, r.T, r.H, r.E, r.part,
+                     r.counts, q, sx);
   return hipGetLastError();
 }
 
-hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const bf16_t* w_down, float* o, hipStream_t s) {
+hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,
+                                bf16_t* a, float* gu, hipStream_t s) {
+  TraceScope trace_scope(K_DECODE_GATEUP, s);
+  const dim3 grid(r.F / kCols, slots(r), decode_ranges(r.T, r.E, r.F, r.k));
+  if (decode_fused(r.T))
+    hipLaunchKernelGGL(k_decode_gateup<true>, grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
+  else
+    hipLaunchKernelGGL(k_decode_gateup<false>, grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
+  return hipGetLastError();
+}
+
+hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const float* gu, const bf16_t* w_down, float* o,
+                              hipStream_t s) {
   TraceScope trace_scope(K_DECODE_DOWN, s);
-#define MOE_CALL(NT) \
-  hipLaunchKernelGGL((k_decode_down<NT, 2>), dim3(r.H / 32, slots(r)), dim3(kDownWaves * kWave), 0, s, r, a, w_down, o)
-  MOE_DECODE_TILES(r.T, MOE_CALL);
-#undef MOE_CALL
+  const dim3 grid(r.H / kCols, slots(r));
+  if (decode_ranges(r.T, r.E, r.F, r.k) > 1)
+    hipLaunchKernelGGL(k_decode_down<true>, grid, dim3(kDownWaves * kWave), 2 * r.T * r.F * sizeof(bf16_t), s, r, a, gu, w_down, o);
+  else
+    hipLaunchKernelGGL(k_decode_down<false>, grid, dim3(kDownWaves * kWave), 0, s, r, a, gu, w_down, o);
   return hipGetLastError();
 }
 
 hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const float* sx, const moe_i8_experts& w,
                                    float* a, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_GATEUP, s);
-#define MOE_CALL(NT) \
-  hipLaunchKernelGGL((k_decode_gateup_i8<NT>), dim3(r.F / 16, slots(r)), dim3(kUpWaves * kWave), 0, s, r, x, sx, w, a)
-  MOE_DECODE_TILES(r.T, MOE_CALL);
-#undef MOE_CALL
+  const dim3 grid(r.F / 16, slots(r));
+  if (decode_fused(r.T))
+    hipLaunchKernelGGL(k_decode_gateup_i8<true>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a);
+  else
+    hipLaunchKernelGGL(k_decode_gateup_i8<false>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a);
   return hipGetLastError();
 }
 
-hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, const moe_i8_experts& w, float* o, hipStream_t s) {
+hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, int8_t* a8, float* sa, const moe_i8_experts& w,
+                                 float* o, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_DOWN, s);
-  hipLaunchKernelGGL(k_decode_down_i8, dim3(r.H / 64, slots(r)), dim3(kDownWaves * kWave), 0, s, r, a, w, o);
+  hipLaunchKernelGGL(k_decode_requant, dim3(cdiv(r.T * r.k, 4)), dim3(256), 0, s, r, a, a8, sa);
+  hipLaunchKernelGGL(k_decode_down_i8, dim3(r.H / (16 * kDownWaves8), slots(r)), dim3(kDownWaves8 * kWave), 0, s, r, a8, sa,
+                     w, o);
   return hipGetLastError();
 }
 
-hipError_t launch_decode_combine(const DecodeRows& r, const float* gates, const float* o, bf16_t* y, hipStream_t s) {
+hipError_t launch_decode_combine(const DecodeRows& r, const float* o, bf16_t* y, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_COMBINE, s);
-  hipLaunchKernelGGL(k_decode_combine, dim3(cdiv(r.H, 1024), r.T), dim3(256), 0, s, r, gates, o, y);
+  hipLaunchKernelGGL(k_decode_combine, dim3(cdiv(r.H, 1024), r.T), dim3(256), 0, s, r, o, y);
   return hipGetLastError();
 }
 

@@ -135,6 +135,11 @@ hipError_t launch_router_fwd(const bf16_t* x, const bf16_t* w_r, const uint8_t* 
                              int E, int k, float* logits, float* part, int32_t* topk_idx, float* gates,
                              float* aux_ws, int32_t* chunk_counts, int32_t* row_token, hipStream_t s);
 int64_t router_part_floats(int T, int E);
+// The second of its two kernels alone: selection and gates from the ranges'
+// sums of the logits (the first in `logits`), counts into chunk_counts, which
+// start at zero.
+hipError_t launch_topk(const uint8_t* mask, int T, int E, int k, float* logits, const float* part, int32_t* topk_idx,
+                       float* gates, float* aux_ws, int32_t* chunk_counts, int32_t* row_token, hipStream_t s);
 int64_t router_loss_ws_floats(int T, int E);
 // out[0..1] = {L_aux, L_z} from those partial sums and the routing counts.
 hipError_t launch_router_loss(const float* aux_ws, int T, int E, int k, const int32_t* counts,

@@ -5,6 +5,7 @@
 
 #include "gemm_core.hpp"
 #include "launch.hpp"
+#include "topk.hpp"
 #include "trace.hpp"
 
 namespace moe {
@@ -25,13 +26,6 @@ static_assert(MOE_MAX_EXPERTS <= 4 * kWave, "at most four experts per lane in th
 // while W_r is read T / 128 times instead of T / 32.
 using RouterTile = Tile<128, 128, 1, 2, 2>;
 constexpr int kRouterTokens = RouterTile::BM;
-// One count for every T: it is the order in which a token's logits are summed,
-// and a passage must select the same experts alone and inside a batch.  16
-// ranges up to T = 1024, where few tokens leave most of the chip idle, took
-// 8.8 us against 12.9 at T = 64 (the top-k 1 us more), but a token's logits
-// then differed in their last bits on either side of that T.
-constexpr int kRouterSplits = 4;
-
 __global__ __launch_bounds__(RouterTile::kThreads) void k_router_logits(const bf16_t* __restrict__ x,
                                                                         const bf16_t* __restrict__ w_r, int T,
                                                                         int H, int E, float* __restrict__ logits,
@@ -45,7 +39,8 @@ __global__ __launch_bounds__(RouterTile::kThreads) void k_router_logits(const bf
   const int t0 = blockIdx.x * kRouterTokens;
   const int rows = min(kRouterTokens, T - t0);
   const int split = blockIdx.y;
-  const int kper = cdiv(cdiv(H, kRouterSplits), BK) * BK;
+  static_assert(BK == 64, "router_range");
+  const int kper = router_range(H);
   const int k0 = min(H, split * kper);
   const int kn = min(H, k0 + kper) - k0;  // 0 for an empty split: its partial sums are zeros
   float* out = split == 0 ? logits : part + static_cast<int64_t>(split - 1) * T * E;
@@ -69,95 +64,6 @@ __global__ __launch_bounds__(RouterTile::kThreads) void k_router_logits(const bf
       }
     }
   }
-}
-
-// Order-preserving key of an fp32 value: a > b  <=>  key(a) > key(b), and
-// -0 == +0 share a key.
-__device__ __forceinline__ uint32_t order_key(float v) {
-  uint32_t u = __float_as_uint(v);
-  if (v == 0.0f) u = 0u;
-  return (u >> 31) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t key) {
-  return __uint_as_float((key >> 31) ? (key & 0x7fffffffu) : ~key);
-}
-
-__device__ __forceinline__ int ballot_count(bool p) { return __popcll(__ballot(p)); }
-
-// Top-k of one token, held by a wave: lane l holds the logits of experts
-// e = l + 64 m, m < PL (key 0 and value 0 where e >= E).  Selection: the k
-// largest logits, ties to the lower expert, in slot order (descending logit,
-// then ascending expert).  Exact: a radix search for the k-th largest order
-// key (each wave-wide count is a ballot and a popcount), then the keys equal
-// to it are taken by lower expert index; an entry's slot counts the selected
-// keys that beat it, broadcast one by one.  Gates
-// g_j = exp(z_j - z_0) / sum_j' exp(z_j' - z_0).  Keys of absent experts are
-// 0, below every logit's key, so they never count.  Returns the largest logit.
-template <int PL>
-__device__ __forceinline__ float topk_select(const float (&val)[PL], const uint32_t (&key)[PL], int k, int lane,
-                                             int32_t* __restrict__ idx_row, float* __restrict__ g_row,
-                                             int32_t* __restrict__ cnt_row) {
-  uint32_t kth = 0u;  // largest P with #{key >= P} >= k
-  for (int b = 31; b >= 0; --b) {
-    const uint32_t cand = kth | (1u << b);
-    int cnt = 0;
-#pragma unroll
-    for (int m = 0; m < PL; ++m) cnt += ballot_count(key[m] >= cand);
-    kth = cnt >= k ? cand : kth;
-  }
-  int above = 0;
-#pragma unroll
-  for (int m = 0; m < PL; ++m) above += ballot_count(key[m] > kth);
-  const int need = k - above;  // entries equal to the k-th key, by lower expert index
-  const unsigned long long below = (1ull << lane) - 1ull;
-  bool sel[PL];
-  unsigned long long selmask[PL];
-  int eq_before = 0;
-#pragma unroll
-  for (int m = 0; m < PL; ++m) {
-    const unsigned long long eq = __ballot(key[m] == kth);
-    const int rank_eq = eq_before + __popcll(eq & below);
-    eq_before += __popcll(eq);
-    sel[m] = key[m] > kth || (key[m] == kth && rank_eq < need);
-    selmask[m] = __ballot(sel[m]);
-  }
-  int slot[PL];
-#pragma unroll
-  for (int m = 0; m < PL; ++m) slot[m] = 0;
-  uint32_t kmax = 0u;
-#pragma unroll
-  for (int mj = 0; mj < PL; ++mj) {
-    unsigned long long msk = selmask[mj];
-    while (msk != 0ull) {
-      const int lj = __builtin_ctzll(msk);
-      msk &= msk - 1ull;
-      const uint32_t kj = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key[mj]), lj));
-      const int ej = lj + kWave * mj;
-      kmax = kj > kmax ? kj : kmax;
-#pragma unroll
-      for (int m = 0; m < PL; ++m) {
-        const int e = lane + kWave * m;
-        slot[m] += (sel[m] && (kj > key[m] || (kj == key[m] && ej < e))) ? 1 : 0;
-      }
-    }
-  }
-  const float top = key_value(kmax);
-  float w = 0.0f;
-  float wm[PL];
-#pragma unroll
-  for (int m = 0; m < PL; ++m) {
-    wm[m] = sel[m] ? expf(val[m] - top) : 0.0f;
-    w += wm[m];
-  }
-  const float sum = wave_sum(w);
-#pragma unroll
-  for (int m = 0; m < PL; ++m)
-    if (sel[m]) {
-      idx_row[slot[m]] = lane + kWave * m;
-      g_row[slot[m]] = wm[m] / sum;
-      atomicAdd(cnt_row + lane + kWave * m, 1);
-    }
-  return top;
 }
 
 // One wave per token: the top-k and gates; masked tokens get expert -1 and
@@ -293,6 +199,11 @@ hipError_t launch_router_fwd(const bf16_t* x, const bf16_t* w_r, const uint8_t* 
     hipLaunchKernelGGL(k_router_logits, dim3(cdiv(T, kRouterTokens), kRouterSplits), dim3(RouterTile::kThreads), 0,
                        s, x, w_r, T, H, E, logits, part, chunk_counts, static_cast<int>(permute_ws_ints(T, E)));
   }
+  return launch_topk(mask, T, E, k, logits, part, topk_idx, gates, aux_ws, chunk_counts, row_token, s);
+}
+
+hipError_t launch_topk(const uint8_t* mask, int T, int E, int k, float* logits, const float* part, int32_t* topk_idx,
+                       float* gates, float* aux_ws, int32_t* chunk_counts, int32_t* row_token, hipStream_t s) {
   {
     TraceScope trace_scope(K_TOPK, s);
     const dim3 grid(cdiv(T, 4)), block(256);

@@ -41,22 +41,36 @@ hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s);
 // ---- the expert layer for a few tokens (decode.hip)
 constexpr int kDecodeMaxT = MOE_DECODE_MAX_T;
 
-// Routing of T <= kDecodeMaxT tokens: topk_idx, gates [T, k], counts [E].  A
-// routed row is named by its slot t k + j.
+// A routed row is named by its slot t k + j.
 struct DecodeRows {
-  const int32_t *topk_idx, *counts;
+  const uint8_t* mask;  // may be null
+  float* part;          // [splits, T, E] the router's sums over its ranges of K
+  int32_t* topk_idx;    // [T, k]
+  float* gates;         // [T, k]
+  int32_t* counts;      // [E]
   int T, H, E, F, k;
 };
-// a [T k, F] = SwiGLU of the slots' tokens through their experts.
+// part, counts = 0 and, with q, the tokens' int8 rows.
+hipError_t launch_decode_router(const DecodeRows& r, const bf16_t* x, const bf16_t* w_r, int8_t* q, float* sx,
+                                hipStream_t s);
+// Whether the gate/up product makes the selection (topk_idx, gates, counts)
+// from part; else it is there before.
+bool decode_fused(int T);
+// SwiGLU of the slots' tokens through their experts: a [2, T k, F] as two
+// summands, or with decode_ranges(..) > 1 each range's G and U, gu [ranges, 2, T k, F].
+int decode_ranges(int T, int E, int F, int k);
 hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,
-                                bf16_t* a, hipStream_t s);
+                                bf16_t* a, float* gu, hipStream_t s);
+// a [T k, F].
 hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const float* sx, const moe_i8_experts& w,
                                    float* a, hipStream_t s);
-// o [T k, H] = a W_down.
-hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const bf16_t* w_down, float* o, hipStream_t s);
-hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, const moe_i8_experts& w, float* o, hipStream_t s);
+// o [T k, H] = the activation through W_down (a8, sa: room for its int8 rows).
+hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const float* gu, const bf16_t* w_down, float* o,
+                              hipStream_t s);
+hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, int8_t* a8, float* sa, const moe_i8_experts& w,
+                                 float* o, hipStream_t s);
 // y [T, H] = sum_j gates o.
-hipError_t launch_decode_combine(const DecodeRows& r, const float* gates, const float* o, bf16_t* y, hipStream_t s);
+hipError_t launch_decode_combine(const DecodeRows& r, const float* o, bf16_t* y, hipStream_t s);
 
 // ---- token sampling (sample.hip)
 struct SampleArgs {

@@ -2,6 +2,7 @@
 // checks, workspace layouts and launch sequences.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -88,42 +89,58 @@ int check_decode_i8(const moe_dims* d) {
 }
 
 struct DecodeWs {
-  float *logits, *router_part, *gates, *o;
-  int32_t *topk_idx, *counts, *row_token;
-  bf16_t* a;  // bf16 experts
-  float *a32, *sx;  // int8 experts
-  int8_t* x8;
+  DecodeRows rows;
+  int32_t* row_token;
+  bf16_t* a;   // bf16 experts: the activation's two summands,
+  float* gu;   // or the ranges' G and U
+  float *a32, *sx, *sa;  // int8 experts
+  int8_t *x8, *a8;
+  float* o;
   size_t bytes;
 };
 DecodeWs decode_layout(const moe_dims* d, bool i8, void* base) {
-  const size_t T = d->T, E = d->E, R = T * d->top_k;
+  const size_t T = d->T, E = d->E, R = T * d->top_k, RF = R * d->F;
   Carve c(base);
   DecodeWs w{};
-  w.logits = c.take<float>(T * E);
-  w.router_part = c.take<float>(static_cast<size_t>(router_part_floats(d->T, d->E)));
-  w.gates = c.take<float>(R);
-  w.topk_idx = c.take<int32_t>(R);
-  w.counts = c.take<int32_t>(static_cast<size_t>(permute_ws_ints(d->T, d->E)));
+  w.rows = {nullptr, nullptr, nullptr, nullptr, nullptr, d->T, d->H, d->E, d->F, d->top_k};
+  w.rows.part = c.take<float>(T * E + static_cast<size_t>(router_part_floats(d->T, d->E)));
+  w.rows.gates = c.take<float>(R);
+  w.rows.topk_idx = c.take<int32_t>(R);
+  w.rows.counts = c.take<int32_t>(E);
   w.row_token = c.take<int32_t>(R);
   if (i8) {
     w.x8 = c.take<int8_t>(T * d->H);
     w.sx = c.take<float>(T);
-    w.a32 = c.take<float>(R * d->F);
+    w.a32 = c.take<float>(RF);
+    w.a8 = c.take<int8_t>(RF);
+    w.sa = c.take<float>(R);
+  } else if (const int ranges = decode_ranges(d->T, d->E, d->F, d->top_k); ranges > 1) {
+    w.gu = c.take<float>(2 * ranges * RF);
   } else {
-    w.a = c.take<bf16_t>(R * d->F);
+    w.a = c.take<bf16_t>(2 * RF);
   }
   w.o = c.take<float>(R * d->H);
   w.bytes = c.off;
   return w;
 }
 
-// Router and selection, moe_infer's own kernels.
-hipError_t route(const moe_dims* d, const bf16_t* x, const bf16_t* w_r, const uint8_t* mask, const DecodeWs& l,
-                 hipStream_t s) {
-  return launch_router_fwd(x, w_r, mask, d->T, d->H, d->E, d->top_k, l.logits, l.router_part, l.topk_idx, l.gates,
-                           nullptr, l.counts, l.row_token, s);
+// A call of fewer tokens may use more: what a size query returns is enough for
+// up to its T.
+size_t decode_bytes(const moe_dims* d, bool i8) {
+  size_t most = 0;
+  for (moe_dims e = *d; e.T > 0; --e.T) most = std::max(most, decode_layout(&e, i8, nullptr).bytes);
+  return most;
 }
-static_assert(MOE_DECODE_MAX_T <= kPermChunk, "the router's first chunk of counts is all of them");
+
+// Router and, but for the fewest tokens, the selection.
+hipError_t route(const DecodeWs& l, const bf16_t* x, const bf16_t* w_r, hipStream_t s) {
+  const DecodeRows& r = l.rows;
+  if (const hipError_t e = launch_decode_router(r, x, w_r, l.x8, l.sx, s); e != hipSuccess || decode_fused(r.T)) return e;
+  // one chunk of counts: the tokens are fewer than the selection's chunk
+  static_assert(MOE_DECODE_MAX_T <= kPermChunk, "counts of one chunk");
+  return launch_topk(r.mask, r.T, r.E, r.k, r.part, r.part + static_cast<int64_t>(r.T) * r.E, r.topk_idx, r.gates, nullptr,
+                     r.counts, l.row_token, s);
+}
 
 // ---- sampling
 int check_sample(const moe_sample_dims* d) {
@@ -198,7 +215,7 @@ int moe_norm_bwd(const moe_norm_dims* d, const void* h, int64_t ldh, const void*
 
 size_t moe_decode_workspace_bytes(const moe_dims* d) {
   if (check_decode(d) != MOE_OK) return 0;
-  return decode_layout(d, false, nullptr).bytes;
+  return decode_bytes(d, false);
 }
 
 int moe_decode(const moe_dims* d, const void* x, const void* w_r, const void* w_gate, const void* w_up,
@@ -209,23 +226,23 @@ int moe_decode(const moe_dims* d, const void* x, const void* w_r, const void* w_
     return rc;
   const bool masked = d->flags & MOE_F_MASK;
   if (masked && token_mask == nullptr) return fail(MOE_ERR_ARG, "MOE_F_MASK set but token_mask is NULL");
-  const DecodeWs l = decode_layout(d, false, ws);
+  DecodeWs l = decode_layout(d, false, ws);
   if (ws_bytes < l.bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, l.bytes);
+  l.rows.mask = masked ? token_mask : nullptr;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bf16_t* xb = static_cast<const bf16_t*>(x);
-  hipError_t e = route(d, xb, static_cast<const bf16_t*>(w_r), masked ? token_mask : nullptr, l, s);
+  hipError_t e = route(l, xb, static_cast<const bf16_t*>(w_r), s);
   if (e != hipSuccess) return hip_status(e, "router");
-  const DecodeRows r{l.topk_idx, l.counts, d->T, d->H, d->E, d->F, d->top_k};
-  e = launch_decode_gateup(r, xb, static_cast<const bf16_t*>(w_gate), static_cast<const bf16_t*>(w_up), l.a, s);
+  e = launch_decode_gateup(l.rows, xb, static_cast<const bf16_t*>(w_gate), static_cast<const bf16_t*>(w_up), l.a, l.gu, s);
   if (e != hipSuccess) return hip_status(e, "gate/up");
-  e = launch_decode_down(r, l.a, static_cast<const bf16_t*>(w_down), l.o, s);
+  e = launch_decode_down(l.rows, l.a, l.gu, static_cast<const bf16_t*>(w_down), l.o, s);
   if (e != hipSuccess) return hip_status(e, "down");
-  return hip_status(launch_decode_combine(r, l.gates, l.o, static_cast<bf16_t*>(y), s), "combine");
+  return hip_status(launch_decode_combine(l.rows, l.o, static_cast<bf16_t*>(y), s), "combine");
 }
 
 size_t moe_decode_i8_workspace_bytes(const moe_dims* d) {
   if (check_decode_i8(d) != MOE_OK) return 0;
-  return decode_layout(d, true, nullptr).bytes;
+  return decode_bytes(d, true);
 }
 
 int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i8_experts* w, const uint8_t* token_mask,
@@ -238,20 +255,18 @@ int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i
     return rc;
   const bool masked = d->flags & MOE_F_MASK;
   if (masked && token_mask == nullptr) return fail(MOE_ERR_ARG, "MOE_F_MASK set but token_mask is NULL");
-  const DecodeWs l = decode_layout(d, true, ws);
+  DecodeWs l = decode_layout(d, true, ws);
   if (ws_bytes < l.bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, l.bytes);
+  l.rows.mask = masked ? token_mask : nullptr;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bf16_t* xb = static_cast<const bf16_t*>(x);
-  hipError_t e = route(d, xb, static_cast<const bf16_t*>(w_r), masked ? token_mask : nullptr, l, s);
+  hipError_t e = route(l, xb, static_cast<const bf16_t*>(w_r), s);
   if (e != hipSuccess) return hip_status(e, "router");
-  e = launch_i8_quant_rows(xb, d->H, d->T, d->H, nullptr, l.x8, l.sx, s);
-  if (e != hipSuccess) return hip_status(e, "quant rows");
-  const DecodeRows r{l.topk_idx, l.counts, d->T, d->H, d->E, d->F, d->top_k};
-  e = launch_decode_gateup_i8(r, l.x8, l.sx, *w, l.a32, s);
+  e = launch_decode_gateup_i8(l.rows, l.x8, l.sx, *w, l.a32, s);
   if (e != hipSuccess) return hip_status(e, "gate/up");
-  e = launch_decode_down_i8(r, l.a32, *w, l.o, s);
+  e = launch_decode_down_i8(l.rows, l.a32, l.a8, l.sa, *w, l.o, s);
   if (e != hipSuccess) return hip_status(e, "down");
-  return hip_status(launch_decode_combine(r, l.gates, l.o, static_cast<bf16_t*>(y), s), "combine");
+  return hip_status(launch_decode_combine(l.rows, l.o, static_cast<bf16_t*>(y), s), "combine");
 }
 
 size_t moe_sample_workspace_bytes(const moe_sample_dims* d) {

@@ -38,7 +38,7 @@ const char* const kNames[K_NUM_KERNELS] = {
     "offsets_from_counts", "gateup_recompute", "router_loss", "router_dx_dense", "lora_rows", "lora_wgrad",
     "gate_bwd", "wgrad_plan", "i8_quant", "i8_weight", "i8_matmul", "i8_gateup", "i8_down", "kv_plan",
     "kv_append", "kv_read", "kv_attention", "kv_combine",
-    "norm_fwd", "norm_bwd", "decode_gateup", "decode_down", "decode_combine", "sample"};
+    "norm_fwd", "norm_bwd", "decode_router", "decode_gateup", "decode_down", "decode_combine", "sample"};
 
 }  // namespace
 

@@ -44,6 +44,7 @@ enum KernelId {
   K_KV_COMBINE,
   K_NORM_FWD,
   K_NORM_BWD,
+  K_DECODE_ROUTER,
   K_DECODE_GATEUP,
   K_DECODE_DOWN,
   K_DECODE_COMBINE,
