@@ -9,8 +9,7 @@
 // with x = logit log2(e) / temperature in fp64 and N = floor of the row's
 // largest x, a weight is the integer rint(2^(x - N) 2^42), at most 2^43, and
 // sums of up to 2^20 of them are exact in 64 bits (weights under 2^-44 of the
-// largest are 0).  2^f is a Taylor polynomial about f = 1/2: its remainder of
-// 6e-15 is below the rounding to an integer.
+// largest are 0).
 //
 // Two launches.  The first reads the logits once, chunk by chunk, and leaves
 // what a row's choice needs of each chunk; the second, a workgroup per row,
@@ -31,19 +30,29 @@ typedef unsigned long long u64;
 constexpr int kGroup = 16, kPiece = kGroup * kWave;  // elements of a lane and of a wave
 constexpr int kChunkWaves = 8, kChunk = kChunkWaves * kPiece;
 constexpr int kOctaves = 44, kPerOctave = 8, kBins = kOctaves * kPerOctave;
-constexpr int kUnit = 42;      // weights are in units of 2^-42 of 2^N
-constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / kWave;
-constexpr int kList = 4096;    // candidates held in LDS
-constexpr int kFastK = 2048;   // the top_k that the list is for
-constexpr int kHeldMax = 8;    // largest keys per thread in the search for the k-th
+constexpr int kUnit = 42;  // weights are in units of 2^-42 of 2^N
+constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
+constexpr int kList = 4096;   // candidates held in LDS
+constexpr int kMine = kList / kRowThreads;
+constexpr int kFastK = 2048;  // the top_k that the list is for
+constexpr int kFine = 1024;   // parts of the list's range
+constexpr int kHeldPieces = 256, kHeldGroups = kHeldPieces * kWave;  // of a row whose groups' keys are held in LDS
+constexpr int kMaxParts = 8;
 
-// What the first launch leaves of a row, `chunks` of each.
+// Workgroups per row of the second launch: as many as leave the chip's 256
+// compute units one each.
+__host__ __device__ inline int parts_of(int B) { return B > 128 ? 1 : B > 32 ? 256 / B : kMaxParts; }
+
+// What the first launch leaves of a row, `chunks` of each; and what a row's
+// workgroups leave each other.
 struct RowStats {
   u64* best;       // [chunks] key << 32 | ~index of the largest
   double* ref;     // [chunks] N of the chunk
   u64* piece_sum;  // [chunks * 8] weights of a piece, in the chunk's unit
   uint32_t* top;   // [chunks * 512] largest key of a group
   u64* bins;       // [chunks * kBins] weights by eighths of an octave below 2^(N + 1)
+  int32_t* done;   // [1 + kMaxParts] workgroups that are through, their candidates
+  u64* lists;      // [parts, kList]
 };
 
 __host__ __device__ inline int chunks_of(int V) { return (V + 7 + kChunk - 1) / kChunk; }  // a row may begin 7 elements into a vector
@@ -63,11 +72,18 @@ struct Ws {
     p += n * kChunkWaves * 8;
     r.bins = reinterpret_cast<u64*>(p) + at * kBins;
     p += n * kBins * 8;
+    r.lists = reinterpret_cast<u64*>(p) + static_cast<size_t>(b) * parts_of(B) * kList;
+    p += static_cast<size_t>(lists(B)) * kList * 8;
     r.top = reinterpret_cast<uint32_t*>(p) + at * (kChunkWaves * kWave);
+    p += n * kChunkWaves * kWave * 4;
+    r.done = reinterpret_cast<int32_t*>(p) + static_cast<size_t>(b) * (1 + kMaxParts);
     return r;
   }
+  // Lists of up to B rows, B parts_of(B) at its largest: more rows never need less room.
+  __host__ __device__ static int lists(int B) { return B > 256 ? B : B > 32 ? 256 : kMaxParts * B; }
   static size_t bytes(int B, int chunks) {
-    return static_cast<size_t>(B) * chunks * (8 + 8 + kChunkWaves * 8 + kBins * 8 + kChunkWaves * kWave * 4);
+    return static_cast<size_t>(B) * chunks * (8 + 8 + kChunkWaves * 8 + kBins * 8 + kChunkWaves * kWave * 4) +
+           static_cast<size_t>(lists(B)) * kList * 8 + static_cast<size_t>(B) * (1 + kMaxParts) * 4;
   }
 };
 
@@ -80,6 +96,8 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((key >> 31) ? (key & 0x7fffffffu) : ~key);
 }
+
+constexpr uint32_t kInfKey = 0xff800000u;  // of infinity, the largest
 
 // A row's settings.
 struct Settings {
@@ -105,28 +123,29 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int b) {
 // x of a value; infinity is past every finite one, so that it alone has weight.
 __device__ __forceinline__ double x_of(float v, double c) { return v == INFINITY ? 1e300 : static_cast<double>(v) * c; }
 
-// The integer weight of x <= N + 1.
-__device__ __forceinline__ u64 weight(double x, double N) {
-  const double n = floor(x), d = N - n;
-  if (!(d <= kUnit + 1.0)) return 0;
-  const double y = (x - n - 0.5) * 0.6931471805599453;
-  double p = 1.0 / 39916800;
-  p = fma(p, y, 1.0 / 3628800);
-  p = fma(p, y, 1.0 / 362880);
-  p = fma(p, y, 1.0 / 40320);
-  p = fma(p, y, 1.0 / 5040);
-  p = fma(p, y, 1.0 / 720);
-  p = fma(p, y, 1.0 / 120);
-  p = fma(p, y, 1.0 / 24);
-  p = fma(p, y, 1.0 / 6);
-  p = fma(p, y, 0.5);
-  p = fma(p, y, 1.0);
-  p = fma(p, y, 1.0);
-  const int e = kUnit - static_cast<int>(d);
-  const double scale = __longlong_as_double(static_cast<long long>(1023 + e) << 52) * 1.4142135623730951;
-  // the sum's unit is 1: its low bits are the rounded integer
-  return static_cast<u64>(__double_as_longlong(fma(p, scale, 0x1p52))) & ((1ull << 52) - 1);
-}
+// The integer weight of x < N + 1: 2^f, |f| <= 1/2, by the polynomial that
+// meets it in the ten Chebyshev points (2^-45.6 of it off at most), times a
+// power of two; the sum with 2^52 has the rounded integer in its low bits.
+// The coefficients are made opaque so that they stay in scalar registers:
+// left to itself the compiler moves each into a vector register before its
+// step, two moves a step.
+struct Weigh {
+  double c[10];
+  __device__ __forceinline__ Weigh()
+      : c{1.0000000000000135,    0.6931471805599462,     0.2402265069564034,     0.05550410866465167,   0.009618129193934313,
+          0.0013333558200794592, 0.0001540343375125101, 1.5252672924850737e-05, 1.325964524488711e-06, 1.0205905413765595e-07} {
+#pragma unroll
+    for (int i = 0; i < 10; ++i) asm("" : "+s"(c[i]));
+  }
+  __device__ __forceinline__ u64 operator()(double x, double N) const {
+    const double n = __builtin_rint(x), f = x - n;
+    double p = c[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = fma(p, f, c[i]);
+    const double w = __builtin_ldexp(p, static_cast<int>(fmax(n - N, -100.0)) + kUnit);
+    return static_cast<u64>(__double_as_longlong(w + 0x1p52)) & ((1ull << 52) - 1);
+  }
+};
 
 // Eighth of an octave below 2^(N + 1) that x lies in.
 __device__ __forceinline__ double bin_of(double x, double N) { return 8.0 * (N + 1.0) - 1.0 - floor(8.0 * x); }
@@ -139,26 +158,35 @@ __device__ __forceinline__ u64 rescale(u64 sum, double ref, double N) {
   return i == 0 ? sum : (sum >> i) + ((sum >> (i - 1)) & 1);
 }
 
-__device__ __forceinline__ u64 wave_add(u64 v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += shfl_xor(v, m);
-  return v;
+// v plus that of another lane, within the vector ALU (through LDS, as a
+// shuffle goes, a 64-bit sum over the wave takes five times as long).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 add_from(u64 v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(v >> 32), CTRL, ROWS, 0xf, false);
+  return v + (static_cast<u64>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo));
 }
+// Sum over this lane and those below: within rows of 16 lanes by shifts of 1,
+// 2, 4, 8, then the last lane's sum of a row on to the next, of a half to the other.
+__device__ __forceinline__ u64 wave_upto(u64 v) {
+  v = add_from<0x111, 0xf>(v);
+  v = add_from<0x112, 0xf>(v);
+  v = add_from<0x114, 0xf>(v);
+  v = add_from<0x118, 0xf>(v);
+  v = add_from<0x142, 0xa>(v);
+  return add_from<0x143, 0xc>(v);
+}
+__device__ __forceinline__ u64 lane_value(u64 v, int lane) {  // `lane` is the same in every lane
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
+  return static_cast<u64>(hi) << 32 | lo;
+}
+__device__ __forceinline__ u64 wave_add(u64 v) { return lane_value(wave_upto(v), kWave - 1); }
+__device__ __forceinline__ u64 wave_before(u64 v) { return wave_upto(v) - v; }
 __device__ __forceinline__ u64 wave_most(u64 v) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) v = max(v, shfl_xor(v, m));
   return v;
-}
-// Sum over the lanes below.
-__device__ __forceinline__ u64 wave_before(u64 v) {
-  const int lane = threadIdx.x & 63;
-  u64 t = v;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const u64 o = __shfl_up(t, d, kWave);
-    if (lane >= d) t += o;
-  }
-  return t - v;
 }
 
 // A row in memory.  Element i lies at place i + skew, place 0 on 16 bytes, so
@@ -184,26 +212,29 @@ struct Row {
     if constexpr (F32) return reinterpret_cast<const float*>(at)[p];
     else return bf2f(reinterpret_cast<const bf16_t*>(at)[p]);
   }
+  // W elements from place p, a multiple of W.
+  __device__ __forceinline__ void vec(int p, float* v) const {
+    if (p >= skew && p + W <= end) {
+      const uint4 w = *reinterpret_cast<const uint4*>(at + static_cast<int64_t>(p) * (16 / W));
+      if constexpr (F32) {
+        v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+      } else {
+        v[0] = lo_bf(w.x), v[1] = hi_bf(w.x), v[2] = lo_bf(w.y), v[3] = hi_bf(w.y);
+        v[W - 4] = lo_bf(w.z), v[W - 3] = hi_bf(w.z), v[W - 2] = lo_bf(w.w), v[W - 1] = hi_bf(w.w);
+      }
+    } else {  // an end of the row: small code rather than fast
+#pragma unroll 1
+      for (int j = 0; j < W; ++j) {
+        const float t = one(p + j);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = i == j ? t : v[i];
+      }
+    }
+  }
   // This lane's group of a piece.
   __device__ __forceinline__ void load(int piece, float (&v)[kGroup]) const {
 #pragma unroll
-    for (int i = 0; i < kGroup / W; ++i) {
-      const int p = place(piece, i * W);
-      if (p >= skew && p + W <= end) {
-        const uint4 w = *reinterpret_cast<const uint4*>(at + static_cast<int64_t>(p) * (16 / W));
-        if constexpr (F32) {
-          v[i * W] = __uint_as_float(w.x), v[i * W + 1] = __uint_as_float(w.y);
-          v[i * W + 2] = __uint_as_float(w.z), v[i * W + 3] = __uint_as_float(w.w);
-        } else {
-          v[i * W] = lo_bf(w.x), v[i * W + 1] = hi_bf(w.x), v[i * W + 2] = lo_bf(w.y), v[i * W + 3] = hi_bf(w.y);
-          v[i * W + W - 4] = lo_bf(w.z), v[i * W + W - 3] = hi_bf(w.z);
-          v[i * W + W - 2] = lo_bf(w.w), v[i * W + W - 1] = hi_bf(w.w);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[i * W + j] = one(p + j);
-      }
-    }
+    for (int i = 0; i < kGroup / W; ++i) vec(place(piece, i * W), v + i * W);
   }
 };
 
@@ -216,6 +247,7 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   const RowStats st = ws.row(b);
   const Settings s = settings_of(a, b);
   const Row<F32> row(a, b);
+  const Weigh weight;
   const int piece = chunk * kChunkWaves + wave;
   float v[kGroup];
   row.load(piece, v);
@@ -236,6 +268,7 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
 #pragma unroll
   for (int w = 0; w < kChunkWaves; ++w) best = max(best, bests[w]);
   if (tid == 0) st.best[chunk] = best;
+  if (tid == 0 && chunk == 0) st.done[0] = 0;
   if (s.greedy) return;
   st.top[chunk * (kChunkWaves * kWave) + tid] = top;
   const bool summed = !s.filter_k && !s.filter_p && !s.filter_m;
@@ -246,9 +279,8 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   u64 sum = 0;
 #pragma unroll
   for (int e = 0; e < kGroup; ++e) {
-    if (key_of(v[e]) == 0) continue;
     const double x = x_of(v[e], s.c);
-    const u64 w = weight(x, N);
+    const u64 of_x = weight(x, N), w = key_of(v[e]) == 0 ? 0 : of_x;  // no branch: most elements count
     sum += w;
     if (binned && w != 0) atomicAdd(&bins[static_cast<int>(fmin(bin_of(x, N), kBins - 1.0))], w);
   }
@@ -263,57 +295,64 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
 
 // ---- second launch
 constexpr int kMaxPieces = (MOE_SAMPLE_MAX_V + 7 + kChunk - 1) / kChunk * kChunkWaves;
-static_assert(kMaxPieces <= 2 * kRowThreads, "two pieces per thread in the choice of the draw's piece");
-struct Shared {
+constexpr int kSumsPerThread = (kMaxPieces + kRowThreads - 1) / kRowThreads;
+struct alignas(16) Shared {
+  uint32_t top[kHeldGroups];    // largest keys of the groups, where the row has no more
+  uint16_t group[kHeldGroups];  // groups with candidates
   u64 list[kList];
   u64 sums[kMaxPieces];  // of the pieces
-  u64 bins[kBins];
-  u64 waves[kRowWaves];
+  u64 bins[kFine];
+  u64 waves[2][kRowWaves];
   u64 found, found2;
-  int count;
+  int count, groups;
 };
 
 // Of a workgroup's values, in thread order: the sum before each, and of all.
-__device__ __forceinline__ u64 block_before(u64 v, u64* waves, u64& all) {
+// Two sets of sums in turn: a set is written again only after the barrier of
+// the call between, hence one barrier a call.
+__device__ __forceinline__ u64 block_before(u64 v, u64 (&waves)[2][kRowWaves], int& turn, u64& all) {
   const int wave = threadIdx.x >> 6;
-  u64 t = wave_before(v);
-  __syncthreads();  // `waves` has been read
-  if ((threadIdx.x & 63) == 63) waves[wave] = t + v;
+  const u64 upto = wave_upto(v);
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 63) waves[turn][wave] = upto;
   __syncthreads();
+  u64 t = upto - v;
   all = 0;
 #pragma unroll
   for (int w = 0; w < kRowWaves; ++w) {
-    if (w < wave) t += waves[w];
-    all += waves[w];
+    if (w < wave) t += waves[turn][w];
+    all += waves[turn][w];
   }
   return t;
 }
-__device__ __forceinline__ u64 block_add(u64 v, u64* waves) {
-  v = wave_add(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-  __syncthreads();
-  u64 t = 0;
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) t += waves[w];
-  return t;
+__device__ __forceinline__ u64 block_add(u64 v, u64 (&waves)[2][kRowWaves], int& turn) {
+  u64 all;
+  block_before(v, waves, turn, all);
+  return all;
 }
 
-// Sorts list[0 .. n) descending (bitonic, padded with zeros).  Ends with a barrier.
-__device__ void sort_list(u64* list, int n) {
+// Sorts list[0 .. n) descending (bitonic, padded with zeros).  Ends with a
+// barrier.  Exchanges over up to 64 entries stay within the 128 entries that a
+// wave has in hand, and a wave's LDS accesses are in order: no barrier there.
+__device__ __forceinline__ void sort_list(u64* list, int n) {
   int size = 2;
   while (size < n) size <<= 1;
   for (int i = n + threadIdx.x; i < size; i += kRowThreads) list[i] = 0;
   __syncthreads();
+#pragma unroll 1
   for (int k = 2; k <= size; k <<= 1)
+#pragma unroll 1
     for (int j = k >> 1; j > 0; j >>= 1) {
+      if (j > kWave || (j == kWave && k > 2 * kWave)) __syncthreads();
+#pragma unroll 1
       for (int i = threadIdx.x; i < size / 2; i += kRowThreads) {
         const int lo = (i & (j - 1)) | ((i & ~(j - 1)) << 1), hi = lo | j;
         const u64 p = list[lo], q = list[hi];
         if ((p < q) == ((lo & k) == 0)) list[lo] = q, list[hi] = p;
       }
-      __syncthreads();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+  __syncthreads();
 }
 
 __device__ __forceinline__ u64 part_of(double share, u64 all) {  // floor(share all)
@@ -323,51 +362,80 @@ __device__ __forceinline__ u64 part_of(double share, u64 all) {  // floor(share 
 template <bool F32>
 struct Choice {
   const SampleArgs& a;
-  const int b, pieces, lane, wave;
+  const int b, part, parts, pieces, lane, wave;
   const Settings s;
   const Row<F32> row;
   const RowStats st;
   Shared& sh;
-  int32_t first;              // the largest element,
-  double x_most, N, x_least;  // its x, the floor of that, the least x that min_p keeps
+  const Weigh weight;
+  int turn = 0;      // of the block's sums
+  int32_t first;     // the largest element,
+  double x_most, N;  // its x, the floor of that
+  u64 min_rank;      // what min_p keeps is of this rank at least
 
-  __device__ Choice(const SampleArgs& a_, const Ws& ws, Shared& sh_)
-      : a(a_), b(blockIdx.x), pieces(ws.chunks * kChunkWaves), lane(threadIdx.x & 63), wave(threadIdx.x >> 6),
-        s(settings_of(a_, b)), row(a_, b), st(ws.row(b)), sh(sh_) {}
+  __device__ __forceinline__ Choice(const SampleArgs& a_, const Ws& ws, Shared& sh_)
+      : a(a_), b(blockIdx.y), part(blockIdx.x), parts(gridDim.x), pieces(ws.chunks * kChunkWaves), lane(threadIdx.x & 63),
+        wave(threadIdx.x >> 6), s(settings_of(a_, b)), row(a_, b), st(ws.row(b)), sh(sh_) {}
+
+  __device__ __forceinline__ u64 before(u64 v, u64& all) { return block_before(v, sh.waves, turn, all); }
+  __device__ __forceinline__ u64 total(u64 v) { return block_add(v, sh.waves, turn); }
 
   // One element: its key and index, larger is earlier in the order.
   __device__ __forceinline__ u64 rank_of(float v, int place) const {
     return static_cast<u64>(key_of(v)) << 32 | static_cast<uint32_t>(~(place - row.skew));
   }
   __device__ __forceinline__ double x_at(u64 rank) const { return x_of(value_of(static_cast<uint32_t>(rank >> 32)), s.c); }
+  __device__ __forceinline__ int piece_of(u64 rank) const {
+    return static_cast<int>((~static_cast<uint32_t>(rank) + row.skew) / kPiece);
+  }
 
-  __device__ void write(int32_t token, double logprob) const {
+  __device__ __forceinline__ void write(int32_t token, double logprob) const {
     a.token[b] = token;
     if (a.logprob != nullptr) a.logprob[b] = static_cast<float>(logprob);
   }
-  __device__ void write(int32_t token, double x, u64 all) const {
-    write(token, (x - N) * 0.6931471805599453 - log(static_cast<double>(all) * 0x1p-42));
+  // By one lane, the token of place p and value v.
+  __device__ __forceinline__ void write(int p, float v, u64 all) const {
+    write(p - row.skew, (x_of(v, s.c) - N) * 0.6931471805599453 - log(static_cast<double>(all) * 0x1p-42));
   }
   // The draw: the running sum that the token's has to pass.
   __device__ __forceinline__ u64 draw(u64 all) const {
     const double u = a.u[b];
     return u > 0.0 ? min(part_of(u, all), all - 1) : 0;
   }
-
-  // Elements of a piece that stay: rank >= least and x >= x_least.
-  __device__ __forceinline__ u64 kept(float v, int place, u64 least) const {
-    if (key_of(v) == 0 || rank_of(v, place) < least) return 0;
-    const double x = x_of(v, s.c);
-    return s.filter_m && x < x_least ? 0 : weight(x, N);
+  // The sum that the shortest prefix reaches.
+  __device__ __forceinline__ u64 needed(u64 all) const {
+    return s.p > 0.0 ? max(static_cast<u64>(ceil(s.p * static_cast<double>(all))), 1ull) : 1;
   }
 
+  // Weight of an element that stays: rank >= least.
+  __device__ __forceinline__ u64 kept(float v, int place, u64 least) const {
+    const u64 w = weight(x_of(v, s.c), N);
+    return key_of(v) == 0 || rank_of(v, place) < least ? 0 : w;
+  }
+
+  // The least key whose x `in` takes, which takes all larger ones: a wave
+  // compares 64 at a time.
+  template <class In>
+  __device__ __forceinline__ uint32_t least_key(In in) const {
+    uint32_t base = 0;
+#pragma unroll 1
+    for (int shift = 26; shift >= 0; shift -= shift == 2 ? 2 : 6) {
+      const uint32_t at = base + (static_cast<uint32_t>(lane) << shift) + ((1u << shift) - 1u);  // a block's last
+      const u64 hit = __ballot(at > kInfKey || in(x_of(value_of(at), s.c)));
+      base += static_cast<uint32_t>(__builtin_ctzll(hit | 1ull << 63)) << shift;
+    }
+    return base;
+  }
+
+  // ---- the draw in index order
   // The token of the running sum `r` within a piece, by the calling wave.
-  __device__ void pick(int piece, u64 r, u64 least, u64 all) const {
+  __device__ __forceinline__ void pick(int piece, u64 r, u64 least, u64 all) const {
     float v[kGroup];
     row.load(piece, v);
     constexpr int W = Row<F32>::W;
+    int token = -1;
+    float value = 0.0f;
     bool done = false;
-    u64 last = 0;  // the last element with weight, should rounding have left r past them all
 #pragma unroll
     for (int i = 0; i < kGroup / W; ++i) {
       u64 w[W], t = 0;
@@ -375,261 +443,507 @@ struct Choice {
       for (int j = 0; j < W; ++j) {
         w[j] = kept(v[i * W + j], row.place(piece, i * W + j), least);
         t += w[j];
-        if (w[j] != 0)
-          last = max(last, static_cast<u64>(row.place(piece, i * W + j) + 1) << 32 | key_of(v[i * W + j]));
       }
-      u64 before = wave_before(t);
-      const u64 total = __shfl(before + t, kWave - 1, kWave);
-      if (!done && r < total) {
+      u64 at = wave_before(t);
+      const u64 sum = lane_value(at + t, kWave - 1);
+      if (!done && r < sum) {
         done = true;
-        if (before <= r && r < before + t)
 #pragma unroll
-          for (int j = 0; j < W; ++j) {
-            if (before <= r && r < before + w[j])
-              write(row.place(piece, i * W + j) - row.skew, x_of(v[i * W + j], s.c), all);
-            before += w[j];
+        for (int j = 0; j < W; ++j) {
+          if (at <= r && r < at + w[j]) {
+            token = row.place(piece, i * W + j);
+            value = v[i * W + j];
           }
+          at += w[j];
+        }
       }
-      if (!done) r -= total;
+      if (!done) r -= sum;
     }
-    if (!done) {
-      last = wave_most(last);
-      if (lane == 0) {
-        if (last != 0) write(static_cast<int>(last >> 32) - 1 - row.skew, x_of(value_of(static_cast<uint32_t>(last)), s.c), all);
-        else write(first, x_most, all);
-      }
+    if (!done) {  // rounding of a chunk's sums has left r past them all: the largest
+      token = lane == 0 ? first + row.skew : -1;
+      value = row.one(first + row.skew);
     }
+    if (token >= 0) write(token, value, all);
   }
 
   // sums[0 .. pieces) hold the pieces' weights: finds the draw's piece and picks there.
-  __device__ void pick_by_sums(u64 least) {
+  __device__ __forceinline__ void pick_by_sums(u64 least) {
     __syncthreads();
-    u64 mine[2], all;
-    const int i0 = threadIdx.x * 2;
-    for (int j = 0; j < 2; ++j) mine[j] = i0 + j < pieces ? sh.sums[i0 + j] : 0;
-    u64 before = block_before(mine[0] + mine[1], sh.waves, all);
+    u64 mine[kSumsPerThread], t = 0, all;
+    const int i0 = threadIdx.x * kSumsPerThread;
+#pragma unroll
+    for (int j = 0; j < kSumsPerThread; ++j) {
+      mine[j] = i0 + j < pieces ? sh.sums[i0 + j] : 0;
+      t += mine[j];
+    }
+    u64 at = before(t, all);
     const u64 r = draw(all);
-    for (int j = 0; j < 2; ++j) {
-      if (before <= r && r < before + mine[j]) {
+#pragma unroll
+    for (int j = 0; j < kSumsPerThread; ++j) {
+      if (at <= r && r < at + mine[j]) {
         sh.found = i0 + j;
-        sh.found2 = r - before;
+        sh.found2 = r - at;
       }
-      before += mine[j];
+      at += mine[j];
     }
     __syncthreads();
     if (wave == 0) pick(static_cast<int>(sh.found), sh.found2, least, all);
   }
 
-  // Weights of what stays, piece by piece; pieces without a group at least as
-  // large as `least` are not read.
-  __device__ void sum_pieces(u64 least) {
-    uint32_t key = static_cast<uint32_t>(least >> 32);
-    for (int piece = wave; piece < pieces; piece += kRowWaves) {
-      const uint32_t top = st.top[piece * kWave + lane];
-      const bool may = top != 0 && top >= key && !(s.filter_m && x_of(value_of(top), s.c) < x_least);
+  // ---- groups.  A row of up to kHeldPieces pieces has its groups' keys in
+  // LDS; of a longer one they are read where they are.
+  __device__ __forceinline__ bool held() const { return pieces <= kHeldPieces; }
+  __device__ __forceinline__ uint32_t top_of(int g) const { return held() ? sh.top[g] : st.top[g]; }
+
+  __device__ __forceinline__ void hold() {
+    if (!held()) return;
+    const int groups = pieces * kWave;  // a multiple of 512
+#pragma unroll 4
+    for (int g = threadIdx.x; g < groups; g += kRowThreads) sh.top[g] = st.top[g];
+    __syncthreads();
+  }
+
+  // Lists the groups whose largest key is at least lo; whether they are a
+  // quarter of all, or the row's keys are not held: then whole pieces are read.
+  __device__ __forceinline__ bool list_groups(uint32_t lo) {
+    if (!held()) return true;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.groups = 0;
+    __syncthreads();
+    const int groups = pieces * kWave;
+#pragma unroll 1
+    for (int i0 = 0; i0 < groups; i0 += 4 * kRowThreads) {
+      bool on[4];
+      u64 m[4];
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int g = i0 + i * kRowThreads + static_cast<int>(threadIdx.x);
+        const uint32_t top = g < groups ? sh.top[g] : 0;
+        on[i] = top != 0 && top >= lo;
+        m[i] = __ballot(on[i]);
+        n += __popcll(m[i]);
+      }
+      if (n == 0) continue;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&sh.groups, n);
+      at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (on[i]) sh.group[at + __popcll(m[i] & ((1ull << lane) - 1))] = static_cast<uint16_t>(i0 + i * kRowThreads + threadIdx.x);
+        at += __popcll(m[i]);
+      }
+    }
+    __syncthreads();
+    return sh.groups * 4 > groups;
+  }
+
+  // f(v, p) for the vectors v from place p on of the listed groups, spread over
+  // all threads; t, what it returned, to add(t, p).
+  template <class F, class Add>
+  __device__ __forceinline__ void each_listed(F f, Add add) {
+    constexpr int W = Row<F32>::W, kVecs = kGroup / W;
+    const int n = sh.groups * kVecs;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kRowThreads) {
+      const int g = sh.group[i / kVecs];
+      const int p = g / kWave * kPiece + i % kVecs * (kWave * W) + g % kWave * W;
+      float v[W];
+      row.vec(p, v);
+      add(f(v, p), p);
+    }
+  }
+  // The same for pieces from, from + step, ... with a group of lo or more, a wave
+  // each, and add(t, piece) by whole waves.
+  template <class F, class Add>
+  __device__ __forceinline__ void each_piece(uint32_t lo, int from, int step, F f, Add add) {
+    constexpr int W = Row<F32>::W;
+#pragma unroll 1
+    for (int piece = from + wave; piece < pieces; piece += step) {
+      const uint32_t top = top_of(piece * kWave + lane);
+      const bool on = top != 0 && top >= lo;
       u64 t = 0;
-      if (__any(may)) {
+      if (__any(on)) {
         float v[kGroup];
         row.load(piece, v);
-        if (may)
+        if (on)
 #pragma unroll
-          for (int e = 0; e < kGroup; ++e) t += kept(v[e], row.place(piece, e), least);
-        t = wave_add(t);
+          for (int e = 0; e < kGroup; e += W) t += f(v + e, row.place(piece, e));
       }
-      if (lane == 0) sh.sums[piece] = t;
+      add(t, piece);
     }
   }
 
-  // Collects what `want` says of groups that `may` says: the count, of which
-  // the first kList are in the list.
-  template <class May, class Want>
-  __device__ int collect(May may, Want want) {
-    __syncthreads();
+  __device__ __forceinline__ void clear_sums() {
+    for (int i = threadIdx.x; i < pieces; i += kRowThreads) sh.sums[i] = 0;
+  }
+
+  // Weights of what stays, by pieces.
+  __device__ __forceinline__ void sum_pieces(u64 least) {
+    each_piece(static_cast<uint32_t>(least >> 32), 0, kRowWaves,
+               [&](const float* v, int p) {
+                 u64 t = 0;
+#pragma unroll
+                 for (int e = 0; e < Row<F32>::W; ++e) t += kept(v[e], p + e, least);
+                 return t;
+               },
+               [&](u64 t, int piece) {
+                 t = wave_add(t);
+                 if (lane == 0) sh.sums[piece] = t;
+               });
+  }
+
+  __device__ __forceinline__ void put_in_list(float v, int place) {
+    const int at = atomicAdd(&sh.count, 1);
+    if (at < kList) sh.list[at] = rank_of(v, place);
+  }
+
+  // Collects the elements of keys from lo on: the count, of which the first
+  // kList are in the list.
+  __device__ __forceinline__ int collect(uint32_t lo) {
+    const bool whole = list_groups(lo);
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    for (int piece = wave; piece < pieces; piece += kRowWaves) {
-      const uint32_t top = st.top[piece * kWave + lane];
-      const bool on = top != 0 && may(top);
-      if (!__any(on)) continue;
-      float v[kGroup];
-      row.load(piece, v);
-      if (!on) continue;
+    auto f = [&](const float* v, int p) -> u64 {
 #pragma unroll
-      for (int e = 0; e < kGroup; ++e)
-        if (const uint32_t key = key_of(v[e]); key != 0 && want(key)) {
-          const int at = atomicAdd(&sh.count, 1);
-          if (at < kList) sh.list[at] = rank_of(v[e], row.place(piece, e));
-        }
-    }
+      for (int e = 0; e < Row<F32>::W; ++e)
+        if (const uint32_t key = key_of(v[e]); key != 0 && key >= lo) put_in_list(v[e], p + e);
+      return 0;
+    };
+    if (whole) each_piece(lo, 0, kRowWaves, f, [](u64, int) {});
+    else each_listed(f, [](u64, int) {});
     __syncthreads();
     return sh.count;
   }
 
-  // A key that k groups (or runs of groups) reach: at least k elements do.
-  __device__ uint32_t floor_of_kth(int k) {
-    const int groups = pieces * kWave, run = cdiv(groups, kRowThreads * kHeldMax);
-    uint32_t top[kHeldMax];
+  // Collects the elements of keys lo .. hi - 1, and sums, by pieces, the
+  // weights of those from hi on that min_p keeps.  Where whole pieces are to be
+  // read the row's workgroups share them: each leaves its pieces' sums and its
+  // list in memory, and the last to be through goes on with all of it.  -1 where
+  // this workgroup has nothing more to do.
+  __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi) {
+    const uint32_t least = max(hi, static_cast<uint32_t>(min_rank >> 32));
+    const bool whole = list_groups(lo);
+    const bool shared = whole && parts > 1;
+    if (!shared && part != 0) return -1;
+    if (threadIdx.x == 0) sh.count = 0;
+    clear_sums();
+    __syncthreads();
+    auto f = [&](const float* v, int p) {
+      u64 t = 0;
 #pragma unroll
-    for (int i = 0; i < kHeldMax; ++i) {
-      top[i] = 0;
-      for (int j = 0; j < run; ++j) {
-        const int g = (i * run + j) * kRowThreads + static_cast<int>(threadIdx.x);
-        if (g < groups) top[i] = max(top[i], st.top[g]);
+      for (int e = 0; e < Row<F32>::W; ++e) {
+        const uint32_t key = key_of(v[e]);
+        const u64 w = weight(x_of(v[e], s.c), N);
+        t += key >= least ? w : 0;
+        if (key != 0 && key >= lo && key < hi) put_in_list(v[e], p + e);
       }
+      return t;
+    };
+    if (!whole) {
+      each_listed(f, [&](u64 t, int p) {
+        if (t != 0) atomicAdd(&sh.sums[p / kPiece], t);
+      });
+      __syncthreads();
+      return sh.count;
     }
-    uint32_t kth = 0;
-    for (int bit = 31; bit >= 8; --bit) {
-      const uint32_t at = kth | 1u << bit;
-      int n = 0;
+    each_piece(lo, part * kRowWaves, parts * kRowWaves, f, [&](u64 t, int piece) {
+      t = wave_add(t);
+      if (lane != 0) return;
+      if (shared) st.piece_sum[piece] = t;
+      else sh.sums[piece] = t;
+    });
+    __syncthreads();
+    if (!shared) return sh.count;
+    const int mine = sh.count;
+    for (int i = threadIdx.x; i < min(mine, kList); i += kRowThreads) st.lists[static_cast<int64_t>(part) * kList + i] = sh.list[i];
+    if (threadIdx.x == 0) st.done[1 + part] = mine;
+    // One thread releases what all wrote before the barrier, and acquires what
+    // the others did for all: a fence by every wave writes the caches back
+    // eight times over (64 us where 64 rows share the chip).  Each wave's own
+    // stores have reached the cache that is written back by then.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+      sh.count = __hip_atomic_fetch_add(st.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (sh.count != parts - 1) return -1;
+    for (int i = threadIdx.x; i < pieces; i += kRowThreads) sh.sums[i] = st.piece_sum[i];
+    int n = 0;
+#pragma unroll 1
+    for (int p = 0; p < parts; ++p) {
+      const int here = st.done[1 + p];
+      for (int i = threadIdx.x; i < here && n + i < kList && i < kList; i += kRowThreads)
+        sh.list[n + i] = st.lists[static_cast<int64_t>(p) * kList + i];
+      n += here;
+    }
+    __syncthreads();
+    return n;
+  }
+
+  // A key that k groups (or sets of groups) reach: at least k elements do.
+  __device__ __forceinline__ uint32_t floor_of_kth(int k) {
+    const int groups = pieces * kWave;
+    if (k <= 128) {
+      // 256 sets of groups do for a small k; the first wave halves the range of keys step by step
+      uint32_t most = 0;
+#pragma unroll 4
+      for (int g = threadIdx.x; g < groups; g += kRowThreads) most = max(most, top_of(g));
+      sh.list[threadIdx.x] = most;
+      __syncthreads();
+      if (wave == 0) {
+        uint32_t top[kRowThreads / (2 * kWave)];
 #pragma unroll
-      for (int i = 0; i < kHeldMax; ++i) n += top[i] >= at ? 1 : 0;
-      if (block_add(n, sh.waves) >= static_cast<u64>(k)) kth = at;
-    }
-    return kth;
-  }
-
-  // The candidates are the list's n largest: filters them in order, draws.
-  __device__ void choose_from_list(int n, int k) {
-    sort_list(sh.list, n);
-    const int m = min(n, k), i0 = threadIdx.x * 4;
-    u64 w[4], t = 0, all;
-    double x[4];
-    for (int j = 0; j < 4; ++j) {
-      const u64 rank = i0 + j < m ? sh.list[i0 + j] : 0;
-      x[j] = rank != 0 ? x_at(rank) : -1e305;
-      w[j] = rank != 0 ? weight(x[j], N) : 0;
-      t += w[j];
-    }
-    u64 before = block_before(t, sh.waves, all);
-    const u64 need = s.filter_p ? max(part_of_up(s.p, all), 1ull) : all;
-    int stay = 0;
-    for (int j = 0; j < 4; ++j) {
-      if (i0 + j < m && w[j] != 0 && before < need && !(s.filter_m && x[j] < x_least)) ++stay;
-      before += w[j];
-    }
-    const int left = static_cast<int>(block_add(stay, sh.waves));  // a prefix: the filters go by the order
-    // the same in index order
-    u64 again[4];
-    for (int j = 0; j < 4; ++j) {
-      const u64 rank = i0 + j < left ? sh.list[i0 + j] : 0;
-      again[j] = rank << 32 | rank >> 32;  // ~index above the key
-    }
-    __syncthreads();
-    for (int j = 0; j < 4; ++j)
-      if (i0 + j < left) sh.list[i0 + j] = again[j];
-    __syncthreads();
-    sort_list(sh.list, left);
-    t = 0;
-    for (int j = 0; j < 4; ++j) {
-      again[j] = i0 + j < left ? sh.list[i0 + j] : 0;
-      x[j] = again[j] != 0 ? x_of(value_of(static_cast<uint32_t>(again[j])), s.c) : -1e305;
-      w[j] = again[j] != 0 ? weight(x[j], N) : 0;
-      t += w[j];
-    }
-    before = block_before(t, sh.waves, all);
-    const u64 r = draw(all);
-    for (int j = 0; j < 4; ++j) {
-      if (before <= r && r < before + w[j]) write(static_cast<int32_t>(~static_cast<uint32_t>(again[j] >> 32)), x[j], all);
-      before += w[j];
-    }
-  }
-
-  // ceil(share all), for a share below 1
-  static __device__ __forceinline__ u64 part_of_up(double share, u64 all) {
-    return share > 0.0 ? static_cast<u64>(ceil(share * static_cast<double>(all))) : 0;
-  }
-
-  // Rank of the last element of the shortest prefix that holds `need` of the
-  // weight, by eighths of an octave; 0 where too many elements share one.
-  __device__ u64 border_by_bins(u64& least) {
-    for (int i = threadIdx.x; i < kBins; i += kRowThreads) sh.bins[i] = 0;
-    __syncthreads();
-    const int chunks = pieces / kChunkWaves;
-    for (int i = threadIdx.x; i < chunks * kBins; i += kRowThreads) {
-      const double ref = st.ref[i / kBins];
-      const double at = i % kBins + kPerOctave * (N - ref);
-      if (at < kBins) {
-        const u64 w = rescale(st.bins[i], ref, N);
-        if (w != 0) atomicAdd(&sh.bins[static_cast<int>(at)], w);
+        for (int i = 0; i < kRowThreads / (2 * kWave); ++i)
+          top[i] = static_cast<uint32_t>(max(sh.list[2 * i * kWave + lane], sh.list[(2 * i + 1) * kWave + lane]));
+        uint32_t kth = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 10; --bit) {
+          const uint32_t at = kth | 1u << bit;
+          int n = 0;
+#pragma unroll
+          for (int i = 0; i < kRowThreads / (2 * kWave); ++i) n += __popcll(__ballot(top[i] >= at));
+          if (n >= k) kth = at;
+        }
+        if (lane == 0) sh.found = kth;
       }
+      __syncthreads();
+      return static_cast<uint32_t>(sh.found);
+    }
+    // more: a histogram of the groups, by 32nds of an octave below the largest
+    auto bin = [&](double x) { return static_cast<int>(fmin((x_most - x) * 32.0, kFine - 1.0)); };
+    clear_bins();
+    __syncthreads();
+    for (int g = threadIdx.x; g < groups; g += kRowThreads)
+      if (const uint32_t top = top_of(g); top != 0) atomicAdd(&sh.bins[bin(x_of(value_of(top), s.c))], 1ull);
+    const int at = find_bin(k);
+    return at < 0 || at == kFine - 1 ? 0 : least_key([&](double x) { return x_most - x < 1e18 && bin(x) <= at; });
+  }
+
+  __device__ __forceinline__ void clear_bins() {
+    for (int i = threadIdx.x; i < kFine; i += kRowThreads) sh.bins[i] = 0;
+  }
+  // The bin at which the bins' running sum reaches `need`, and in found2 what
+  // of it is left before that bin; -1 where it does not.  Begins and ends with a barrier.
+  __device__ __forceinline__ int find_bin(u64 need) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.found = kFine;
+    constexpr int per = kFine / kRowThreads;
+    u64 mine[per], t = 0, all;
+#pragma unroll
+    for (int j = 0; j < per; ++j) {
+      mine[j] = sh.bins[threadIdx.x * per + j];
+      t += mine[j];
+    }
+    u64 at = before(t, all);
+#pragma unroll
+    for (int j = 0; j < per; ++j) {
+      if (at < need && need <= at + mine[j]) {
+        sh.found = threadIdx.x * per + j;
+        sh.found2 = need - at;
+      }
+      at += mine[j];
     }
     __syncthreads();
-    u64 all;
-    const u64 mine = threadIdx.x < kBins ? sh.bins[threadIdx.x] : 0;
-    const u64 before = block_before(mine, sh.waves, all);
-    const u64 need = max(part_of_up(s.p, all), 1ull);
-    if (before < need && need <= before + mine) {
-      sh.found = threadIdx.x;
-      sh.found2 = need - before;
-    }
+    return sh.found == kFine ? -1 : static_cast<int>(sh.found);
+  }
+
+  // Of the list's n elements of rank >= least, all of x_top - x < kFine / scale,
+  // the rank of the last of the shortest prefix that counts (COUNT) or weighs
+  // `need`: by fine bins, then by the order within one.  `none` where they do not reach it.
+  template <bool COUNT>
+  __device__ __forceinline__ u64 border(int n, u64 least, u64 need, double x_top, double scale, u64 none) {
+    u64* const few = reinterpret_cast<u64*>(sh.top);  // the groups' keys have served
+    static_assert(sizeof(sh.top) >= sizeof(sh.list), "a bin may hold all of the list");
+    auto bin = [&](u64 rank) { return static_cast<int>(fmin(fmax((x_top - x_at(rank)) * scale, 0.0), kFine - 1.0)); };
+    auto measure = [&](u64 rank) -> u64 {
+      if constexpr (COUNT) return 1;
+      else return weight(x_at(rank), N);
+    };
     __syncthreads();
-    const double bin = static_cast<double>(sh.found);
+    clear_bins();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kRowThreads)
+      if (const u64 rank = sh.list[i]; rank >= least) atomicAdd(&sh.bins[bin(rank)], measure(rank));
+    const int at = find_bin(need);
+    if (at < 0) return none;
     const u64 rest = sh.found2;
-    const int n = collect([&](uint32_t top) { return bin_of(x_of(value_of(top), s.c), N) <= bin; },
-                          [&](uint32_t key) { return bin_of(x_of(value_of(key), s.c), N) == bin; });
-    if (n > kList || n == 0) return 0;
-    sort_list(sh.list, n);
-    u64 w[4], t = 0;
-    const int i0 = threadIdx.x * 4;
-    for (int j = 0; j < 4; ++j) {
-      w[j] = i0 + j < n ? weight(x_at(sh.list[i0 + j]), N) : 0;
-      t += w[j];
-    }
-    u64 sum, at = block_before(t, sh.waves, sum);
-    if (threadIdx.x == 0) sh.found = sh.list[n - 1];  // should rounding have left `rest` past them all
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kRowThreads)
+      if (const u64 rank = sh.list[i]; rank >= least && bin(rank) == at) few[atomicAdd(&sh.count, 1)] = rank;
     __syncthreads();
-    for (int j = 0; j < 4; ++j) {
-      if (at < rest && rest <= at + w[j]) sh.found = sh.list[i0 + j];
-      at += w[j];
+    const int m = sh.count;
+    if (threadIdx.x == 0) sh.found = none;
+    if (m <= kWave) {
+      if (wave == 0) {
+        const u64 rank = lane < m ? few[lane] : 0, w = rank != 0 ? measure(rank) : 0;
+        u64 less = 0;
+#pragma unroll 1
+        for (int j = 0; j < m; ++j) {
+          const u64 other = lane_value(rank, j), ow = lane_value(w, j);
+          less += other > rank ? ow : 0;
+        }
+        if (less < rest && rest <= less + w) sh.found = rank;
+      }
+    } else {
+      sort_list(few, m);
+      const int i0 = threadIdx.x * kMine;
+      u64 t = 0, all;
+#pragma unroll 1
+      for (int j = i0; j < min(i0 + kMine, m); ++j) t += measure(few[j]);
+      u64 less = before(t, all);
+#pragma unroll 1
+      for (int j = i0; j < min(i0 + kMine, m); ++j) {
+        const u64 w = measure(few[j]);
+        if (less < rest && rest <= less + w) sh.found = few[j];
+        less += w;
+      }
     }
     __syncthreads();
-    least = sh.found;
-    return least;
+    return sh.found;
+  }
+  // The weights of the list's elements of rank >= least, to their pieces' sums.
+  __device__ __forceinline__ void add_to_sums(int n, u64 least) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kRowThreads)
+      if (const u64 rank = sh.list[i]; rank >= least) atomicAdd(&sh.sums[piece_of(rank)], weight(x_at(rank), N));
   }
 
-  // Count or weight of the elements of rank >= at (and >= least).
-  template <bool COUNT>
-  __device__ u64 measure(u64 at) {
-    const uint32_t key = static_cast<uint32_t>(at >> 32);
-    u64 t = 0;
-    for (int piece = wave; piece < pieces; piece += kRowWaves) {
-      const uint32_t top = st.top[piece * kWave + lane];
-      const bool may = top != 0 && top >= key;
-      if (!__any(may)) continue;
-      float v[kGroup];
-      row.load(piece, v);
-      if (!may) continue;
-#pragma unroll
-      for (int e = 0; e < kGroup; ++e)
-        if (key_of(v[e]) != 0 && rank_of(v[e], row.place(piece, e)) >= at) t += COUNT ? 1 : weight(x_of(v[e], s.c), N);
+  // The candidates are the list's n largest, of keys from lo on: filters them, draws.
+  __device__ __forceinline__ void choose_from_list(int n, int k, uint32_t lo) {
+    const double x_lo = lo != 0 ? x_of(value_of(lo), s.c) : x_most - kOctaves, span = x_most - x_lo;
+    const double scale = span > 0.0 && span < 1e18 ? kFine / span : 0.0;
+    u64 least = n > k ? border<true>(n, 0, k, x_most, scale, 0) : 0;
+    if (s.filter_p) {
+      u64 t = 0;
+#pragma unroll 1
+      for (int i = threadIdx.x; i < n; i += kRowThreads)
+        if (const u64 rank = sh.list[i]; rank >= least) t += weight(x_at(rank), N);
+      least = max(least, border<false>(n, least, needed(total(t)), x_most, scale, 0));
     }
-    return block_add(t, sh.waves);
+    least = max(least, min_rank);
+    clear_sums();
+    __syncthreads();
+    add_to_sums(n, least);
+    pick_by_sums(least);
   }
-  // The largest rank whose elements measure `need`, bit by bit: for what the
-  // lists do not hold (thousands of equal logits, a top_k of thousands).  A
-  // row of up to 16 pieces stays in registers meanwhile.
+
+  // The same for up to a wave of candidates, by the first wave alone: places
+  // and sums in the order, then in index order, from one comparison with each of
+  // the others.
+  __device__ __forceinline__ void choose_from_few(int n, int k) {
+    if (wave != 0) return;
+    const u64 rank = lane < n ? sh.list[lane] : 0;
+    u64 w = rank != 0 ? weight(x_at(rank), N) : 0;
+    int place = 0;
+    u64 less = 0;
+#pragma unroll 1
+    for (int j = 0; j < n; j += 4)  // lanes from n on hold zeros
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u64 other = lane_value(rank, j + i), ow = lane_value(w, j + i);
+        if (other > rank) {
+          ++place;
+          less += ow;
+        }
+      }
+    if (place >= k) w = 0;
+    if (s.filter_p && less >= needed(wave_add(w))) w = 0;
+    if (rank < min_rank) w = 0;
+    const u64 all = wave_add(w), r = draw(all);
+    const uint32_t index = ~static_cast<uint32_t>(rank);
+    less = 0;
+#pragma unroll 1
+    for (int j = 0; j < n; j += 4)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u64 ow = lane_value(w, j + i);
+        if (static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(index), j + i)) < index) less += ow;
+      }
+    if (less <= r && r < less + w)
+      write(static_cast<int>(index) + row.skew, value_of(static_cast<uint32_t>(rank >> 32)), all);
+  }
+
+  // The eighth of an octave in which the shortest prefix ends that holds top_p
+  // of the weight: its keys lo .. hi - 1, and the weight that is needed of it.
+  __device__ __forceinline__ u64 border_bin(uint32_t& lo, uint32_t& hi, int& bin) {
+    const int chunks = pieces / kChunkWaves;
+    __syncthreads();
+    clear_bins();
+    __syncthreads();
+    // a thread per bin, four chunks' on their way at a time
+    if (threadIdx.x < kBins) {
+      u64 t = 0;
+#pragma unroll 1
+      for (int c = 0; c < chunks; c += 4) {
+        u64 w[4];
+        double ref[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ref[j] = c + j < chunks ? st.ref[c + j] : -1e305;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const double from = static_cast<int>(threadIdx.x) - kPerOctave * (N - ref[j]);
+          w[j] = from >= 0.0 ? st.bins[static_cast<int64_t>(c + j) * kBins + static_cast<int>(from)] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t += rescale(w[j], ref[j], N);
+      }
+      sh.bins[threadIdx.x] = t;
+    }
+    __syncthreads();
+    u64 t = 0;
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads) t += sh.bins[i];
+    bin = find_bin(needed(total(t)));
+    const double at = bin;
+    lo = least_key([&](double x) { return bin_of(x, N) <= at; });
+    hi = least_key([&](double x) { return bin_of(x, N) < at; });
+    return sh.found2;
+  }
+
+  // ---- what the lists do not hold (thousands of equal logits, a top_k of
+  // thousands).  Count or weight of the elements of rank >= at.
   template <bool COUNT>
-  __device__ u64 search(u64 need) {
+  __device__ __forceinline__ u64 measure(u64 at) {
+    u64 t = 0;
+    each_piece(static_cast<uint32_t>(at >> 32), 0, kRowWaves,
+               [&](const float* v, int p) {
+                 u64 n = 0;
+#pragma unroll
+                 for (int e = 0; e < Row<F32>::W; ++e)
+                   if (key_of(v[e]) != 0 && rank_of(v[e], p + e) >= at) n += COUNT ? 1 : weight(x_of(v[e], s.c), N);
+                 return n;
+               },
+               [&](u64 n, int) { t += n; });
+    return total(t);
+  }
+  // The largest rank whose elements measure `need`, bit by bit.  A row of up
+  // to 8 pieces stays in registers meanwhile.
+  template <bool COUNT>
+  __device__ __forceinline__ u64 search(u64 need) {
     u64 at = 0;
     if (pieces <= kRowWaves) {
       float v[kGroup];
       u64 rank[kGroup], w[kGroup];
-      if (wave < pieces) row.load(wave, v);
+      row.load(wave, v);
 #pragma unroll
       for (int e = 0; e < kGroup; ++e) {
         const bool on = wave < pieces && key_of(v[e]) != 0;
         rank[e] = on ? rank_of(v[e], row.place(wave, e)) : 0;
         w[e] = !on ? 0 : COUNT ? 1 : weight(x_of(v[e], s.c), N);
       }
+#pragma unroll 1
       for (int bit = 63; bit >= 0; --bit) {
         const u64 next = at | 1ull << bit;
         u64 t = 0;
 #pragma unroll
         for (int e = 0; e < kGroup; ++e) t += rank[e] >= next ? w[e] : 0;
-        if (block_add(t, sh.waves) >= need) at = next;
+        if (total(t) >= need) at = next;
       }
       return at;
     }
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 next = at | 1ull << bit;
       if (measure<COUNT>(next) >= need) at = next;
@@ -637,13 +951,15 @@ struct Choice {
     return at;
   }
 
-  __device__ void run() {
+  __device__ __forceinline__ void run() {
     // the row's largest
     u64 best = 0;
     for (int i = lane; i < pieces / kChunkWaves; i += kWave) best = max(best, st.best[i]);
     best = wave_most(best);
     const uint32_t most = static_cast<uint32_t>(best >> 32);
     first = static_cast<int32_t>(~static_cast<uint32_t>(best));
+    const bool alone = s.greedy || most == 0 || s.filter_k || !(s.filter_p || s.filter_m);
+    if (alone && part != 0) return;
     if (most == 0) {  // nothing to take
       if (threadIdx.x == 0) write(-1, -INFINITY);
       return;
@@ -654,28 +970,56 @@ struct Choice {
     }
     x_most = x_of(value_of(most), s.c);
     N = floor(x_most);
-    x_least = s.filter_m ? x_most + log2(s.m) : 0.0;
-    if (!s.filter_k && !s.filter_p && !s.filter_m) {
+    min_rank = 0;
+    if (s.filter_m) {
+      const double x_least = x_most + log2(s.m);
+      min_rank = static_cast<u64>(least_key([&](double x) { return x >= x_least; })) << 32;
+    }
+    u64 least = 0;
+    if (s.filter_k) {
+      hold();
+      if (s.k <= kFastK) {
+        const uint32_t lo = floor_of_kth(s.k);
+        const int n = collect(lo);
+        if (n <= kWave) {
+          choose_from_few(n, s.k);
+          return;
+        }
+        if (n <= kList) {
+          choose_from_list(n, s.k, lo);
+          return;
+        }
+      }
+      least = search<true>(s.k);
+      if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
+    } else if (s.filter_p) {
+      hold();
+      uint32_t lo, hi;
+      int bin;
+      const u64 need = border_bin(lo, hi, bin);
+      const int n = collect_and_sum(lo, hi);
+      if (n < 0) return;
+      if (n > 0 && n <= kList) {
+        least = max(border<false>(n, 0, need, N + 1.0 - bin * (1.0 / kPerOctave), kFine * kPerOctave, static_cast<u64>(lo) << 32),
+                    min_rank);
+        add_to_sums(n, least);
+        pick_by_sums(least);
+        return;
+      }
+      least = search<false>(needed(measure<false>(0)));
+    } else if (s.filter_m) {
+      hold();
+      const uint32_t lo = static_cast<uint32_t>(min_rank >> 32);
+      if (collect_and_sum(lo, lo) < 0) return;
+      pick_by_sums(min_rank);
+      return;
+    } else {
       for (int i = threadIdx.x; i < pieces; i += kRowThreads)
         sh.sums[i] = rescale(st.piece_sum[i], st.ref[i / kChunkWaves], N);
       pick_by_sums(0);
       return;
     }
-    u64 least = 0;
-    if (s.filter_k) {
-      if (s.k <= kFastK) {
-        const uint32_t at = floor_of_kth(s.k);
-        const int n = collect([&](uint32_t top) { return top >= at; }, [&](uint32_t key) { return key >= at; });
-        if (n <= kList) {
-          choose_from_list(n, s.k);
-          return;
-        }
-      }
-      least = search<true>(s.k);
-      if (s.filter_p) least = max(least, search<false>(max(part_of_up(s.p, measure<false>(least)), 1ull)));
-    } else if (s.filter_p && border_by_bins(least) == 0) {
-      least = search<false>(max(part_of_up(s.p, measure<false>(0)), 1ull));
-    }
+    least = max(least, min_rank);
     sum_pieces(least);
     pick_by_sums(least);
   }
@@ -696,10 +1040,10 @@ hipError_t launch_sample(const SampleArgs& a, void* base, hipStream_t s) {
   TraceScope trace_scope(K_SAMPLE, s);
   if (a.fp32) {
     hipLaunchKernelGGL(k_sample_chunks<true>, dim3(ws.chunks, a.B), dim3(kChunkWaves * kWave), 0, s, a, ws);
-    hipLaunchKernelGGL(k_sample_rows<true>, dim3(a.B), dim3(kRowThreads), 0, s, a, ws);
+    hipLaunchKernelGGL(k_sample_rows<true>, dim3(parts_of(a.B), a.B), dim3(kRowThreads), 0, s, a, ws);
   } else {
     hipLaunchKernelGGL(k_sample_chunks<false>, dim3(ws.chunks, a.B), dim3(kChunkWaves * kWave), 0, s, a, ws);
-    hipLaunchKernelGGL(k_sample_rows<false>, dim3(a.B), dim3(kRowThreads), 0, s, a, ws);
+    hipLaunchKernelGGL(k_sample_rows<false>, dim3(parts_of(a.B), a.B), dim3(kRowThreads), 0, s, a, ws);
   }
   return hipGetLastError();
 }
