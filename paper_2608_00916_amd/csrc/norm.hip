@@ -26,9 +26,9 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
   return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
-// A row belongs to WAVES waves, VEC 16-byte vectors per lane, so a row of up
-// to 2048 columns is one wave's (no barrier), one of up to 8192 four waves'
-// and the longest, 32768, sixteen waves'.
+// A row belongs to WAVES waves, VEC 16-byte vectors per lane: in the forward a
+// row of up to 2048 columns is one wave's (no barrier), one of up to 8192 four
+// waves' and the longest, 32768, sixteen waves'.
 template <int WAVES>
 constexpr int kRowThreads = WAVES * kWave;
 // Waves of a workgroup: several rows where a row is one wave's.
@@ -142,24 +142,33 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kFwdRows<WAVES>) void k_norm_fw
 //   dx = s (g - n mean(g n)) + dh,   dw = sum_t dy n.
 // Both means of a row come from one pass over its registers.  A workgroup
 // takes rows blockIdx.x, + gridDim.x, ... (times its rows at a time) and keeps
-// its share of dw in registers; the shares are added in a fixed order by
-// k_norm_dw, so dw does not depend on timing.
+// its share of dw in registers, or in LDS for rows of over 16384, whose
+// registers are full; the shares are added in a fixed order by k_norm_dw, so
+// dw does not depend on timing.  Few registers per lane are what counts:
+// rows of 2048 by one wave of four vectors a lane (210 registers, two waves per
+// SIMD) took 36 us at 8192 x 2048, the adding of the shares included, four
+// waves of one vector 26 (5.2 TB/s of what is read and written; a copy reaches
+// 5.4, the forward 6.5).
 template <int WAVES, int VEC>
 __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bwd(NormBwd a) {
   constexpr int ROWS = kBwdRows<WAVES>, RT = kRowThreads<WAVES>;
   __shared__ float2 sums[2][ROWS][WAVES];
-  extern __shared__ float dws[];  // H floats where a workgroup has more than one row at a time
+  constexpr bool kInLds = VEC > 2;
+  extern __shared__ float dws[];  // H floats where a workgroup has more than one row at a time, or kInLds
   const int in_row = threadIdx.x % RT, wave = in_row >> 6, slot = threadIdx.x / RT;
   const int H = a.H;
   const float inv_h = 1.0f / static_cast<float>(H);
-  float acc[VEC][8];
+  float acc[kInLds ? 1 : VEC][8];
   uint4 wv[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
     const int c = (i * RT + in_row) * 8;
     wv[i] = c < H ? *reinterpret_cast<const uint4*>(a.w + c) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = 0.0f;
+    for (int j = 0; j < 8; ++j) {  // LDS: a lane's own entries, side by side with its neighbours': no barrier
+      if constexpr (!kInLds) acc[i][j] = 0.0f;
+      else dws[(i * 8 + j) * RT + in_row] = 0.0f;
+    }
   }
   int turn = 0;
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * ROWS; base < a.T; base += static_cast<int64_t>(gridDim.x) * ROWS) {
@@ -172,7 +181,7 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
       const bool in = on && c < H;
       hv[i] = in ? *reinterpret_cast<const uint4*>(a.h + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
       dv[i] = in ? *reinterpret_cast<const uint4*>(a.dy + row * a.lddy + c) : make_uint4(0, 0, 0, 0);
-      uv[i] = in && a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
+      if constexpr (!kInLds) uv[i] = in && a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
     }
     float sq = 0.0f, gh = 0.0f;
 #pragma unroll
@@ -211,10 +220,13 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
       unpack8(hv[i], h);
       unpack8(dv[i], d);
       unpack8(wv[i], w);
+      if constexpr (kInLds)  // no registers to hold it meanwhile
+        uv[i] = a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
       unpack8(uv[i], u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        acc[i][j] = fmaf(d[j], h[j] * s, acc[i][j]);
+        float& sum = kInLds ? dws[(i * 8 + j) * RT + in_row] : acc[kInLds ? 0 : i][j];
+        sum = fmaf(d[j], h[j] * s, sum);
         u[j] = fmaf(s, fmaf(-h[j], c1, d[j] * w[j]), u[j]);
       }
       *reinterpret_cast<uint4*>(a.dx + row * H + c) = pack8(u);
@@ -239,8 +251,11 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
     for (int i = 0; i < VEC; ++i) {
       const int c = (i * RT + in_row) * 8;
       if (c >= H) continue;
-      *reinterpret_cast<float4*>(part + c) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-      *reinterpret_cast<float4*>(part + c + 4) = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = kInLds ? dws[(i * 8 + j) * RT + in_row] : acc[kInLds ? 0 : i][j];
+      *reinterpret_cast<float4*>(part + c) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(part + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
     }
   }
 }
@@ -255,7 +270,7 @@ __global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ part
   const int per = cdiv(n, 16), first = run * per, last = min(n, first + per);
   float t = 0.0f;
   if (c < H) {
-#pragma unroll 8
+#pragma unroll 16
     for (int i = first; i < last; ++i) t += part[static_cast<int64_t>(i) * H + c];
   }
   red[run][lane] = t;
@@ -268,8 +283,9 @@ __global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ part
   else static_cast<bf16_t*>(dw)[c] = f2bf(t);
 }
 
-// Waves of a row by its length.
-int row_waves(int H) { return H <= 2048 ? 1 : H <= 8192 ? 4 : 16; }
+// Waves of a row by its length: forward and backward.
+int fwd_waves(int H) { return H <= 2048 ? 1 : H <= 8192 ? 4 : 16; }
+int bwd_waves(int H) { return H <= 1024 ? 1 : H <= 4096 ? 4 : 16; }
 
 template <int WAVES, int VEC>
 void start_fwd(const NormFwd& a, hipStream_t s) {
@@ -280,46 +296,54 @@ template <int WAVES, int VEC>
 void start_bwd(const NormBwd& a, hipStream_t s) {
   constexpr int rows = kBwdRows<WAVES>;
   hipLaunchKernelGGL((k_norm_bwd<WAVES, VEC>), dim3(norm_bwd_parts(a.T, a.H)), dim3(kRowThreads<WAVES> * rows),
-                     rows > 1 ? a.H * sizeof(float) : 0, s, a);
+                     (VEC > 2 ? VEC * 8 * kRowThreads<WAVES> : rows > 1 ? a.H : 0) * sizeof(float), s, a);
 }
 
 }  // namespace
 
-#define MOE_NORM_ROWS(START, A, S)                                 \
-  do {                                                             \
-    const int waves = row_waves((A).H), vec = cdiv((A).H, waves * 512); \
-    if (waves == 1) {                                              \
-      if (vec == 1) START<1, 1>(A, S);                             \
-      else if (vec == 2) START<1, 2>(A, S);                        \
-      else if (vec == 3) START<1, 3>(A, S);                        \
-      else START<1, 4>(A, S);                                      \
-    } else if (waves == 4) {                                       \
-      if (vec == 2) START<4, 2>(A, S);                             \
-      else if (vec == 3) START<4, 3>(A, S);                        \
-      else START<4, 4>(A, S);                                      \
-    } else {                                                       \
-      if (vec == 2) START<16, 2>(A, S);                            \
-      else if (vec == 3) START<16, 3>(A, S);                       \
-      else START<16, 4>(A, S);                                     \
-    }                                                              \
-  } while (0)
-
 hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t s) {
   TraceScope trace_scope(K_NORM_FWD, s);
-  MOE_NORM_ROWS(start_fwd, a, s);
+  const int waves = fwd_waves(a.H), vec = cdiv(a.H, waves * 512);
+  if (waves == 1) {
+    if (vec == 1) start_fwd<1, 1>(a, s);
+    else if (vec == 2) start_fwd<1, 2>(a, s);
+    else if (vec == 3) start_fwd<1, 3>(a, s);
+    else start_fwd<1, 4>(a, s);
+  } else if (waves == 4) {
+    if (vec == 2) start_fwd<4, 2>(a, s);
+    else if (vec == 3) start_fwd<4, 3>(a, s);
+    else start_fwd<4, 4>(a, s);
+  } else {
+    if (vec == 2) start_fwd<16, 2>(a, s);
+    else if (vec == 3) start_fwd<16, 3>(a, s);
+    else start_fwd<16, 4>(a, s);
+  }
   return hipGetLastError();
 }
 
 // Workgroups of the backward, hence shares of dw: enough to fill the chip, few
-// enough that adding them costs little.
+// enough that adding them costs little (a share is written and read again in
+// fp32: 256 of rows of 5120 are 8% of what 3001 rows move, 512 are 17%).
 int norm_bwd_parts(int T, int H) {
-  const int waves = row_waves(H), rows = waves == 1 ? kBwdRows<1> : waves == 4 ? kBwdRows<4> : kBwdRows<16>;
-  return std::min(cdiv(T, rows), 512);
+  const int waves = bwd_waves(H), rows = waves == 1 ? kBwdRows<1> : waves == 4 ? kBwdRows<4> : kBwdRows<16>;
+  return std::min(cdiv(T, rows), waves == 16 ? 256 : 512);
 }
 
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s) {
   TraceScope trace_scope(K_NORM_BWD, s);
-  MOE_NORM_ROWS(start_bwd, a, s);
+  const int waves = bwd_waves(a.H), vec = cdiv(a.H, waves * 512);
+  if (waves == 1) {
+    if (vec == 1) start_bwd<1, 1>(a, s);
+    else start_bwd<1, 2>(a, s);
+  } else if (waves == 4) {
+    if (vec == 1) start_bwd<4, 1>(a, s);
+    else start_bwd<4, 2>(a, s);
+  } else {
+    if (vec == 1) start_bwd<16, 1>(a, s);
+    else if (vec == 2) start_bwd<16, 2>(a, s);
+    else if (vec == 3) start_bwd<16, 3>(a, s);
+    else start_bwd<16, 4>(a, s);
+  }
   hipLaunchKernelGGL(k_norm_dw, dim3(cdiv(a.H, 64)), dim3(1024), 0, s, a.part, norm_bwd_parts(a.T, a.H), a.H, a.dw,
                      a.dw_fp32);
   return hipGetLastError();
