@@ -30,7 +30,7 @@ namespace {
 // products; the workgroup's four waves are the ranges.  Further workgroups
 // round the tokens to int8 rows (q null: none), work that needs no launch of its own.
 constexpr int kRouterCols = 32;
-__global__ __launch_bounds__(kRouterSplits* kWave) void k_decode_router(const bf16_t* __restrict__ x,
+__global__ __launch_bounds__(kRouterSplits* kWave, 1) void k_decode_router(const bf16_t* __restrict__ x,
                                                                         const bf16_t* __restrict__ w_r, int T, int H,
                                                                         int E, float* __restrict__ part,
                                                                         int32_t* __restrict__ counts,
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kRouterSplits* kWave) void k_decode_router(const bf
   const int range = router_range(H), k0 = min(H, wave * range), k1 = min(H, k0 + range);
   const bool in_e = e0 < E, in_t = t < T;  // E is even
   f32x4 acc[2] = {};
-  constexpr int U = 8;
+  constexpr int U = 16;  // a range of H = 2048 at once: the latency of one access bounds it
   for (int k = k0; k < k1; k += U * 32) {
     uint32_t w[U][8];
     uint4 xv[U];
@@ -296,7 +296,7 @@ constexpr int kUpWaves = 8, kDownWaves = 4;
 
 // gridDim.z ranges of K: 1 where the tiles fill the chip, and the activation
 // is written; else a range's G and U are, and the down product adds them up.
-template <int NT>
+template <int NT, int U>
 __device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ x,
                                              const bf16_t* const (&b)[2], bf16_t* __restrict__ a, float* __restrict__ gu,
                                              float* red) {
@@ -312,7 +312,7 @@ __device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& ro
   };
   f32x4 acc[NT][2][4] = {};
   auto begin = [] {};
-  few_rows<NT, 2, 1, NT == 1 ? 2 : 1>(b, r.F, blockIdx.z * kUpWaves + wave, r.H / 32, gridDim.z * kUpWaves, begin, get, acc);
+  few_rows<NT, 2, 1, U>(b, r.F, blockIdx.z * kUpWaves + wave, r.H / 32, gridDim.z * kUpWaves, begin, get, acc);
   const int64_t R = static_cast<int64_t>(r.T) * r.k;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -338,8 +338,10 @@ __device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& ro
   }
 }
 
-template <bool FUSED>
-__global__ __launch_bounds__(kUpWaves* kWave, 4) void k_decode_gateup(DecodeRows r, const bf16_t* __restrict__ x,
+// With ranges of K there is at most one workgroup per compute unit: four steps'
+// weights in flight a wave instead of two workgroups.
+template <bool FUSED, bool RANGES>
+__global__ __launch_bounds__(kUpWaves* kWave, RANGES ? 2 : 4) void k_decode_gateup(DecodeRows r, const bf16_t* __restrict__ x,
                                                                    const bf16_t* __restrict__ w_gate,
                                                                    const bf16_t* __restrict__ w_up,
                                                                    bf16_t* __restrict__ a, float* __restrict__ gu) {
@@ -355,9 +357,9 @@ __global__ __launch_bounds__(kUpWaves* kWave, 4) void k_decode_gateup(DecodeRows
   const bf16_t* const b[2] = {w_gate + base, w_up + base};
   // more than 16 rows in pairs of tiles: what comes in again then is few experts' weights
   if (FUSED || rows.n <= 16) {
-    gateup_tiles<1>(r, rows, 0, x, b, a, gu, red);
+    gateup_tiles<1, RANGES ? 4 : 2>(r, rows, 0, x, b, a, gu, red);
   } else {
-    for (int t = 0; t < rows.n; t += 32) gateup_tiles<2>(r, rows, t, x, b, a, gu, red);
+    for (int t = 0; t < rows.n; t += 32) gateup_tiles<2, 1>(r, rows, t, x, b, a, gu, red);
   }
 }
 
@@ -434,10 +436,11 @@ __global__ __launch_bounds__(kDownWaves* kWave, 5) void k_decode_down(DecodeRows
 // against 5.5 at 16 tokens).
 
 // Products of 16 NT int8 rows with 16 channels of NB matrices (pointers at the
-// lane's channel and quarter), units u0, u0 + stride, ... < u1 of 128 k, U of them in flight.
-template <int NT, int NB, int U>
+// lane's channel and quarter), units u0, u0 + stride, ... < u1 of 128 k, U of
+// them in flight; begin() as in few_rows.
+template <int NT, int NB, int U, class Begin>
 __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const int8_t* const (&x)[NT], int u0, int u1,
-                                            int stride, i32x4 (&acc)[NT][NB]) {
+                                            int stride, Begin& begin, i32x4 (&acc)[NT][NB]) {
   auto batch = [&](int unit, auto count) {
     constexpr int n = decltype(count)::value;
     uint4 w[n][2][NB], v[n][2][NT];
@@ -448,10 +451,16 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const 
         const int k = (unit + i * stride) * 128 + h * 64;
 #pragma unroll
         for (int m = 0; m < NB; ++m) w[i][h][m] = *reinterpret_cast<const uint4*>(b[m] + k);
+      }
+    begin();
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-          v[i][h][t] = x[t] != nullptr ? *reinterpret_cast<const uint4*>(x[t] + k) : make_uint4(0, 0, 0, 0);
-      }
+          v[i][h][t] = x[t] != nullptr ? *reinterpret_cast<const uint4*>(x[t] + (unit + i * stride) * 128 + h * 64)
+                                       : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < n; ++i)
 #pragma unroll
@@ -473,7 +482,8 @@ constexpr int kUpWaves8 = 2, kDownWaves8 = 4;
 template <int NT>
 __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows& rows, int first,
                                                 const int8_t* __restrict__ x, const float* __restrict__ sx,
-                                                const moe_i8_experts& w, float* __restrict__ a, int* red) {
+                                                const moe_i8_experts& w, float* __restrict__ a, float* __restrict__ top,
+                                                int* red) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, H = r.H;
   const int64_t channel = static_cast<int64_t>(rows.expert) * r.F + blockIdx.x * 16;
   const int quad = (lane >> 4) * 16;
@@ -486,7 +496,8 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
     xr[t] = i < n ? x + static_cast<int64_t>(rows.slot[i] / r.k) * H + quad : nullptr;
   }
   i32x4 acc[NT][2] = {};
-  few_rows_i8<NT, 2, 1>(b, xr, wave, H / 128, kUpWaves8, acc);
+  auto begin = [] {};
+  few_rows_i8<NT, 2, 1>(b, xr, wave, H / 128, kUpWaves8, begin, acc);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (first + t * 16 >= n) break;
@@ -494,12 +505,18 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
     put_parts(acc[t], red);
     __syncthreads();
     for (int i = threadIdx.x; i < 256; i += kUpWaves8 * kWave) {
-      const int m = first + t * 16 + entry_row(i), c = entry_lane(i);
-      if (m >= n) continue;
-      const float s = sx[rows.slot[m] / r.k];
+      const int m = first + t * 16 + entry_row(i), c = entry_lane(i), slot = rows.slot[min(m, n - 1)];
+      const float s = sx[slot / r.k];
       const float g = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 0, i))) * s * w.s_gate[channel + c];
       const float u = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 1, i))) * s * w.s_up[channel + c];
-      a[static_cast<int64_t>(rows.slot[m]) * r.F + blockIdx.x * 16 + c] = silu_f(g) * u;
+      const float v = silu_f(g) * u;
+      // the row's largest of these 16 channels, in lanes 4, 8, 16 and 32 apart
+      uint32_t most = __float_as_uint(v) & 0x7fffffffu;
+#pragma unroll
+      for (int d = 4; d <= 32; d <<= 1) most = max(most, static_cast<uint32_t>(shfl_xor(static_cast<int>(most), d)));
+      if (m >= n) continue;
+      a[static_cast<int64_t>(slot) * r.F + blockIdx.x * 16 + c] = v;
+      if (c == 0) top[static_cast<int64_t>(slot) * (r.F / 16) + blockIdx.x] = __uint_as_float(most);
     }
   }
 }
@@ -507,7 +524,7 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
 template <bool FUSED>
 __global__ __launch_bounds__(kUpWaves8* kWave, 6) void k_decode_gateup_i8(DecodeRows r, const int8_t* __restrict__ x,
                                                                        const float* __restrict__ sx, moe_i8_experts w,
-                                                                       float* __restrict__ a) {
+                                                                       float* __restrict__ a, float* __restrict__ top) {
   __shared__ Rows rows;
   __shared__ int red[kUpWaves8 * 2 * 256];
   if constexpr (FUSED) {
@@ -517,36 +534,47 @@ __global__ __launch_bounds__(kUpWaves8* kWave, 6) void k_decode_gateup_i8(Decode
     if (!read_rows(r, rows)) return;
   }
   if (FUSED || rows.n <= 16) {
-    gateup_tiles_i8<1>(r, rows, 0, x, sx, w, a, red);
+    gateup_tiles_i8<1>(r, rows, 0, x, sx, w, a, top, red);
   } else {
-    for (int t = 0; t < rows.n; t += 32) gateup_tiles_i8<2>(r, rows, t, x, sx, w, a, red);
+    for (int t = 0; t < rows.n; t += 32) gateup_tiles_i8<2>(r, rows, t, x, sx, w, a, top, red);
   }
 }
 
-// The activation's rows as int8 rows, a wave per slot.
-__global__ __launch_bounds__(256) void k_decode_requant(DecodeRows r, const float* __restrict__ a, int8_t* __restrict__ q,
-                                                        float* __restrict__ scale) {
-  const int lane = threadIdx.x & 63, slot = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (slot >= r.T * r.k || r.topk_idx[slot] < 0) return;
-  const float* src = a + static_cast<int64_t>(slot) * r.F;
+// A slot's row of the activation as an int8 row, by one wave; its scale.
+__device__ __forceinline__ float round_row(const DecodeRows& r, int slot, const float* __restrict__ a,
+                                           const float* __restrict__ top, int8_t* q) {
+  const int lane = threadIdx.x & 63, parts = r.F / 16;
+  const float* const tops = top + static_cast<int64_t>(slot) * parts;
+  const float* const src = a + static_cast<int64_t>(slot) * r.F;
   uint32_t m = 0;
-  for (int c = lane * 4; c < r.F; c += 256) {
-    const uint4 v = *reinterpret_cast<const uint4*>(src + c);
-    m = max(max(m, max(v.x & 0x7fffffffu, v.y & 0x7fffffffu)), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
-  }
+  for (int i = lane; i < parts; i += kWave) m = max(m, __float_as_uint(tops[i]));
   const Rounder rd(wave_umax(m));
+#pragma unroll 4
   for (int c = lane * 4; c < r.F; c += 256) {
     const float4 v = *reinterpret_cast<const float4*>(src + c);
-    *reinterpret_cast<uint32_t*>(q + static_cast<int64_t>(slot) * r.F + c) = pack4(rd(v.x), rd(v.y), rd(v.z), rd(v.w));
+    *reinterpret_cast<uint32_t*>(q + c) = pack4(rd(v.x), rd(v.y), rd(v.z), rd(v.w));
   }
-  if (lane == 0) scale[slot] = rd.scale;
+  return rd.scale;
 }
 
-// O = A W_down: 16 channels per wave, all of F, so no sum over waves.
-template <int NT>
-__device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& rows, int first,
-                                              const int8_t* __restrict__ a, const float* __restrict__ sa,
-                                              const moe_i8_experts& w, float* __restrict__ o) {
+// The activation's rows as int8 rows, a wave per slot: where every workgroup of
+// the down product would otherwise round many rows for itself.
+__global__ __launch_bounds__(256) void k_decode_requant(DecodeRows r, const float* __restrict__ a,
+                                                        const float* __restrict__ top, int8_t* __restrict__ q,
+                                                        float* __restrict__ scale) {
+  const int slot = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (slot >= r.T * r.k || r.topk_idx[slot] < 0) return;
+  const float s = round_row(r, slot, a, top, q + static_cast<int64_t>(slot) * r.F);
+  if ((threadIdx.x & 63) == 0) scale[slot] = s;
+}
+
+// O = A W_down: 16 channels per wave, all of F, so no sum over waves.  The
+// rows' int8 values and scales are the slots', in a and sa, or (ROUND) rows 0, 1,
+// .. of LDS, rounded by begin() under the first weights' way here.
+template <int NT, int U, bool ROUND, class Begin>
+__device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& rows, int first, const int8_t* a,
+                                              const float* sa, const moe_i8_experts& w, float* __restrict__ o,
+                                              Begin& begin) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, F = r.F;
   const int column = (blockIdx.x * kDownWaves8 + wave) * 16 + (lane & 15);
   const int64_t channel = static_cast<int64_t>(rows.expert) * r.H + column;
@@ -556,10 +584,10 @@ __device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& r
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int i = first + t * 16 + (lane & 15);
-    ar[t] = i < n ? a + static_cast<int64_t>(rows.slot[i]) * F + quad : nullptr;
+    ar[t] = i < n ? a + static_cast<int64_t>(ROUND ? i : rows.slot[i]) * F + quad : nullptr;
   }
   i32x4 acc[NT][1] = {};
-  few_rows_i8<NT, 1, 2>(b, ar, 0, F / 128, 1, acc);
+  few_rows_i8<NT, 1, U>(b, ar, 0, F / 128, 1, begin, acc);
   const float sd = w.s_down[channel];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -567,7 +595,7 @@ __device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& r
     for (int i = 0; i < 4; ++i) {
       const int m = first + t * 16 + 4 * (lane >> 4) + i;
       if (m < n)
-        o[static_cast<int64_t>(rows.slot[m]) * r.H + column] = static_cast<float>(unwrap(acc[t][0][i])) * sa[rows.slot[m]] * sd;
+        o[static_cast<int64_t>(rows.slot[m]) * r.H + column] = static_cast<float>(unwrap(acc[t][0][i])) * sa[ROUND ? m : rows.slot[m]] * sd;
     }
 }
 
@@ -576,23 +604,59 @@ __global__ __launch_bounds__(kDownWaves8* kWave, 6) void k_decode_down_i8(Decode
                                                                        float* __restrict__ o) {
   __shared__ Rows rows;
   if (!read_rows(r, rows)) return;
+  auto begin = [] {};
   if (rows.n <= 16) {
-    down_tiles_i8<1>(r, rows, 0, a, sa, w, o);
+    down_tiles_i8<1, 2, false>(r, rows, 0, a, sa, w, o, begin);
   } else {
-    for (int t = 0; t < rows.n; t += 32) down_tiles_i8<2>(r, rows, t, a, sa, w, o);
+    for (int t = 0; t < rows.n; t += 32) down_tiles_i8<2, 2, false>(r, rows, t, a, sa, w, o, begin);
   }
 }
 
-// y[t] = sum_j gates o, in slot order; 0 for a token without rows.
+// The same from the activation itself, for up to kFusedT tokens.
+__global__ __launch_bounds__(kDownWaves8* kWave) void k_decode_down_i8_few(DecodeRows r, const float* __restrict__ a,
+                                                                          const float* __restrict__ top,
+                                                                          moe_i8_experts w, float* __restrict__ o) {
+  __shared__ Rows rows;
+  __shared__ float sa[kFusedT];
+  extern __shared__ __attribute__((aligned(16))) int8_t a8[];  // [rows, F]
+  if (!read_rows(r, rows)) return;
+  bool begun = false;
+  auto begin = [&] {
+    if (begun) return;
+    begun = true;
+    for (int i = threadIdx.x >> 6; i < rows.n; i += kDownWaves8) {
+      const float s = round_row(r, rows.slot[i], a, top, a8 + i * r.F);
+      if ((threadIdx.x & 63) == 0) sa[i] = s;
+    }
+    __syncthreads();
+  };
+  down_tiles_i8<1, 6, true>(r, rows, 0, a8, sa, w, o, begin);
+}
+
+// y[t] = sum_j gates o, in slot order; 0 for a token without rows.  Eight
+// slots' values are on their way at once.
 __global__ __launch_bounds__(256) void k_decode_combine(DecodeRows r, const float* __restrict__ o, bf16_t* __restrict__ y) {
   const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= r.H) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (r.topk_idx[t * r.k] >= 0)
-    for (int j = 0; j < r.k; ++j) {
-      const float g = r.gates[t * r.k + j];
-      const float4 v = *reinterpret_cast<const float4*>(o + static_cast<int64_t>(t * r.k + j) * r.H + c);
-      s.x = fmaf(g, v.x, s.x), s.y = fmaf(g, v.y, s.y), s.z = fmaf(g, v.z, s.z), s.w = fmaf(g, v.w, s.w);
+  if (uniform_load(r.topk_idx + t * r.k) >= 0)
+    for (int j0 = 0; j0 < r.k; j0 += 8) {
+      float4 v[8];
+      float g[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool in = j0 + j < r.k;
+        const int slot = t * r.k + min(j0 + j, r.k - 1);
+        v[j] = *reinterpret_cast<const float4*>(o + static_cast<int64_t>(slot) * r.H + c);
+        g[j] = uniform_load(r.gates + slot);
+        v[j] = make_float4(in ? v[j].x : 0.f, in ? v[j].y : 0.f, in ? v[j].z : 0.f, in ? v[j].w : 0.f);
+        g[j] = in ? g[j] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        s.x = fmaf(g[j], v[j].x, s.x), s.y = fmaf(g[j], v[j].y, s.y);
+        s.z = fmaf(g[j], v[j].z, s.z), s.w = fmaf(g[j], v[j].w, s.w);
+      }
     }
   *reinterpret_cast<uint2*>(y + static_cast<int64_t>(t) * r.H + c) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
 }
@@ -627,10 +691,12 @@ hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16
                                 bf16_t* a, float* gu, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_GATEUP, s);
   const dim3 grid(r.F / kCols, slots(r), decode_ranges(r.T, r.E, r.F, r.k));
-  if (decode_fused(r.T))
-    hipLaunchKernelGGL(k_decode_gateup<true>, grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
+  if (grid.z > 1)
+    hipLaunchKernelGGL((k_decode_gateup<true, true>), grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
+  else if (decode_fused(r.T))
+    hipLaunchKernelGGL((k_decode_gateup<true, false>), grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
   else
-    hipLaunchKernelGGL(k_decode_gateup<false>, grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
+    hipLaunchKernelGGL((k_decode_gateup<false, false>), grid, dim3(kUpWaves * kWave), 0, s, r, x, w_gate, w_up, a, gu);
   return hipGetLastError();
 }
 
@@ -646,22 +712,27 @@ hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const float*
 }
 
 hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const float* sx, const moe_i8_experts& w,
-                                   float* a, hipStream_t s) {
+                                   float* a, float* top, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_GATEUP, s);
   const dim3 grid(r.F / 16, slots(r));
   if (decode_fused(r.T))
-    hipLaunchKernelGGL(k_decode_gateup_i8<true>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a);
+    hipLaunchKernelGGL(k_decode_gateup_i8<true>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
   else
-    hipLaunchKernelGGL(k_decode_gateup_i8<false>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a);
+    hipLaunchKernelGGL(k_decode_gateup_i8<false>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
   return hipGetLastError();
 }
 
-hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, int8_t* a8, float* sa, const moe_i8_experts& w,
-                                 float* o, hipStream_t s) {
+hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, const float* top, int8_t* a8, float* sa,
+                                 const moe_i8_experts& w, float* o, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_DOWN, s);
-  hipLaunchKernelGGL(k_decode_requant, dim3(cdiv(r.T * r.k, 4)), dim3(256), 0, s, r, a, a8, sa);
-  hipLaunchKernelGGL(k_decode_down_i8, dim3(r.H / (16 * kDownWaves8), slots(r)), dim3(kDownWaves8 * kWave), 0, s, r, a8, sa,
-                     w, o);
+  const dim3 grid(r.H / (16 * kDownWaves8), slots(r)), block(kDownWaves8 * kWave);
+  // rows in LDS: an expert has at most T
+  if (decode_fused(r.T) && r.T * r.F <= 65536) {
+    hipLaunchKernelGGL(k_decode_down_i8_few, grid, block, r.T * r.F, s, r, a, top, w, o);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(k_decode_requant, dim3(cdiv(r.T * r.k, 4)), dim3(256), 0, s, r, a, top, a8, sa);
+  hipLaunchKernelGGL(k_decode_down_i8, grid, block, 0, s, r, a8, sa, w, o);
   return hipGetLastError();
 }
 

@@ -61,14 +61,14 @@ bool decode_fused(int T);
 int decode_ranges(int T, int E, int F, int k);
 hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,
                                 bf16_t* a, float* gu, hipStream_t s);
-// a [T k, F].
+// a [T k, F], top [T k, F / 16] the largest magnitudes of 16 columns each.
 hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const float* sx, const moe_i8_experts& w,
-                                   float* a, hipStream_t s);
+                                   float* a, float* top, hipStream_t s);
 // o [T k, H] = the activation through W_down (a8, sa: room for its int8 rows).
 hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const float* gu, const bf16_t* w_down, float* o,
                               hipStream_t s);
-hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, int8_t* a8, float* sa, const moe_i8_experts& w,
-                                 float* o, hipStream_t s);
+hipError_t launch_decode_down_i8(const DecodeRows& r, const float* a, const float* top, int8_t* a8, float* sa,
+                                 const moe_i8_experts& w, float* o, hipStream_t s);
 // y [T, H] = sum_j gates o.
 hipError_t launch_decode_combine(const DecodeRows& r, const float* o, bf16_t* y, hipStream_t s);
 

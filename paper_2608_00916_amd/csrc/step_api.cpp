@@ -93,7 +93,7 @@ struct DecodeWs {
   int32_t* row_token;
   bf16_t* a;   // bf16 experts: the activation's two summands,
   float* gu;   // or the ranges' G and U
-  float *a32, *sx, *sa;  // int8 experts
+  float *a32, *top, *sx, *sa;  // int8 experts
   int8_t *x8, *a8;
   float* o;
   size_t bytes;
@@ -112,6 +112,7 @@ DecodeWs decode_layout(const moe_dims* d, bool i8, void* base) {
     w.x8 = c.take<int8_t>(T * d->H);
     w.sx = c.take<float>(T);
     w.a32 = c.take<float>(RF);
+    w.top = c.take<float>(RF / 16);
     w.a8 = c.take<int8_t>(RF);
     w.sa = c.take<float>(R);
   } else if (const int ranges = decode_ranges(d->T, d->E, d->F, d->top_k); ranges > 1) {
@@ -262,9 +263,9 @@ int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i
   const bf16_t* xb = static_cast<const bf16_t*>(x);
   hipError_t e = route(l, xb, static_cast<const bf16_t*>(w_r), s);
   if (e != hipSuccess) return hip_status(e, "router");
-  e = launch_decode_gateup_i8(l.rows, l.x8, l.sx, *w, l.a32, s);
+  e = launch_decode_gateup_i8(l.rows, l.x8, l.sx, *w, l.a32, l.top, s);
   if (e != hipSuccess) return hip_status(e, "gate/up");
-  e = launch_decode_down_i8(l.rows, l.a32, l.a8, l.sa, *w, l.o, s);
+  e = launch_decode_down_i8(l.rows, l.a32, l.top, l.a8, l.sa, *w, l.o, s);
   if (e != hipSuccess) return hip_status(e, "down");
   return hip_status(launch_decode_combine(l.rows, l.o, static_cast<bf16_t*>(y), s), "combine");
 }

@@ -45,13 +45,14 @@ template <int PL>
 __device__ __forceinline__ float topk_select(const float (&val)[PL], const uint32_t (&key)[PL], int k, int lane,
                                              int32_t* __restrict__ idx_row, float* __restrict__ g_row,
                                              int32_t* __restrict__ cnt_row) {
-  uint32_t kth = 0u;  // largest P with #{key >= P} >= k
+  uint32_t kth = 0u;  // largest P with #{key >= P} >= k, or the first found with k
   for (int b = 31; b >= 0; --b) {
     const uint32_t cand = kth | (1u << b);
     int cnt = 0;
 #pragma unroll
     for (int m = 0; m < PL; ++m) cnt += ballot_count(key[m] >= cand);
     kth = cnt >= k ? cand : kth;
+    if (cnt == k) break;  // exactly the k largest reach it: no lower bit changes the selection
   }
   int above = 0;
 #pragma unroll
