@@ -526,7 +526,8 @@ typedef struct moe_sample_dims {
 } moe_sample_dims;
 #define MOE_F_LOGITS_FP32 32u /* moe_sample_dims: the logits are fp32, else bf16 */
 
-/*   logits       [B, V], row pitch ld >= V elements
+/*   logits       [B, V], row pitch ld >= V elements; like all but ws it
+ *                may begin at any element (not only on 16 bytes)
  *   temperature, top_p, min_p  [B] fp32, top_k [B] int32, each on the device, or NULL: off (temperature: 1)
  *   u            [B] fp32
  *   token        [B] int32

@@ -139,7 +139,7 @@ __device__ __forceinline__ bool read_rows(const DecodeRows& r, Rows& rows) {
 // Selection of up to kFusedT tokens by every workgroup of the gate/up product
 // for itself, a wave per token, instead of a launch between the router and it;
 // the first workgroup leaves it for the launches after.
-constexpr int kFusedT = 8;
+constexpr int kFusedT = kDecodeFusedT;
 struct Selection {
   int32_t idx[kFusedT * MOE_MAX_TOPK];
   float gates[kFusedT * MOE_MAX_TOPK];
@@ -665,9 +665,6 @@ __global__ __launch_bounds__(256) void k_decode_combine(DecodeRows r, const floa
 int slots(const DecodeRows& r) { return std::min(r.E, r.T * r.k); }
 
 }  // namespace
-
-// Whether the selection is made by the gate/up product.
-bool decode_fused(int T) { return T <= kFusedT; }
 
 // Ranges of K of the bf16 gate/up product: two where few tokens leave its
 // tiles fewer than the chip's 256 compute units.  The down product then holds

@@ -301,22 +301,35 @@ void start_bwd(const NormBwd& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t s) {
+// A grid dimension holds fewer than 2^32 threads: rows in slices.
+constexpr int kSlice = 1 << 21;
+
+hipError_t launch_norm_fwd(const NormFwd& all, hipStream_t s) {
   TraceScope trace_scope(K_NORM_FWD, s);
-  const int waves = fwd_waves(a.H), vec = cdiv(a.H, waves * 512);
-  if (waves == 1) {
-    if (vec == 1) start_fwd<1, 1>(a, s);
-    else if (vec == 2) start_fwd<1, 2>(a, s);
-    else if (vec == 3) start_fwd<1, 3>(a, s);
-    else start_fwd<1, 4>(a, s);
-  } else if (waves == 4) {
-    if (vec == 2) start_fwd<4, 2>(a, s);
-    else if (vec == 3) start_fwd<4, 3>(a, s);
-    else start_fwd<4, 4>(a, s);
-  } else {
-    if (vec == 2) start_fwd<16, 2>(a, s);
-    else if (vec == 3) start_fwd<16, 3>(a, s);
-    else start_fwd<16, 4>(a, s);
+  const int waves = fwd_waves(all.H), vec = cdiv(all.H, waves * 512);
+  for (int64_t t = 0; t < all.T; t += kSlice) {
+    NormFwd a = all;
+    const int64_t out = t * a.H;
+    a.T = static_cast<int>(std::min<int64_t>(kSlice, all.T - t));
+    a.x += t * a.ldx;
+    if (a.r != nullptr) a.r += t * a.ldr;
+    if (a.h != nullptr) a.h += out;
+    if (a.y != nullptr) a.y += out;
+    if (a.q != nullptr) a.q += out, a.scale += t;
+    if (waves == 1) {
+      if (vec == 1) start_fwd<1, 1>(a, s);
+      else if (vec == 2) start_fwd<1, 2>(a, s);
+      else if (vec == 3) start_fwd<1, 3>(a, s);
+      else start_fwd<1, 4>(a, s);
+    } else if (waves == 4) {
+      if (vec == 2) start_fwd<4, 2>(a, s);
+      else if (vec == 3) start_fwd<4, 3>(a, s);
+      else start_fwd<4, 4>(a, s);
+    } else {
+      if (vec == 2) start_fwd<16, 2>(a, s);
+      else if (vec == 3) start_fwd<16, 3>(a, s);
+      else start_fwd<16, 4>(a, s);
+    }
   }
   return hipGetLastError();
 }

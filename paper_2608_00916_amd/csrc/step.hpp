@@ -55,7 +55,8 @@ hipError_t launch_decode_router(const DecodeRows& r, const bf16_t* x, const bf16
                                 hipStream_t s);
 // Whether the gate/up product makes the selection (topk_idx, gates, counts)
 // from part; else it is there before.
-bool decode_fused(int T);
+constexpr int kDecodeFusedT = 8;
+inline bool decode_fused(int T) { return T <= kDecodeFusedT; }
 // SwiGLU of the slots' tokens through their experts: a [2, T k, F] as two
 // summands, or with decode_ranges(..) > 1 each range's G and U, gu [ranges, 2, T k, F].
 int decode_ranges(int T, int E, int F, int k);

@@ -125,11 +125,16 @@ DecodeWs decode_layout(const moe_dims* d, bool i8, void* base) {
   return w;
 }
 
-// A call of fewer tokens may use more: what a size query returns is enough for
-// up to its T.
+// A call of fewer tokens may use more, where their product is split over K:
+// what a size query returns is enough for up to its T.
 size_t decode_bytes(const moe_dims* d, bool i8) {
-  size_t most = 0;
-  for (moe_dims e = *d; e.T > 0; --e.T) most = std::max(most, decode_layout(&e, i8, nullptr).bytes);
+  size_t most = decode_layout(d, i8, nullptr).bytes;
+  if (i8) return most;
+  moe_dims e = *d;
+  for (e.T = d->T - 1; e.T > 0; --e.T) {
+    if (!decode_fused(e.T)) e.T = kDecodeFusedT;
+    if (decode_ranges(e.T, e.E, e.F, e.top_k) > 1) most = std::max(most, decode_layout(&e, i8, nullptr).bytes);
+  }
   return most;
 }
 
@@ -155,6 +160,15 @@ int check_given(std::initializer_list<std::pair<const char*, const void*>> ps) {
   for (const auto& p : ps)
     if (p.second != nullptr)
       if (int rc = check_ptrs({p})) return rc;
+  return MOE_OK;
+}
+
+int check_elements(std::initializer_list<std::pair<const char*, const void*>> ps, int size, bool required) {
+  for (const auto& p : ps) {
+    if (p.second == nullptr && required) return fail(MOE_ERR_ARG, "%s is NULL", p.first);
+    if (reinterpret_cast<uintptr_t>(p.second) % size != 0)
+      return fail(MOE_ERR_ALIGN, "%s is not aligned to its elements", p.first);
+  }
   return MOE_OK;
 }
 
@@ -228,7 +242,8 @@ int moe_decode(const moe_dims* d, const void* x, const void* w_r, const void* w_
   const bool masked = d->flags & MOE_F_MASK;
   if (masked && token_mask == nullptr) return fail(MOE_ERR_ARG, "MOE_F_MASK set but token_mask is NULL");
   DecodeWs l = decode_layout(d, false, ws);
-  if (ws_bytes < l.bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, l.bytes);
+  if (const size_t need = decode_bytes(d, false); ws_bytes < need)
+    return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   l.rows.mask = masked ? token_mask : nullptr;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bf16_t* xb = static_cast<const bf16_t*>(x);
@@ -281,10 +296,14 @@ int moe_sample(const moe_sample_dims* d, const void* logits, int64_t ld, const f
   if (int rc = check_sample(d)) return rc;
   if (ld < d->V) return fail(MOE_ERR_ARG, "ld=%lld is less than %d", static_cast<long long>(ld), d->V);
   if (ld > (1ll << 31)) return fail(MOE_ERR_ARG, "ld=%lld exceeds 2^31", static_cast<long long>(ld));
-  if (int rc = check_ptrs({{"logits", logits}, {"u", u}, {"token", token}, {"ws", ws}})) return rc;
-  if (int rc = check_given({{"temperature", temperature}, {"top_k", top_k}, {"top_p", top_p}, {"min_p", min_p},
-                            {"logprob", logprob}}))
+  // logits, settings and outputs are read and written by the element: any slice of a tensor will do
+  const int size = d->flags & MOE_F_LOGITS_FP32 ? 4 : 2;
+  if (int rc = check_elements({{"logits", logits}}, size, true)) return rc;
+  if (int rc = check_elements({{"u", u}, {"token", token}}, 4, true)) return rc;
+  if (int rc = check_elements({{"temperature", temperature}, {"top_k", top_k}, {"top_p", top_p}, {"min_p", min_p},
+                               {"logprob", logprob}}, 4, false))
     return rc;
+  if (int rc = check_ptrs({{"ws", ws}})) return rc;
   const size_t need = sample_ws(d->B, d->V);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   const SampleArgs a{logits, ld, (d->flags & MOE_F_LOGITS_FP32) != 0, d->B, d->V, temperature, top_p, min_p, top_k, u,

@@ -85,6 +85,27 @@ def test_norm(T, H, residual):
             assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
 
 
+def test_norm_of_many_rows():
+    """More rows than one launch takes: the last ones as the first."""
+    import torch
+    import paper_2608_00916_amd as moe
+    T, H = 2 ** 21 + 5, 16
+    say("norm many rows", T)
+    x = bf16(gen(1).standard_normal((5, H))).repeat(T // 5 + 1, 1)[:T].contiguous()
+    r = x.flip(1).contiguous()
+    w = bf16(1 + 0.1 * gen(2).standard_normal(H))
+    h, y, q, scale = moe.RMSNorm(T, w, out="both").forward(x, r)
+    for a in (h, y, q, scale[:, None]):
+        rows = a[: T // 5 * 5].view(T // 5, 5, -1)
+        assert torch.equal(rows, rows[:1].expand_as(rows)) and torch.equal(a[-5:], a[T % 5:T % 5 + 5])
+    dx, dw = moe.RMSNorm(T, w, dw_fp32=True, backward=True).backward(x, r)
+    rows = dx[: T // 5 * 5].view(T // 5, 5, -1)
+    assert torch.equal(rows, rows[:1].expand_as(rows))
+    rx, rw, _, mw = R.norm_bwd(host(x[:5]), host(w), host(r[:5]), 0.0, 1e-6)
+    # 512 shares of 512 rows in chains of 512 per wave, 8 and 48 more: 2^-24 each of the terms' size
+    near(dw, rw * (T // 5), 2.0 ** -14 * mw * (T // 5) + mw, "dw")
+
+
 def test_norm_strides_and_places():
     """Rows apart, and sums and norms written over their inputs."""
     import torch
@@ -182,7 +203,8 @@ def test_norm_backward_against_differences():
 # ------------------------------------------------------------------ the expert layer for a few tokens
 DECODE = [(1, 128, 8, 128, 1), (1, 2048, 128, 768, 8), (2, 256, 8, 384, 8), (16, 512, 16, 256, 2), (17, 384, 8, 128, 3),
           (33, 128, 16, 640, 4), (64, 1152, 8, 128, 8), (64, 128, 256, 128, 6), (5, 4096, 8, 1280, 2), (3, 256, 32, 2176, 32),
-          (31, 640, 40, 384, 5)]
+          (31, 640, 40, 384, 5), (8, 128, 8, 1920, 8), (8, 128, 8, 8320, 2), (7, 128, 256, 128, 32), (4, 2048, 64, 768, 8),
+          (9, 1024, 128, 256, 4)]
 
 
 def layer(T, H, E, F, k, seed=0):
@@ -277,6 +299,54 @@ def test_decode_masks(i8, on):
             y = op.forward(t["x"], *(t[n] for n in ("w_r", "w_gate", "w_up", "w_down")), mask)
         check_layer(y, t, idx, gates, stand, on)
         assert (host(y)[on == 0] == 0).all()
+
+
+@pytest.mark.parametrize("T,H,E,k", [(1, 2048, 128, 8), (5, 1152, 256, 4), (8, 384, 64, 8), (16, 2048, 128, 8), (64, 640, 256, 16)])
+def test_decode_selects_as_the_block_does(T, H, E, k):
+    """Experts in pairs whose logits differ by a few roundings of the sum, so that which of a
+    pair is taken hangs on its last bits: the same as in moe_infer, for every token."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode near ties", T, H, E, k)
+    F = 128
+    g = gen(T + E)
+    w_r = bf16(0.05 * g.standard_normal((H, E)))
+    w_r[:, 1::2] = w_r[:, ::2]
+    x = bf16(g.standard_normal((T, H)))
+    # the pair's sums meet the same terms, but for two channels that trade places in x
+    x[:, 1] = x[:, 0]
+    swap = w_r[0, ::2].clone()
+    w_r[0, 1::2], w_r[1, 1::2] = w_r[1, ::2], swap
+    x[:, H // 2] = x[:, 0]
+    w_r[0, 1::2], w_r[H // 2, 1::2] = w_r[H // 2, ::2].clone(), w_r[0, 1::2].clone()
+    w = [bf16(g.standard_normal(s) * s[1] ** -0.5) for s in ((E, H, F), (E, H, F), (E, F, H))]
+    y = moe.MoEDecode(T, H, E, F, k).forward(x, w_r, *w).float()
+    z = moe.MoEInfer(T, H, E, F, k).forward(x, w_r, *w).float()
+    # a token with another expert would be off by a large part of itself
+    assert float(((y - z).norm(dim=1) / z.norm(dim=1)).max()) < 5 * BF
+
+
+@pytest.mark.parametrize("T", [3, 20])
+@pytest.mark.parametrize("i8", [False, True])
+def test_decode_keeps_tokens_apart(T, i8):
+    """A token that is not finite spoils no other one, and rows behind the last token stay."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode apart", T, i8)
+    t, idx, gates = layer(T, 256, 16, 128, 4)
+    made = moe.MoEDecodeI8 if i8 else moe.MoEDecode
+    w = [eight(t)[0]] if i8 else [t[n] for n in ("w_gate", "w_up", "w_down")]
+    op = made(T + 5, 256, 16, 128, 4)
+    want = op.forward(t["x"], t["w_r"], *w).clone()
+    op.y.fill_(7.0)
+    x = t["x"].clone()
+    x[1, 5], x[T - 1, 9] = float("nan"), float("inf")
+    y = op.forward(x, t["w_r"], *w)
+    assert torch.isnan(y[1]).any()
+    for i in range(T):
+        if i not in (1, T - 1):
+            assert torch.equal(y[i], want[i]), i
+    assert (op.y[T:] == 7).all()
 
 
 def test_decode_far_weights():
@@ -425,6 +495,29 @@ def test_sample_odd_settings():
         i, lp = R.sample(r, float(np.float32(uu)), tt, kk, 1.0 if np.isnan(pp) else float(np.float32(pp)), 0.0 if np.isnan(mm) else float(np.float32(mm)))
         assert int(got[0][b]) == i, (b, cases[b])
         assert abs(float(got[1][b]) - lp) <= 2.0 ** -24 * abs(lp) + V * 2.0 ** -43
+
+
+def test_sample_rows_behind_and_many():
+    """Fewer rows than made for; more rows than compute units; a row alone and among others."""
+    import torch
+    import paper_2608_00916_amd as moe
+    V = 9001
+    say("sample rows", V)
+    logits = rows_of(300, V, 5, True)
+    u = dev(gen(6).random(300).astype(np.float32))
+    full = lambda v, n, dtype=np.float32: dev(np.full(n, v, dtype))  # noqa: E731
+    op = moe.Sampler(300, V)
+    for s in (lambda n: dict(top_p=full(0.95, n), temperature=full(1.5, n)), lambda n: dict(min_p=full(1e-4, n)),
+              lambda n: dict(top_k=full(300, n, np.int32), top_p=full(0.9, n))):
+        token, logprob = (o.clone() for o in op.forward(logits, u, **s(300)))
+        check_tokens(logits, u, (token, logprob), **s(300))
+        for b in (1, 3, 40, 130):
+            op.token.fill_(-7)
+            got = op.forward(logits[:b], u[:b], **s(b))
+            assert torch.equal(got[0], token[:b]) and torch.equal(got[1], logprob[:b])
+            assert (op.token[b:] == -7).all()
+        one = moe.Sampler(1, V).forward(logits[7:8], u[7:8], **s(1))
+        assert torch.equal(one[0], token[7:8]) and torch.equal(one[1], logprob[7:8])
 
 
 def test_sample_largest():

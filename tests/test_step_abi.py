@@ -103,9 +103,9 @@ def test_sample_refusals():
     d = _lib.MoeSampleDims(4, 1000, _lib.MOE_F_LOGITS_FP32)
     need = L.moe_sample_workspace_bytes(ref(d))
     ok = [ref(d), FAKE, 1000, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, need, None]
-    for at, v, code in ((0, None, ARG), (1, None, ARG), (1, FAKE + 4, ALIGN), (2, 999, ARG), (3, FAKE + 4, ALIGN),
-                        (4, FAKE + 8, ALIGN), (7, None, ARG), (8, None, ARG), (9, FAKE + 2, ALIGN), (10, None, ARG),
-                        (11, need - 1, WS), (2, 1 << 33, ARG)):
+    for at, v, code in ((0, None, ARG), (1, None, ARG), (1, FAKE + 2, ALIGN), (2, 999, ARG), (3, FAKE + 2, ALIGN),
+                        (4, FAKE + 1, ALIGN), (7, None, ARG), (8, None, ARG), (9, FAKE + 2, ALIGN), (10, None, ARG),
+                        (10, FAKE + 8, ALIGN), (11, need - 1, WS), (2, 1 << 33, ARG)):
         args = list(ok)
         args[at] = v
         call("moe_sample", code, *args)
