@@ -22,24 +22,32 @@ namespace moe {
 
 namespace {
 
+// An address as a wave's base and a lane's 32-bit offset, the form that leaves
+// the address arithmetic to the scalar unit.
+template <class T>
+__device__ __forceinline__ const char* at_bytes(const T* base, uint32_t offset) {
+  return reinterpret_cast<const char*>(base) + offset;
+}
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // ---- router
 // Logits in the router's own order of summation, so that the selection is
 // moe_infer's bit for bit: range s of K goes through the same instructions in
-// the same order into plane s of part [kRouterSplits, T, E].  A wave takes
-// one range, 32 experts and 16 tokens, its loads all issued ahead of the
-// products; the workgroup's four waves are the ranges.  Further workgroups
-// round the tokens to int8 rows (q null: none), work that needs no launch of its own.
+// the same order into plane s of part [kRouterSplits, T, E].  A workgroup of
+// one wave takes one range, 32 experts and 16 tokens, its loads all issued ahead
+// of the products: what one compute unit can fetch bounds it.  Further
+// workgroups round the tokens to int8 rows (q null: none), work that needs no
+// launch of its own.
 constexpr int kRouterCols = 32;
-__global__ __launch_bounds__(kRouterSplits* kWave, 1) void k_decode_router(const bf16_t* __restrict__ x,
+__global__ __launch_bounds__(kWave, 1) void k_decode_router(const bf16_t* __restrict__ x,
                                                                         const bf16_t* __restrict__ w_r, int T, int H,
                                                                         int E, float* __restrict__ part,
                                                                         int32_t* __restrict__ counts,
                                                                         int8_t* __restrict__ q, float* __restrict__ sx) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x;
   const int cols = cdiv(E, kRouterCols), tiles = cols * cdiv(T, 16);
-  if (static_cast<int>(blockIdx.x) >= tiles) {  // a token's int8 row per wave
-    const int t = (blockIdx.x - tiles) * kRouterSplits + wave;
-    if (t >= T) return;
+  if (static_cast<int>(blockIdx.x) >= tiles * kRouterSplits) {  // a token's int8 row
+    const int t = blockIdx.x - tiles * kRouterSplits;
     const bf16_t* src = x + static_cast<int64_t>(t) * H;
     uint32_t m = 0;
     for (int c = lane * 8; c < H; c += 512) m = max(m, top8(*reinterpret_cast<const uint4*>(src + c)));
@@ -51,23 +59,26 @@ __global__ __launch_bounds__(kRouterSplits* kWave, 1) void k_decode_router(const
   }
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < E; i += blockDim.x) counts[i] = 0;
-  const int e0 = blockIdx.x % cols * kRouterCols + (lane & 15) * 2, t = blockIdx.x / cols * 16 + (lane & 15);
+  const int split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const int e0 = tile % cols * kRouterCols + (lane & 15) * 2, t = tile / cols * 16 + (lane & 15);
   const int quad = (lane >> 4) * 8;
-  const int range = router_range(H), k0 = min(H, wave * range), k1 = min(H, k0 + range);
+  const int range = router_range(H), k0 = min(H, split * range), k1 = min(H, k0 + range);
   const bool in_e = e0 < E, in_t = t < T;  // E is even
   f32x4 acc[2] = {};
   constexpr int U = 16;  // a range of H = 2048 at once: the latency of one access bounds it
+  // lanes past the experts or the tokens read the first ones; what they hold is not stored
+  const uint32_t w_at = static_cast<uint32_t>(quad * E + (in_e ? e0 : 0)) * 2, x_at = static_cast<uint32_t>(quad) * 2;
+  const bf16_t* const x_row = x + static_cast<int64_t>(in_t ? t : 0) * H;
   for (int k = k0; k < k1; k += U * 32) {
     uint32_t w[U][8];
     uint4 xv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = k + u * 32 + quad;
-      const bool in = k + u * 32 < k1;
-      xv[u] = in && in_t ? *reinterpret_cast<const uint4*>(x + static_cast<int64_t>(t) * H + at) : make_uint4(0, 0, 0, 0);
+      if (k + u * 32 >= k1) break;
+      xv[u] = *reinterpret_cast<const uint4*>(at_bytes(x_row + k + u * 32, x_at));
 #pragma unroll
       for (int r = 0; r < 8; ++r)
-        w[u][r] = in && in_e ? *reinterpret_cast<const uint32_t*>(w_r + static_cast<int64_t>(at + r) * E + e0) : 0u;
+        w[u][r] = *reinterpret_cast<const uint32_t*>(at_bytes(w_r + static_cast<int64_t>(k + u * 32 + r) * E, w_at));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -84,8 +95,8 @@ __global__ __launch_bounds__(kRouterSplits* kWave, 1) void k_decode_router(const
   }
   // lane l holds experts 2 (4 (l / 16) + i) + p of the tile for token l % 16
   if (!in_t) return;
-  float* out = part + (static_cast<int64_t>(wave) * T + t) * E;
-  const int first = blockIdx.x % cols * kRouterCols + 8 * (lane >> 4);
+  float* out = part + (static_cast<int64_t>(split) * T + t) * E;
+  const int first = tile % cols * kRouterCols + 8 * (lane >> 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (first + 2 * i < E) *reinterpret_cast<float2*>(out + first + 2 * i) = make_float2(acc[0][i], acc[1][i]);
@@ -206,7 +217,7 @@ __device__ __forceinline__ uint4 column(const uint2 (&v)[8], int p) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint2 stream8(const bf16_t* p) {
+__device__ __forceinline__ uint2 stream8(const char* p) {
   typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p)));
 }
@@ -225,18 +236,18 @@ __device__ __forceinline__ void few_rows(const bf16_t* const (&b)[NB], int N, in
                                          const Get& get, f32x4 (&acc)[NT][NB][4]) {
   const int lane = threadIdx.x & 63;
   const int quad = (lane >> 4) * 8;
-  const int64_t col = (lane & 15) * 4;
+  const uint32_t at = (static_cast<uint32_t>(quad) * N + (lane & 15) * 4) * 2;  // N <= 2^24
   auto batch = [&](int s, auto count) {
     constexpr int n = decltype(count)::value;
     uint2 v[n][NB][8];
     uint4 xv[n][NT][PARTS];
 #pragma unroll
     for (int u = 0; u < n; ++u) {
-      const int k = (s + u * stride) * 32 + quad;
+      const int k = (s + u * stride) * 32;
 #pragma unroll
       for (int m = 0; m < NB; ++m)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[u][m][r] = stream8(b[m] + static_cast<int64_t>(k + r) * N + col);
+        for (int r = 0; r < 8; ++r) v[u][m][r] = stream8(at_bytes(b[m] + static_cast<int64_t>(k + r) * N, at));
     }
     begin();
 #pragma unroll
@@ -300,7 +311,7 @@ template <int NT, int U>
 __device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ x,
                                              const bf16_t* const (&b)[2], bf16_t* __restrict__ a, float* __restrict__ gu,
                                              float* red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = rows.n;
   const bf16_t* xr[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -353,7 +364,7 @@ __global__ __launch_bounds__(kUpWaves* kWave, RANGES ? 2 : 4) void k_decode_gate
   } else {
     if (!read_rows(r, rows)) return;
   }
-  const int64_t base = static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * kCols;
+  const int64_t base = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.H * r.F + blockIdx.x * kCols;
   const bf16_t* const b[2] = {w_gate + base, w_up + base};
   // more than 16 rows in pairs of tiles: what comes in again then is few experts' weights
   if (FUSED || rows.n <= 16) {
@@ -368,7 +379,7 @@ template <int NT, bool RANGES>
 __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ a,
                                            const float* __restrict__ gu, const bf16_t* const (&b)[1],
                                            float* __restrict__ o, bf16_t* act, float* red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = rows.n;
   const int64_t RF = static_cast<int64_t>(r.T) * r.k * r.F;
   int64_t row[NT];
 #pragma unroll
@@ -397,7 +408,7 @@ __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows
     __syncthreads();
   };
   f32x4 acc[NT][1][4] = {};
-  few_rows<NT, 1, 2, NT == 1 ? 2 : 1>(b, r.H, wave, r.F / 32, kDownWaves, begin, get, acc);
+  few_rows<NT, 1, 2, RANGES ? 6 : NT == 1 ? 2 : 1>(b, r.H, wave, r.F / 32, kDownWaves, begin, get, acc);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (first + t * 16 >= n) break;
@@ -414,14 +425,14 @@ __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows
 }
 
 template <bool RANGES>
-__global__ __launch_bounds__(kDownWaves* kWave, 5) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
+__global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 5) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
                                                                    const float* __restrict__ gu,
                                                                    const bf16_t* __restrict__ w_down,
                                                                    float* __restrict__ o) {
   __shared__ Rows rows;
   __shared__ float red[kDownWaves * 4 * 256];
   if (!read_rows(r, rows)) return;
-  const bf16_t* const b[1] = {w_down + static_cast<int64_t>(rows.expert) * r.H * r.F + blockIdx.x * kCols};
+  const bf16_t* const b[1] = {w_down + static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.H * r.F + blockIdx.x * kCols};
   extern __shared__ bf16_t act[];
   if (RANGES || rows.n <= 16) {
     down_tiles<1, RANGES>(r, rows, 0, a, gu, b, o, act, red);
@@ -435,12 +446,14 @@ __global__ __launch_bounds__(kDownWaves* kWave, 5) void k_decode_down(DecodeRows
 // line (loads with the non-temporal policy lost its second half: 4.1 TB/s
 // against 5.5 at 16 tokens).
 
-// Products of 16 NT int8 rows with 16 channels of NB matrices (pointers at the
-// lane's channel and quarter), units u0, u0 + stride, ... < u1 of 128 k, U of
+// Products of 16 NT int8 rows (pointers at the lane's row and quarter) with 16
+// channels of NB matrices of pitch K (pointers at the first), units u0, u0 + stride, ... < u1 of 128 k, U of
 // them in flight; begin() as in few_rows.
 template <int NT, int NB, int U, class Begin>
-__device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const int8_t* const (&x)[NT], int u0, int u1,
-                                            int stride, Begin& begin, i32x4 (&acc)[NT][NB]) {
+__device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], int K, const int8_t* const (&x)[NT], int u0,
+                                            int u1, int stride, Begin& begin, i32x4 (&acc)[NT][NB]) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t at = static_cast<uint32_t>(lane & 15) * K + (lane >> 4) * 16;  // K <= 2^17
   auto batch = [&](int unit, auto count) {
     constexpr int n = decltype(count)::value;
     uint4 w[n][2][NB], v[n][2][NT];
@@ -450,7 +463,7 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const 
       for (int h = 0; h < 2; ++h) {
         const int k = (unit + i * stride) * 128 + h * 64;
 #pragma unroll
-        for (int m = 0; m < NB; ++m) w[i][h][m] = *reinterpret_cast<const uint4*>(b[m] + k);
+        for (int m = 0; m < NB; ++m) w[i][h][m] = *reinterpret_cast<const uint4*>(at_bytes(b[m] + k, at));
       }
     begin();
 #pragma unroll
@@ -475,20 +488,21 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], const 
   for (; unit < u1; unit += stride) batch(unit, std::integral_constant<int, 1>{});
 }
 
-// Short workgroups that many fit a compute unit: two waves and one unit of k
-// in flight in each reached 5.5 TB/s at 16 tokens, eight waves 4.2.
-constexpr int kUpWaves8 = 2, kDownWaves8 = 4;
+// Where the tiles are many, short workgroups of which many fit a compute unit:
+// two waves and one unit of k in flight in each reached 5.5 TB/s at 16 tokens,
+// eight waves 4.2.  Where they are so few that each compute unit has one or
+// two, eight waves with all of K in flight at once.
+constexpr int kUpWaves8 = 2, kUpWaves8Few = 8, kDownWaves8 = 4;
 
-template <int NT>
+template <int NT, int WAVES, int U>
 __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows& rows, int first,
                                                 const int8_t* __restrict__ x, const float* __restrict__ sx,
                                                 const moe_i8_experts& w, float* __restrict__ a, float* __restrict__ top,
                                                 int* red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, H = r.H;
-  const int64_t channel = static_cast<int64_t>(rows.expert) * r.F + blockIdx.x * 16;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = rows.n, H = r.H;
+  const int64_t channel = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.F + blockIdx.x * 16;
   const int quad = (lane >> 4) * 16;
-  const int64_t at = (channel + (lane & 15)) * H + quad;
-  const int8_t* const b[2] = {w.w_gate + at, w.w_up + at};
+  const int8_t* const b[2] = {w.w_gate + channel * H, w.w_up + channel * H};
   const int8_t* xr[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -497,18 +511,18 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
   }
   i32x4 acc[NT][2] = {};
   auto begin = [] {};
-  few_rows_i8<NT, 2, 1>(b, xr, wave, H / 128, kUpWaves8, begin, acc);
+  few_rows_i8<NT, 2, U>(b, H, xr, wave, H / 128, WAVES, begin, acc);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (first + t * 16 >= n) break;
     __syncthreads();  // the last tile has been read
     put_parts(acc[t], red);
     __syncthreads();
-    for (int i = threadIdx.x; i < 256; i += kUpWaves8 * kWave) {
+    for (int i = threadIdx.x; i < 256; i += WAVES * kWave) {
       const int m = first + t * 16 + entry_row(i), c = entry_lane(i), slot = rows.slot[min(m, n - 1)];
       const float s = sx[slot / r.k];
-      const float g = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 0, i))) * s * w.s_gate[channel + c];
-      const float u = static_cast<float>(unwrap(sum_parts<kUpWaves8, 2>(red, 1, i))) * s * w.s_up[channel + c];
+      const float g = static_cast<float>(unwrap(sum_parts<WAVES, 2>(red, 0, i))) * s * w.s_gate[channel + c];
+      const float u = static_cast<float>(unwrap(sum_parts<WAVES, 2>(red, 1, i))) * s * w.s_up[channel + c];
       const float v = silu_f(g) * u;
       // the row's largest of these 16 channels, in lanes 4, 8, 16 and 32 apart
       uint32_t most = __float_as_uint(v) & 0x7fffffffu;
@@ -521,12 +535,12 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
   }
 }
 
-template <bool FUSED>
-__global__ __launch_bounds__(kUpWaves8* kWave, 6) void k_decode_gateup_i8(DecodeRows r, const int8_t* __restrict__ x,
+template <bool FUSED, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, WAVES == kUpWaves8 ? 6 : 2) void k_decode_gateup_i8(DecodeRows r, const int8_t* __restrict__ x,
                                                                        const float* __restrict__ sx, moe_i8_experts w,
                                                                        float* __restrict__ a, float* __restrict__ top) {
   __shared__ Rows rows;
-  __shared__ int red[kUpWaves8 * 2 * 256];
+  __shared__ int red[WAVES * 2 * 256];
   if constexpr (FUSED) {
     __shared__ Selection sel;
     if (!select_rows(r, sel, rows)) return;
@@ -534,9 +548,9 @@ __global__ __launch_bounds__(kUpWaves8* kWave, 6) void k_decode_gateup_i8(Decode
     if (!read_rows(r, rows)) return;
   }
   if (FUSED || rows.n <= 16) {
-    gateup_tiles_i8<1>(r, rows, 0, x, sx, w, a, top, red);
+    gateup_tiles_i8<1, WAVES, WAVES == kUpWaves8 ? 1 : 2>(r, rows, 0, x, sx, w, a, top, red);
   } else {
-    for (int t = 0; t < rows.n; t += 32) gateup_tiles_i8<2>(r, rows, t, x, sx, w, a, top, red);
+    for (int t = 0; t < rows.n; t += 32) gateup_tiles_i8<2, WAVES, 1>(r, rows, t, x, sx, w, a, top, red);
   }
 }
 
@@ -575,11 +589,11 @@ template <int NT, int U, bool ROUND, class Begin>
 __device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& rows, int first, const int8_t* a,
                                               const float* sa, const moe_i8_experts& w, float* __restrict__ o,
                                               Begin& begin) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = rows.n, F = r.F;
-  const int column = (blockIdx.x * kDownWaves8 + wave) * 16 + (lane & 15);
-  const int64_t channel = static_cast<int64_t>(rows.expert) * r.H + column;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = rows.n, F = r.F;
+  const int first_column = (blockIdx.x * kDownWaves8 + wave) * 16, column = first_column + (lane & 15);
+  const int64_t channel = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.H + first_column;
   const int quad = (lane >> 4) * 16;
-  const int8_t* const b[1] = {w.w_down + channel * F + quad};
+  const int8_t* const b[1] = {w.w_down + channel * F};
   const int8_t* ar[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -587,8 +601,8 @@ __device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& r
     ar[t] = i < n ? a + static_cast<int64_t>(ROUND ? i : rows.slot[i]) * F + quad : nullptr;
   }
   i32x4 acc[NT][1] = {};
-  few_rows_i8<NT, 1, U>(b, ar, 0, F / 128, 1, begin, acc);
-  const float sd = w.s_down[channel];
+  few_rows_i8<NT, 1, U>(b, F, ar, 0, F / 128, 1, begin, acc);
+  const float sd = w.s_down[channel + (lane & 15)];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -667,20 +681,19 @@ int slots(const DecodeRows& r) { return std::min(r.E, r.T * r.k); }
 }  // namespace
 
 // Ranges of K of the bf16 gate/up product: two where few tokens leave its
-// tiles fewer than the chip's 256 compute units.  The down product then holds
-// the rows of an expert in LDS, at most 64 KB: with T k < E they are at most
-// the grid's slots, hence slots F < 256 kCols values, and else E >= 8 slots
-// leave F < 32 kCols for at most kFusedT rows.
+// tiles fewer than half of the chip's 256 compute units.  The down product then
+// holds the rows of an expert in LDS, at most 32 KB: with T k < E they are at
+// most the grid's slots, hence slots F <= 128 kCols values of two bf16, and else
+// E >= 8 slots leave F <= 16 kCols for at most kFusedT rows.
 int decode_ranges(int T, int E, int F, int k) {
-  return decode_fused(T) && F / kCols * std::min(E, T * k) < 256 ? 2 : 1;
+  return decode_fused(T) && F / kCols * std::min(E, T * k) <= 128 ? 2 : 1;
 }
 
 hipError_t launch_decode_router(const DecodeRows& r, const bf16_t* x, const bf16_t* w_r, int8_t* q, float* sx,
                                 hipStream_t s) {
   TraceScope trace_scope(K_DECODE_ROUTER, s);
-  const int tiles = cdiv(r.E, kRouterCols) * cdiv(r.T, 16), more = q != nullptr ? cdiv(r.T, kRouterSplits) : 0;
-  hipLaunchKernelGGL(k_decode_router, dim3(tiles + more), dim3(kRouterSplits * kWave), 0, s, x, w_r, r.T, r.H, r.E, r.part,
-                     r.counts, q, sx);
+  const int tiles = cdiv(r.E, kRouterCols) * cdiv(r.T, 16) * kRouterSplits, more = q != nullptr ? r.T : 0;
+  hipLaunchKernelGGL(k_decode_router, dim3(tiles + more), dim3(kWave), 0, s, x, w_r, r.T, r.H, r.E, r.part, r.counts, q, sx);
   return hipGetLastError();
 }
 
@@ -712,10 +725,12 @@ hipError_t launch_decode_gateup_i8(const DecodeRows& r, const int8_t* x, const f
                                    float* a, float* top, hipStream_t s) {
   TraceScope trace_scope(K_DECODE_GATEUP, s);
   const dim3 grid(r.F / 16, slots(r));
-  if (decode_fused(r.T))
-    hipLaunchKernelGGL(k_decode_gateup_i8<true>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
+  if (decode_fused(r.T) && grid.x * grid.y <= 1024)
+    hipLaunchKernelGGL((k_decode_gateup_i8<true, kUpWaves8Few>), grid, dim3(kUpWaves8Few * kWave), 0, s, r, x, sx, w, a, top);
+  else if (decode_fused(r.T))
+    hipLaunchKernelGGL((k_decode_gateup_i8<true, kUpWaves8>), grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
   else
-    hipLaunchKernelGGL(k_decode_gateup_i8<false>, grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
+    hipLaunchKernelGGL((k_decode_gateup_i8<false, kUpWaves8>), grid, dim3(kUpWaves8 * kWave), 0, s, r, x, sx, w, a, top);
   return hipGetLastError();
 }
 

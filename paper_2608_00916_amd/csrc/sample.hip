@@ -34,6 +34,7 @@ constexpr int kUnit = 42;  // weights are in units of 2^-42 of 2^N
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
 constexpr int kList = 4096;   // candidates held in LDS
 constexpr int kMine = kList / kRowThreads;
+constexpr int kFewGroups = 2048;  // groups with candidates, one or two in each, of which the list is likely to hold all
 constexpr int kFastK = 2048;  // the top_k that the list is for
 constexpr int kFine = 1024;   // parts of the list's range
 constexpr int kHeldPieces = 256, kHeldGroups = kHeldPieces * kWave;  // of a row whose groups' keys are held in LDS
@@ -503,10 +504,10 @@ struct Choice {
     __syncthreads();
   }
 
-  // Lists the groups whose largest key is at least lo; whether they are a
-  // quarter of all, or the row's keys are not held: then whole pieces are read.
-  __device__ __forceinline__ bool list_groups(uint32_t lo) {
-    if (!held()) return true;
+  // Lists the groups whose largest key is at least lo, and counts them; -1 where
+  // the row's keys are not held.
+  __device__ __forceinline__ int list_groups(uint32_t lo) {
+    if (!held()) return -1;
     __syncthreads();
     if (threadIdx.x == 0) sh.groups = 0;
     __syncthreads();
@@ -535,7 +536,7 @@ struct Choice {
       }
     }
     __syncthreads();
-    return sh.groups * 4 > groups;
+    return sh.groups;
   }
 
   // f(v, p) for the vectors v from place p on of the listed groups, spread over
@@ -598,10 +599,9 @@ struct Choice {
     if (at < kList) sh.list[at] = rank_of(v, place);
   }
 
-  // Collects the elements of keys from lo on: the count, of which the first
-  // kList are in the list.
-  __device__ __forceinline__ int collect(uint32_t lo) {
-    const bool whole = list_groups(lo);
+  // Collects the elements of keys from lo on (`whole`: of all pieces, else of
+  // the listed groups): the count, of which the first kList are in the list.
+  __device__ __forceinline__ int collect(uint32_t lo, bool whole) {
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     auto f = [&](const float* v, int p) -> u64 {
@@ -617,17 +617,13 @@ struct Choice {
   }
 
   // Collects the elements of keys lo .. hi - 1, and sums, by pieces, the
-  // weights of those from hi on that min_p keeps.  Where whole pieces are to be
-  // read the row's workgroups share them: each leaves its pieces' sums and its
-  // list in memory, and the last to be through goes on with all of it.  -1 where
-  // this workgroup has nothing more to do.
-  __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi) {
+  // weights of those from hi on that min_p keeps, from whole pieces.  The row's
+  // workgroups may share them: each leaves its pieces' sums and its list in
+  // memory, and the last to be through goes on with all of it.  -1 where this
+  // workgroup has nothing more to do.
+  __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi, bool shared) {
     const uint32_t least = max(hi, static_cast<uint32_t>(min_rank >> 32));
-    const bool whole = list_groups(lo);
-    const bool shared = whole && parts > 1;
-    if (!shared && part != 0) return -1;
     if (threadIdx.x == 0) sh.count = 0;
-    clear_sums();
     __syncthreads();
     auto f = [&](const float* v, int p) {
       u64 t = 0;
@@ -640,14 +636,7 @@ struct Choice {
       }
       return t;
     };
-    if (!whole) {
-      each_listed(f, [&](u64 t, int p) {
-        if (t != 0) atomicAdd(&sh.sums[p / kPiece], t);
-      });
-      __syncthreads();
-      return sh.count;
-    }
-    each_piece(lo, part * kRowWaves, parts * kRowWaves, f, [&](u64 t, int piece) {
+    each_piece(lo, shared ? part * kRowWaves : 0, shared ? parts * kRowWaves : kRowWaves, f, [&](u64 t, int piece) {
       t = wave_add(t);
       if (lane != 0) return;
       if (shared) st.piece_sum[piece] = t;
@@ -813,8 +802,7 @@ struct Choice {
 
   // The candidates are the list's n largest, of keys from lo on: filters them, draws.
   __device__ __forceinline__ void choose_from_list(int n, int k, uint32_t lo) {
-    const double x_lo = lo != 0 ? x_of(value_of(lo), s.c) : x_most - kOctaves, span = x_most - x_lo;
-    const double scale = span > 0.0 && span < 1e18 ? kFine / span : 0.0;
+    const double scale = scale_from(lo);
     u64 least = n > k ? border<true>(n, 0, k, x_most, scale, 0) : 0;
     if (s.filter_p) {
       u64 t = 0;
@@ -823,7 +811,17 @@ struct Choice {
         if (const u64 rank = sh.list[i]; rank >= least) t += weight(x_at(rank), N);
       least = max(least, border<false>(n, least, needed(total(t)), x_most, scale, 0));
     }
-    least = max(least, min_rank);
+    choose(n, max(least, min_rank));
+  }
+
+  // Fine bins per unit of x from the largest down to key lo's.
+  __device__ __forceinline__ double scale_from(uint32_t lo) const {
+    const double x_lo = lo != 0 ? x_of(value_of(lo), s.c) : x_most - kOctaves, span = x_most - x_lo;
+    return span > 0.0 && span < 1e18 ? kFine / span : 0.0;
+  }
+  // Draws from the list's elements of rank >= least.
+  __device__ __forceinline__ void choose(int n, u64 least) {
+    __syncthreads();
     clear_sums();
     __syncthreads();
     add_to_sums(n, least);
@@ -868,7 +866,7 @@ struct Choice {
 
   // The eighth of an octave in which the shortest prefix ends that holds top_p
   // of the weight: its keys lo .. hi - 1, and the weight that is needed of it.
-  __device__ __forceinline__ u64 border_bin(uint32_t& lo, uint32_t& hi, int& bin) {
+  __device__ __forceinline__ u64 border_bin(uint32_t& lo, uint32_t& hi, int& bin, u64& need) {
     const int chunks = pieces / kChunkWaves;
     __syncthreads();
     clear_bins();
@@ -895,7 +893,8 @@ struct Choice {
     __syncthreads();
     u64 t = 0;
     for (int i = threadIdx.x; i < kBins; i += kRowThreads) t += sh.bins[i];
-    bin = find_bin(needed(total(t)));
+    need = needed(total(t));
+    bin = find_bin(need);
     const double at = bin;
     lo = least_key([&](double x) { return bin_of(x, N) <= at; });
     hi = least_key([&](double x) { return bin_of(x, N) < at; });
@@ -980,7 +979,7 @@ struct Choice {
       hold();
       if (s.k <= kFastK) {
         const uint32_t lo = floor_of_kth(s.k);
-        const int n = collect(lo);
+        const int groups = list_groups(lo), n = collect(lo, groups < 0 || groups > pieces * kWave / 4);
         if (n <= kWave) {
           choose_from_few(n, s.k);
           return;
@@ -992,27 +991,39 @@ struct Choice {
       }
       least = search<true>(s.k);
       if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
-    } else if (s.filter_p) {
+    } else if (s.filter_p || s.filter_m) {
       hold();
-      uint32_t lo, hi;
-      int bin;
-      const u64 need = border_bin(lo, hi, bin);
-      const int n = collect_and_sum(lo, hi);
+      uint32_t lo = static_cast<uint32_t>(min_rank >> 32), hi = lo;
+      int bin = 0;
+      u64 need = 0, rest = 0;
+      if (s.filter_p) rest = border_bin(lo, hi, bin, need);
+      // few groups: all that is left is likely to fit the list
+      const int groups = list_groups(lo);
+      const bool few = groups >= 0 && groups <= kFewGroups;
+      if (few) {
+        if (part != 0) return;
+        const int n = collect(lo, false);
+        if (n <= kList) {
+          const u64 floor = static_cast<u64>(lo) << 32;
+          if (s.filter_p) least = border<false>(n, 0, need, x_most, scale_from(lo), floor);
+          choose(n, max(least, min_rank));
+          return;
+        }
+      }
+      const int n = collect_and_sum(lo, hi, !few && parts > 1);
       if (n < 0) return;
+      if (!s.filter_p) {
+        pick_by_sums(min_rank);
+        return;
+      }
       if (n > 0 && n <= kList) {
-        least = max(border<false>(n, 0, need, N + 1.0 - bin * (1.0 / kPerOctave), kFine * kPerOctave, static_cast<u64>(lo) << 32),
+        least = max(border<false>(n, 0, rest, N + 1.0 - bin * (1.0 / kPerOctave), kFine * kPerOctave, static_cast<u64>(lo) << 32),
                     min_rank);
         add_to_sums(n, least);
         pick_by_sums(least);
         return;
       }
       least = search<false>(needed(measure<false>(0)));
-    } else if (s.filter_m) {
-      hold();
-      const uint32_t lo = static_cast<uint32_t>(min_rank >> 32);
-      if (collect_and_sum(lo, lo) < 0) return;
-      pick_by_sums(min_rank);
-      return;
     } else {
       for (int i = threadIdx.x; i < pieces; i += kRowThreads)
         sh.sums[i] = rescale(st.piece_sum[i], st.ref[i / kChunkWaves], N);

@@ -203,7 +203,7 @@ def test_norm_backward_against_differences():
 # ------------------------------------------------------------------ the expert layer for a few tokens
 DECODE = [(1, 128, 8, 128, 1), (1, 2048, 128, 768, 8), (2, 256, 8, 384, 8), (16, 512, 16, 256, 2), (17, 384, 8, 128, 3),
           (33, 128, 16, 640, 4), (64, 1152, 8, 128, 8), (64, 128, 256, 128, 6), (5, 4096, 8, 1280, 2), (3, 256, 32, 2176, 32),
-          (31, 640, 40, 384, 5), (8, 128, 8, 1920, 8), (8, 128, 8, 8320, 2), (7, 128, 256, 128, 32), (4, 2048, 64, 768, 8),
+          (31, 640, 40, 384, 5), (8, 128, 8, 1920, 8), (8, 128, 8, 1024, 8), (8, 128, 8, 8320, 2), (7, 128, 256, 128, 32), (4, 2048, 64, 768, 8),
           (9, 1024, 128, 256, 4)]
 
 
