@@ -177,6 +177,18 @@ __device__ __forceinline__ u64 wave_upto(u64 v) {
   v = add_from<0x142, 0xa>(v);
   return add_from<0x143, 0xc>(v);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_upto(int v) {
+  v = add_from<0x111, 0xf>(v);
+  v = add_from<0x112, 0xf>(v);
+  v = add_from<0x114, 0xf>(v);
+  v = add_from<0x118, 0xf>(v);
+  v = add_from<0x142, 0xa>(v);
+  return add_from<0x143, 0xc>(v);
+}
 __device__ __forceinline__ u64 lane_value(u64 v, int lane) {  // `lane` is the same in every lane
   const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane);
   const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
@@ -252,15 +264,15 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   const int piece = chunk * kChunkWaves + wave;
   float v[kGroup];
   row.load(piece, v);
-  u64 best = 0;
-  uint32_t top = 0;
+  float most = -INFINITY;  // of what is not NaN
 #pragma unroll
-  for (int e = 0; e < kGroup; ++e) {
-    const uint32_t key = key_of(v[e]);
-    top = max(top, key);
-    best = max(best, static_cast<u64>(key) << 32 | static_cast<uint32_t>(~(row.place(piece, e) - row.skew)));
-  }
-  best = wave_most(best);
+  for (int e = 0; e < kGroup; ++e) most = fmaxf(most, v[e]);
+  const uint32_t top = key_of(most);
+  uint32_t first = 0;  // ~index of the group's first element of that value
+#pragma unroll
+  for (int e = 0; e < kGroup; ++e)
+    if (v[e] == most) first = max(first, static_cast<uint32_t>(~(row.place(piece, e) - row.skew)));
+  u64 best = wave_most(static_cast<u64>(top) << 32 | first);
   if (lane == 0) bests[wave] = best;
   const bool binned = s.filter_p && !s.greedy && !s.filter_k;
   if (binned)
@@ -274,21 +286,26 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   st.top[chunk * (kChunkWaves * kWave) + tid] = top;
   const bool summed = !s.filter_k && !s.filter_p && !s.filter_m;
   if (!summed && !binned) return;
-  const uint32_t most = static_cast<uint32_t>(best >> 32);
-  const double N = most == 0 ? -1e305 : floor(x_of(value_of(most), s.c));
+  const uint32_t largest = static_cast<uint32_t>(best >> 32);
+  const double N = largest == 0 ? -1e305 : floor(x_of(value_of(largest), s.c));
   if (tid == 0) st.ref[chunk] = N;
-  u64 sum = 0;
-#pragma unroll
-  for (int e = 0; e < kGroup; ++e) {
-    const double x = x_of(v[e], s.c);
-    const u64 of_x = weight(x, N), w = key_of(v[e]) == 0 ? 0 : of_x;  // no branch: most elements count
-    sum += w;
-    if (binned && w != 0) atomicAdd(&bins[static_cast<int>(fmin(bin_of(x, N), kBins - 1.0))], w);
-  }
+  auto weight_of = [&](float value, double x) -> u64 {  // no branch: most elements count
+    const u64 w = weight(x, N);
+    return value > -INFINITY ? w : 0;
+  };
   if (summed) {
+    u64 sum = 0;
+#pragma unroll
+    for (int e = 0; e < kGroup; ++e) sum += weight_of(v[e], x_of(v[e], s.c));
     sum = wave_add(sum);
     if (lane == 0) st.piece_sum[piece] = sum;
     return;
+  }
+#pragma unroll
+  for (int e = 0; e < kGroup; ++e) {
+    const double x = x_of(v[e], s.c);
+    const u64 w = weight_of(v[e], x);
+    if (w != 0) atomicAdd(&bins[static_cast<int>(fmin(bin_of(x, N), kBins - 1.0))], w);
   }
   __syncthreads();
   for (int i = tid; i < kBins; i += kChunkWaves * kWave) st.bins[static_cast<int64_t>(chunk) * kBins + i] = bins[i];
@@ -540,36 +557,43 @@ struct Choice {
   }
 
   // f(v, p) for the vectors v from place p on of the listed groups, spread over
-  // all threads; t, what it returned, to add(t, p).
-  template <class F, class Add>
-  __device__ __forceinline__ void each_listed(F f, Add add) {
+  // all threads; whole waves call it, lanes without a vector with -infinities.
+  template <class F>
+  __device__ __forceinline__ void each_listed(F f) {
     constexpr int W = Row<F32>::W, kVecs = kGroup / W;
     const int n = sh.groups * kVecs;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += kRowThreads) {
-      const int g = sh.group[i / kVecs];
-      const int p = g / kWave * kPiece + i % kVecs * (kWave * W) + g % kWave * W;
-      float v[W];
-      row.vec(p, v);
-      add(f(v, p), p);
+    for (int first = wave * kWave; first < n; first += 2 * kRowThreads) {
+      float v[2][W];
+      int p[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int i = first + j * kRowThreads + lane;
+        const int g = sh.group[min(i, n - 1) / kVecs];
+        p[j] = g / kWave * kPiece + i % kVecs * (kWave * W) + g % kWave * W;
+        row.vec(p[j], v[j]);
+        if (i >= n)
+#pragma unroll
+          for (int e = 0; e < W; ++e) v[j][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) f(v[j], p[j]);
     }
   }
-  // The same for pieces from, from + step, ... with a group of lo or more, a wave
-  // each, and add(t, piece) by whole waves.
+  // The same for the whole pieces from, from + step, ... that have a group of lo
+  // or more, a wave each, and add(the sum of what f returned, piece).
   template <class F, class Add>
   __device__ __forceinline__ void each_piece(uint32_t lo, int from, int step, F f, Add add) {
     constexpr int W = Row<F32>::W;
 #pragma unroll 1
     for (int piece = from + wave; piece < pieces; piece += step) {
       const uint32_t top = top_of(piece * kWave + lane);
-      const bool on = top != 0 && top >= lo;
       u64 t = 0;
-      if (__any(on)) {
+      if (__any(top != 0 && top >= lo)) {
         float v[kGroup];
         row.load(piece, v);
-        if (on)
 #pragma unroll
-          for (int e = 0; e < kGroup; e += W) t += f(v + e, row.place(piece, e));
+        for (int e = 0; e < kGroup; e += W) t += f(v + e, row.place(piece, e));
       }
       add(t, piece);
     }
@@ -594,9 +618,27 @@ struct Choice {
                });
   }
 
-  __device__ __forceinline__ void put_in_list(float v, int place) {
-    const int at = atomicAdd(&sh.count, 1);
-    if (at < kList) sh.list[at] = rank_of(v, place);
+  // Elements of a vector whose keys are lo .. hi - 1 (hi 0: all from lo on) to the
+  // list; a wave's places in it come from one addition to the count.
+  __device__ __forceinline__ void put_in_list(const float* v, int p, uint32_t lo, uint32_t hi) {
+    constexpr int W = Row<F32>::W;
+    uint32_t hits = 0;
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const uint32_t key = key_of(v[e]);
+      hits |= key != 0 && key >= lo && (hi == 0 || key < hi) ? 1u << e : 0u;
+    }
+    if (!__any(hits != 0)) return;
+    const int n = __popc(hits), upto = wave_upto(n);
+    int base = 0;
+    if (lane == kWave - 1) base = atomicAdd(&sh.count, upto);
+    int at = __builtin_amdgcn_readlane(base, kWave - 1) + upto - n;
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+      if (hits >> e & 1) {
+        if (at < kList) sh.list[at] = rank_of(v[e], p + e);
+        ++at;
+      }
   }
 
   // Collects the elements of keys from lo on (`whole`: of all pieces, else of
@@ -605,13 +647,11 @@ struct Choice {
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     auto f = [&](const float* v, int p) -> u64 {
-#pragma unroll
-      for (int e = 0; e < Row<F32>::W; ++e)
-        if (const uint32_t key = key_of(v[e]); key != 0 && key >= lo) put_in_list(v[e], p + e);
+      put_in_list(v, p, lo, 0);
       return 0;
     };
     if (whole) each_piece(lo, 0, kRowWaves, f, [](u64, int) {});
-    else each_listed(f, [](u64, int) {});
+    else each_listed(f);
     __syncthreads();
     return sh.count;
   }
@@ -629,11 +669,10 @@ struct Choice {
       u64 t = 0;
 #pragma unroll
       for (int e = 0; e < Row<F32>::W; ++e) {
-        const uint32_t key = key_of(v[e]);
         const u64 w = weight(x_of(v[e], s.c), N);
-        t += key >= least ? w : 0;
-        if (key != 0 && key >= lo && key < hi) put_in_list(v[e], p + e);
+        t += key_of(v[e]) >= least ? w : 0;
       }
+      if (lo < hi) put_in_list(v, p, lo, hi);
       return t;
     };
     each_piece(lo, shared ? part * kRowWaves : 0, shared ? parts * kRowWaves : kRowWaves, f, [&](u64 t, int piece) {
@@ -871,22 +910,22 @@ struct Choice {
     __syncthreads();
     clear_bins();
     __syncthreads();
-    // a thread per bin, four chunks' on their way at a time
+    // a thread per bin, eight chunks' on their way at a time
     if (threadIdx.x < kBins) {
       u64 t = 0;
 #pragma unroll 1
-      for (int c = 0; c < chunks; c += 4) {
-        u64 w[4];
-        double ref[4];
+      for (int c = 0; c < chunks; c += 8) {
+        u64 w[8];
+        double ref[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ref[j] = c + j < chunks ? st.ref[c + j] : -1e305;
+        for (int j = 0; j < 8; ++j) ref[j] = c + j < chunks ? st.ref[c + j] : -1e305;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
           const double from = static_cast<int>(threadIdx.x) - kPerOctave * (N - ref[j]);
           w[j] = from >= 0.0 ? st.bins[static_cast<int64_t>(c + j) * kBins + static_cast<int>(from)] : 0;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t += rescale(w[j], ref[j], N);
+        for (int j = 0; j < 8; ++j) t += rescale(w[j], ref[j], N);
       }
       sh.bins[threadIdx.x] = t;
     }
@@ -951,6 +990,7 @@ struct Choice {
   }
 
   __device__ __forceinline__ void run() {
+    if (!s.greedy && (s.filter_k || s.filter_p || s.filter_m) && !(part != 0 && s.filter_k)) hold();
     // the row's largest
     u64 best = 0;
     for (int i = lane; i < pieces / kChunkWaves; i += kWave) best = max(best, st.best[i]);
@@ -976,7 +1016,6 @@ struct Choice {
     }
     u64 least = 0;
     if (s.filter_k) {
-      hold();
       if (s.k <= kFastK) {
         const uint32_t lo = floor_of_kth(s.k);
         const int groups = list_groups(lo), n = collect(lo, groups < 0 || groups > pieces * kWave / 4);
@@ -992,7 +1031,6 @@ struct Choice {
       least = search<true>(s.k);
       if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
     } else if (s.filter_p || s.filter_m) {
-      hold();
       uint32_t lo = static_cast<uint32_t>(min_rank >> 32), hi = lo;
       int bin = 0;
       u64 need = 0, rest = 0;
