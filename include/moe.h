@@ -32,7 +32,8 @@
  *     static scratch array of moe_fwd_noalloc aside, which the HIP runtime
  *     reserves on each GPU when it loads the library's device code).
  *   - "bf16" tensors are IEEE bfloat16 (2 bytes); accumulation is fp32.
- *   - Every device pointer must be 16-byte aligned.
+ *   - Every device pointer must be 16-byte aligned, but for those of moe_sample
+ *     (aligned to their elements).
  *   - Calls are asynchronous on `stream` (a hipStream_t; NULL = the null
  *     stream) and never synchronise the host; counts stay on the device.
  *   - All argument checks happen before any launch: on an error nothing is

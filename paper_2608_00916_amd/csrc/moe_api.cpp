@@ -676,6 +676,6 @@ int moe_experts_bwd(const moe_experts_dims* d, const void* xp, const void* w_gat
 
 const char* moe_last_error(void) { return g_err; }
 
-int moe_version(void) { return 200; }
+int moe_version(void) { return 300; }
 
 }  // extern "C"

@@ -619,3 +619,64 @@ def test_norms_train_around_the_block():
         # the block's gradients hold to 2e-2 of the largest; along a random direction errors add up in squares
         size = np.linalg.norm(host(dx)) + np.linalg.norm(host(dw))
         assert abs(got - diff) <= 2e-2 * 3 * size
+
+
+def test_sampling_on_two_streams_at_once():
+    """Flat rows, which a row's workgroups share: two samplers side by side, again and again, the same tokens."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("sample streams")
+    B, V = 24, 60000
+    ops = [moe.Sampler(B, V) for _ in range(2)]
+    logits = [rows_of(B, V, 20 + i, True) for i in range(2)]
+    u = dev(gen(3).random(B).astype(np.float32))
+    t, p = dev(np.full(B, 2.0, np.float32)), dev(np.full(B, 0.97, np.float32))
+    want = []
+    for op, l in zip(ops, logits):
+        got = [o.clone() for o in op.forward(l, u, temperature=t, top_p=p)]
+        check_tokens(l, u, got, temperature=t, top_p=p)
+        want.append(got)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    seen = [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                seen[i].append([o.clone() for o in ops[i].forward(logits[i], u, temperature=t, top_p=p)])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for got in seen[i]:
+            assert torch.equal(got[0], want[i][0]) and torch.equal(got[1], want[i][1])
+
+
+def test_norm_training_step_in_two_graphs():
+    """Forward and backward captured twice with buffers of their own, replayed in turn with eager calls between."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("norm graphs")
+    T, H = 77, 1280
+    g = gen(9)
+    w = bf16(1 + 0.1 * g.standard_normal(H))
+    x, r, dy = (bf16(g.standard_normal((T, H))) for _ in range(3))
+
+    def step(op):
+        h, y, q, scale = op.forward(x, r)
+        dx, dw = op.backward(h, dy, y)
+        return h, y, q, scale, dx, dw
+
+    ops = [moe.RMSNorm(T, w, out="both", dw_fp32=True, backward=True) for _ in range(3)]
+    step(ops[2])
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for op in ops[:2]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(step(op))
+        graphs.append(graph)
+    for i in range(6):
+        for t in (x, r, dy):
+            t.copy_(bf16(g.standard_normal((T, H))))
+        want = [o.clone() for o in step(ops[2])]
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[i % 2], want)), i

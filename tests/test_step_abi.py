@@ -145,6 +145,27 @@ def test_tensors_that_do_not_fit():
         moe.Sampler(1, 2 ** 20 + 1, device="cpu")
 
 
+def test_masks_and_devices_that_do_not_fit(monkeypatch):
+    from paper_2608_00916_amd import step
+    d = _lib.MoeDims(4, 128, 8, 128, 2, 0, 0.0, 0.0)
+    for mask in (torch.ones(4, dtype=torch.uint8), torch.ones(4, dtype=torch.bool)):
+        with pytest.raises(ValueError, match="no mask"):
+            step._mask(mask, d)
+    d.flags = _lib.MOE_F_MASK
+    with pytest.raises(ValueError, match="must be uint8 or bool"):
+        step._mask(torch.ones(4), d)
+    with pytest.raises(ValueError, match="token_mask has"):
+        step._mask(torch.ones(3, dtype=torch.bool), d)
+
+    class There:
+        def get_device(self):
+            return 1
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="on device 1, the current one is 0"):
+        step._on(There(), None)
+
+
 def test_norm_backward_form_against_differences():
     """The 64-bit gradient is that of the 64-bit norm, by central differences of sum(dy v) + sum(dh h)."""
     g = np.random.default_rng(0)
