@@ -441,30 +441,52 @@ __global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 5) void k_decode_do
   }
 }
 
-// ---- int8 weights.  They are K-contiguous: lane l reads 16 bytes of channel
-// l % 16, the instruction's operand as it is, and two loads a whole 128-byte
-// line (loads with the non-temporal policy lost its second half: 4.1 TB/s
-// against 5.5 at 16 tokens).
+// ---- int8 weights.  They are K-contiguous, and the instruction takes 16
+// bytes of channel l % 16 per lane, half a line of each of 16 channels: the down
+// product (rows of F) loads them so.  The gate/up product (rows of H, longer
+// than a wave's share) brings whole 128-byte lines of 8 channels by a load, lane
+// l the bytes 16 c of channel l % 8, c = l / 16 and 4 more in the upper half of
+// 16 lanes; two such loads, of channels 0 .. 7 and 8 .. 15, become two operands by
+// an exchange between the halves.  With that its loads can pass the caches: 77 ->
+// 66 us at 64 tokens (6.0 TB/s), where half lines lose their other half.  The down
+// product lost by it (48 -> 53 us).
+__device__ __forceinline__ uint32_t line_at(int K) {  // K <= 2^17
+  const int lane = threadIdx.x & 63;
+  return static_cast<uint32_t>(lane & 7) * K + ((lane >> 4) + 4 * ((lane >> 3) & 1)) * 16;
+}
+__device__ __forceinline__ uint32_t with_upper(uint32_t a, uint32_t b) {  // lanes 8 .. 15 of 16: b of 8 lanes below
+  return __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);
+}
+__device__ __forceinline__ uint32_t with_lower(uint32_t b, uint32_t a) {  // lanes 0 .. 7 of 16: a of 8 lanes above
+  return __builtin_amdgcn_update_dpp(b, a, 0x128, 0xf, 0x3, false);
+}
+__device__ __forceinline__ void to_operands(uint4& a, uint4& b) {
+  const uint4 u = a, v = b;
+  a = make_uint4(with_upper(u.x, v.x), with_upper(u.y, v.y), with_upper(u.z, v.z), with_upper(u.w, v.w));
+  b = make_uint4(with_lower(v.x, u.x), with_lower(v.y, u.y), with_lower(v.z, u.z), with_lower(v.w, u.w));
+}
 
 // Products of 16 NT int8 rows (pointers at the lane's row and quarter) with 16
 // channels of NB matrices of pitch K (pointers at the first), units u0, u0 + stride, ... < u1 of 128 k, U of
 // them in flight; begin() as in few_rows.
-template <int NT, int NB, int U, class Begin>
+template <int NT, int NB, int U, bool LINES, class Begin>
 __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], int K, const int8_t* const (&x)[NT], int u0,
                                             int u1, int stride, Begin& begin, i32x4 (&acc)[NT][NB]) {
   const int lane = threadIdx.x & 63;
-  const uint32_t at = static_cast<uint32_t>(lane & 15) * K + (lane >> 4) * 16;  // K <= 2^17
+  const uint32_t at = LINES ? line_at(K) : static_cast<uint32_t>(lane & 15) * K + (lane >> 4) * 16;
   auto batch = [&](int unit, auto count) {
     constexpr int n = decltype(count)::value;
     uint4 w[n][2][NB], v[n][2][NT];
 #pragma unroll
     for (int i = 0; i < n; ++i)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = (unit + i * stride) * 128 + h * 64;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int m = 0; m < NB; ++m) w[i][h][m] = *reinterpret_cast<const uint4*>(at_bytes(b[m] + k, at));
-      }
+        for (int m = 0; m < NB; ++m) {
+          const int8_t* const from = b[m] + (unit + i * stride) * 128;
+          if constexpr (LINES) w[i][h][m] = load_nt(at_bytes(from + static_cast<int64_t>(8 * h) * K, at));
+          else w[i][h][m] = *reinterpret_cast<const uint4*>(at_bytes(from + 64 * h, at));
+        }
     begin();
 #pragma unroll
     for (int i = 0; i < n; ++i)
@@ -474,6 +496,11 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], int K,
         for (int t = 0; t < NT; ++t)
           v[i][h][t] = x[t] != nullptr ? *reinterpret_cast<const uint4*>(x[t] + (unit + i * stride) * 128 + h * 64)
                                        : make_uint4(0, 0, 0, 0);
+    if constexpr (LINES)
+#pragma unroll
+      for (int i = 0; i < n; ++i)
+#pragma unroll
+        for (int m = 0; m < NB; ++m) to_operands(w[i][0][m], w[i][1][m]);
 #pragma unroll
     for (int i = 0; i < n; ++i)
 #pragma unroll
@@ -489,8 +516,8 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], int K,
 }
 
 // Where the tiles are many, short workgroups of which many fit a compute unit:
-// two waves and one unit of k in flight in each reached 5.5 TB/s at 16 tokens,
-// eight waves 4.2.  Where they are so few that each compute unit has one or
+// two waves and one unit of k in flight in each (eight waves took 1.3 times as
+// long at 16 tokens).  Where they are so few that each compute unit has one or
 // two, eight waves with all of K in flight at once.
 constexpr int kUpWaves8 = 2, kUpWaves8Few = 8, kDownWaves8 = 4;
 
@@ -511,7 +538,7 @@ __device__ __forceinline__ void gateup_tiles_i8(const DecodeRows& r, const Rows&
   }
   i32x4 acc[NT][2] = {};
   auto begin = [] {};
-  few_rows_i8<NT, 2, U>(b, H, xr, wave, H / 128, WAVES, begin, acc);
+  few_rows_i8<NT, 2, U, true>(b, H, xr, wave, H / 128, WAVES, begin, acc);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (first + t * 16 >= n) break;
@@ -601,7 +628,7 @@ __device__ __forceinline__ void down_tiles_i8(const DecodeRows& r, const Rows& r
     ar[t] = i < n ? a + static_cast<int64_t>(ROUND ? i : rows.slot[i]) * F + quad : nullptr;
   }
   i32x4 acc[NT][1] = {};
-  few_rows_i8<NT, 1, U>(b, F, ar, 0, F / 128, 1, begin, acc);
+  few_rows_i8<NT, 1, U, false>(b, F, ar, 0, F / 128, 1, begin, acc);
   const float sd = w.s_down[channel + (lane & 15)];
 #pragma unroll
   for (int t = 0; t < NT; ++t)

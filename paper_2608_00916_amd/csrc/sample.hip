@@ -373,6 +373,7 @@ __device__ __forceinline__ void sort_list(u64* list, int n) {
   __syncthreads();
 }
 
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ u64 part_of(double share, u64 all) {  // floor(share all)
   return static_cast<u64>(share * static_cast<double>(all));
 }
@@ -867,40 +868,45 @@ struct Choice {
     pick_by_sums(least);
   }
 
-  // The same for up to a wave of candidates, by the first wave alone: places
-  // and sums in the order, then in index order, from one comparison with each of
-  // the others.
+  // The same for up to a wave of candidates, a lane each: places and sums in
+  // the order, then sums in index order, from a comparison with each of the
+  // others, an eighth of them by each of the waves.
   __device__ __forceinline__ void choose_from_few(int n, int k) {
-    if (wave != 0) return;
+    static_assert(kRowWaves * 8 == kWave && 2 * kRowThreads <= kFine, "eight others a wave, two sets of sums in bins");
     const u64 rank = lane < n ? sh.list[lane] : 0;
-    u64 w = rank != 0 ? weight(x_at(rank), N) : 0;
-    int place = 0;
-    u64 less = 0;
-#pragma unroll 1
-    for (int j = 0; j < n; j += 4)  // lanes from n on hold zeros
+    u64 w = rank != 0 ? weight(x_at(rank), N) : 0, t = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u64 other = lane_value(rank, j + i), ow = lane_value(w, j + i);
-        if (other > rank) {
-          ++place;
-          less += ow;
-        }
-      }
-    if (place >= k) w = 0;
-    if (s.filter_p && less >= needed(wave_add(w))) w = 0;
+    for (int i = 0; i < 8; ++i) {
+      const int j = wave_index() * 8 + i;
+      const u64 other = lane_value(rank, j), ow = lane_value(w, j);
+      t += other > rank ? ow | 1ull << 56 : 0;  // weights sum to less than 2^50, places above them
+    }
+    t = add_up(t, 0);
+    if (static_cast<int>(t >> 56) >= k) w = 0;
+    if (s.filter_p && (t & ((1ull << 56) - 1)) >= needed(wave_add(w))) w = 0;
     if (rank < min_rank) w = 0;
     const u64 all = wave_add(w), r = draw(all);
     const uint32_t index = ~static_cast<uint32_t>(rank);
-    less = 0;
-#pragma unroll 1
-    for (int j = 0; j < n; j += 4)
+    t = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u64 ow = lane_value(w, j + i);
-        if (static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(index), j + i)) < index) less += ow;
-      }
-    if (less <= r && r < less + w)
+    for (int i = 0; i < 8; ++i) {
+      const int j = wave_index() * 8 + i;
+      const u64 ow = lane_value(w, j);
+      t += static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(index), j)) < index ? ow : 0;
+    }
+    t = add_up(t, 1);
+    if (wave == 0 && t <= r && r < t + w)
       write(static_cast<int>(index) + row.skew, value_of(static_cast<uint32_t>(rank >> 32)), all);
+  }
+  // The sum of the waves' values of a lane, in set 0 or 1 of the bins.
+  __device__ __forceinline__ u64 add_up(u64 v, int set) {
+    u64* const at = sh.bins + set * kRowThreads;
+    at[threadIdx.x] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int i = 0; i < kRowWaves; ++i) v += at[i * kWave + lane];
+    return v;
   }
 
   // The eighth of an octave in which the shortest prefix ends that holds top_p
