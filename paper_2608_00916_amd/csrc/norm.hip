@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
   constexpr int ROWS = kBwdRows<WAVES>, RT = kRowThreads<WAVES>;
   __shared__ float2 sums[2][ROWS][WAVES];
   constexpr bool kInLds = VEC > 2;
-  extern __shared__ float dws[];  // H floats where a workgroup has more than one row at a time, or kInLds
+  extern __shared__ __attribute__((aligned(16))) float dws[];  // ROWS H floats where there are rows at a time, or kInLds
   const int in_row = threadIdx.x % RT, wave = in_row >> 6, slot = threadIdx.x / RT;
   const int H = a.H;
   const float inv_h = 1.0f / static_cast<float>(H);
@@ -248,18 +248,21 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bw
     }
   }
   float* part = a.part + static_cast<int64_t>(blockIdx.x) * H;
-  if constexpr (ROWS > 1) {
-    for (int k = 0; k < ROWS; ++k) {  // the rows' shares one after another
-      if (k > 0) __syncthreads();
-      if (slot != k) continue;
+  if constexpr (ROWS > 1) {  // the rows' shares side by side in LDS, then added in their order
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int c = (i * RT + in_row) * 8;
-        if (c >= H) continue;
-        float* at = k + 1 < ROWS ? dws + c : part + c;
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (i * RT + in_row) * 8;
+      if (c >= H) continue;
+      float* const at = dws + slot * H + c;
+      *reinterpret_cast<float4*>(at) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      *reinterpret_cast<float4*>(at + 4) = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < H; c += RT * ROWS) {
+      float t = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) at[j] = k == 0 ? acc[i][j] : dws[c + j] + acc[i][j];
-      }
+      for (int k = 0; k < ROWS; ++k) t += dws[k * H + c];
+      part[c] = t;
     }
   } else {
 #pragma unroll
@@ -311,7 +314,7 @@ template <int WAVES, int VEC>
 void start_bwd(const NormBwd& a, hipStream_t s) {
   constexpr int rows = kBwdRows<WAVES>;
   hipLaunchKernelGGL((k_norm_bwd<WAVES, VEC>), dim3(norm_bwd_parts(a.T, a.H)), dim3(kRowThreads<WAVES> * rows),
-                     (VEC > 2 ? VEC * 8 * kRowThreads<WAVES> : rows > 1 ? a.H : 0) * sizeof(float), s, a);
+                     (VEC > 2 ? VEC * 8 * kRowThreads<WAVES> : rows > 1 ? rows * a.H : 0) * sizeof(float), s, a);
 }
 
 }  // namespace
