@@ -357,7 +357,7 @@ hipError_t launch_norm_fwd(const NormFwd& all, hipStream_t s) {
 // fp32: 256 of rows of 5120 are 8% of what 3001 rows move, 512 are 17%).
 int norm_bwd_parts(int T, int H) {
   const int waves = bwd_waves(H), rows = waves == 1 ? kBwdRows<1> : waves == 4 ? kBwdRows<4> : kBwdRows<16>;
-  return std::min(cdiv(T, rows), waves == 16 ? 256 : 512);
+  return std::min((T - 1) / rows + 1, waves == 16 ? 256 : 512);  // no sum that T near 2^31 overflows
 }
 
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s) {

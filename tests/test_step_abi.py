@@ -166,6 +166,13 @@ def test_masks_and_devices_that_do_not_fit(monkeypatch):
         step._on(There(), None)
 
 
+def test_norm_workspace_of_the_most_rows():
+    """As many shares of dw as for fewer rows: their number must not overflow near 2^31 rows."""
+    for H in (8, 2048, 32768):
+        few, most = (moe.moe_norm_bwd_workspace_bytes(moe.norm_dims(T, H)) for T in (10 ** 6, 2 ** 31 - 1))
+        assert 0 < most == few, H
+
+
 def test_norm_backward_form_against_differences():
     """The 64-bit gradient is that of the 64-bit norm, by central differences of sum(dy v) + sum(dh h)."""
     g = np.random.default_rng(0)
