@@ -36,10 +36,12 @@ def _bf_rows(name, t, shape):
     return _rows(t)
 
 
-def _on(t, stream):
+def _on(t, stream, *others):
     """The stream's handle; tensors of another device than the current one are refused."""
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"tensors on device {t.get_device()}, the current one is {torch.cuda.current_device()}")
+    at = torch.cuda.current_device()
+    for t in (t, *others):
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors on device {t.get_device()}, the current one is {at}")
     return _s(stream)
 
 
@@ -67,7 +69,7 @@ def moe_norm_fwd(d, x, residual, w, h=None, y=None, q=None, scale=None, stream=N
         _shape("scale", scale, shape[:1])
     pr, ldr = (None, 0) if residual is None else _rows(residual)
     check(lib().moe_norm_fwd(_ref(d), *_rows(x), pr, ldr, _p(w, _bf), _p(h, _bf), _p(y, _bf), _p(q, torch.int8),
-                             _p(scale, _f32), _on(x, stream)))
+                             _p(scale, _f32), _on(x, stream, residual, w, h, y, q, scale)))
 
 
 def moe_norm_bwd_workspace_bytes(d: MoeNormDims) -> int:
@@ -86,7 +88,7 @@ def moe_norm_bwd(d, h, w, dy, dh, dx, dw, ws, stream=None):
     pu, ldu = (None, 0) if dh is None else _rows(dh)
     check(lib().moe_norm_bwd(_ref(d), *_rows(h), _p(w, _bf), *_rows(dy), pu, ldu, _p(dx, _bf),
                              _p(dw, _f32 if d.flags & MOE_F_DW_FP32 else _bf), _p(ws), ws.numel() * ws.element_size(),
-                             _on(h, stream)))
+                             _on(h, stream, w, dy, dh, dx, dw, ws)))
 
 
 class RMSNorm(_Held):
@@ -152,11 +154,11 @@ class RMSNorm(_Held):
         w, h, y, q, scale = self._b
         if residual is None:
             check(lib().moe_norm_fwd(d, *_bf_rows("x", x, shape), None, 0, w, None, y, q, scale,
-                                     _on(x, stream)))
+                                     _on(x, stream, self.weight)))
             outs = None, self.y, self.q, self.scale
         else:
             check(lib().moe_norm_fwd(d, *_bf_rows("x", x, shape), *_bf_rows("residual", residual, shape), w, h, y, q,
-                                     scale, _on(x, stream)))
+                                     scale, _on(x, stream, residual, self.weight)))
             outs = self.h, self.y, self.q, self.scale
         return outs if shape is self._full[0] else tuple(None if o is None else o[:shape[0]] for o in outs)
 
@@ -169,7 +171,7 @@ class RMSNorm(_Held):
         shape, d = self._dims(h)
         u = (None, 0) if dh is None else _bf_rows("dh", dh, shape)
         check(lib().moe_norm_bwd(d, *_bf_rows("h", h, shape), self._b[0], *_bf_rows("dy", dy, shape), *u, *self._g,
-                                 _on(h, stream)))
+                                 _on(h, stream, dy, dh, self.weight)))
         return (self.dx if shape is self._full[0] else self.dx[:shape[0]]), self.dw
 
 
@@ -199,7 +201,8 @@ def moe_decode(d, x, w_r, w_gate, w_up, w_down, token_mask, y, ws, stream=None):
     _least(x=(x, d.T * d.H), w_r=(w_r, d.H * d.E), w_gate=(w_gate, n), w_up=(w_up, n), w_down=(w_down, n),
            y=(y, d.T * d.H))
     check(lib().moe_decode(_ref(d), *(_p(t, _bf) for t in (x, w_r, w_gate, w_up, w_down)), _mask(token_mask, d),
-                           _p(y, _bf), _p(ws), ws.numel() * ws.element_size(), _on(x, stream)))
+                           _p(y, _bf), _p(ws), ws.numel() * ws.element_size(),
+                           _on(x, stream, w_r, w_gate, w_up, w_down, token_mask, y, ws)))
 
 
 def moe_decode_i8(d, x, w_r, w: MoeI8Experts, token_mask, y, ws, stream=None):
@@ -207,7 +210,13 @@ def moe_decode_i8(d, x, w_r, w: MoeI8Experts, token_mask, y, ws, stream=None):
     _check_weights(w, d.E, d.H, d.F)
     _least(x=(x, d.T * d.H), w_r=(w_r, d.H * d.E), y=(y, d.T * d.H))
     check(lib().moe_decode_i8(_ref(d), _p(x, _bf), _p(w_r, _bf), _ref(w), _mask(token_mask, d), _p(y, _bf), _p(ws),
-                              ws.numel() * ws.element_size(), _on(x, stream)))
+                              ws.numel() * ws.element_size(),
+                              _on(x, stream, w_r, token_mask, y, ws, *_tensors(w))))
+
+
+def _tensors(w):
+    """Those of an int8 experts' descriptor; one made by hand holds pointers alone."""
+    return getattr(w, "tensors", ())
 
 
 class MoEDecode(_Held):
@@ -247,7 +256,7 @@ class MoEDecode(_Held):
         _shape("w_up", w_up, (d.E, d.H, d.F))
         _shape("w_down", w_down, (d.E, d.F, d.H))
         check(lib().moe_decode(_ref(d), *p, _p(w_gate, _bf), _p(w_up, _bf), _p(w_down, _bf), _mask(token_mask, d),
-                               *self._b, _on(x, stream)))
+                               *self._b, _on(x, stream, w_r, w_gate, w_up, w_down, token_mask, self.y)))
         return self._out(d.T)
 
 
@@ -260,7 +269,8 @@ class MoEDecodeI8(MoEDecode):
         """The layer's output for x [t, H], t <= T."""
         d, p = self._args(x, w_r)
         _check_weights(w, d.E, d.H, d.F)
-        check(lib().moe_decode_i8(_ref(d), *p, _ref(w), _mask(token_mask, d), *self._b, _on(x, stream)))
+        check(lib().moe_decode_i8(_ref(d), *p, _ref(w), _mask(token_mask, d), *self._b,
+                                  _on(x, stream, w_r, token_mask, self.y, *_tensors(w))))
         return self._out(d.T)
 
 
@@ -292,7 +302,8 @@ def moe_sample(d, logits, temperature, top_k, top_p, min_p, u, token, logprob, w
         _shape("logprob", logprob, (d.B,))
     check(lib().moe_sample(_ref(d), *_rows(logits, _f32 if d.flags & MOE_F_LOGITS_FP32 else _bf),
                            *_settings(d.B, temperature, top_k, top_p, min_p, u), _p(token, _i32), _p(logprob, _f32),
-                           _p(ws), ws.numel() * ws.element_size(), _on(logits, stream)))
+                           _p(ws), ws.numel() * ws.element_size(),
+                           _on(logits, stream, temperature, top_k, top_p, min_p, u, token, logprob, ws)))
 
 
 class Sampler(_Held):
@@ -320,5 +331,6 @@ class Sampler(_Held):
         _shape("logits", logits, (b, self.d.V))
         d = sample_dims(b, self.d.V, logits.dtype == _f32)
         check(lib().moe_sample(_ref(d), *_rows(logits, _f32 if logits.dtype == _f32 else _bf),
-                               *_settings(b, temperature, top_k, top_p, min_p, u), *self._b, _on(logits, stream)))
+                               *_settings(b, temperature, top_k, top_p, min_p, u), *self._b,
+                               _on(logits, stream, temperature, top_k, top_p, min_p, u, self.token)))
         return (self.token, self.logprob) if b == self.d.B else (self.token[:b], self.logprob[:b])

@@ -165,6 +165,14 @@ def test_masks_and_devices_that_do_not_fit(monkeypatch):
     with pytest.raises(ValueError, match="on device 1, the current one is 0"):
         step._on(There(), None)
 
+    class Here:
+        def get_device(self):
+            return 0
+
+    with pytest.raises(ValueError, match="on device 1, the current one is 0"):  # not the first alone
+        step._on(Here(), 0, None, There())
+    assert step._on(Here(), 17, None, Here()) == 17
+
 
 def test_norm_workspace_of_the_most_rows():
     """As many shares of dw as for fewer rows: their number must not overflow near 2^31 rows."""
