@@ -419,7 +419,7 @@ struct Choice {
   // The draw: the running sum that the token's has to pass.
   __device__ __forceinline__ u64 draw(u64 all) const {
     const double u = a.u[b];
-    return u > 0.0 ? min(part_of(u, all), all - 1) : 0;
+    return u >= 1.0 ? all - 1 : u > 0.0 ? min(part_of(u, all), all - 1) : 0;  // no integer of what passes 64 bits
   }
   // The sum that the shortest prefix reaches.
   __device__ __forceinline__ u64 needed(u64 all) const {
