@@ -90,9 +90,9 @@ struct Ws {
 
 // Order-preserving key; 0 for what is never taken (-infinity, NaN, absent).
 __device__ __forceinline__ uint32_t key_of(float v) {
-  if (!(v > -INFINITY)) return 0u;
   const uint32_t u = v == 0.0f ? 0u : __float_as_uint(v);
-  return (u >> 31) ? ~u : (u | 0x80000000u);
+  const uint32_t key = u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+  return v > -INFINITY ? key : 0u;
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((key >> 31) ? (key & 0x7fffffffu) : ~key);
@@ -122,7 +122,16 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int b) {
 }
 
 // x of a value; infinity is past every finite one, so that it alone has weight.
-__device__ __forceinline__ double x_of(float v, double c) { return v == INFINITY ? 1e300 : static_cast<double>(v) * c; }
+// Where `in` is false, one of no weight: chosen here, because a choice after
+// the weight makes the compiler put each weight behind a branch of its own, one
+// chain of dependent steps at a time (the rows of 256 x 50001: 30 us with it).
+__device__ __forceinline__ double x_if(bool in, float v, double c) {
+  const double x = static_cast<double>(v) * c;
+  constexpr int kFar = 0x7e37e43c;  // upper half of 1e300
+  const int hi = v == INFINITY ? kFar : __double2hiint(x);
+  return __hiloint2double(in ? hi : kFar | 1 << 31, __double2loint(x));
+}
+__device__ __forceinline__ double x_of(float v, double c) { return x_if(true, v, c); }
 
 // The integer weight of x < N + 1: 2^f, |f| <= 1/2, by the polynomial that
 // meets it in the ten Chebyshev points (2^-45.6 of it off at most), times a
@@ -289,22 +298,18 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   const uint32_t largest = static_cast<uint32_t>(best >> 32);
   const double N = largest == 0 ? -1e305 : floor(x_of(value_of(largest), s.c));
   if (tid == 0) st.ref[chunk] = N;
-  auto weight_of = [&](float value, double x) -> u64 {  // no branch: most elements count
-    const u64 w = weight(x, N);
-    return value > -INFINITY ? w : 0;
-  };
   if (summed) {
     u64 sum = 0;
 #pragma unroll
-    for (int e = 0; e < kGroup; ++e) sum += weight_of(v[e], x_of(v[e], s.c));
+    for (int e = 0; e < kGroup; ++e) sum += weight(x_if(v[e] > -INFINITY, v[e], s.c), N);
     sum = wave_add(sum);
     if (lane == 0) st.piece_sum[piece] = sum;
     return;
   }
 #pragma unroll
   for (int e = 0; e < kGroup; ++e) {
-    const double x = x_of(v[e], s.c);
-    const u64 w = weight_of(v[e], x);
+    const double x = x_if(v[e] > -INFINITY, v[e], s.c);
+    const u64 w = weight(x, N);
     if (w != 0) atomicAdd(&bins[static_cast<int>(fmin(bin_of(x, N), kBins - 1.0))], w);
   }
   __syncthreads();
@@ -428,8 +433,7 @@ struct Choice {
 
   // Weight of an element that stays: rank >= least.
   __device__ __forceinline__ u64 kept(float v, int place, u64 least) const {
-    const u64 w = weight(x_of(v, s.c), N);
-    return key_of(v) == 0 || rank_of(v, place) < least ? 0 : w;
+    return weight(x_if(key_of(v) != 0 && rank_of(v, place) >= least, v, s.c), N);
   }
 
   // The least key whose x `in` takes, which takes all larger ones: a wave
@@ -670,8 +674,7 @@ struct Choice {
       u64 t = 0;
 #pragma unroll
       for (int e = 0; e < Row<F32>::W; ++e) {
-        const u64 w = weight(x_of(v[e], s.c), N);
-        t += key_of(v[e]) >= least ? w : 0;
+        t += weight(x_if(key_of(v[e]) >= least, v[e], s.c), N);
       }
       if (lo < hi) put_in_list(v, p, lo, hi);
       return t;
@@ -840,35 +843,12 @@ struct Choice {
       if (const u64 rank = sh.list[i]; rank >= least) atomicAdd(&sh.sums[piece_of(rank)], weight(x_at(rank), N));
   }
 
-  // The candidates are the list's n largest, of keys from lo on: filters them, draws.
-  __device__ __forceinline__ void choose_from_list(int n, int k, uint32_t lo) {
-    const double scale = scale_from(lo);
-    u64 least = n > k ? border<true>(n, 0, k, x_most, scale, 0) : 0;
-    if (s.filter_p) {
-      u64 t = 0;
-#pragma unroll 1
-      for (int i = threadIdx.x; i < n; i += kRowThreads)
-        if (const u64 rank = sh.list[i]; rank >= least) t += weight(x_at(rank), N);
-      least = max(least, border<false>(n, least, needed(total(t)), x_most, scale, 0));
-    }
-    choose(n, max(least, min_rank));
-  }
-
   // Fine bins per unit of x from the largest down to key lo's.
   __device__ __forceinline__ double scale_from(uint32_t lo) const {
     const double x_lo = lo != 0 ? x_of(value_of(lo), s.c) : x_most - kOctaves, span = x_most - x_lo;
     return span > 0.0 && span < 1e18 ? kFine / span : 0.0;
   }
-  // Draws from the list's elements of rank >= least.
-  __device__ __forceinline__ void choose(int n, u64 least) {
-    __syncthreads();
-    clear_sums();
-    __syncthreads();
-    add_to_sums(n, least);
-    pick_by_sums(least);
-  }
-
-  // The same for up to a wave of candidates, a lane each: places and sums in
+  // Filters and draws from a list of up to a wave of candidates, a lane each: places and sums in
   // the order, then sums in index order, from a comparison with each of the
   // others, an eighth of them by each of the waves.
   __device__ __forceinline__ void choose_from_few(int n, int k) {
@@ -956,7 +936,8 @@ struct Choice {
                  u64 n = 0;
 #pragma unroll
                  for (int e = 0; e < Row<F32>::W; ++e)
-                   if (key_of(v[e]) != 0 && rank_of(v[e], p + e) >= at) n += COUNT ? 1 : weight(x_of(v[e], s.c), N);
+                   if (const bool in = key_of(v[e]) != 0 && rank_of(v[e], p + e) >= at; COUNT) n += in;
+                   else n += weight(x_if(in, v[e], s.c), N);
                  return n;
                },
                [&](u64 n, int) { t += n; });
@@ -975,7 +956,7 @@ struct Choice {
       for (int e = 0; e < kGroup; ++e) {
         const bool on = wave < pieces && key_of(v[e]) != 0;
         rank[e] = on ? rank_of(v[e], row.place(wave, e)) : 0;
-        w[e] = !on ? 0 : COUNT ? 1 : weight(x_of(v[e], s.c), N);
+        w[e] = COUNT ? on : weight(x_if(on, v[e], s.c), N);
       }
 #pragma unroll 1
       for (int bit = 63; bit >= 0; --bit) {
@@ -1020,62 +1001,79 @@ struct Choice {
       const double x_least = x_most + log2(s.m);
       min_rank = static_cast<u64>(least_key([&](double x) { return x >= x_least; })) << 32;
     }
+    // Each way ends in the same steps, which stand once at the end: what a
+    // workgroup runs it runs once, so that the size of its code counts.
     u64 least = 0;
+    int n = 0;            // candidates in the list, where it holds them all,
+    bool listed = false;  // of which top_p's border comes at `need` past x_top;
+    bool apart = false;   // the list is all there is, the pieces' sums are not begun
+    bool summed = false;  // the pieces' sums are complete
+    u64 need = 0, none = 0;
+    double x_top = x_most, scale = 0.0;
     if (s.filter_k) {
       if (s.k <= kFastK) {
         const uint32_t lo = floor_of_kth(s.k);
-        const int groups = list_groups(lo), n = collect(lo, groups < 0 || groups > pieces * kWave / 4);
+        const int groups = list_groups(lo);
+        n = collect(lo, groups < 0 || groups > pieces * kWave / 4);
         if (n <= kWave) {
           choose_from_few(n, s.k);
           return;
         }
-        if (n <= kList) {
-          choose_from_list(n, s.k, lo);
-          return;
+        listed = apart = n <= kList;
+        if (listed) {
+          scale = scale_from(lo);
+          if (n > s.k) least = border<true>(n, 0, s.k, x_top, scale, 0);
+          if (s.filter_p) {
+            u64 t = 0;
+#pragma unroll 1
+            for (int i = threadIdx.x; i < n; i += kRowThreads)
+              if (const u64 rank = sh.list[i]; rank >= least) t += weight(x_at(rank), N);
+            need = needed(total(t));
+          }
         }
       }
-      least = search<true>(s.k);
-      if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
+      if (!listed) least = search<true>(s.k);
     } else if (s.filter_p || s.filter_m) {
       uint32_t lo = static_cast<uint32_t>(min_rank >> 32), hi = lo;
       int bin = 0;
-      u64 need = 0, rest = 0;
+      u64 rest = 0;
       if (s.filter_p) rest = border_bin(lo, hi, bin, need);
+      none = static_cast<u64>(lo) << 32;
       // few groups: all that is left is likely to fit the list
       const int groups = list_groups(lo);
       const bool few = groups >= 0 && groups <= kFewGroups;
       if (few) {
         if (part != 0) return;
-        const int n = collect(lo, false);
-        if (n <= kList) {
-          const u64 floor = static_cast<u64>(lo) << 32;
-          if (s.filter_p) least = border<false>(n, 0, need, x_most, scale_from(lo), floor);
-          choose(n, max(least, min_rank));
-          return;
-        }
+        n = collect(lo, false);
+        listed = apart = n <= kList;
+        scale = scale_from(lo);
       }
-      const int n = collect_and_sum(lo, hi, !few && parts > 1);
-      if (n < 0) return;
-      if (!s.filter_p) {
-        pick_by_sums(min_rank);
-        return;
+      if (!listed) {
+        n = collect_and_sum(lo, hi, !few && parts > 1);
+        if (n < 0) return;
+        summed = !s.filter_p;
+        listed = !summed && n > 0 && n <= kList;
+        need = rest, x_top = N + 1.0 - bin * (1.0 / kPerOctave), scale = kFine * kPerOctave;
       }
-      if (n > 0 && n <= kList) {
-        least = max(border<false>(n, 0, rest, N + 1.0 - bin * (1.0 / kPerOctave), kFine * kPerOctave, static_cast<u64>(lo) << 32),
-                    min_rank);
-        add_to_sums(n, least);
-        pick_by_sums(least);
-        return;
-      }
-      least = search<false>(needed(measure<false>(0)));
     } else {
       for (int i = threadIdx.x; i < pieces; i += kRowThreads)
         sh.sums[i] = rescale(st.piece_sum[i], st.ref[i / kChunkWaves], N);
-      pick_by_sums(0);
-      return;
+      summed = true;
     }
-    least = max(least, min_rank);
-    sum_pieces(least);
+    if (listed) {
+      if (s.filter_p) least = max(least, border<false>(n, least, need, x_top, scale, none));
+      least = max(least, min_rank);
+      __syncthreads();
+      if (apart) clear_sums();
+      __syncthreads();
+      add_to_sums(n, least);
+    } else if (!summed) {
+      if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
+      least = max(least, min_rank);
+      sum_pieces(least);
+    } else {
+      least = min_rank;
+    }
     pick_by_sums(least);
   }
 };
