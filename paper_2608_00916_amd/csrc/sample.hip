@@ -520,9 +520,10 @@ struct Choice {
 
   __device__ __forceinline__ void hold() {
     if (!held()) return;
-    const int groups = pieces * kWave;  // a multiple of 512
+    const int vecs = pieces * (kWave / 4);  // a multiple of 128
 #pragma unroll 4
-    for (int g = threadIdx.x; g < groups; g += kRowThreads) sh.top[g] = st.top[g];
+    for (int i = threadIdx.x; i < vecs; i += kRowThreads)
+      reinterpret_cast<uint4*>(sh.top)[i] = reinterpret_cast<const uint4*>(st.top)[i];
     __syncthreads();
   }
 
@@ -534,13 +535,14 @@ struct Choice {
     if (threadIdx.x == 0) sh.groups = 0;
     __syncthreads();
     const int groups = pieces * kWave;
+    constexpr int kAtOnce = 8;  // per addition to the count
 #pragma unroll 1
-    for (int i0 = 0; i0 < groups; i0 += 4 * kRowThreads) {
-      bool on[4];
-      u64 m[4];
+    for (int i0 = 0; i0 < groups; i0 += kAtOnce * kRowThreads) {
+      bool on[kAtOnce];
+      u64 m[kAtOnce];
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kAtOnce; ++i) {
         const int g = i0 + i * kRowThreads + static_cast<int>(threadIdx.x);
         const uint32_t top = g < groups ? sh.top[g] : 0;
         on[i] = top != 0 && top >= lo;
@@ -552,7 +554,7 @@ struct Choice {
       if (lane == 0) at = atomicAdd(&sh.groups, n);
       at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kAtOnce; ++i) {
         if (on[i]) sh.group[at + __popcll(m[i] & ((1ull << lane) - 1))] = static_cast<uint16_t>(i0 + i * kRowThreads + threadIdx.x);
         at += __popcll(m[i]);
       }
@@ -701,16 +703,17 @@ struct Choice {
     __syncthreads();
     if (sh.count != parts - 1) return -1;
     for (int i = threadIdx.x; i < pieces; i += kRowThreads) sh.sums[i] = st.piece_sum[i];
-    int n = 0;
-#pragma unroll 1
-    for (int p = 0; p < parts; ++p) {
-      const int here = st.done[1 + p];
-      for (int i = threadIdx.x; i < here && n + i < kList && i < kList; i += kRowThreads)
-        sh.list[n + i] = st.lists[static_cast<int64_t>(p) * kList + i];
-      n += here;
+    // a wave per part
+    static_assert(kMaxParts <= kRowWaves, "a part each");
+    const int here = lane < parts ? st.done[1 + lane] : 0, upto = wave_upto(here);
+    if (const int p = wave_index(); p < parts) {
+      const int at = __builtin_amdgcn_readlane(upto - here, p);
+      const int m = min(__builtin_amdgcn_readlane(here, p), kList - at);  // lists that are cut short make n pass kList
+#pragma unroll 4
+      for (int i = lane; i < m; i += kWave) sh.list[at + i] = st.lists[static_cast<int64_t>(p) * kList + i];
     }
     __syncthreads();
-    return n;
+    return __builtin_amdgcn_readlane(upto, kWave - 1);
   }
 
   // A key that k groups (or sets of groups) reach: at least k elements do.
