@@ -31,6 +31,8 @@ constexpr int kGroup = 16, kPiece = kGroup * kWave;  // elements of a lane and o
 constexpr int kChunkWaves = 8, kChunk = kChunkWaves * kPiece;
 constexpr int kOctaves = 44, kPerOctave = 8, kBins = kOctaves * kPerOctave;
 constexpr int kUnit = 42;  // weights are in units of 2^-42 of 2^N
+// 1024 threads a row: two waves more a SIMD won 1 to 2 us of 256 rows and lost 1 to 2
+// of one row and of a small top-k.
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
 constexpr int kList = 4096;   // candidates held in LDS
 constexpr int kMine = kList / kRowThreads;
@@ -124,7 +126,8 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int b) {
 // x of a value; infinity is past every finite one, so that it alone has weight.
 // Where `in` is false, one of no weight: chosen here, because a choice after
 // the weight makes the compiler put each weight behind a branch of its own, one
-// chain of dependent steps at a time (the rows of 256 x 50001: 30 us with it).
+// chain of dependent steps at a time (256 rows of 50001 at top-p 0.9: 73 us with
+// it, 70 without).
 __device__ __forceinline__ double x_if(bool in, float v, double c) {
   const double x = static_cast<double>(v) * c;
   constexpr int kFar = 0x7e37e43c;  // upper half of 1e300
@@ -489,8 +492,9 @@ struct Choice {
     if (token >= 0) write(token, value, all);
   }
 
-  // sums[0 .. pieces) hold the pieces' weights: finds the draw's piece and picks there.
-  __device__ __forceinline__ void pick_by_sums(u64 least) {
+  // sums[0 .. pieces) hold the pieces' weights (or, of_chunks, each chunk's first
+  // the chunk's): finds the draw's piece and picks there.
+  __device__ __forceinline__ void pick_by_sums(u64 least, bool of_chunks) {
     __syncthreads();
     u64 mine[kSumsPerThread], t = 0, all;
     const int i0 = threadIdx.x * kSumsPerThread;
@@ -510,7 +514,31 @@ struct Choice {
       at += mine[j];
     }
     __syncthreads();
-    if (wave == 0) pick(static_cast<int>(sh.found), sh.found2, least, all);
+    int piece = static_cast<int>(sh.found);
+    u64 rest = sh.found2;
+    if (of_chunks) {  // its pieces, a wave each
+      static_assert(kChunkWaves == kRowWaves, "a wave per piece");
+      float v[kGroup];
+      row.load(piece + wave_index(), v);
+      u64 sum = 0;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) sum += kept(v[e], row.place(piece + wave_index(), e), least);
+      sum = wave_add(sum);
+      turn ^= 1;
+      if (lane == 0) sh.waves[turn][wave] = sum;
+      __syncthreads();
+      bool found = false;
+      int w = 0;
+#pragma unroll
+      for (int i = 0; i < kRowWaves; ++i) {
+        const u64 here = sh.waves[turn][i];
+        found = found || rest < here;
+        if (!found) rest -= here, ++w;
+      }
+      if (found) piece += w;
+      else rest = ~0ull;  // rounding of the chunk's sum: past all of a piece's
+    }
+    if (wave == 0) pick(piece, rest, least, all);
   }
 
   // ---- groups.  A row of up to kHeldPieces pieces has its groups' keys in
@@ -663,25 +691,26 @@ struct Choice {
     return sh.count;
   }
 
-  // Collects the elements of keys lo .. hi - 1, and sums, by pieces, the
+  // Collects the elements of keys lo .. hi - 1, and (`sums`) sums, by pieces, the
   // weights of those from hi on that min_p keeps, from whole pieces.  The row's
   // workgroups may share them: each leaves its pieces' sums and its list in
   // memory, and the last to be through goes on with all of it.  -1 where this
   // workgroup has nothing more to do.
-  __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi, bool shared) {
+  __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi, bool shared, bool sums) {
     const uint32_t least = max(hi, static_cast<uint32_t>(min_rank >> 32));
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     auto f = [&](const float* v, int p) {
       u64 t = 0;
+      if (sums) {
 #pragma unroll
-      for (int e = 0; e < Row<F32>::W; ++e) {
-        t += weight(x_if(key_of(v[e]) >= least, v[e], s.c), N);
+        for (int e = 0; e < Row<F32>::W; ++e) t += weight(x_if(key_of(v[e]) >= least, v[e], s.c), N);
       }
       if (lo < hi) put_in_list(v, p, lo, hi);
       return t;
     };
     each_piece(lo, shared ? part * kRowWaves : 0, shared ? parts * kRowWaves : kRowWaves, f, [&](u64 t, int piece) {
+      if (!sums) return;
       t = wave_add(t);
       if (lane != 0) return;
       if (shared) st.piece_sum[piece] = t;
@@ -702,7 +731,8 @@ struct Choice {
       sh.count = __hip_atomic_fetch_add(st.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (sh.count != parts - 1) return -1;
-    for (int i = threadIdx.x; i < pieces; i += kRowThreads) sh.sums[i] = st.piece_sum[i];
+    if (sums)
+      for (int i = threadIdx.x; i < pieces; i += kRowThreads) sh.sums[i] = st.piece_sum[i];
     // a wave per part
     static_assert(kMaxParts <= kRowWaves, "a part each");
     const int here = lane < parts ? st.done[1 + lane] : 0, upto = wave_upto(here);
@@ -839,11 +869,11 @@ struct Choice {
     __syncthreads();
     return sh.found;
   }
-  // The weights of the list's elements of rank >= least, to their pieces' sums.
-  __device__ __forceinline__ void add_to_sums(int n, u64 least) {
+  // The weights of the list's elements of rank >= least, to the sums of their pieces or chunks.
+  __device__ __forceinline__ void add_to_sums(int n, u64 least, bool of_chunks) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += kRowThreads)
-      if (const u64 rank = sh.list[i]; rank >= least) atomicAdd(&sh.sums[piece_of(rank)], weight(x_at(rank), N));
+      if (const u64 rank = sh.list[i]; rank >= least) atomicAdd(&sh.sums[piece_of(rank) & (of_chunks ? -kChunkWaves : -1)], weight(x_at(rank), N));
   }
 
   // Fine bins per unit of x from the largest down to key lo's.
@@ -929,6 +959,23 @@ struct Choice {
     return sh.found2;
   }
 
+  // The chunks' weights in bins before `bin`, each as its first piece's sum.
+  __device__ __forceinline__ void sum_chunks(int bin) {
+    __syncthreads();
+    clear_sums();
+    __syncthreads();
+#pragma unroll 1
+    for (int c = wave_index(); c < pieces / kChunkWaves; c += kRowWaves) {
+      const double ref = st.ref[c], shift = kPerOctave * (N - ref);
+      u64 t = 0;
+#pragma unroll
+      for (int i0 = 0; i0 < kBins; i0 += kWave)
+        if (const int i = i0 + lane; i < kBins && i + shift < bin) t += st.bins[static_cast<int64_t>(c) * kBins + i];
+      t = wave_add(t);
+      if (lane == 0) sh.sums[c * kChunkWaves] = rescale(t, ref, N);
+    }
+  }
+
   // ---- what the lists do not hold (thousands of equal logits, a top_k of
   // thousands).  Count or weight of the elements of rank >= at.
   template <bool COUNT>
@@ -1011,6 +1058,7 @@ struct Choice {
     bool listed = false;  // of which top_p's border comes at `need` past x_top;
     bool apart = false;   // the list is all there is, the pieces' sums are not begun
     bool summed = false;  // the pieces' sums are complete
+    bool chunked = false;  // the sums are the chunks', from their bins: no weight is computed again but in the draw's
     u64 need = 0, none = 0;
     double x_top = x_most, scale = 0.0;
     if (s.filter_k) {
@@ -1052,10 +1100,18 @@ struct Choice {
         scale = scale_from(lo);
       }
       if (!listed) {
-        n = collect_and_sum(lo, hi, !few && parts > 1);
+        // Where min_p takes nothing off before the border's bin, the bins' weights are
+        // what stays.  Using them pays from about four pieces a wave (256 flat rows of
+        // 50001 in bf16: 70 us, 66 with them; 64 of 131072: 61, 59), and costs steps of
+        // its own where there are fewer (one row of 131072: 35, 37).  The row's length
+        // alone decides, so that its bits do not depend on how many rows there are.
+        chunked = s.filter_p && static_cast<uint32_t>(min_rank >> 32) <= hi && pieces > 4 * kRowWaves;
+        n = collect_and_sum(lo, hi, !few && parts > 1, !chunked);
         if (n < 0) return;
         summed = !s.filter_p;
         listed = !summed && n > 0 && n <= kList;
+        chunked = chunked && listed;
+        if (chunked) sum_chunks(bin);
         need = rest, x_top = N + 1.0 - bin * (1.0 / kPerOctave), scale = kFine * kPerOctave;
       }
     } else {
@@ -1069,7 +1125,7 @@ struct Choice {
       __syncthreads();
       if (apart) clear_sums();
       __syncthreads();
-      add_to_sums(n, least);
+      add_to_sums(n, least, chunked);
     } else if (!summed) {
       if (s.filter_p) least = max(least, search<false>(needed(measure<false>(least))));
       least = max(least, min_rank);
@@ -1077,7 +1133,7 @@ struct Choice {
     } else {
       least = min_rank;
     }
-    pick_by_sums(least);
+    pick_by_sums(least, chunked);
   }
 };
 

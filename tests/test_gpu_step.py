@@ -520,6 +520,34 @@ def test_sample_rows_behind_and_many():
         assert torch.equal(one[0], token[7:8]) and torch.equal(one[1], logprob[7:8])
 
 
+@pytest.mark.parametrize("fp32,pad", [(True, 40001), (False, 40008)])
+def test_sample_flat_rows_by_chunks(fp32, pad):
+    """Rows long and flat enough that the draw goes by whole chunks: min_p before, in and after the
+    border of top_p, and each row alone with the bits that it has among the others."""
+    import torch
+    import paper_2608_00916_amd as moe
+    B, V = 135, 40000
+    say("sample flat", fp32, pad)
+    wide = torch.zeros((B, pad), device="cuda", dtype=torch.float32 if fp32 else torch.bfloat16)
+    wide[:, :V] = rows_of(B, V, 21, fp32)
+    logits = wide[:, :V]
+    logits[:, 9000:17000] -= 100.0  # a chunk far below the others
+    logits[5, V - 1] = 13.0         # the largest in the last, part-filled one
+    g = gen(22)
+    u = g.random(B).astype(np.float32)
+    u[:4] = 0.0, 1.0, 0.9999999, 1e-7
+    u, t = dev(u), dev(g.choice([1.0, 2.0, 5.0], B).astype(np.float32))
+    p = dev(g.choice([0.5, 0.9, 0.99], B).astype(np.float32))
+    m = dev(g.choice([0.0, 1e-9, 1e-3, 0.02, 0.3], B).astype(np.float32))
+    op = moe.Sampler(B, V)
+    for s in (dict(temperature=t, top_p=p), dict(temperature=t, top_p=p, min_p=m)):
+        token, logprob = (o.clone() for o in op.forward(logits, u, **s))
+        check_tokens(logits, u, (token, logprob), **s)
+        for b in range(0, B, 9):
+            one = op.forward(logits[b:b + 1], u[b:b + 1], **{n: v[b:b + 1] for n, v in s.items()})
+            assert torch.equal(one[0], token[b:b + 1]) and torch.equal(one[1], logprob[b:b + 1]), b
+
+
 def test_sample_largest():
     import paper_2608_00916_amd as moe
     V = 1 << 20
