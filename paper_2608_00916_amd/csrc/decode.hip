@@ -357,7 +357,7 @@ __global__ __launch_bounds__(kUpWaves* kWave, RANGES ? 2 : 4) void k_decode_gate
                                                                    const bf16_t* __restrict__ w_up,
                                                                    bf16_t* __restrict__ a, float* __restrict__ gu) {
   __shared__ Rows rows;
-  __shared__ float red[kUpWaves * 8 * 256];
+  __shared__ __attribute__((aligned(16))) float red[kUpWaves * 8 * 256];
   if constexpr (FUSED) {
     __shared__ Selection sel;
     if (!select_rows(r, sel, rows)) return;
@@ -430,10 +430,10 @@ __global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 5) void k_decode_do
                                                                    const bf16_t* __restrict__ w_down,
                                                                    float* __restrict__ o) {
   __shared__ Rows rows;
-  __shared__ float red[kDownWaves * 4 * 256];
+  __shared__ __attribute__((aligned(16))) float red[kDownWaves * 4 * 256];
   if (!read_rows(r, rows)) return;
   const bf16_t* const b[1] = {w_down + static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.H * r.F + blockIdx.x * kCols};
-  extern __shared__ bf16_t act[];
+  extern __shared__ __attribute__((aligned(16))) bf16_t act[];  // [rows][2][F]
   if (RANGES || rows.n <= 16) {
     down_tiles<1, RANGES>(r, rows, 0, a, gu, b, o, act, red);
   } else {
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES == kUpWaves8 ? 6 : 2) void k_de
                                                                        const float* __restrict__ sx, moe_i8_experts w,
                                                                        float* __restrict__ a, float* __restrict__ top) {
   __shared__ Rows rows;
-  __shared__ int red[WAVES * 2 * 256];
+  __shared__ __attribute__((aligned(16))) int red[WAVES * 2 * 256];
   if constexpr (FUSED) {
     __shared__ Selection sel;
     if (!select_rows(r, sel, rows)) return;
