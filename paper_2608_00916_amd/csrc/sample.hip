@@ -676,11 +676,18 @@ struct Choice {
       }
   }
 
+  // A count begins again at zero behind a barrier of its own: every wave has read
+  // the count before it by then, and whether that fits the list decides its way.
+  __device__ __forceinline__ void start_count() {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+  }
+
   // Collects the elements of keys from lo on (`whole`: of all pieces, else of
   // the listed groups): the count, of which the first kList are in the list.
   __device__ __forceinline__ int collect(uint32_t lo, bool whole) {
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
+    start_count();
     auto f = [&](const float* v, int p) -> u64 {
       put_in_list(v, p, lo, 0);
       return 0;
@@ -698,8 +705,7 @@ struct Choice {
   // workgroup has nothing more to do.
   __device__ __forceinline__ int collect_and_sum(uint32_t lo, uint32_t hi, bool shared, bool sums) {
     const uint32_t least = max(hi, static_cast<uint32_t>(min_rank >> 32));
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
+    start_count();
     auto f = [&](const float* v, int p) {
       u64 t = 0;
       if (sums) {

@@ -21,3 +21,15 @@ def test_dynamic_lds_is_aligned_for_vectors(path):
     alignment it is declared with; all of them are read by 16 bytes."""
     for decl in re.findall(r"extern\s+__shared__[^;]*;", text(path)):
         assert "aligned(16)" in decl or "alignas(16)" in decl, decl
+
+
+def test_shared_counts_change_behind_a_barrier():
+    """All waves branch on the counts of a row's workgroup, so between one reading and the next
+    store there is a barrier, in the function that stores."""
+    sample = text(os.path.join(CSRC, "sample.hip"))
+    stores = list(re.finditer(r"sh\.(count|groups)\s*=(?!=)", sample))
+    assert len(stores) >= 4
+    for m in stores:
+        before = sample[sample.rfind("__device__", 0, m.start()):m.start()]
+        assert "__syncthreads()" in before, sample[m.start() - 200:m.end() + 20]
+        assert f"sh.{m[1]}" not in before[before.rfind("__syncthreads()"):], before[-200:]
