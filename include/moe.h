@@ -490,7 +490,7 @@ int moe_norm_bwd(const moe_norm_dims* d, const void* h, int64_t ldh, const void*
 
 /* moe_infer for at most MOE_DECODE_MAX_T tokens: the same layer with the same
  * selection and gates, bit for bit, in tiles for few rows.  G, U and O stay
- * fp32, and A enters the down product as two bf16 (to 2^-17 of itself), so Y is closer to the
+ * fp32, and A enters the down product whole (as three bf16), so Y is closer to the
  * equations than moe_infer's and not its bits.  Arguments and flags as
  * moe_infer.
  *   ws  moe_decode_workspace_bytes(d) bytes of scratch, enough for fewer tokens too */

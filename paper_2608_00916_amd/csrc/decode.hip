@@ -292,14 +292,23 @@ __device__ __forceinline__ S sum_parts(const S* red, int f, int at) {
 __device__ __forceinline__ int entry_row(int at) { return 4 * (at >> 6) + (at & 3); }
 __device__ __forceinline__ int entry_lane(int at) { return (at >> 2) & 15; }
 
-// The activation as two bf16: the product with the second adds what the first
-// leaves out, so A enters the down product to 2^-17 of itself, at the price of
-// one more matrix instruction under the same weights.
-__device__ __forceinline__ void split_bf16(float v, bf16_t& hi, bf16_t& lo) {
-  hi = f2bf(v);
-  const float d = v - bf2f(hi);
-  lo = fabsf(d) < INFINITY ? f2bf(d) : 0;  // infinities and NaN are the first's alone
-}
+// The activation as three bf16, each the upper half of what those before it
+// leave: 3 x 8 bits are all of an fp32, so A enters the down product as it is, at
+// the price of two more matrix instructions under the same weights.  Two, rounded
+// (2^-17 of A), moved the output by 2.4e-6 of its norm before its rounding to bf16,
+// where fp32 sums move it by 4e-7.
+struct Split {
+  bf16_t part[kDecodeParts];
+  __device__ __forceinline__ explicit Split(float v) {
+    const bool finite = fabsf(v) < INFINITY;
+#pragma unroll
+    for (int i = 0; i < kDecodeParts; ++i) {
+      const uint32_t bits = __float_as_uint(v);
+      part[i] = finite || i == 0 ? static_cast<bf16_t>(bits >> 16) : 0;  // infinities and NaN are the first's alone
+      v -= __uint_as_float(bits & 0xffff0000u);
+    }
+  }
+};
 
 // Waves per workgroup: the gate/up product splits a long K (H), the down
 // product a shorter one (F).
@@ -340,7 +349,9 @@ __device__ __forceinline__ void gateup_tiles(const DecodeRows& r, const Rows& ro
       const float g = sum_parts<kUpWaves, 8>(red, p, at), u = sum_parts<kUpWaves, 8>(red, 4 + p, at);
       const int64_t to = static_cast<int64_t>(rows.slot[m]) * r.F + blockIdx.x * kCols + entry_lane(at) * 4 + p;
       if (gridDim.z == 1) {
-        split_bf16(silu_f(g) * u, a[to], a[to + R * r.F]);
+        const Split s(silu_f(g) * u);
+#pragma unroll
+        for (int j = 0; j < kDecodeParts; ++j) a[to + j * R * r.F] = s.part[j];
       } else {
         gu[to + 2 * blockIdx.z * R * r.F] = g;
         gu[to + (2 * blockIdx.z + 1) * R * r.F] = u;
@@ -374,7 +385,7 @@ __global__ __launch_bounds__(kUpWaves* kWave, RANGES ? 2 : 4) void k_decode_gate
   }
 }
 
-// The activation comes from a, or (RANGES) from LDS, act [rows][2][F].
+// The activation comes from a, or (RANGES) from LDS, act [rows][kDecodeParts][F].
 template <int NT, bool RANGES>
 __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows, int first, const bf16_t* __restrict__ a,
                                            const float* __restrict__ gu, const bf16_t* const (&b)[1],
@@ -385,14 +396,13 @@ __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int i = first + t * 16 + (lane & 15);
-    row[t] = i >= n ? -1 : RANGES ? 2 * i * r.F : static_cast<int64_t>(rows.slot[i]) * r.F;
+    row[t] = i >= n ? -1 : RANGES ? kDecodeParts * i * r.F : static_cast<int64_t>(rows.slot[i]) * r.F;
   }
-  auto get = [&](int t, int k, uint4 (&v)[2]) {
-    v[0] = v[1] = make_uint4(0, 0, 0, 0);
-    if (row[t] < 0) return;
+  auto get = [&](int t, int k, uint4 (&v)[kDecodeParts]) {
     const bf16_t* src = (RANGES ? act : a) + row[t] + k;
-    v[0] = *reinterpret_cast<const uint4*>(src);
-    v[1] = *reinterpret_cast<const uint4*>(src + (RANGES ? r.F : RF));
+#pragma unroll
+    for (int i = 0; i < kDecodeParts; ++i)
+      v[i] = row[t] >= 0 ? *reinterpret_cast<const uint4*>(src + i * (RANGES ? r.F : RF)) : make_uint4(0, 0, 0, 0);
   };
   // the ranges' sums and SwiGLU, under the first weights' way here
   bool begun = false;
@@ -403,12 +413,14 @@ __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows
       const int m = i / r.F, c = i % r.F;
       const float* src = gu + static_cast<int64_t>(rows.slot[m]) * r.F + c;
       const float g = src[0] + src[2 * RF], u = src[RF] + src[3 * RF];
-      split_bf16(silu_f(g) * u, act[2 * m * r.F + c], act[(2 * m + 1) * r.F + c]);
+      const Split s(silu_f(g) * u);
+#pragma unroll
+      for (int j = 0; j < kDecodeParts; ++j) act[(kDecodeParts * m + j) * r.F + c] = s.part[j];
     }
     __syncthreads();
   };
   f32x4 acc[NT][1][4] = {};
-  few_rows<NT, 1, 2, RANGES ? 6 : NT == 1 ? 2 : 1>(b, r.H, wave, r.F / 32, kDownWaves, begin, get, acc);
+  few_rows<NT, 1, kDecodeParts, RANGES ? 6 : NT == 1 ? 2 : 1>(b, r.H, wave, r.F / 32, kDownWaves, begin, get, acc);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (first + t * 16 >= n) break;
@@ -424,8 +436,10 @@ __device__ __forceinline__ void down_tiles(const DecodeRows& r, const Rows& rows
   }
 }
 
+// Four waves per SIMD hold a pair of tiles in registers; five spilled 68 bytes a
+// lane (64 tokens: 223 us, 227 with them).
 template <bool RANGES>
-__global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 5) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
+__global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 4) void k_decode_down(DecodeRows r, const bf16_t* __restrict__ a,
                                                                    const float* __restrict__ gu,
                                                                    const bf16_t* __restrict__ w_down,
                                                                    float* __restrict__ o) {
@@ -433,7 +447,7 @@ __global__ __launch_bounds__(kDownWaves* kWave, RANGES ? 2 : 5) void k_decode_do
   __shared__ __attribute__((aligned(16))) float red[kDownWaves * 4 * 256];
   if (!read_rows(r, rows)) return;
   const bf16_t* const b[1] = {w_down + static_cast<int64_t>(__builtin_amdgcn_readfirstlane(rows.expert)) * r.H * r.F + blockIdx.x * kCols};
-  extern __shared__ __attribute__((aligned(16))) bf16_t act[];  // [rows][2][F]
+  extern __shared__ __attribute__((aligned(16))) bf16_t act[];  // [rows][kDecodeParts][F]
   if (RANGES || rows.n <= 16) {
     down_tiles<1, RANGES>(r, rows, 0, a, gu, b, o, act, red);
   } else {
@@ -709,8 +723,8 @@ int slots(const DecodeRows& r) { return std::min(r.E, r.T * r.k); }
 
 // Ranges of K of the bf16 gate/up product: two where few tokens leave its
 // tiles fewer than half of the chip's 256 compute units.  The down product then
-// holds the rows of an expert in LDS, at most 32 KB: with T k < E they are at
-// most the grid's slots, hence slots F <= 128 kCols values of two bf16, and else
+// holds the rows of an expert in LDS, at most 48 KB: with T k < E they are at
+// most the grid's slots, hence slots F <= 128 kCols values of three bf16, and else
 // E >= 8 slots leave F <= 16 kCols for at most kFusedT rows.
 int decode_ranges(int T, int E, int F, int k) {
   return decode_fused(T) && F / kCols * std::min(E, T * k) <= 128 ? 2 : 1;
@@ -742,7 +756,7 @@ hipError_t launch_decode_down(const DecodeRows& r, const bf16_t* a, const float*
   TraceScope trace_scope(K_DECODE_DOWN, s);
   const dim3 grid(r.H / kCols, slots(r));
   if (decode_ranges(r.T, r.E, r.F, r.k) > 1)
-    hipLaunchKernelGGL(k_decode_down<true>, grid, dim3(kDownWaves * kWave), 2 * r.T * r.F * sizeof(bf16_t), s, r, a, gu, w_down, o);
+    hipLaunchKernelGGL(k_decode_down<true>, grid, dim3(kDownWaves * kWave), kDecodeParts * r.T * r.F * sizeof(bf16_t), s, r, a, gu, w_down, o);
   else
     hipLaunchKernelGGL(k_decode_down<false>, grid, dim3(kDownWaves * kWave), 0, s, r, a, gu, w_down, o);
   return hipGetLastError();

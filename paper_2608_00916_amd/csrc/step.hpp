@@ -40,6 +40,7 @@ hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s);
 
 // ---- the expert layer for a few tokens (decode.hip)
 constexpr int kDecodeMaxT = MOE_DECODE_MAX_T;
+constexpr int kDecodeParts = 3;  // bf16 summands of a value of the activation
 
 // A routed row is named by its slot t k + j.
 struct DecodeRows {
@@ -57,7 +58,7 @@ hipError_t launch_decode_router(const DecodeRows& r, const bf16_t* x, const bf16
 // from part; else it is there before.
 constexpr int kDecodeFusedT = 8;
 inline bool decode_fused(int T) { return T <= kDecodeFusedT; }
-// SwiGLU of the slots' tokens through their experts: a [2, T k, F] as two
+// SwiGLU of the slots' tokens through their experts: a [kDecodeParts, T k, F] as
 // summands, or with decode_ranges(..) > 1 each range's G and U, gu [ranges, 2, T k, F].
 int decode_ranges(int T, int E, int F, int k);
 hipError_t launch_decode_gateup(const DecodeRows& r, const bf16_t* x, const bf16_t* w_gate, const bf16_t* w_up,

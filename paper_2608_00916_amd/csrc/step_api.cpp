@@ -91,7 +91,7 @@ int check_decode_i8(const moe_dims* d) {
 struct DecodeWs {
   DecodeRows rows;
   int32_t* row_token;
-  bf16_t* a;   // bf16 experts: the activation's two summands,
+  bf16_t* a;   // bf16 experts: the activation's summands,
   float* gu;   // or the ranges' G and U
   float *a32, *top, *sx, *sa;  // int8 experts
   int8_t *x8, *a8;
@@ -118,7 +118,7 @@ DecodeWs decode_layout(const moe_dims* d, bool i8, void* base) {
   } else if (const int ranges = decode_ranges(d->T, d->E, d->F, d->top_k); ranges > 1) {
     w.gu = c.take<float>(2 * ranges * RF);
   } else {
-    w.a = c.take<bf16_t>(2 * RF);
+    w.a = c.take<bf16_t>(kDecodeParts * RF);
   }
   w.o = c.take<float>(R * d->H);
   w.bytes = c.off;

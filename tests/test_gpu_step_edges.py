@@ -4,7 +4,8 @@ weights that are not finite.  Tolerances are derived where they stand."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_step import check_tokens, dev, gen, host, rows_of, say
+from tests import step_ref as R
+from tests.test_gpu_step import BF, DECODE, SLACK, check_tokens, dev, gen, host, near, rows_of, say
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +33,51 @@ def test_sample_short_rows_with_long_lists(V, fp32):
             assert (again[0] == token).all() and (again[1] == logprob).all()
         some = few.forward(logits[9:12], u[9:12], **{n: v[9:12] for n, v in s.items()})
         assert (some[0] == token[9:12]).all() and (some[1] == logprob[9:12]).all()
+
+
+def numbers(g, shape, most, unit):
+    """Multiples of `unit` of up to `most` units, uniform, in bf16 (exact)."""
+    import torch
+    return (torch.randint(-most, most + 1, shape, device="cuda", generator=g) * unit).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,H,E,F,k", DECODE)
+def test_decode_activation_is_whole(T, H, E, F, k):
+    """Each output is the difference of two activations that agree to 9 to 12 bits, so that it
+    shows the bits below a bf16's.
+
+    Inputs and weights are few units, so logits, G and U are exact sums.  A pair's G are equal, its
+    U a unit apart, so silu(G), off by less than 2^-18 of itself, is a common factor; its A are
+    rounded to fp32 and their summands added, 2^-20 of A at most."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode whole activation", T, H, E, F, k)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T + H + E + F)
+    w_r = numbers(g, (H, E), 60, 2.0 ** -10)
+    x = torch.randint(0, 2, (2 * T + 8, H), device="cuda", generator=g).mul_(2).sub_(1).to(torch.bfloat16)
+    idx, gates, gap = R.route(host(x), host(w_r), k)
+    at = np.nonzero(gap > 1e-4)[0][:T]
+    assert len(at) == T
+    x, idx, gates = x[at].contiguous(), idx[at], gates[at]
+    w_gate, w_up = numbers(g, (E, H, F), 60, 2.0 ** -10), numbers(g, (E, H, F), 100, 2.0 ** -7)
+    w_gate[:, :, 1::2] = w_gate[:, :, ::2]
+    w_up[:, :, 1::2] = w_up[:, :, ::2]
+    row = torch.randint(0, H, (F // 2,), device="cuda", generator=g)
+    w_up[:, row, torch.arange(1, F, 2, device="cuda")] += 2.0 ** -7
+    w_down = torch.zeros((E, F, H), dtype=torch.bfloat16, device="cuda")
+    c = torch.arange(H, device="cuda")
+    first = c % (F // 2) * 2
+    w_down[:, first, c], w_down[:, first + 1, c] = 1.0, -1.0
+    y = moe.MoEDecode(T, H, E, F, k).forward(x, w_r, w_gate, w_up, w_down)
+    X, want, tol = host(x), np.zeros((T, H)), np.zeros((T, H))
+    first = first.cpu().numpy()
+    for e in np.unique(idx):
+        wg, wu = host(w_gate[e]), host(w_up[e])
+        for t, j in zip(*np.nonzero(idx == e)):
+            G = X[t] @ wg
+            a = G / (1 + np.exp(-G)) * (X[t] @ wu)
+            o = a[first] - a[first + 1]
+            want[t] += gates[t, j] * o
+            tol[t] += gates[t, j] * (2.0 ** -18 * np.abs(o) + 2.0 ** -20 * np.abs(a[first]))
+    near(y, want, SLACK * BF * np.abs(want) + tol, "y")
