@@ -490,8 +490,9 @@ int moe_norm_bwd(const moe_norm_dims* d, const void* h, int64_t ldh, const void*
 
 /* moe_infer for at most MOE_DECODE_MAX_T tokens: the same layer with the same
  * selection and gates, bit for bit, in tiles for few rows.  G, U and O stay
- * fp32, and A enters the down product whole (as three bf16), so Y is closer to the
- * equations than moe_infer's and not its bits.  Arguments and flags as
+ * fp32, and A enters the down product whole (as three bf16 that add up to it, 2^-25
+ * of it aside), so Y is closer to the equations than moe_infer's and not its bits; an
+ * infinite weight gives what it gives there.  Arguments and flags as
  * moe_infer.
  *   ws  moe_decode_workspace_bytes(d) bytes of scratch, enough for fewer tokens too */
 #define MOE_DECODE_MAX_T 64

@@ -297,14 +297,22 @@ __device__ __forceinline__ int entry_lane(int at) { return (at >> 2) & 15; }
 // the price of two more matrix instructions under the same weights.  Two, rounded
 // (2^-17 of A), moved the output by 2.4e-6 of its norm before its rounding to bf16,
 // where fp32 sums move it by 4e-7.
+//
+// All three have A's sign and none is zero where A is not, so that an infinite
+// weight meets them as it meets A (a zero would make NaN of it): where nothing is
+// left a summand is 2^-26 of A's power of two (2^-126 where that is less), below
+// the last bit of an fp32.  All three are infinite, or NaN, where A is; a NaN comes
+// from arithmetic, quiet, so its upper half is one.
 struct Split {
   bf16_t part[kDecodeParts];
   __device__ __forceinline__ explicit Split(float v) {
-    const bool finite = fabsf(v) < INFINITY;
+    const uint32_t all = __float_as_uint(v), exponent = all >> 23 & 0xff;
+    const bool some = (all & 0x7fff0000u) != 0;
+    const bf16_t least = some ? (all >> 16 & 0x8000u) | (exponent > 27 ? exponent - 26 : 1) << 7 : 0;
 #pragma unroll
     for (int i = 0; i < kDecodeParts; ++i) {
       const uint32_t bits = __float_as_uint(v);
-      part[i] = finite || i == 0 ? static_cast<bf16_t>(bits >> 16) : 0;  // infinities and NaN are the first's alone
+      part[i] = i == 0 || exponent == 0xff ? all >> 16 : (bits & 0x7fff0000u) != 0 ? bits >> 16 : least;
       v -= __uint_as_float(bits & 0xffff0000u);
     }
   }

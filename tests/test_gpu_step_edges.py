@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import step_ref as R
-from tests.test_gpu_step import BF, DECODE, SLACK, check_tokens, dev, gen, host, near, rows_of, say
+from tests.test_gpu_step import BF, DECODE, SLACK, bf16, check_tokens, dev, gen, host, layer, near, rows_of, say
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,59 @@ def test_decode_activation_is_whole(T, H, E, F, k):
             want[t] += gates[t, j] * o
             tol[t] += gates[t, j] * (2.0 ** -18 * np.abs(o) + 2.0 ** -20 * np.abs(a[first]))
     near(y, want, SLACK * BF * np.abs(want) + tol, "y")
+
+
+def same_or_near(got, want, tol, what):
+    """Infinities and NaN where `want` has them, the rest within tol."""
+    got, odd = host(got), ~np.isfinite(want)
+    assert odd.any()
+    assert np.array_equal(got[odd], want[odd], equal_nan=True), what
+    assert (np.abs(got - want) <= tol)[~odd].all(), what
+
+
+@pytest.mark.parametrize("T,H,E,F,k", [(1, 2048, 128, 768, 8), (2, 256, 8, 384, 8), (5, 1152, 16, 2176, 2), (8, 128, 8, 1024, 8),
+                                       (9, 256, 8, 256, 2), (40, 256, 8, 128, 4)])
+@pytest.mark.parametrize("short", [False, True])
+def test_decode_weights_that_are_not_finite(T, H, E, F, k, short):
+    """Infinities in W_down, of one sign or both in a column, NaN, and infinities where A is 0; with
+    A as it comes, or (`short`) of few bits, which leave nothing to its second and third summand."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode infinities", T, H, E, F, k, short)
+    t, _, _ = layer(T, H, E, F, k)
+    t["w_r"][0] = 0.0
+    x = bf16(gen(T + F).standard_normal((3 * T + 20, H)))
+    x[:, 0] = 1.0
+    idx, gates, gap = R.route(host(x), host(t["w_r"]), k)
+    at = np.nonzero(gap > 1e-3)[0][:T]
+    t["x"], idx, gates = x[at].contiguous(), idx[at], gates[at]
+    assert len(at) == T
+    if short:  # G = 64, where silu(G) = G, and U = +-1/16 to +-4
+        g = torch.Generator(device="cuda")
+        g.manual_seed(T)
+        size = torch.exp2(torch.randint(-4, 3, (E, F), device="cuda", generator=g).float())
+        t["w_gate"].zero_()
+        t["w_up"].zero_()
+        t["w_gate"][:, 0] = 64.0
+        t["w_up"][:, 0] = size * (torch.randint(0, 2, (E, F), device="cuda", generator=g) * 2 - 1)
+    t["w_up"][:, :, 7] = 0.0
+    inf, w = float("inf"), t["w_down"]
+    w[:, 3, 0], w[:, F - 1, 0] = inf, inf
+    w[:, 5, 1] = -inf
+    w[:, 9, 2], w[:, 10, 2] = inf, -inf
+    w[:, 7, 3] = inf
+    w[:, 6, 4] = float("nan")
+    w[::2, 11, H - 1] = inf
+    args = [t[n] for n in ("x", "w_r", "w_gate", "w_up", "w_down")]
+    with np.errstate(invalid="ignore"):
+        want, mag = R.experts(host(t["x"]), idx, gates, lambda e: [host(t[n][e]) for n in ("w_gate", "w_up", "w_down")])
+        y = moe.MoEDecode(T, H, E, F, k).forward(*args)
+        same_or_near(y, want, SLACK * BF * (mag + np.abs(want)), "y")
+    z = moe.MoEInfer(T, H, E, F, k).forward(*args)
+    odd = ~z.isfinite()
+    assert torch.equal(torch.nan_to_num(y[odd], 7.0), torch.nan_to_num(z[odd], 7.0))
+    # and one in W_up, which makes the activation infinite
+    t["w_up"][idx[0, 0], 0, 2] = inf
+    with np.errstate(invalid="ignore"):
+        want, mag = R.experts(host(t["x"]), idx, gates, lambda e: [host(t[n][e]) for n in ("w_gate", "w_up", "w_down")])
+        same_or_near(moe.MoEDecode(T, H, E, F, k).forward(*args), want, SLACK * BF * (mag + np.abs(want)), "y")
