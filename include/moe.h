@@ -518,7 +518,7 @@ int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i
  *            weights, in index order, passes u times their sum
  * A temperature of 0 or less (or NaN) takes the first in the order.  NaN in
  * top_p or min_p turns that filter off; u below 0 or NaN counts as 0, u of 1
- * and more takes the last.  A logit of -infinity or NaN is never taken; +infinity
+ * and more takes the last of any weight.  A logit of -infinity or NaN is never taken; +infinity
  * leaves only its like.  A row without a logit to take has token -1 and
  * logprob -infinity. */
 #define MOE_SAMPLE_MAX_V 1048576

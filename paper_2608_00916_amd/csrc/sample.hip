@@ -9,7 +9,9 @@
 // with x = logit log2(e) / temperature in fp64 and N = floor of the row's
 // largest x, a weight is the integer rint(2^(x - N) 2^42), at most 2^43, and
 // sums of up to 2^20 of them are exact in 64 bits (weights under 2^-44 of the
-// largest are 0).
+// largest are 0).  What the first launch sums is in the unit of a chunk's own N and
+// rounded once, as a sum, to the row's; the draw goes on in the chunk's unit within
+// a piece that such a sum has led to, so that what the sum counts is there.
 //
 // Two launches.  The first reads the logits once, chunk by chunk, and leaves
 // what a row's choice needs of each chunk; the second, a workgroup per row,
@@ -435,8 +437,8 @@ struct Choice {
   }
 
   // Weight of an element that stays: rank >= least.
-  __device__ __forceinline__ u64 kept(float v, int place, u64 least) const {
-    return weight(x_if(key_of(v) != 0 && rank_of(v, place) >= least, v, s.c), N);
+  __device__ __forceinline__ u64 kept(float v, int place, u64 least, double unit) const {
+    return weight(x_if(key_of(v) != 0 && rank_of(v, place) >= least, v, s.c), unit);
   }
 
   // The least key whose x `in` takes, which takes all larger ones: a wave
@@ -454,21 +456,26 @@ struct Choice {
   }
 
   // ---- the draw in index order
-  // The token of the running sum `r` within a piece, by the calling wave.
-  __device__ __forceinline__ void pick(int piece, u64 r, u64 least, u64 all) const {
+  // The token of the running sum `r` within a piece, by the calling wave; the last
+  // of any weight where r is past them all (u of 1 and more, a sum rounded up).
+  __device__ __forceinline__ void pick(int piece, u64 r, u64 least, u64 all, double unit) const {
     float v[kGroup];
     row.load(piece, v);
     constexpr int W = Row<F32>::W;
-    int token = -1;
-    float value = 0.0f;
+    int token = -1, last = -1;
+    float value = 0.0f, last_value = 0.0f;
     bool done = false;
 #pragma unroll
     for (int i = 0; i < kGroup / W; ++i) {
       u64 w[W], t = 0;
 #pragma unroll
       for (int j = 0; j < W; ++j) {
-        w[j] = kept(v[i * W + j], row.place(piece, i * W + j), least);
+        w[j] = kept(v[i * W + j], row.place(piece, i * W + j), least, unit);
         t += w[j];
+        if (w[j] != 0) {
+          last = row.place(piece, i * W + j);
+          last_value = v[i * W + j];
+        }
       }
       u64 at = wave_before(t);
       const u64 sum = lane_value(at + t, kWave - 1);
@@ -485,16 +492,19 @@ struct Choice {
       }
       if (!done) r -= sum;
     }
-    if (!done) {  // rounding of a chunk's sums has left r past them all: the largest
-      token = lane == 0 ? first + row.skew : -1;
-      value = row.one(first + row.skew);
+    if (!done) {
+      int most = last;
+#pragma unroll
+      for (int m = 32; m >= 1; m >>= 1) most = max(most, shfl_xor(most, m));
+      if (last == most) token = last, value = last_value;
     }
     if (token >= 0) write(token, value, all);
   }
 
   // sums[0 .. pieces) hold the pieces' weights (or, of_chunks, each chunk's first
-  // the chunk's): finds the draw's piece and picks there.
-  __device__ __forceinline__ void pick_by_sums(u64 least, bool of_chunks) {
+  // the chunk's): finds the draw's piece and picks there.  `rescaled`: they are
+  // rounded from sums in their chunk's unit, in which the draw then goes on.
+  __device__ __forceinline__ void pick_by_sums(u64 least, bool of_chunks, bool rescaled) {
     __syncthreads();
     u64 mine[kSumsPerThread], t = 0, all;
     const int i0 = threadIdx.x * kSumsPerThread;
@@ -515,30 +525,35 @@ struct Choice {
     }
     __syncthreads();
     int piece = static_cast<int>(sh.found);
-    u64 rest = sh.found2;
+    const double unit = rescaled ? st.ref[piece / kChunkWaves] : N;
+    // a sum that is not 0 is of a unit within 2^-64, and its part no more than it was there
+    u64 rest = a.u[b] >= 1.0f ? ~0ull : sh.found2 << static_cast<int>(N - unit);
     if (of_chunks) {  // its pieces, a wave each
       static_assert(kChunkWaves == kRowWaves, "a wave per piece");
       float v[kGroup];
       row.load(piece + wave_index(), v);
       u64 sum = 0;
 #pragma unroll
-      for (int e = 0; e < kGroup; ++e) sum += kept(v[e], row.place(piece + wave_index(), e), least);
+      for (int e = 0; e < kGroup; ++e) sum += kept(v[e], row.place(piece + wave_index(), e), least, unit);
       sum = wave_add(sum);
       turn ^= 1;
       if (lane == 0) sh.waves[turn][wave] = sum;
       __syncthreads();
       bool found = false;
-      int w = 0;
+      int w = 0;  // the piece, or the last of any weight
 #pragma unroll
       for (int i = 0; i < kRowWaves; ++i) {
         const u64 here = sh.waves[turn][i];
-        found = found || rest < here;
-        if (!found) rest -= here, ++w;
+        if (!found && here != 0) {
+          w = i;
+          found = rest < here;
+          if (!found) rest -= here;
+        }
       }
-      if (found) piece += w;
-      else rest = ~0ull;  // rounding of the chunk's sum: past all of a piece's
+      piece += w;
+      if (!found) rest = ~0ull;
     }
-    if (wave == 0) pick(piece, rest, least, all);
+    if (wave == 0) pick(piece, rest, least, all, unit);
   }
 
   // ---- groups.  A row of up to kHeldPieces pieces has its groups' keys in
@@ -644,7 +659,7 @@ struct Choice {
                [&](const float* v, int p) {
                  u64 t = 0;
 #pragma unroll
-                 for (int e = 0; e < Row<F32>::W; ++e) t += kept(v[e], p + e, least);
+                 for (int e = 0; e < Row<F32>::W; ++e) t += kept(v[e], p + e, least, N);
                  return t;
                },
                [&](u64 t, int piece) {
@@ -1065,6 +1080,7 @@ struct Choice {
     bool apart = false;   // the list is all there is, the pieces' sums are not begun
     bool summed = false;  // the pieces' sums are complete
     bool chunked = false;  // the sums are the chunks', from their bins: no weight is computed again but in the draw's
+    bool rescaled = false;  // the sums are rounded from their chunks' units
     u64 need = 0, none = 0;
     double x_top = x_most, scale = 0.0;
     if (s.filter_k) {
@@ -1118,12 +1134,13 @@ struct Choice {
         listed = !summed && n > 0 && n <= kList;
         chunked = chunked && listed;
         if (chunked) sum_chunks(bin);
+        rescaled = chunked;
         need = rest, x_top = N + 1.0 - bin * (1.0 / kPerOctave), scale = kFine * kPerOctave;
       }
     } else {
       for (int i = threadIdx.x; i < pieces; i += kRowThreads)
         sh.sums[i] = rescale(st.piece_sum[i], st.ref[i / kChunkWaves], N);
-      summed = true;
+      summed = rescaled = true;
     }
     if (listed) {
       if (s.filter_p) least = max(least, border<false>(n, least, need, x_top, scale, none));
@@ -1139,7 +1156,7 @@ struct Choice {
     } else {
       least = min_rank;
     }
-    pick_by_sums(least, chunked);
+    pick_by_sums(least, chunked, rescaled);
   }
 };
 

@@ -137,3 +137,53 @@ def test_decode_weights_that_are_not_finite(T, H, E, F, k, short):
     with np.errstate(invalid="ignore"):
         want, mag = R.experts(host(t["x"]), idx, gates, lambda e: [host(t[n][e]) for n in ("w_gate", "w_up", "w_down")])
         same_or_near(moe.MoEDecode(T, H, E, F, k).forward(*args), want, SLACK * BF * (mag + np.abs(want)), "y")
+
+
+def ends(B):
+    """u at and past the ends of [0, 1), one after the other."""
+    return np.resize(np.array([1.0, 0.0, 2.0, np.nan, -1.0, 1.0 - 2.0 ** -24, 1e-7, np.inf], np.float32), B)
+
+
+@pytest.mark.parametrize("V,pad,fp32", [(20000, 20000, True), (20003, 20011, False), (40000, 40001, True), (70001, 70008, False)])
+def test_sample_draws_at_the_ends(V, pad, fp32):
+    """u of 0 and of 1 and more over chunks of different largest logits: the first and the last that stay."""
+    import torch
+    import paper_2608_00916_amd as moe
+    B = 64
+    say("sample ends", V, pad, fp32)
+    g = gen(V)
+    wide = torch.zeros((B, pad), device="cuda", dtype=torch.float32 if fp32 else torch.bfloat16)
+    wide[:, :V] = dev(g.standard_normal((B, V)).astype(np.float32)).to(wide.dtype)
+    logits = wide[:, :V]
+    logits[::2, 11000] = 9.0  # the largest in one chunk alone
+    u = dev(ends(B))
+    t, p = dev(g.choice([0.7, 1.0, 2.0], B).astype(np.float32)), dev(g.choice([0.5, 0.9, 0.99], B).astype(np.float32))
+    m, k = dev(g.choice([1e-9, 1e-3, 0.02], B).astype(np.float32)), dev(g.choice([40, 300, 5000], B).astype(np.int32))
+    op = moe.Sampler(B, V)
+    plain = op.forward(logits, u)[0].cpu().numpy()
+    assert (plain[::8] == V - 1).all() and (plain[2::8] == V - 1).all() and (plain[7::8] == V - 1).all()
+    assert (plain[1::8] == 0).all() and (plain[3::8] == 0).all() and (plain[4::8] == 0).all()
+    for s in (dict(), dict(temperature=t), dict(temperature=t, top_p=p), dict(temperature=t, top_p=p, min_p=m),
+              dict(temperature=t, min_p=m), dict(temperature=t, top_k=k), dict(top_k=k, top_p=p)):
+        say("  ", list(s))
+        check_tokens(logits, u, op.forward(logits, u, **s), **s)
+
+
+@pytest.mark.parametrize("below", [25.0, 28.0, 31.0, 33.0, 100.0])
+@pytest.mark.parametrize("head", [True, False])
+def test_sample_draws_from_chunks_far_below(below, head):
+    """A first, or last, chunk whose weights are too small, one by one or together, for the row's
+    unit (2^-43 of its largest, 29.8 below): its sums count, and the draw finds what they counted."""
+    import torch
+    import paper_2608_00916_amd as moe
+    B, V, n = 16, 24576, 8192
+    say("sample far below", below, head)
+    logits = dev((0.01 * gen(int(below)).standard_normal((B, V))).astype(np.float32))
+    part = logits[:, :n] if head else logits[:, V - n:]
+    part -= below
+    logits[:, n + 5] = 0.5
+    u = dev(np.full(B, 0.0 if head else 1.0, np.float32))
+    token = moe.Sampler(B, V).forward(logits, u)[0]
+    # 1024 weights of e^-33 are 2^-37.6 of one, still a few units; of e^-100 nothing
+    want = (n if head else V - n - 1) if below > 40 else (0 if head else V - 1)
+    assert (token == want).all(), token
