@@ -187,3 +187,38 @@ def test_sample_draws_from_chunks_far_below(below, head):
     # 1024 weights of e^-33 are 2^-37.6 of one, still a few units; of e^-100 nothing
     want = (n if head else V - n - 1) if below > 40 else (0 if head else V - 1)
     assert (token == want).all(), token
+
+
+@pytest.mark.parametrize("T,H,E,k", [(1, 2048, 128, 8), (1, 128, 8, 2), (3, 1152, 256, 2), (8, 384, 64, 4), (9, 2048, 128, 8), (40, 640, 16, 2),
+                                     (64, 4096, 256, 32)])
+@pytest.mark.parametrize("size", [1e-6, 3e-5, 1e-2])
+def test_decode_gates_are_the_block_s_bits(T, H, E, k, size):
+    """Experts whose outputs are +-1, a pattern of signs each: a token's outputs are sums and
+    differences of its gates, nearly equal ones where the logits are small, so they show the
+    gates' last bits, and their signs which experts they are.  The same bits as moe_infer, where
+    such outputs are exact too; and near the formula: logits are off by 2^-18 of their terms' sizes (at
+    most 64 additions in a row), a gate by that and 2^-21 of itself."""
+    import torch
+    import paper_2608_00916_amd as moe
+    say("decode gates", T, H, E, k, size)
+    F = 128
+    g = gen(T + H + k)
+    w_r = bf16(size * g.standard_normal((H, E)))
+    w_r[0] = 0.0
+    x = bf16(g.standard_normal((T, H)))
+    x[:, 0] = 1.0
+    w_gate, w_up = (torch.zeros((E, H, F), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    w_down = torch.zeros((E, F, H), dtype=torch.bfloat16, device="cuda")
+    w_gate[:, 0], w_up[:, 0] = 64.0, 2.0 ** -6  # G = 64, silu(G) = G, A = 1
+    signs = g.choice([-1.0, 1.0], (E, H))
+    w_down[:, 77] = bf16(signs)
+    args = (x, w_r, w_gate, w_up, w_down)
+    y = moe.MoEDecode(T, H, E, F, k).forward(*args)
+    assert torch.equal(y, moe.MoEInfer(T, H, E, F, k).forward(*args))
+    X, W = host(x), host(w_r)
+    idx, gates, gap = R.route(X, W, k)
+    off = 2.0 ** -18 * (np.abs(X) @ np.abs(W)).max(-1)
+    want = np.einsum("tj,tjh->th", gates, signs[idx])
+    clear = gap > 2 * off
+    assert clear.sum() >= T // 2
+    near(y[dev(clear)], want[clear], SLACK * BF * np.abs(want[clear]) + (4 * off[clear, None] + 2.0 ** -20), "y")
