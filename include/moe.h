@@ -491,7 +491,7 @@ int moe_norm_bwd(const moe_norm_dims* d, const void* h, int64_t ldh, const void*
 /* moe_infer for at most MOE_DECODE_MAX_T tokens: the same layer with the same
  * selection and gates, bit for bit, in tiles for few rows.  G, U and O stay
  * fp32, and A enters the down product whole (as three bf16 that add up to it, 2^-25
- * of it aside), so Y is closer to the equations than moe_infer's and not its bits; an
+ * of it or 2^-125 aside), so Y is closer to the equations than moe_infer's and not its bits; an
  * infinite weight gives what it gives there.  Arguments and flags as
  * moe_infer.
  *   ws  moe_decode_workspace_bytes(d) bytes of scratch, enough for fewer tokens too */
@@ -508,7 +508,8 @@ int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i
 
 /* The next token of each of B rows of V logits, from a given number u in [0, 1)
  * per row.  Larger logits come first, equal ones by lower index.
- *   weights  e^((logit - largest) / temperature), held to 2^-43
+ *   weights  e^((logit - largest) / temperature), held to 2^-43 of the largest, or
+ *            to 2^-52 |logit| / temperature of themselves where that is more
  *   top_k    the first top_k stay; 0 or less, or V or more: all
  *   top_p    of those the shortest prefix whose weights reach top_p of their
  *            sum stays, one at least; 1 or more: all
@@ -520,7 +521,10 @@ int moe_decode_i8(const moe_dims* d, const void* x, const void* w_r, const moe_i
  * top_p or min_p turns that filter off; u below 0 or NaN counts as 0, u of 1
  * and more takes the last of any weight.  A logit of -infinity or NaN is never taken; +infinity
  * leaves only its like.  A row without a logit to take has token -1 and
- * logprob -infinity. */
+ * logprob -infinity.  Weights are summed by chunks of 8192 logits, counted from the
+ * 16 bytes that the row begins in, and each sum is rounded to 2^-43 of the row's
+ * largest weight: a draw or a border nearer than that to the next token may be that
+ * token's where the row begins elsewhere within its 16 bytes. */
 #define MOE_SAMPLE_MAX_V 1048576
 typedef struct moe_sample_dims {
   int32_t B, V;   /* 1 <= B <= 65535, 1 <= V <= MOE_SAMPLE_MAX_V */

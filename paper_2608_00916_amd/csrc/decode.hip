@@ -539,8 +539,8 @@ __device__ __forceinline__ void few_rows_i8(const int8_t* const (&b)[NB], int K,
 
 // Where the tiles are many, short workgroups of which many fit a compute unit:
 // two waves and one unit of k in flight in each (eight waves took 1.3 times as
-// long at 16 tokens).  Where they are so few that each compute unit has one or
-// two, eight waves with all of K in flight at once.
+// long at 16 tokens).  Where they are so few that a compute unit has four at
+// most, eight waves with all of K in flight at once.
 constexpr int kUpWaves8 = 2, kUpWaves8Few = 8, kDownWaves8 = 4;
 
 template <int NT, int WAVES, int U>

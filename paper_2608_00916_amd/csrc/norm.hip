@@ -147,8 +147,9 @@ __global__ __launch_bounds__(kRowThreads<WAVES>* kFwdRows<WAVES>) void k_norm_fw
 // dw does not depend on timing.  Few registers per lane are what counts:
 // rows of 2048 by one wave of four vectors a lane (210 registers, two waves per
 // SIMD) took 36 us at 8192 x 2048, the adding of the shares included, four
-// waves of one vector 26 (5.2 TB/s of what is read and written; a copy reaches
-// 5.4, the forward 6.5).
+// waves of one vector 25 (5.3 TB/s of what is read and written; a copy reaches
+// 5.4, the forward 6.5), both in a row of calls on the same tensors, a part of
+// which the last-level cache serves; from HBM the call takes 30.
 template <int WAVES, int VEC>
 __global__ __launch_bounds__(kRowThreads<WAVES>* kBwdRows<WAVES>) void k_norm_bwd(NormBwd a) {
   constexpr int ROWS = kBwdRows<WAVES>, RT = kRowThreads<WAVES>;

@@ -38,7 +38,9 @@ constexpr int kUnit = 42;  // weights are in units of 2^-42 of 2^N
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
 constexpr int kList = 4096;   // candidates held in LDS
 constexpr int kMine = kList / kRowThreads;
-constexpr int kFewGroups = 2048;  // groups with candidates, one or two in each, of which the list is likely to hold all
+// Groups with candidates, one or two in each of a long row, of which the list is likely
+// to hold all; a row of up to 32 pieces has no more, and where it is flat is counted twice.
+constexpr int kFewGroups = 2048;
 constexpr int kFastK = 2048;  // the top_k that the list is for
 constexpr int kFine = 1024;   // parts of the list's range
 constexpr int kHeldPieces = 256, kHeldGroups = kHeldPieces * kWave;  // of a row whose groups' keys are held in LDS
@@ -128,8 +130,9 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int b) {
 // x of a value; infinity is past every finite one, so that it alone has weight.
 // Where `in` is false, one of no weight: chosen here, because a choice after
 // the weight makes the compiler put each weight behind a branch of its own, one
-// chain of dependent steps at a time (256 rows of 50001 at top-p 0.9: 73 us with
-// it, 70 without).
+// chain of dependent steps at a time (at temperature 1 and top-p 0.9 one row of
+// 131072: 37.1 us with it, 36.4 without; 64 rows: 60.0, 59.3; 256 of 50001 in bf16
+// the same).
 __device__ __forceinline__ double x_if(bool in, float v, double c) {
   const double x = static_cast<double>(v) * c;
   constexpr int kFar = 0x7e37e43c;  // upper half of 1e300
@@ -997,8 +1000,10 @@ struct Choice {
     }
   }
 
-  // ---- what the lists do not hold (thousands of equal logits, a top_k of
-  // thousands).  Count or weight of the elements of rank >= at.
+  // ---- what the lists do not hold (more than kList elements in the border's bin of a
+  // flat row, thousands of equal logits, a top_k of thousands): 64 passes over the row,
+  // 3 to 4 ms at 160000 to 200000 normal logits of temperature 1 and top-p 0.95, where
+  // 120000 take 40 us.  Count or weight of the elements of rank >= at.
   template <bool COUNT>
   __device__ __forceinline__ u64 measure(u64 at) {
     u64 t = 0;
@@ -1123,9 +1128,10 @@ struct Choice {
       }
       if (!listed) {
         // Where min_p takes nothing off before the border's bin, the bins' weights are
-        // what stays.  Using them pays from about four pieces a wave (256 flat rows of
-        // 50001 in bf16: 70 us, 66 with them; 64 of 131072: 61, 59), and costs steps of
-        // its own where there are fewer (one row of 131072: 35, 37).  The row's length
+        // what stays.  Using them pays from about four pieces a wave where a row has few
+        // workgroups (at temperature 1 and top-p 0.9 256 rows of 50001 in bf16: 73 us, 69
+        // with them; 64 of 131072: 61, 59), and costs steps of its own where it has many
+        // (one row of 131072: 35.6, 36.5).  The row's length
         // alone decides, so that its bits do not depend on how many rows there are.
         chunked = s.filter_p && static_cast<uint32_t>(min_rank >> 32) <= hi && pieces > 4 * kRowWaves;
         n = collect_and_sum(lo, hi, !few && parts > 1, !chunked);

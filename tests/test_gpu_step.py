@@ -4,8 +4,9 @@ Tolerances, from the formats.  A bf16 output is off by 2^-8 of itself (half a
 step).  A row's sum of squares takes at most 32 additions per lane and 16 over
 lanes and waves, 2^-24 each, so the factor 1 / rms is off by under 2^-18; dw
 sums at most 100 terms in a row, 2^-17.  An int8 row's value is off by half its
-scale.  The expert layer's activation is rounded to bf16 (2^-8 of each) between
-the products; its int8 form is held as in the other 8-bit tests (0.6% of the
+scale.  The expert layer's activation enters the second product whole; its
+last bits are held in test_gpu_step_edges.py, here y to 2^-8 of its terms'
+sizes; its int8 form is held as in the other 8-bit tests (0.6% of the
 output's norm).  A token is exact; its log probability is rounded to fp32, and
 the weights behind it are held to 2^-43 each."""
 import numpy as np
