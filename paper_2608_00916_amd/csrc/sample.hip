@@ -127,6 +127,10 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int b) {
   return s;
 }
 
+// N of a chunk with nothing to take: below every logit's (5e83 at most), above the x
+// of what has no weight, so that the difference is one that weighs nothing.
+constexpr double kNoLogits = -1e290;
+
 // x of a value; infinity is past every finite one, so that it alone has weight.
 // Where `in` is false, one of no weight: chosen here, because a choice after
 // the weight makes the compiler put each weight behind a branch of its own, one
@@ -304,7 +308,7 @@ __global__ __launch_bounds__(kChunkWaves* kWave) void k_sample_chunks(SampleArgs
   const bool summed = !s.filter_k && !s.filter_p && !s.filter_m;
   if (!summed && !binned) return;
   const uint32_t largest = static_cast<uint32_t>(best >> 32);
-  const double N = largest == 0 ? -1e305 : floor(x_of(value_of(largest), s.c));
+  const double N = largest == 0 ? kNoLogits : floor(x_of(value_of(largest), s.c));
   if (tid == 0) st.ref[chunk] = N;
   if (summed) {
     u64 sum = 0;
@@ -961,7 +965,7 @@ struct Choice {
         u64 w[8];
         double ref[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ref[j] = c + j < chunks ? st.ref[c + j] : -1e305;
+        for (int j = 0; j < 8; ++j) ref[j] = c + j < chunks ? st.ref[c + j] : kNoLogits;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const double from = static_cast<int>(threadIdx.x) - kPerOctave * (N - ref[j]);

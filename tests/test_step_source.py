@@ -3,6 +3,7 @@ would break without failing a run here."""
 import glob
 import os
 import re
+import struct
 
 import pytest
 
@@ -33,3 +34,14 @@ def test_shared_counts_change_behind_a_barrier():
         before = sample[sample.rfind("__device__", 0, m.start()):m.start()]
         assert "__syncthreads()" in before, sample[m.start() - 200:m.end() + 20]
         assert f"sh.{m[1]}" not in before[before.rfind("__syncthreads()"):], before[-200:]
+
+
+def test_sampling_chunk_without_logits():
+    """The N of a chunk with nothing to take lies between the x of what is never taken, whose
+    exponent is held from below only before it becomes an integer, and that of every logit."""
+    sample = text(os.path.join(CSRC, "sample.hip"))
+    absent = struct.unpack("<d", struct.pack("<Q", (int(re.search(r"kFar = (0x[0-9a-f]+)", sample)[1], 16) | 1 << 31) << 32))[0]
+    none = re.search(r"largest == 0 \? (\S+) :", sample)[1]
+    none = re.search(rf"\b{none} = (\S+);", sample)[1] if none.startswith("k") else none
+    least = -3.4028235e38 * 1.4426950408889634 / 2.0 ** -149
+    assert absent < float(none) - 1e6 < least - 1e6, (absent, none, least)
