@@ -478,7 +478,8 @@ int moe_norm_fwd(const moe_norm_dims* d, const void* x, int64_t ldx, const void*
 
 /* Backward.  With n = h s and g = dy w:
  *   dx = s (g - n mean_c(g n)) + dh,  dw = sum_t dy n
- * dx is the gradient of x and of the residual alike.
+ * dx is the gradient of x and of the residual alike.  A row whose squares pass fp32
+ * (s = 0) has dx = dh, or NaN where the sum of dy w h passes fp32 too.
  *   h   the rows that were normed (the stored sum; x without a residual), pitch ldh
  *   dy  [T, H] bf16, pitch lddy;  dh the gradient that reaches h past the norm, pitch lddh, or NULL
  *   dx  [T, H] bf16; may be dy or dh itself where that has pitch H, else overlaps nothing
